@@ -79,7 +79,9 @@ typedef enum {
   COTTN_OP_BWD_CAUSAL = 1,
   COTTN_OP_FWD_BIDIR = 2,
   COTTN_OP_BWD_BIDIR = 3,
-  COTTN_OP_STEP = 4
+  COTTN_OP_STEP = 4,
+  COTTN_OP_FWD_DECAY = 5,
+  COTTN_OP_BWD_DECAY = 6
 } cottn_op;
 
 /* Bytes of workspace the given operation needs for these arguments (0 for COTTN_OP_STEP).
@@ -284,6 +286,61 @@ int cottn_scale_from_m_varlen(const float* m, const int* seq_len, float* s, int 
                               void* hip_stream);
 int cottn_scale_backward_varlen(const float* m, const int* seq_len, const float* ds, float* dm,
                                 int B, int H, void* hip_stream);
+
+/* ---- a decay for each head ------------------------------------------------------------------
+ * The recurrence of Sec. 5 with a state that forgets: with g_h = exp(log_decay[h]),
+ *   H_i = g_h H_(i-1) + kh_i^T v_i,   o_i = s_h qh_i H_i,   that is
+ *   O_i = s_h sum over j <= i of g_h^(i-j) (qh_i . kh_j) v_j.
+ * log_decay: float[H] device pointer, values <= 0 (0 keeps everything, -inf nothing but the row itself; a value above 0
+ * counts as 0).  It is a constant of the head: the backward gives no gradient for it.
+ * States are float[B][H][dk][dv], H after the last row, without s; dk and dv are each one of 32, 64, 128.  Chunks are the
+ * library's own (64 rows, fp32 32).  All dtypes; states and ds are accurate to fp32 whatever the dtype (16-bit operands
+ * enter them in two parts).  Workspaces: cottn_workspace_bytes_dkdv with COTTN_OP_FWD_DECAY and COTTN_OP_BWD_DECAY, chunk 0.
+ *
+ * Forward.  seq_len: NULL, or int[B] as in the *_varlen calls, and then s is float[B][H] (else float[H]); the state is that
+ * after a sequence's own last row.  state_in: NULL (zeros) or the state before row 0.  state: NULL or out; the two must not
+ * overlap (COTTN_E_ARG).  N = 0 copies state_in to state.
+ * Backward, of the same call: gradients with respect to the raw Q, K, V and to s.  seq_len, s, state_in as in the forward
+ * call; ds is float[H], with seq_len float[B][H].  For a sequence in pieces, last piece first (all optional):
+ *   rev_state_in   sum over the rows i behind this piece of g^(i-n) qh_i^T dO_i, n the piece's number of rows: the
+ *                  rev_state_out of the piece behind;
+ *   rev_state_out  the same at this piece's row 0; s g times it is the gradient with respect to state_in.  Must overlap
+ *                  neither rev_state_in nor state_in (COTTN_E_ARG).
+ * fwd_workspace: NULL, or the workspace of the matching completed cottn_fwd_causal_decay call, untouched since (same K, V,
+ * log_decay, seq_len, sizes, dtype and eps, and the same cottn_tune_segments; as in cottn_bwd_causal). */
+int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const float* s, const float* log_decay,
+                           const int* seq_len, const float* state_in, void* O, float* state, void* workspace,
+                           size_t workspace_bytes, int B, int H, int N, int dk, int dv, int dtype, float eps, void* hip_stream);
+int cottn_bwd_causal_decay(const void* Q, const void* K, const void* V, const float* s, const float* log_decay,
+                           const int* seq_len, const void* dO, const float* state_in, const float* rev_state_in, void* dQ,
+                           void* dK, void* dV, float* ds, float* rev_state_out, const void* fwd_workspace,
+                           size_t fwd_workspace_bytes, void* workspace, size_t workspace_bytes, int B, int H, int N, int dk,
+                           int dv, int dtype, float eps, void* hip_stream);
+
+/* One token with a decay (log_decay may be NULL: none), where a sequence may go on from another one's state, as the beams
+ * of a beam search do:
+ *   state[b] = g state_in[parent[b]] + kh^T v,  o[b] = s qh state[b].
+ * state_in: float[B_in][H][dk][dv].  parent: int[B]; several sequences may have the same parent; a value that is none of
+ * 0 .. B_in - 1 starts from zeros.  Then state, float[B][H][dk][dv], must not overlap state_in (COTTN_E_ARG).
+ * parent NULL: every sequence goes on from its own state, B_in must be B, and state may be state_in (in place) or not
+ * overlap it.  s is float[H]; q, k, v, o as in cottn_step_dkdv. */
+int cottn_step_decay(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const float* state_in,
+                     const int* parent, int B_in, float* state, void* o, int B, int H, int dk, int dv, int dtype, float eps,
+                     void* hip_stream);
+
+/* ---- trees of drafted tokens ------------------------------------------------------------------
+ * T <= COTTN_MOST_DRAFTS tokens for each sequence that form a tree (or several): parent is int[B][T], parent[b][i] a token
+ * before i, or anything else for a root.  q, k are [B][H][T][dk] and v, o [B][H][T][dv]; log_decay may be NULL: no decay.
+ * cottn_tree gives every token's output as if the tokens on its path had been fed one by one to cottn_step_decay, and leaves
+ * state, float[B][H][dk][dv], as it is:
+ *   o_i = s [ g^(depth_i + 1) qh_i state + sum over j = i and its ancestors of g^(depth_i - depth_j) (qh_i . kh_j) v_j ]
+ * with depth 0 at the roots.  cottn_tree_accept takes state on along the path to token last[b] of each sequence, in place;
+ * where last[b] is none of 0 .. T - 1 nothing is accepted and the state stays.  T = 0 does nothing. */
+#define COTTN_MOST_DRAFTS 64
+int cottn_tree(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const int* parent,
+               const float* state, void* o, int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream);
+int cottn_tree_accept(const void* k, const void* v, const float* log_decay, const int* parent, const int* last, float* state,
+                      int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream);
 
 /* Per-kernel timing for benchmarks.  After cottn_profile_start(), every kernel the library
  * launches carries two HIP events of its own (attached to the dispatch, so they mark the

@@ -50,7 +50,8 @@ _marshal = _import_marshal()
 library_path = os.path.join(_HERE, "libcottn.so")
 
 COTTN_F32, COTTN_BF16, COTTN_F16 = 0, 1, 2
-OP_FWD_CAUSAL, OP_BWD_CAUSAL, OP_FWD_BIDIR, OP_BWD_BIDIR, OP_STEP = range(5)
+OP_FWD_CAUSAL, OP_BWD_CAUSAL, OP_FWD_BIDIR, OP_BWD_BIDIR, OP_STEP, OP_FWD_DECAY, OP_BWD_DECAY = range(7)
+MOST_DRAFTS = 64  # COTTN_MOST_DRAFTS of include/cottn.h
 
 
 class CottnError(RuntimeError):
@@ -129,6 +130,16 @@ def _load():
     lib.cottn_scale_from_m.argtypes = [fp, fp, i, f, vp]
     lib.cottn_scale_backward.restype = i
     lib.cottn_scale_backward.argtypes = [fp, fp, fp, i, f, vp]
+    lib.cottn_fwd_causal_decay.restype = i
+    lib.cottn_fwd_causal_decay.argtypes = [vp] * 10 + [sz] + [i] * 6 + [f, vp]
+    lib.cottn_bwd_causal_decay.restype = i
+    lib.cottn_bwd_causal_decay.argtypes = [vp] * 15 + [sz, vp, sz] + [i] * 6 + [f, vp]
+    lib.cottn_step_decay.restype = i
+    lib.cottn_step_decay.argtypes = [vp] * 7 + [i, vp, vp] + [i] * 5 + [f, vp]
+    lib.cottn_tree.restype = i
+    lib.cottn_tree.argtypes = [vp] * 8 + [i] * 6 + [f, vp]
+    lib.cottn_tree_accept.restype = i
+    lib.cottn_tree_accept.argtypes = [vp] * 6 + [i] * 6 + [f, vp]
     lib.cottn_profile_start.restype = i
     lib.cottn_profile_stop.restype = i
     lib.cottn_profile_count.restype = i
@@ -785,6 +796,141 @@ def cottn_step_dkdv(q, k, v, s, state, o=None, eps=1e-6, stream=None):
                              dt, eps, _stream(stream))
     _check(st, "cottn_step_dkdv")
     return o
+
+
+# ---- a decay for each head; beams and trees of drafted tokens ------------------------------------
+
+def cottn_fwd_causal_decay(Q, K, V, s, log_decay, seq_len=None, state_in=None, O=None, state=None, workspace=None, eps=1e-6,
+                           stream=None):
+    """O_i = s_h sum over j <= i of g_h^(i-j) (qhat_i . khat_j) v_j with g = exp(log_decay) (float32 [H], <= 0); returns O
+    (like V; Q and K may have another width).  With seq_len (int32 [B]) a padded batch, and s float32 [B, H], else [H].
+    state_in, if given, is the state before the first row, and `state` receives that after the last one, both float32
+    [B, H, d_key, d_value] and not the same memory."""
+    B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
+    if O is None:
+        O = torch.empty_like(V)
+    _rows_like(Q, K=K)
+    _rows_like(V, O=O)
+    if seq_len is not None:
+        _check_lengths(seq_len, B, Q.device)
+    _f32("s", s, H if seq_len is None else B * H, Q.device)
+    _f32("log_decay", log_decay, H, Q.device)
+    _f32("state_in", state_in, B * H * dk * dv, Q.device, optional=True)
+    _f32("state", state, B * H * dk * dv, Q.device, optional=True)
+    _on_gpu(Q)
+    workspace, have = _workspace_dkdv(OP_FWD_DECAY, B, H, N, dk, dv, 0, dt, Q.device, workspace, stream)
+    st = lib.cottn_fwd_causal_decay(_ptr(Q), _ptr(K), _ptr(V), _ptr(s), _ptr(log_decay), _ptr(seq_len), _ptr(state_in),
+                                    _ptr(O), _ptr(state), _ptr(workspace), have, B, H, N, dk, dv, dt, eps, _stream(stream))
+    _check(st, "cottn_fwd_causal_decay")
+    return O
+
+
+def cottn_bwd_causal_decay(Q, K, V, s, log_decay, dO, seq_len=None, state_in=None, rev_state_in=None, dQ=None, dK=None, dV=None,
+                           ds=None, rev_state_out=None, workspace=None, eps=1e-6, stream=None, fwd_workspace=None):
+    """Gradients of cottn_fwd_causal_decay wrt raw Q, K, V and s (log_decay is a constant of the head); returns
+    (dQ, dK, dV, ds), ds float32 [H], or [B, H] with seq_len.  state_in as in the forward call; rev_state_in and rev_state_out
+    hand the reverse-time state from one piece of a sequence to the piece before (include/cottn.h).  fwd_workspace: the
+    workspace tensor of the matching forward call (untouched since), or None."""
+    B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
+    dQ, dK, dV, ds = _grads_dkdv(Q, V, dQ, dK, dV, ds, H if seq_len is None else (B, H))
+    _rows_like(Q, K=K, dQ=dQ, dK=dK)
+    _rows_like(V, dO=dO, dV=dV)
+    if seq_len is not None:
+        _check_lengths(seq_len, B, Q.device)
+    scales = H if seq_len is None else B * H
+    _f32("s", s, scales, Q.device)
+    _f32("ds", ds, scales, Q.device)
+    _f32("log_decay", log_decay, H, Q.device)
+    for name, t in (("state_in", state_in), ("rev_state_in", rev_state_in), ("rev_state_out", rev_state_out)):
+        _f32(name, t, B * H * dk * dv, Q.device, optional=True)
+    _on_gpu(Q)
+    workspace, have = _workspace_dkdv(OP_BWD_DECAY, B, H, N, dk, dv, 0, dt, Q.device, workspace, stream)
+    st = lib.cottn_bwd_causal_decay(_ptr(Q), _ptr(K), _ptr(V), _ptr(s), _ptr(log_decay), _ptr(seq_len), _ptr(dO),
+                                    _ptr(state_in), _ptr(rev_state_in), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ds),
+                                    _ptr(rev_state_out), _ptr(fwd_workspace), _bytes(fwd_workspace, Q.device),
+                                    _ptr(workspace), have, B, H, N, dk, dv, dt, eps, _stream(stream))
+    _check(st, "cottn_bwd_causal_decay")
+    return dQ, dK, dV, ds
+
+
+def _token_widths(q, v, dims, shape):
+    """Sizes of q and of v, which differ in their last one at most; `shape` is what they are called in an error."""
+    if q.dim() != dims or v.dim() != dims:
+        raise ValueError("rows must be %s, got shapes %s and %s" % (shape, tuple(q.shape), tuple(v.shape)))
+    if tuple(v.shape[:-1]) != tuple(q.shape[:-1]) or v.dtype != q.dtype or v.device != q.device:
+        raise ValueError("v must be %s %s on %s, got %s %s on %s" % (
+            tuple(q.shape[:-1]) + ("d_value",), q.dtype, q.device, tuple(v.shape), v.dtype, v.device))
+    return tuple(q.shape[:-1]) + (q.shape[-1], v.shape[-1], _dtype_code(q))
+
+
+def _indices(name, t, shape, device):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or t.device != device:
+        raise TypeError("%s must be an int32 tensor of shape %s on %s" % (name, shape, device))
+
+
+def cottn_step_decay(q, k, v, s, log_decay, state, state_in=None, parent=None, o=None, eps=1e-6, stream=None):
+    """One token of B sequences: state = g state_in[parent] + khat^T v; returns o = s_h qhat state (like v).  q, k are
+    [B, H, d_key] and v [B, H, d_value]; log_decay (float32 [H], or None: no decay); states float32 [B, H, d_key, d_value].
+    Without state_in, `state` is updated in place; with it, `state` is written (not the same memory).  parent (int32 [B], with
+    state_in [B_in, H, d_key, d_value]): whose state each sequence goes on from; a value outside starts from zeros."""
+    B, H, dk, dv, dt = _token_widths(q, v, 3, "[B, H, d]")
+    if o is None:
+        o = torch.empty_like(v)
+    _tokens_like(q, k=k)
+    _tokens_like(v, o=o)
+    _f32("s", s, H, q.device)
+    _f32("log_decay", log_decay, H, q.device, optional=True)
+    _f32("state", state, B * H * dk * dv, q.device)
+    B_in = B
+    if parent is not None:
+        _indices("parent", parent, (B,), q.device)
+        if state_in is None:
+            raise ValueError("parent needs state_in")
+        if state_in.dim() != 4:
+            raise ValueError("state_in must be [B_in, H, d_key, d_value], got shape %s" % (tuple(state_in.shape),))
+        B_in = state_in.shape[0]
+    if state_in is not None:
+        _f32("state_in", state_in, B_in * H * dk * dv, q.device)
+    _on_gpu(q)
+    st = lib.cottn_step_decay(_ptr(q), _ptr(k), _ptr(v), _ptr(s), _ptr(log_decay), _ptr(state if state_in is None else state_in),
+                              _ptr(parent), B_in, _ptr(state), _ptr(o), B, H, dk, dv, dt, eps, _stream(stream))
+    _check(st, "cottn_step_decay")
+    return o
+
+
+def cottn_tree(q, k, v, s, state, parent, log_decay=None, o=None, eps=1e-6, stream=None):
+    """Outputs of up to 64 drafted tokens for each sequence that form a tree over `state` (float32 [B, H, d_key, d_value],
+    left as it is): each token's, as if the tokens on its path had been fed one by one.  q, k are [B, H, T, d_key], v
+    [B, H, T, d_value], parent int32 [B, T]: a token before, or anything else for a root; returns o (like v)."""
+    B, H, T, dk, dv, dt = _token_widths(q, v, 4, "[B, H, T, d]")
+    if o is None:
+        o = torch.empty_like(v)
+    _tokens_like(q, k=k)
+    _tokens_like(v, o=o)
+    _f32("s", s, H, q.device)
+    _f32("log_decay", log_decay, H, q.device, optional=True)
+    _f32("state", state, B * H * dk * dv, q.device)
+    _indices("parent", parent, (B, T), q.device)
+    _on_gpu(q)
+    st = lib.cottn_tree(_ptr(q), _ptr(k), _ptr(v), _ptr(s), _ptr(log_decay), _ptr(parent), _ptr(state), _ptr(o), B, H, T, dk, dv,
+                        dt, eps, _stream(stream))
+    _check(st, "cottn_tree")
+    return o
+
+
+def cottn_tree_accept(k, v, state, parent, last, log_decay=None, eps=1e-6, stream=None):
+    """Takes `state` on along the path to token last[b] (int32 [B]) of each sequence's tree, in place (k, v, parent as in
+    cottn_tree); where last[b] is not a token nothing is accepted.  Returns state."""
+    B, H, T, dk, dv, dt = _token_widths(k, v, 4, "[B, H, T, d]")
+    _f32("log_decay", log_decay, H, k.device, optional=True)
+    _f32("state", state, B * H * dk * dv, k.device)
+    _indices("parent", parent, (B, T), k.device)
+    _indices("last", last, (B,), k.device)
+    _on_gpu(k)
+    st = lib.cottn_tree_accept(_ptr(k), _ptr(v), _ptr(log_decay), _ptr(parent), _ptr(last), _ptr(state), B, H, T, dk, dv, dt, eps,
+                               _stream(stream))
+    _check(st, "cottn_tree_accept")
+    return state
 
 
 def profile_start():

@@ -242,6 +242,40 @@ bool make_plan(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype
 
 namespace {
 
+// The split of a call with a decay, the same for the forward and its backward.
+struct DecayPlan {
+  int G, seg_rows;
+  bool carried;   // DecayArgs
+};
+bool make_decay_plan(int B, int H, int N, int dk, int dv, int chunk, int dtype, DecayPlan* plan) {
+  if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
+  const int C = dtype == COTTN_F32 ? 32 : 64;
+  if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != C)) return false;
+  const long units = long(B) * H, n_chunks = (long(N) + C - 1) / C;
+  long want = g_tuned_segments;
+  if (want <= 0) want = n_chunks > 0 ? causal_segments(units, N, n_chunks, C, dtype, dk, dv) : 1;
+  if (want > n_chunks) want = n_chunks;
+  if (want < 1) want = 1;
+  const long steps = n_chunks > 0 ? (n_chunks + want - 1) / want : 1, G = n_chunks > 0 ? (n_chunks + steps - 1) / steps : 1;
+  if (!threads_fit(units * G, 512)) return false;
+  plan->G = int(G);
+  plan->seg_rows = int(steps * C);
+  plan->carried = G > 1 && !causal_totals_in_place(units, int(G), dk, dv, dtype == COTTN_F32) && threads_fit(units, dk * dv / 4);
+  return true;
+}
+// forward: the states of G segments; backward: two such arrays, and the segments' parts of ds
+size_t decay_workspace_bytes(int op, int B, int H, int dk, int dv, const DecayPlan& p) {
+  const long units = long(B) * H;
+  const size_t states = p.G > 1 ? state_slots_bytes(units * p.G, dk, dv) : 0;
+  return op == COTTN_OP_FWD_DECAY ? states : 2 * states + round_up_256(size_t(units) * p.G * sizeof(float));
+}
+
+// whether n floats at p and m floats at q have one in common
+bool overlap(const float* p, double n, const float* q, double m) {
+  const double a = double(reinterpret_cast<uintptr_t>(p)), b = double(reinterpret_cast<uintptr_t>(q));
+  return p != nullptr && q != nullptr && a < b + 4.0 * m && b < a + 4.0 * n;
+}
+
 // The walk of a causal call: even shares where the plan has them, also for a padded batch (96 units of 1024
 // rows at most, 16-bit 128 x 128, lengths spread evenly from a quarter of that: forward + backward 107 -> 101 us against
 // segments, 272 units 287 -> 250 (with the forward alone 33 -> 37 and 93 -> 81), 68 of 5010 373 -> 322; fp32 64 x 64 282 of 571 170 -> 165), but where sequences
@@ -325,6 +359,10 @@ size_t cottn_workspace_bytes_dkdv(int op, int B, int H, int N, int dk, int dv, i
                ? 0
                : size_t(-1);
   }
+  if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY) {
+    DecayPlan plan;
+    return make_decay_plan(B, H, N, dk, dv, chunk, dtype, &plan) ? decay_workspace_bytes(op, B, H, dk, dv, plan) : size_t(-1);
+  }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_STEP) return size_t(-1);
   SeqPlan plan;
   if (!make_plan(op, B, H, N, dk, dv, chunk, dtype, &plan)) return size_t(-1);
@@ -336,6 +374,10 @@ size_t cottn_workspace_bytes(int op, int B, int H, int N, int d, int chunk, int 
 }
 
 int cottn_segments_dkdv(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype) {
+  if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY) {
+    DecayPlan plan;
+    return make_decay_plan(B, H, N, dk, dv, chunk, dtype, &plan) ? plan.G : 0;
+  }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_BWD_BIDIR) return 0;
   SeqPlan plan;
   if (!make_plan(op, B, H, N, dk, dv, chunk, dtype, &plan)) return 0;
@@ -758,6 +800,123 @@ int cottn_bwd_bidir_dkdv(const void* Q, const void* K, const void* V, const floa
                          float eps, void* hip_stream) {
   return bwd_bidir_any(Q, K, V, s, nullptr, dO, dQ, dK, dV, ds, fwd_workspace, fwd_workspace_bytes,
                        workspace, workspace_bytes, B, H, N, dk, dv, dtype, eps, hip_stream);
+}
+
+// ---- a decay for each head ------------------------------------------------------------------------
+int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const float* s, const float* log_decay,
+                           const int* seq_len, const float* state_in, void* O, float* state, void* workspace,
+                           size_t workspace_bytes, int B, int H, int N, int dk, int dv, int dtype, float eps, void* hip_stream) {
+  const void* req[] = {s, Q, K, V, O};
+  int st = check_common(req, N == 0 ? 1 : 5, B, H, N, dk, dv, dtype, eps);   // (no rows: tensors without memory)
+  if (st != COTTN_OK) return st;
+  if (log_decay == nullptr) return COTTN_E_NULL;
+  if (!is_aligned(log_decay, 4) || !is_aligned(state, 16) || !is_aligned(state_in, 16)) return COTTN_E_ALIGN;
+  const double states = double(B) * H * dk * dv;
+  if (overlap(state_in, states, state, states)) return COTTN_E_ARG;
+  if ((st = check_lengths(seq_len)) != COTTN_OK) return st;
+  DecayPlan plan;
+  if (!make_decay_plan(B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
+  st = check_workspace(workspace, workspace_bytes, decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan));
+  if (st != COTTN_OK) return st;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (N == 0) {
+    if (state == nullptr) return COTTN_OK;
+    return map_hip(state_in == nullptr ? zero_f32(state, long(states), stream) : copy_state(state, state_in, long(states), stream));
+  }
+  DecayArgs a{};
+  a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.O = O; a.state = state; a.state_in = state_in;
+  a.seq_len = seq_len; a.workspace = workspace;
+  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows; a.carried = plan.carried;
+  a.eps = eps; a.stream = stream;
+  return map_hip(dtype == COTTN_BF16 ? fwd_decay_bf16(a) : dtype == COTTN_F16 ? fwd_decay_f16(a) : fwd_decay_f32w(a));
+}
+
+int cottn_bwd_causal_decay(const void* Q, const void* K, const void* V, const float* s, const float* log_decay,
+                           const int* seq_len, const void* dO, const float* state_in, const float* rev_state_in, void* dQ,
+                           void* dK, void* dV, float* ds, float* rev_state_out, const void* fwd_workspace,
+                           size_t fwd_workspace_bytes, void* workspace, size_t workspace_bytes, int B, int H, int N, int dk,
+                           int dv, int dtype, float eps, void* hip_stream) {
+  const void* req[] = {s, ds, Q, K, V, dO, dQ, dK, dV};
+  int st = check_common(req, N == 0 ? 2 : 9, B, H, N, dk, dv, dtype, eps);
+  if (st != COTTN_OK) return st;
+  if (log_decay == nullptr) return COTTN_E_NULL;
+  if (!is_aligned(log_decay, 4) || !is_aligned(state_in, 16) || !is_aligned(rev_state_in, 16) || !is_aligned(rev_state_out, 16))
+    return COTTN_E_ALIGN;
+  const double states = double(B) * H * dk * dv;
+  if (overlap(rev_state_in, states, rev_state_out, states) || overlap(state_in, states, rev_state_out, states)) return COTTN_E_ARG;
+  if ((st = check_lengths(seq_len)) != COTTN_OK) return st;
+  DecayPlan plan;
+  if (!make_decay_plan(B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
+  st = check_workspace(workspace, workspace_bytes, decay_workspace_bytes(COTTN_OP_BWD_DECAY, B, H, dk, dv, plan));
+  if (st != COTTN_OK) return st;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (N == 0) {
+    hipError_t e = zero_f32(ds, seq_len != nullptr ? long(B) * H : H, stream);
+    if (e == hipSuccess && rev_state_out != nullptr)
+      e = rev_state_in != nullptr ? copy_state(rev_state_out, rev_state_in, long(states), stream)
+                                  : zero_f32(rev_state_out, long(states), stream);
+    return map_hip(e);
+  }
+  DecayArgs a{};
+  a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.ds = ds;
+  a.state_in = state_in; a.rev_state_in = rev_state_in; a.rev_state_out = rev_state_out; a.seq_len = seq_len;
+  a.workspace = workspace;
+  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows; a.carried = plan.carried;
+  a.eps = eps; a.stream = stream;
+  if (fwd_workspace != nullptr && plan.G > 1) {
+    st = check_workspace(fwd_workspace, fwd_workspace_bytes, decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan));
+    if (st != COTTN_OK) return st;
+    a.saved_fwd_states = static_cast<const float*>(fwd_workspace);
+  }
+  return map_hip(dtype == COTTN_BF16 ? bwd_decay_bf16(a) : dtype == COTTN_F16 ? bwd_decay_f16(a) : bwd_decay_f32w(a));
+}
+
+int cottn_step_decay(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const float* state_in,
+                     const int* parent, int B_in, float* state, void* o, int B, int H, int dk, int dv, int dtype, float eps,
+                     void* hip_stream) {
+  const void* req[] = {q, k, v, s, state_in, state, o};
+  int st = check_common(req, 7, B, H, 1, dk, dv, dtype, eps);
+  if (st != COTTN_OK) return st;
+  if (!is_aligned(log_decay, 4) || !is_aligned(parent, 4)) return COTTN_E_ALIGN;
+  if (B_in < 1 || (parent == nullptr && B_in != B) || !threads_fit(long(B) * H, 256)) return COTTN_E_SHAPE;
+  const double one = double(H) * dk * dv;
+  if (!(parent == nullptr && state_in == state) && overlap(state_in, B_in * one, state, B * one)) return COTTN_E_ARG;
+  StepDecayArgs a{};
+  a.q = q; a.k = k; a.v = v; a.s = s; a.log_decay = log_decay; a.from = state_in; a.parent = parent; a.n_from = B_in;
+  a.to = state; a.o = o; a.B = B; a.H = H; a.dk = dk; a.dv = dv; a.eps = eps;
+  a.stream = static_cast<hipStream_t>(hip_stream);
+  return map_hip(step_decay_any(a, dtype));
+}
+
+// ---- trees of drafted tokens ----------------------------------------------------------------------
+int cottn_tree(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const int* parent,
+               const float* state, void* o, int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream) {
+  const void* req[] = {s, state, q, k, v, o};
+  int st = check_common(req, T == 0 ? 2 : 6, B, H, T, dk, dv, dtype, eps);
+  if (st != COTTN_OK) return st;
+  if (parent == nullptr && T > 0) return COTTN_E_NULL;
+  if (!is_aligned(log_decay, 4) || !is_aligned(parent, 4)) return COTTN_E_ALIGN;
+  if (T > COTTN_MOST_DRAFTS || !threads_fit(long(B) * H, 512)) return COTTN_E_SHAPE;
+  if (T == 0) return COTTN_OK;
+  TreeArgs a{};
+  a.q = q; a.k = k; a.v = v; a.s = s; a.log_decay = log_decay; a.parent = parent; a.state = const_cast<float*>(state); a.o = o;
+  a.B = B; a.H = H; a.n_tokens = T; a.dk = dk; a.dv = dv; a.eps = eps; a.stream = static_cast<hipStream_t>(hip_stream);
+  return map_hip(dtype == COTTN_BF16 ? tree_bf16(a) : dtype == COTTN_F16 ? tree_f16(a) : tree_f32w(a));
+}
+
+int cottn_tree_accept(const void* k, const void* v, const float* log_decay, const int* parent, const int* last, float* state,
+                      int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream) {
+  const void* req[] = {state, k, v};
+  int st = check_common(req, T == 0 ? 1 : 3, B, H, T, dk, dv, dtype, eps);
+  if (st != COTTN_OK) return st;
+  if ((parent == nullptr && T > 0) || last == nullptr) return COTTN_E_NULL;
+  if (!is_aligned(log_decay, 4) || !is_aligned(parent, 4) || !is_aligned(last, 4)) return COTTN_E_ALIGN;
+  if (T > COTTN_MOST_DRAFTS || !threads_fit(long(B) * H, 256)) return COTTN_E_SHAPE;
+  if (T == 0) return COTTN_OK;
+  TreeArgs a{};
+  a.k = k; a.v = v; a.log_decay = log_decay; a.parent = parent; a.last = last; a.state = state;
+  a.B = B; a.H = H; a.n_tokens = T; a.dk = dk; a.dv = dv; a.eps = eps; a.stream = static_cast<hipStream_t>(hip_stream);
+  return map_hip(tree_accept_any(a, dtype));
 }
 
 int cottn_profile_start(void) {

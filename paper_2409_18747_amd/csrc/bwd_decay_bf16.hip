@@ -1,0 +1,655 @@
+// Causal cosine attention with a decay for each head, backward (gfx950): the formulas stand in decay.h.  This file builds the
+// bfloat16 kernels, the IEEE half ones when it is included with COTTN_ELEM_F16 defined and the fp32 ones with
+// COTTN_ELEM_F32 and COTTN_F32_WHOLE.
+//
+// Two scans of a segment.  The first walks forward in time with H and gives dQ; it also forms G = sum over a chunk's rows of
+// g^i' qh_i^T dO_i, from which it leaves the segment's reverse-time total for the second, and ds.  The second walks backward in
+// time with R and gives dK and dV.
+//
+// ds = sum_i (sum_j g^(i-j) (qh_i . kh_j) v_j) . dO_i is a result in fp32 and a sum of terms of both signs, so it is not taken from
+// results of rounded operands: the rows before a chunk give g <H, G>, element by element from two fp32 matrices whose operands are
+// carried in two parts, and the chunk itself gives the sum of its two masked fp32 tiles' products before they are rounded.
+//
+// The chain rule through x / max(|x|, eps): dx = s r (dxh - xh (xh . dxh)) with r = 1 / max(|x|, eps); rows at or below eps have
+// dx = s r dxh.
+#include "device_common.h"
+#include "launch.h"
+#include "tile_io.h"
+#include "workspace.h"
+#include "decay.h"
+
+namespace cottn {
+namespace COTTN_NS {
+namespace {
+
+template <int DK, int DV, int C, int CS>
+struct DecayBwdCfg {
+  static constexpr int RG = C / 16, NW = RG * CS, NT = NW * 64;
+  static constexpr int NKT = DK / 16 / CS, NVT = DV / 16 / CS;   // result column tiles of a wave
+  static constexpr int KSK = DK / 32, KSV = DV / 32, NP = C / 32;
+  static constexpr int TPK = tile_pitch(DK, C), TPV = tile_pitch(DV, C), SP = lds_pitch(DV);
+  static constexpr int TILEK = C * TPK, TILEV = C * TPV, STATE = DK * SP;
+  static constexpr int LDS_BYTES = LDS_ELEM * (2 * TILEK + 2 * TILEV + STATE) + 4 * 8 * C;
+  // dQ rows are staged in the wave's own query rows
+  static constexpr int WAVES = decay_waves(LDS_BYTES, NW, CS);
+};
+
+// xh . dxh of a row and its removal from dxh, where the tile holds x' with xh = left x'
+template <int NTILES>
+__device__ __forceinline__ void take_out_row(f32x4* acc, const float (&xv)[NTILES][4], float dot, float left, float whole,
+                                             float inv_eps) {
+  const float c = whole == inv_eps ? 0.f : left * (left * dot);
+#pragma unroll
+  for (int nt = 0; nt < NTILES; ++nt)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[nt][v] -= xv[nt][v] * c;
+}
+
+// Factors of rows, which of them by the lane of the row: [0] ROW_NORM `left`, [1] that times g^e1(row), [2] STATE_UNIT
+// left g^e2(row), [3] `whole`.
+template <class Stage, int C, class E1, class E2>
+__device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stage>& f, const Decay& g, E1 e1, E2 e2) {
+  const int which = threadIdx.x % Stage::LPR;
+#pragma unroll
+  for (int p = 0; p < Stage::PASSES; ++p) {
+    const int lr = p * Stage::RPP + threadIdx.x / Stage::LPR;
+    const int e = which == 1 ? e1(lr) : which == 2 ? e2(lr) : 0;
+    if ((C % Stage::RPP == 0 || lr < C) && which < 4) rows[which * C + lr] = (which == 3 ? f.whole[p] : f.left[p]) * g.after(float(e)) *
+                                                         (which == 2 ? STATE_UNIT : which == 3 ? 1.f : ROW_NORM);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// dQ of a segment, first chunk to last.  H and G sit in accumulators with the values down and the keys along, tile (x, y):
+// element [v] of lane (r, q4) is H[key 16 row_tile(y) + r][value 16 col_tile(x) + 4 q4 + v].
+template <int DK, int DV, int C, int CS>
+COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
+    const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
+    const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ dQ,
+    const float* __restrict__ fwd_states, float* __restrict__ rev_totals, float* __restrict__ ds_partial,
+    const float* __restrict__ state_in, const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units,
+    float inv_eps, int carried) {
+  using Cfg = DecayBwdCfg<DK, DV, C, CS>;
+  using ST = SplitTiles<DK, DV, Cfg::RG, CS>;   // key rows, value columns
+  using StageK = TileStage<DK, C, Cfg::NT>;
+  using StageV = TileStage<DV, C, Cfg::NT>;
+  constexpr int RG = Cfg::RG, NKT = Cfg::NKT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
+  COTTN_LDS_ARRAY(lds_t, Qs, Cfg::TILEK, 0)
+  COTTN_LDS_ARRAY(lds_t, Ks, Cfg::TILEK, 1)
+  COTTN_LDS_ARRAY(lds_t, Vs, Cfg::TILEV, 2)
+  COTTN_LDS_ARRAY(lds_t, Gs, Cfg::TILEV, 3)
+  COTTN_LDS_ARRAY(lds_t, St, Cfg::STATE, 4)
+  COTTN_LDS_ARRAY(float, krows, 4 * C, 5)
+  COTTN_LDS_ARRAY(float, qrows, 4 * C, 6)
+  COTTN_LDS_ARRAY(float, xdot, CS > 1 ? CS * C : 1, 7)
+  COTTN_LDS_ARRAY(float, ds_wave, Cfg::NW, 8)
+  Unparted un;
+  fetch_argument_now(Q, K, V, dO, s, log_decay, dQ, fwd_states, rev_totals, ds_partial, state_in, lengths, H, G, seg_rows, N,
+                     units, inv_eps, carried);
+  int unit, seg;
+  unit_and_segment(blockIdx.x, units, G, unit, seg);
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
+  const int rg = w % RG, cp = w / RG;
+  const elem_t* Qu = Q + size_t(unit) * N * DK;
+  const elem_t* Ku = K + size_t(unit) * N * DK;
+  const elem_t* Vu = V + size_t(unit) * N * DV;
+  const elem_t* Gu = dO + size_t(unit) * N * DV;
+  elem_t* dQu = dQ + size_t(unit) * N * DK;
+  const int there = valid_rows(lengths, unit, H, N), row_begin = seg * seg_rows, piece_end = min(N, row_begin + seg_rows);
+  const int row_end = max(row_begin, min(there, piece_end));
+  float* ds_out = ds_partial + size_t(unit) * G.n + seg;
+  if (row_begin == row_end) {
+    if (tid == 0) *ds_out = 0.f;
+    zero_rows<DK>(dQu, row_begin, piece_end);
+    return;
+  }
+  StageK qst, kst;
+  StageV vst, gst;
+  qst.fetch(Qu, row_begin, row_end);
+  kst.fetch(Ku, row_begin, row_end);
+  vst.fetch(Vu, row_begin, row_end);
+  gst.fetch(Gu, row_begin, row_end);
+  const int head = unit - quotient(unit, H) * H.n;
+  const Decay g(log_decay[head]);
+  const float scale = s[lengths != nullptr ? unit : head];
+
+  f32x4 sacc[ST::NCT][ST::NRT], racc[ST::NCT][ST::NRT];
+#pragma unroll
+  for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+    for (int y = 0; y < ST::NRT; ++y) sacc[x][y] = racc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bool active = ST::active(rg, cp), with_rev = seg > 0;   // (no workgroup needs the first segment's total)
+  if (active && seg > 0) {
+    const float* slots = fwd_states + size_t(unit) * G.n * DK * DV;
+    add_decayed_states<false>(sacc, carried ? seg : 0, carried ? seg : seg - 1, g, seg_rows, [&](int slot, int x, int y) {
+      return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
+                                             tiled_state_offset(ST::row_tile(rg, cp, y), ST::col_tile(rg, cp, x), DV / 16, l));
+    });
+  }
+  if (active && state_in != nullptr) {
+    const float since = STATE_UNIT * g.after(float(row_begin));
+    const float* src = state_in + size_t(unit) * DK * DV;
+#pragma unroll
+    for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+      for (int y = 0; y < ST::NRT; ++y) {
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::row_tile(rg, cp, y) + r) * DV +
+                                                        16 * ST::col_tile(rg, cp, x) + 4 * q4);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sacc[x][y][v] = __builtin_fmaf(since, t[v], sacc[x][y][v]);
+      }
+  }
+
+  const float row = float(16 * rg + r), to_row = ROW_NORM * g.after(row + 1.f), once = g.after(1.f);
+  float on_diagonal[4];
+#pragma unroll
+  for (int v = 0; v < 4; ++v) on_diagonal[v] = 4 * q4 + v <= r ? g.after(float(r - 4 * q4 - v)) : 0.f;
+  const Kept whole_chunk(g, float(C));
+  float ds_lane = 0.f;
+  RowPieces<DK, NKT> finished;
+#pragma unroll
+  for (int j = 0; j < RowPieces<DK, NKT>::PER_LANE; ++j) finished.v[j] = uint4{0u, 0u, 0u, 0u};
+  const int colk = 16 * NKT * cp;
+  for (int row0 = row_begin; row0 < row_end; row0 += C) {
+    const int n = min(C, row_end - row0);
+    if (active) {
+#pragma unroll
+      for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y)
+          store4_lds(St + (16 * ST::row_tile(rg, cp, y) + r) * SP + 16 * ST::col_tile(rg, cp, x) + 4 * q4, PER_UNIT * sacc[x][y][0],
+                     PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
+    }
+    {
+      RowFactors<StageK> f;
+      f.commit(qst, Qs, inv_eps, un);
+      store_factors<StageK, C>(qrows, f, g, [](int) { return 0; }, [](int i) { return i; });
+      f.commit(kst, Ks, inv_eps, un);
+      store_factors<StageK, C>(krows, f, g, [](int j) { return 15 - j % 16; }, [n](int j) { return max(n - 1 - j, 0); });
+      vst.commit_plain(Vs, un);
+      gst.commit_plain(Gs, un);
+    }
+    if (row0 + C < row_end) {
+      qst.fetch(Qu, row0 + C, row_end);
+      kst.fetch(Ku, row0 + C, row_end);
+      vst.fetch(Vu, row0 + C, row_end);
+      gst.fetch(Gu, row0 + C, row_end);
+    }
+    if (row0 > row_begin) store_row_pieces<DK, NKT>(finished, dQu, row0 - C + 16 * rg, row_end, l, colk);
+    __syncthreads();
+
+    // G of the chunk, ds of the rows before it, and the segment's reverse-time total
+    if (active) {
+      f32x4 gacc[ST::NCT][ST::NRT];
+#pragma unroll
+      for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y) gacc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < Cfg::NP; ++p) {
+        const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+        float wt[8];
+        token_weights(qrows + 2 * C, t0, t1, wt);
+        frag8 gcol[ST::NCT];
+#pragma unroll
+        for (int x = 0; x < ST::NCT; ++x) gcol[x] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::col_tile(rg, cp, x), r);
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y) {
+          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::row_tile(rg, cp, y), r), wt);
+#pragma unroll
+          for (int x = 0; x < ST::NCT; ++x) gacc[x][y] = mma16_weighted(gcol[x], q, gacc[x][y]);
+        }
+      }
+      const float at = g.after(float(row0 - row_begin));
+      float t = 0.f;
+#pragma unroll
+      for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            t = __builtin_fmaf(sacc[x][y][v], gacc[x][y][v], t);
+            racc[x][y][v] = __builtin_fmaf(at, gacc[x][y][v], racc[x][y][v]);
+          }
+      ds_lane += PER_UNIT * PER_UNIT * once * t;
+      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
+#pragma unroll
+      for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y) sacc[x][y] = kept.of(sacc[x][y]);
+    }
+
+    // what the state gives: dqh^T = H dO^T, then the row's factor
+    frag8 gf[Cfg::KSV], qf[Cfg::KSK];
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSV; ++ks) gf[ks] = lds_row_frag(Gs + (16 * rg + r) * TPV + 32 * ks, q4);
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSK; ++ks) qf[ks] = lds_row_frag(Qs + (16 * rg + r) * TPK + 32 * ks, q4);
+    f32x4 dq[NKT];
+#pragma unroll
+    for (int nt = 0; nt < NKT; ++nt) dq[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSV; ++ks) {
+      frag8 sf[NKT];
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) sf[nt] = lds_row_frag(St + (colk + 16 * nt + r) * SP + 32 * ks, q4);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) dq[nt] = mma16(sf[nt], gf[ks], dq[nt]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NKT; ++nt)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) dq[nt][v] *= to_row;
+
+    // the chunk itself, 32 tokens at a time
+    float ds_row = 0.f;
+#pragma unroll
+    for (int p = 0; p < Cfg::NP; ++p) {
+      const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+      if (2 * p <= rg) {
+        frag8 af;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int jt = 2 * p + half;
+          f32x4 ta = {0.f, 0.f, 0.f, 0.f}, tp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSV; ++ks) ta = mma16(lds_row_frag(Vs + (16 * jt + r) * TPV + 32 * ks, q4), gf[ks], ta);
+          // (one wave of a row group forms the tiles of ds)
+          if (CS == 1 || cp == p % CS) {
+#pragma unroll
+            for (int ks = 0; ks < Cfg::KSK; ++ks) tp = mma16(lds_row_frag(Ks + (16 * jt + r) * TPK + 32 * ks, q4), qf[ks], tp);
+          }
+          // ta[v] = dO_(16 rg + r) . v_(16 jt + 4 q4 + v)
+          const f32x4 kj = *reinterpret_cast<const f32x4*>(krows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
+          const float below = g.after(row - float(16 * jt + 15));   // (jt < rg)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            ta[v] = jt > rg ? 0.f : ta[v] * (kj[v] * (jt == rg ? on_diagonal[v] : below));
+            ds_row = __builtin_fmaf(tp[v], ta[v], ds_row);
+          }
+          put_four(af, half, ta);
+        }
+        frag8 kc[NKT];
+#pragma unroll
+        for (int nt = 0; nt < NKT; ++nt) kc[nt] = lds_col_frag(Ks, TPK, t0, t1, colk + 16 * nt, r);
+#pragma unroll
+        for (int nt = 0; nt < NKT; ++nt) dq[nt] = mma16_add(kc[nt], af, dq[nt]);
+      }
+      if (active) {   // the state after the chunk
+        float wt[8];
+        token_weights(krows + 2 * C, t0, t1, wt);
+        frag8 vcol[ST::NCT];
+#pragma unroll
+        for (int x = 0; x < ST::NCT; ++x) vcol[x] = lds_col_frag(Vs, TPV, t0, t1, 16 * ST::col_tile(rg, cp, x), r);
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y) {
+          const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::row_tile(rg, cp, y), r), wt);
+#pragma unroll
+          for (int x = 0; x < ST::NCT; ++x) sacc[x][y] = mma16_weighted(vcol[x], k, sacc[x][y]);
+        }
+      }
+    }
+
+    const float left = 1.f / ROW_NORM * qrows[16 * rg + r], whole = qrows[3 * C + 16 * rg + r];
+    ds_lane += 1.f / ROW_NORM * left * ds_row;
+    float xv[NKT][4];
+    float t = dot_with_row<NKT, TPK>(dq, Qs + 16 * rg * TPK, colk, xv, r, q4);
+    if (CS > 1) {   // the row's dot product over the columns of all its waves
+      if (q4 == 0) xdot[cp * C + 16 * rg + r] = t;
+      __syncthreads();
+      t = 0.f;
+#pragma unroll
+      for (int i = 0; i < CS; ++i) t += xdot[i * C + 16 * rg + r];
+    }
+    take_out_row<NKT>(dq, xv, t, left, whole, inv_eps);
+    // every wave has read all query rows for G: they take the finished ones
+    if (CS == 1) __syncthreads();
+    gather_rows_transposed<DK, NKT>(dq, 1.f / ROW_NORM * scale * whole, Qs + 16 * rg * TPK, l, finished, un, colk);
+    __syncthreads();
+  }
+  store_row_pieces<DK, NKT>(finished, dQu, row_begin + (row_end - row_begin - 1) / C * C + 16 * rg, row_end, l, colk);
+  if (lengths != nullptr) zero_rows<DK>(dQu, row_end, piece_end);
+  if (with_rev && active) {
+    float* out = rev_totals + (size_t(unit) * G.n + seg) * DK * DV;
+#pragma unroll
+    for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+      for (int y = 0; y < ST::NRT; ++y)
+        store_state_words(out + tiled_state_offset(ST::row_tile(rg, cp, y), ST::col_tile(rg, cp, x), DV / 16, l), racc[x][y]);
+  }
+  ds_lane = group_sum<64>(ds_lane);
+  if (l == 0) ds_wave[w] = ds_lane;
+  __syncthreads();
+  if (tid == 0) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < Cfg::NW; ++i) t += ds_wave[i];
+    *ds_out = t;
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// dK and dV of a segment, last chunk to first.  R sits in accumulators with the values down and the keys along, tile (x, y):
+// element [v] of lane (r, q4) is R[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  The first workgroups also add up
+// ds from what the dQ scan left.
+template <int DK, int DV, int C, int CS>
+COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
+    const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
+    const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ dK, elem_t* __restrict__ dV,
+    const float* __restrict__ rev_states, const float* __restrict__ ds_partial, float* __restrict__ ds,
+    const float* __restrict__ rev_in, float* __restrict__ rev_out, const int* __restrict__ lengths, int B, Divisor H, Divisor G,
+    int seg_rows, int N, float inv_eps, int carried) {
+  using Cfg = DecayBwdCfg<DK, DV, C, CS>;
+  using ST = SplitTiles<DV, DK, Cfg::RG, CS>;   // value rows, key columns
+  using StageK = TileStage<DK, C, Cfg::NT>;
+  using StageV = TileStage<DV, C, Cfg::NT>;
+  constexpr int RG = Cfg::RG, NKT = Cfg::NKT, NVT = Cfg::NVT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
+  COTTN_LDS_ARRAY(lds_t, Qs, Cfg::TILEK, 0)
+  COTTN_LDS_ARRAY(lds_t, Ks, Cfg::TILEK, 1)
+  COTTN_LDS_ARRAY(lds_t, Vs, Cfg::TILEV, 2)
+  COTTN_LDS_ARRAY(lds_t, Gs, Cfg::TILEV, 3)
+  COTTN_LDS_ARRAY(lds_t, Rl, Cfg::STATE, 4)
+  COTTN_LDS_ARRAY(float, krows, 4 * C, 5)
+  COTTN_LDS_ARRAY(float, qrows, 4 * C, 6)
+  COTTN_LDS_ARRAY(float, xdot, CS > 1 ? CS * C : 1, 7)
+  Unparted un;
+  fetch_argument_now(Q, K, V, dO, s, log_decay, dK, dV, rev_states, ds_partial, ds, rev_in, rev_out, lengths, B, H, G, seg_rows,
+                     N, inv_eps, carried);
+  int unit, seg;
+  unit_and_segment(blockIdx.x, B * H.n, G, unit, seg);
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
+  const int rg = w % RG, cp = w / RG;
+  const elem_t* Qu = Q + size_t(unit) * N * DK;
+  const elem_t* Ku = K + size_t(unit) * N * DK;
+  const elem_t* Vu = V + size_t(unit) * N * DV;
+  const elem_t* Gu = dO + size_t(unit) * N * DV;
+  elem_t* dKu = dK + size_t(unit) * N * DK;
+  elem_t* dVu = dV + size_t(unit) * N * DV;
+  const int there = valid_rows(lengths, unit, H, N), row_begin = seg * seg_rows, piece_end = min(N, row_begin + seg_rows);
+  const int row_end = max(row_begin, min(there, piece_end));
+  const int last_row0 = row_begin + (row_end - row_begin - 1) / C * C;
+  StageK qst, kst;
+  StageV vst, gst;
+  if (row_begin < row_end) {
+    qst.fetch(Qu, last_row0, row_end);
+    kst.fetch(Ku, last_row0, row_end);
+    vst.fetch(Vu, last_row0, row_end);
+    gst.fetch(Gu, last_row0, row_end);
+  }
+  // ds[h]: over batches and segments; with lengths ds[b][h], over segments
+  if (int(blockIdx.x) < (lengths != nullptr ? B * H.n : H.n) && w == 0) {
+    float t = 0.f;
+    const int n = lengths != nullptr ? G.n : B * G.n;
+    for (int i = l; i < n; i += 64)
+      t += lengths != nullptr ? ds_partial[size_t(blockIdx.x) * G.n + i]
+                              : ds_partial[(size_t(quotient(i, G)) * H.n + blockIdx.x) * G.n + (i - quotient(i, G) * G.n)];
+    t = group_sum<64>(t);
+    if (l == 0) ds[blockIdx.x] = t;
+  }
+  if (row_begin == row_end && seg > 0) {
+    zero_rows<DK>(dKu, row_begin, piece_end);
+    zero_rows<DV>(dVu, row_begin, piece_end);
+    return;
+  }
+  const int head = unit - quotient(unit, H) * H.n;
+  const Decay g(log_decay[head]);
+  const float scale = s[lengths != nullptr ? unit : head];
+
+  f32x4 racc[ST::NCT][ST::NRT];
+#pragma unroll
+  for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+    for (int y = 0; y < ST::NRT; ++y) racc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bool active = ST::active(rg, cp);
+  if (active && there > piece_end) {
+    const float* slots = rev_states + size_t(unit) * G.n * DK * DV;
+    const int last = (there - 1) / seg_rows;
+    add_decayed_states<true>(racc, carried ? seg : seg + 1, carried ? seg : last, g, seg_rows, [&](int slot, int x, int y) {
+      return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
+                                             tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l));
+    });
+  }
+  if (active && rev_in != nullptr) {
+    const float until = STATE_UNIT * g.after(float(there - row_end));
+    const float* src = rev_in + size_t(unit) * DK * DV;
+#pragma unroll
+    for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+      for (int y = 0; y < ST::NRT; ++y) {
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(rg, cp, x) + r) * DV +
+                                                        16 * ST::row_tile(rg, cp, y) + 4 * q4);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) racc[x][y][v] = __builtin_fmaf(until, t[v], racc[x][y][v]);
+      }
+  }
+
+  const float row = float(16 * rg + r);   // of the chunk: this lane's key
+  float on_diagonal[4];                   // g^(i-j) for the queries i of the tile of the wave's own rows
+#pragma unroll
+  for (int v = 0; v < 4; ++v) on_diagonal[v] = 4 * q4 + v >= r ? g.after(float(4 * q4 + v - r)) : 0.f;
+  const Kept whole_chunk(g, float(C));
+  const int colk = 16 * NKT * cp, colv = 16 * NVT * cp;
+  RowPieces<DK, NKT> done_k;
+  RowPieces<DV, NVT> done_v;
+#pragma unroll
+  for (int j = 0; j < RowPieces<DK, NKT>::PER_LANE; ++j) done_k.v[j] = uint4{0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < RowPieces<DV, NVT>::PER_LANE; ++j) done_v.v[j] = uint4{0u, 0u, 0u, 0u};
+  for (int row0 = last_row0; row0 >= row_begin && row_begin < row_end; row0 -= C) {
+    const int n = min(C, row_end - row0);
+    if (active) {
+      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
+#pragma unroll
+      for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y) {
+          store4_lds(Rl + (16 * ST::col_tile(rg, cp, x) + r) * SP + 16 * ST::row_tile(rg, cp, y) + 4 * q4, PER_UNIT * racc[x][y][0],
+                     PER_UNIT * racc[x][y][1], PER_UNIT * racc[x][y][2], PER_UNIT * racc[x][y][3], un);
+          racc[x][y] = kept.of(racc[x][y]);
+        }
+    }
+    {
+      RowFactors<StageK> f;
+      f.commit(qst, Qs, inv_eps, un);
+      store_factors<StageK, C>(qrows, f, g, [](int i) { return i % 16; }, [](int i) { return i; });
+      f.commit(kst, Ks, inv_eps, un);
+      store_factors<StageK, C>(krows, f, g, [](int) { return 0; }, [](int) { return 0; });
+      vst.commit_plain(Vs, un);
+      gst.commit_plain(Gs, un);
+    }
+    if (row0 > row_begin) {
+      qst.fetch(Qu, row0 - C, row_end);
+      kst.fetch(Ku, row0 - C, row_end);
+      vst.fetch(Vu, row0 - C, row_end);
+      gst.fetch(Gu, row0 - C, row_end);
+    }
+    if (row0 < last_row0) {
+      store_row_pieces<DK, NKT>(done_k, dKu, row0 + C + 16 * rg, row_end, l, colk);
+      store_row_pieces<DV, NVT>(done_v, dVu, row0 + C + 16 * rg, row_end, l, colv);
+    }
+    __syncthreads();
+
+    // what the state gives: dv^T = R^T k^T and dkh^T = R v^T, then the rows' factors
+    frag8 kf[Cfg::KSK], vf[Cfg::KSV];
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSK; ++ks) kf[ks] = lds_row_frag(Ks + (16 * rg + r) * TPK + 32 * ks, q4);
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSV; ++ks) vf[ks] = lds_row_frag(Vs + (16 * rg + r) * TPV + 32 * ks, q4);
+    const float left = 1.f / ROW_NORM * krows[16 * rg + r], whole = krows[3 * C + 16 * rg + r];
+    f32x4 dk[NKT], dv[NVT];
+#pragma unroll
+    for (int nt = 0; nt < NKT; ++nt) dk[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int nt = 0; nt < NVT; ++nt) dv[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSK; ++ks) {
+      frag8 rcol[NVT];
+#pragma unroll
+      for (int nt = 0; nt < NVT; ++nt) rcol[nt] = lds_col_frag_ks(Rl, SP, ks, q4, colv + 16 * nt, r);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NVT; ++nt) dv[nt] = mma16(rcol[nt], kf[ks], dv[nt]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < Cfg::KSV; ++ks) {
+      frag8 rrow[NKT];
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) rrow[nt] = lds_row_frag(Rl + (colk + 16 * nt + r) * SP + 32 * ks, q4);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) dk[nt] = mma16(rrow[nt], vf[ks], dk[nt]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float to_end = g.after(fmaxf(float(n) - row, 0.f));
+#pragma unroll
+    for (int nt = 0; nt < NVT; ++nt)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) dv[nt][v] *= left * to_end;
+#pragma unroll
+    for (int nt = 0; nt < NKT; ++nt)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) dk[nt][v] *= ROW_NORM * to_end;
+
+    // the chunk itself, 32 queries at a time
+#pragma unroll
+    for (int p = 0; p < Cfg::NP; ++p) {
+      const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+      if (2 * p + 1 >= rg) {
+        frag8 pf, af;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int it = 2 * p + half;
+          f32x4 tp = {0.f, 0.f, 0.f, 0.f}, ta = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSK; ++ks) tp = mma16(lds_row_frag(Qs + (16 * it + r) * TPK + 32 * ks, q4), kf[ks], tp);
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSV; ++ks) ta = mma16(lds_row_frag(Gs + (16 * it + r) * TPV + 32 * ks, q4), vf[ks], ta);
+          // tp[v] = q_(16 it + 4 q4 + v) . k_(16 rg + r)
+          const f32x4 qi = *reinterpret_cast<const f32x4*>(qrows + (it == rg ? 0 : C) + 16 * it + 4 * q4);
+          const float above = g.after(float(16 * it) - row);   // (it > rg)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float f = it < rg ? 0.f : qi[v] * (it == rg ? on_diagonal[v] : above);
+            tp[v] = it < rg ? 0.f : tp[v] * (f * (1.f / ROW_NORM * left));
+            ta[v] = it < rg ? 0.f : ta[v] * f;
+          }
+          put_four(pf, half, tp);
+          put_four(af, half, ta);
+        }
+        frag8 gc[NVT], qc[NKT];
+#pragma unroll
+        for (int nt = 0; nt < NVT; ++nt) gc[nt] = lds_col_frag(Gs, TPV, t0, t1, colv + 16 * nt, r);
+#pragma unroll
+        for (int nt = 0; nt < NVT; ++nt) dv[nt] = mma16_add(gc[nt], pf, dv[nt]);
+#pragma unroll
+        for (int nt = 0; nt < NKT; ++nt) qc[nt] = lds_col_frag(Qs, TPK, t0, t1, colk + 16 * nt, r);
+#pragma unroll
+        for (int nt = 0; nt < NKT; ++nt) dk[nt] = mma16_add(qc[nt], af, dk[nt]);
+      }
+      if (active) {   // the state before the chunk
+        float wt[8];
+        token_weights(qrows + 2 * C, t0, t1, wt);
+        frag8 grow[ST::NRT];
+#pragma unroll
+        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
+#pragma unroll
+        for (int x = 0; x < ST::NCT; ++x) {
+          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
+#pragma unroll
+          for (int y = 0; y < ST::NRT; ++y) racc[x][y] = mma16_weighted(grow[y], q, racc[x][y]);
+        }
+      }
+    }
+
+    float xv[NKT][4];
+    float t = dot_with_row<NKT, TPK>(dk, Ks + 16 * rg * TPK, colk, xv, r, q4);
+    if (CS > 1) {
+      if (q4 == 0) xdot[cp * C + 16 * rg + r] = t;
+      __syncthreads();   // and the rows of Ks and Vs are read by all waves of the row group
+      t = 0.f;
+#pragma unroll
+      for (int i = 0; i < CS; ++i) t += xdot[i * C + 16 * rg + r];
+    }
+    take_out_row<NKT>(dk, xv, t, left, whole, inv_eps);
+    // (the row group's own rows of Ks and Vs are read by its own waves only)
+    if (CS == 1) wave_lds_sync();
+    gather_rows_transposed<DK, NKT>(dk, 1.f / ROW_NORM * scale * whole, Ks + 16 * rg * TPK, l, done_k, un, colk);
+    gather_rows_transposed<DV, NVT>(dv, scale, Vs + 16 * rg * TPV, l, done_v, un, colv);
+    __syncthreads();
+  }
+  if (row_begin < row_end) {
+    store_row_pieces<DK, NKT>(done_k, dKu, row_begin + 16 * rg, row_end, l, colk);
+    store_row_pieces<DV, NVT>(done_v, dVu, row_begin + 16 * rg, row_end, l, colv);
+  }
+  if (lengths != nullptr) {
+    zero_rows<DK>(dKu, row_end, piece_end);
+    zero_rows<DV>(dVu, row_end, piece_end);
+  }
+  if (rev_out != nullptr && seg == 0 && active) {
+    float* out = rev_out + size_t(unit) * DK * DV;
+#pragma unroll
+    for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+      for (int y = 0; y < ST::NRT; ++y)
+        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(rg, cp, x) + r) * DV + 16 * ST::row_tile(rg, cp, y) + 4 * q4) =
+            PER_UNIT * racc[x][y];
+  }
+}
+
+template <int DK, int DV, int C, int CS>
+hipError_t run_bwd_decay(const DecayArgs& a) {
+  const int units = a.B * a.H;
+  const elem_t* Q = static_cast<const elem_t*>(a.Q);
+  const elem_t* K = static_cast<const elem_t*>(a.K);
+  const elem_t* V = static_cast<const elem_t*>(a.V);
+  const elem_t* dO = static_cast<const elem_t*>(a.dO);
+  char* ws = static_cast<char*>(a.workspace);
+  const size_t states = state_slots_bytes(a.G > 1 ? long(units) * a.G : 0, DK, DV);
+  float* own_fwd = reinterpret_cast<float*>(ws);
+  float* rev = reinterpret_cast<float*>(ws + states);
+  float* ds_partial = reinterpret_cast<float*>(ws + 2 * states);
+  const float* fwd = a.saved_fwd_states;
+  hipError_t err = hipSuccess;
+  if (a.G > 1 && fwd == nullptr) {
+    err = COTTN_SYM(launch_decay_totals)(a, own_fwd);
+    if (err == hipSuccess && a.carried) err = launch_decay_carry(a, own_fwd, false);
+    if (err != hipSuccess) return err;
+    fwd = own_fwd;
+  }
+  const dim3 grid(units * a.G), block(64 * (C / 16) * CS);
+  const Divisor H(a.H), G(a.G);
+  const float inv_eps = 1.0f / a.eps;
+  err = launch_kernel(COTTN_SYM_STR(bwd_decay_dq), COTTN_SYM(bwd_decay_dq)<DK, DV, C, CS>, grid, block, 0, a.stream, Q, K, V, dO, a.s,
+                      a.log_decay, static_cast<elem_t*>(a.dQ), fwd, rev, ds_partial, a.state_in, a.seq_len, H, G, a.seg_rows, a.N,
+                      units, inv_eps, int(a.carried));
+  if (err == hipSuccess && a.G > 1 && a.carried) err = launch_decay_carry(a, rev, true);
+  if (err != hipSuccess) return err;
+  return launch_kernel(COTTN_SYM_STR(bwd_decay_dkdv), COTTN_SYM(bwd_decay_dkdv)<DK, DV, C, CS>, grid, block, 0, a.stream, Q, K, V, dO,
+                       a.s, a.log_decay, static_cast<elem_t*>(a.dK), static_cast<elem_t*>(a.dV), rev, ds_partial, a.ds,
+                       a.rev_state_in, a.rev_state_out, a.seq_len, a.B, H, G, a.seg_rows, a.N, inv_eps, int(a.carried));
+}
+
+}  // namespace
+}  // namespace COTTN_NS
+
+using namespace COTTN_NS;
+
+// Rows of a chunk and waves on a row group: as in the backward without decay (bwd_causal_bf16.hip: BwdSplit).
+hipError_t COTTN_SYM(bwd_decay)(const DecayArgs& a) {
+#define COTTN_CASE(DK, DV)                                                                                             \
+  case DK * 1000 + DV: {                                                                                               \
+    constexpr bool WIDE = DK != DV && DK >= 64 && DV >= 64;                                                            \
+    return run_bwd_decay<DK, DV, ELEM_IS_F32 || WIDE ? 32 : 64, ELEM_IS_F32 || WIDE || (DK == 128 && DV == 128) ? 2 : 1>(a); \
+  }
+  switch (a.dk * 1000 + a.dv) {
+    COTTN_CASE(32, 32) COTTN_CASE(32, 64) COTTN_CASE(32, 128) COTTN_CASE(64, 32) COTTN_CASE(64, 64) COTTN_CASE(64, 128)
+    COTTN_CASE(128, 32) COTTN_CASE(128, 64) COTTN_CASE(128, 128)
+    default: return hipErrorInvalidValue;
+  }
+#undef COTTN_CASE
+}
+
+}  // namespace cottn

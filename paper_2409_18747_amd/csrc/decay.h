@@ -1,0 +1,206 @@
+// What the kernels of attention with a decay for each head share.  With g = exp(log_decay[h]) the state
+// before row i + 1 is H_i = g H_(i-1) + kh_i^T v_i, so that row j reaches row i with the weight g^(i-j).
+//
+// A chunk takes rows b .. e-1 (n = e - b of them); H is the state after row b-1 and R = sum over i >= e of
+// g^(i-e) qh_i^T dO_i the reverse-time state.  Then with i', j' counted from b
+//     o_i   = s [ g^(i'+1) qh_i H + sum_{j<=i} g^(i-j) (qh_i . kh_j) v_j ],   H <- g^n H + sum_j g^(n-1-j') kh_j^T v_j
+//     dqh_i = s [ g^(i'+1) dO_i H^T + sum_{j<=i} g^(i-j) (dO_i . v_j) kh_j ]
+//     dkh_j = s [ g^(n-j') v_j R^T + sum_{i>=j} g^(i-j) (dO_i . v_j) qh_i ]
+//     dv_j  = s [ g^(n-j') kh_j R + sum_{i>=j} g^(i-j) (qh_i . kh_j) dO_i ],  R <- g^n R + sum_i g^i' qh_i^T dO_i
+// Every exponent that is formed is one of these, or a part of one that is not negative itself: a weight may
+// underflow, none overflows, however strong the decay.
+//
+// Included behind tile_io.h, and as often.
+
+namespace cottn {
+namespace COTTN_NS {
+
+#ifdef COTTN_ELEM_F16
+constexpr bool ELEM_IS_F16 = true;
+#else
+constexpr bool ELEM_IS_F16 = false;
+#endif
+
+// The decay of a head as logarithms.  Values above 0 count as 0; one of -inf (nothing is kept) becomes a finite
+// number, so that 0 rows later the weight is 1 and not NaN.
+struct Decay {
+  float ln, l2;
+  __device__ __forceinline__ explicit Decay(float log_decay) {
+    ln = log_decay > 0.f ? 0.f : log_decay;
+    ln = ln < -1e30f ? -1e30f : ln;   // (NaN stays)
+    l2 = 1.44269504f * ln;
+  }
+  // g^n for n >= 0
+  __device__ __forceinline__ float after(float n) const { return __builtin_amdgcn_exp2f(l2 * n); }
+};
+
+// What a state is multiplied by n rows later: x * times + x * plus.  A factor just below 1 is 1 - d with a d of its own, whose
+// relative error is that of fp32: as one rounded number, g^64 of a head that hardly forgets would be off by up to 2^-25
+// with the same sign in every chunk, 3e-5 of what is oldest after 1024 chunks.
+struct Kept {
+  float times, plus;
+  __device__ __forceinline__ Kept(const Decay& g, float n) {
+    const float d = -expm1f(g.ln * n);
+    times = d < 0.5f ? 1.f : g.after(n);
+    plus = d < 0.5f ? -d : 0.f;
+  }
+  __device__ __forceinline__ f32x4 of(f32x4 x) const {
+    f32x4 y;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) y[v] = __builtin_fmaf(x[v], plus, x[v] * times);
+    return y;
+  }
+};
+
+// Rows are raw in LDS and every factor of a row (1 / norm, decay) goes to fp32 results, to the masked tiles before they are
+// rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.
+//   fp16: rows of q and k times the power of two that brings their norm to 32 .. 64 (exact but for elements 2^-20 below the
+// norm), so that the factors left are alike for short and long rows.  The tiles of dO . v take them ROW_NORM times larger and
+// leave fp16 for none of them, neither for the 1 / eps of a short row nor for the small ones of a long one.
+constexpr float ROW_NORM = ELEM_IS_F16 ? 64.f : 1.f;
+template <class Stage>
+struct RowFactors {
+  float left[Stage::PASSES];    // what the row in the tile is to be multiplied by
+  float whole[Stage::PASSES];   // min(1 / norm, 1 / eps)
+  __device__ __forceinline__ void commit(const Stage& stage, lds_t* tile, float inv_eps, Unparted& un) {
+    stage.row_rinv(inv_eps, whole);
+    if constexpr (ELEM_IS_F16) {
+      float power[Stage::PASSES];
+#pragma unroll
+      for (int p = 0; p < Stage::PASSES; ++p) {
+        const uint32_t bits = __builtin_bit_cast(uint32_t, whole[p]);
+        power[p] = 0.5f * ROW_NORM * __builtin_bit_cast(float, bits & 0x7F800000u);
+        left[p] = 2.f / ROW_NORM * __builtin_bit_cast(float, (bits & 0x007FFFFFu) | 0x3F800000u);
+      }
+      stage.commit_scaled(tile, power, un);
+    } else {
+#pragma unroll
+      for (int p = 0; p < Stage::PASSES; ++p) left[p] = whole[p];
+      stage.commit_plain(tile, un);
+    }
+  }
+};
+
+// An operand fragment whose k slots are tokens, each token's values times a weight: in two parts, the second what rounding the
+// first left over (16 bits and more of the product together), since states are results in fp32 and ds is formed from them.
+// Whole fp32: one.
+struct WeightedFrag {
+  frag8 first;
+#ifndef COTTN_ELEM_F32
+  frag8 rest;
+#endif
+};
+__device__ __forceinline__ WeightedFrag weighted(const frag8& x, const float (&w)[8]) {
+  WeightedFrag f;
+#if defined(COTTN_F32_WHOLE)
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.first[j] = x[j] * w[j];
+#elif !defined(COTTN_ELEM_F32)
+  const u32x4 words = __builtin_bit_cast(u32x4, x);
+  u32x4 hi, lo;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b, ha, hb;
+    unpack2(words[i], a, b);
+    hi[i] = pack2(a * w[2 * i], b * w[2 * i + 1]);
+    unpack2(hi[i], ha, hb);
+    lo[i] = pack2(__builtin_fmaf(a, w[2 * i], -ha), __builtin_fmaf(b, w[2 * i + 1], -hb));
+  }
+  f.first = __builtin_bit_cast(frag8, hi);
+  f.rest = __builtin_bit_cast(frag8, lo);
+#endif
+  return f;
+}
+// sum += a b over 32 tokens, the weighted operand second
+__device__ __forceinline__ f32x4 mma16_weighted(const frag8& a, const WeightedFrag& b, f32x4 sum) {
+#ifndef COTTN_ELEM_F32
+  sum = mma16(a, b.rest, sum);
+  return mma16(a, b.first, sum);
+#else
+  return mma16_add(a, b.first, sum);
+#endif
+}
+// the weights of the tokens t0 .. t0+3 and t1 .. t1+3
+__device__ __forceinline__ void token_weights(const float* of, int t0, int t1, float (&w)[8]) {
+  const f32x4 lo = *reinterpret_cast<const f32x4*>(of + t0), hi = *reinterpret_cast<const f32x4*>(of + t1);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    w[v] = lo[v];
+    w[4 + v] = hi[v];
+  }
+}
+
+// Accumulators hold states in units of 1 / STATE_UNIT, and the weights that tokens enter them with are as many times larger: in
+// fp16 the second part of kh_j g^n, 2^-11 of it, would else lie below the smallest normal number (2^-14) and lose up to 2^-25,
+// whatever the weight.  (|kh| <= 1: no product is over 2^14.)
+constexpr float STATE_UNIT = ELEM_IS_F16 ? 16384.f : 1.f, PER_UNIT = 1.f / STATE_UNIT;
+
+// Fills half of an operand fragment with four values.
+__device__ __forceinline__ void put_four(frag8& frag, int half, f32x4 x) {
+#if defined(COTTN_F32_WHOLE)
+#pragma unroll
+  for (int v = 0; v < 4; ++v) frag[4 * half + v] = x[v];
+#elif !defined(COTTN_ELEM_F32)
+  u32x4 words = __builtin_bit_cast(u32x4, frag);
+  words[2 * half + 0] = pack2(x[0], x[1]);
+  words[2 * half + 1] = pack2(x[2], x[3]);
+  frag = __builtin_bit_cast(frag8, words);
+#endif
+}
+
+// The states that other workgroups left at the start of segment g: sum over the slots first .. last of g^(seg_rows * (distance
+// from `last` or `first`)), nearest slot with weight 1, two at a time with all loads before the first addition.
+template <bool REVERSE, int NCT, int NRT, class LoadTile>
+__device__ __forceinline__ void add_decayed_states(f32x4 (&acc)[NCT][NRT], int first, int last, const Decay& g, int seg_rows,
+                                                   LoadTile load) {
+  constexpr int BATCH = states_at_once(NCT * NRT);
+  for (int base = first; base <= last; base += BATCH) {
+    f32x4 t[BATCH][NCT][NRT];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+      for (int x = 0; x < NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < NRT; ++y) t[i][x][y] = load(min(base + i, last), x, y);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      if (base + i > last) break;
+      const float w = g.after(float(REVERSE ? base + i - first : last - base - i) * float(seg_rows));
+#pragma unroll
+      for (int x = 0; x < NCT; ++x)
+#pragma unroll
+        for (int y = 0; y < NRT; ++y)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) acc[x][y][v] = __builtin_fmaf(w, t[i][x][y][v], acc[x][y][v]);
+    }
+  }
+}
+
+// A tree of up to 64 drafted tokens, lane l with node l: parent[i] is a node before i; any other value makes i a root.
+// path: the node and its ancestors as bits (in the order of their depths, since parents come first).
+struct TreeNode {
+  unsigned long long path = 0;
+  __device__ __forceinline__ TreeNode(const int* __restrict__ parent, int n_tokens, int l) {
+    int up = l < n_tokens ? parent[l] : -1;
+    up = up >= 0 && up < l ? up : -1;
+    path = 1ull << l;
+#pragma unroll
+    for (int i = 0; i < 6; ++i) {   // paths of 2^i nodes, then of twice as many
+      const unsigned long long above = __shfl(path, up < 0 ? l : up, 64);
+      const int next = __shfl(up, up < 0 ? l : up, 64);
+      path |= above;
+      up = next;
+    }
+  }
+  __device__ __forceinline__ int depth() const { return __builtin_popcountll(path) - 1; }
+};
+
+// waves per SIMD that registers are capped for: two workgroups to a compute unit where the LDS holds them
+constexpr int decay_waves(int lds_bytes, int waves, int waves_per_group) {
+  const int own = waves / 4 < 1 ? 1 : waves / 4, at_once = (160 * 1024) / lds_bytes >= 2 ? 2 : 1;
+  const int most = waves_per_group > 1 ? 4 : 2;
+  return own * at_once <= most ? own * at_once : own > most ? own : most;
+}
+
+}  // namespace COTTN_NS
+}  // namespace cottn

@@ -247,6 +247,44 @@ struct StepArgs {
   hipStream_t stream;
 };
 
+// Attention with a decay for each head (decay.h): G segments of seg_rows rows, a whole number of chunks, per (batch, head).
+// The states that other workgroups need are the segments' totals, which the scans weigh and add up, or `carried`, when
+// a launch of its own has turned them into the states at the segments' starts (reverse-time: ends).
+struct DecayArgs {
+  const void* Q; const void* K; const void* V; const float* s; const float* log_decay;
+  const void* dO;                   // backward only
+  void* O; float* state;            // forward only (state may be null)
+  const float* state_in;            // may be null
+  const float* rev_state_in; float* rev_state_out;   // backward only, may be null
+  const int* seq_len;               // null, or int[B] row counts: then s and ds are [B][H]
+  void* dQ; void* dK; void* dV; float* ds;           // backward only
+  const float* saved_fwd_states;    // backward only: null, or what the forward left in its workspace
+  void* workspace;
+  int B, H, N, dk, dv, G, seg_rows;
+  bool carried;
+  float eps;
+  hipStream_t stream;
+};
+
+struct StepDecayArgs {
+  const void* q; const void* k; const void* v; const float* s; const float* log_decay;   // log_decay may be null: no decay
+  const float* from; const int* parent; int n_from;   // states of n_from sequences; parent null or int[B]
+  float* to; void* o;
+  int B, H, dk, dv;
+  float eps;
+  hipStream_t stream;
+};
+
+// A tree of n_tokens <= 64 drafted tokens for each sequence: q, k [B][H][n_tokens][dk], v, o [B][H][n_tokens][dv], parent
+// int[B][n_tokens]; accepting takes last int[B] and no q, s, o.
+struct TreeArgs {
+  const void* q; const void* k; const void* v; const float* s; const float* log_decay;
+  const int* parent; const int* last; float* state; void* o;
+  int B, H, n_tokens, dk, dv;
+  float eps;
+  hipStream_t stream;
+};
+
 // defined in the kernel files; every function only enqueues work on args.stream
 hipError_t fwd_causal_bf16(const CausalArgs& a);
 hipError_t bwd_causal_bf16(const CausalArgs& a);
@@ -266,6 +304,22 @@ hipError_t bwd_causal_f32w(const CausalArgs& a);
 hipError_t fwd_bidir_f32w(const CausalArgs& a);
 hipError_t bwd_bidir_f32w(const CausalArgs& a);
 hipError_t step_any(const StepArgs& a, int dtype);
+hipError_t fwd_decay_bf16(const DecayArgs& a);
+hipError_t bwd_decay_bf16(const DecayArgs& a);
+hipError_t fwd_decay_f16(const DecayArgs& a);
+hipError_t bwd_decay_f16(const DecayArgs& a);
+hipError_t fwd_decay_f32w(const DecayArgs& a);
+hipError_t bwd_decay_f32w(const DecayArgs& a);
+// totals of all segments but the last, and their carrying (for both passes)
+hipError_t launch_decay_totals_bf16(const DecayArgs& a, float* dst);
+hipError_t launch_decay_totals_f16(const DecayArgs& a, float* dst);
+hipError_t launch_decay_totals_f32w(const DecayArgs& a, float* dst);
+hipError_t launch_decay_carry(const DecayArgs& a, float* slots, bool reverse);
+hipError_t step_decay_any(const StepDecayArgs& a, int dtype);
+hipError_t tree_bf16(const TreeArgs& a);
+hipError_t tree_f16(const TreeArgs& a);
+hipError_t tree_f32w(const TreeArgs& a);
+hipError_t tree_accept_any(const TreeArgs& a, int dtype);
 
 // small fp32 state kernels shared by all element types (defined next to their kernels)
 hipError_t launch_fwd_state_carry(float* seg_state, int units, int G, int elems, hipStream_t st);
