@@ -61,7 +61,8 @@ __device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stag
 
 // ---------------------------------------------------------------------------------------
 // dQ of a segment, first chunk to last.  H and G sit in accumulators with the values down and the keys along, tile (x, y):
-// element [v] of lane (r, q4) is H[key 16 row_tile(y) + r][value 16 col_tile(x) + 4 q4 + v].
+// element [v] of lane (r, q4) is H[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  A wave has few key tiles and all
+// values (of its part): fragments of keys and queries are the ones that weights go to, 40 instructions each.
 template <int DK, int DV, int C, int CS>
 COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
@@ -70,7 +71,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const float* __restrict__ state_in, const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units,
     float inv_eps, int carried) {
   using Cfg = DecayBwdCfg<DK, DV, C, CS>;
-  using ST = SplitTiles<DK, DV, Cfg::RG, CS>;   // key rows, value columns
+  using ST = SplitTiles<DV, DK, Cfg::RG, CS>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
   using StageV = TileStage<DV, C, Cfg::NT>;
   constexpr int RG = Cfg::RG, NKT = Cfg::NKT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
@@ -123,7 +124,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const float* slots = fwd_states + size_t(unit) * G.n * DK * DV;
     add_decayed_states<false>(sacc, carried ? seg : 0, carried ? seg : seg - 1, g, seg_rows, [&](int slot, int x, int y) {
       return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
-                                             tiled_state_offset(ST::row_tile(rg, cp, y), ST::col_tile(rg, cp, x), DV / 16, l));
+                                             tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l));
     });
   }
   if (active && state_in != nullptr) {
@@ -133,8 +134,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::row_tile(rg, cp, y) + r) * DV +
-                                                        16 * ST::col_tile(rg, cp, x) + 4 * q4);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(rg, cp, x) + r) * DV +
+                                                        16 * ST::row_tile(rg, cp, y) + 4 * q4);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sacc[x][y][v] = __builtin_fmaf(since, t[v], sacc[x][y][v]);
       }
@@ -157,7 +158,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
         for (int y = 0; y < ST::NRT; ++y)
-          store4_lds(St + (16 * ST::row_tile(rg, cp, y) + r) * SP + 16 * ST::col_tile(rg, cp, x) + 4 * q4, PER_UNIT * sacc[x][y][0],
+          store4_lds(St + (16 * ST::col_tile(rg, cp, x) + r) * SP + 16 * ST::row_tile(rg, cp, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
                      PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
     }
     {
@@ -190,14 +191,13 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
         const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
         float wt[8];
         token_weights(qrows + 2 * C, t0, t1, wt);
-        frag8 gcol[ST::NCT];
+        frag8 grow[ST::NRT];
 #pragma unroll
-        for (int x = 0; x < ST::NCT; ++x) gcol[x] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::col_tile(rg, cp, x), r);
+        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) {
-          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::row_tile(rg, cp, y), r), wt);
-#pragma unroll
-          for (int x = 0; x < ST::NCT; ++x) gacc[x][y] = mma16_weighted(gcol[x], q, gacc[x][y]);
+        for (int x = 0; x < ST::NCT; ++x) {
+          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
+          mma16_weighted(grow, q, [&](int y) -> f32x4& { return gacc[x][y]; });
         }
       }
       const float at = g.after(float(row0 - row_begin));
@@ -280,14 +280,13 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
       if (active) {   // the state after the chunk
         float wt[8];
         token_weights(krows + 2 * C, t0, t1, wt);
-        frag8 vcol[ST::NCT];
+        frag8 vrow[ST::NRT];
 #pragma unroll
-        for (int x = 0; x < ST::NCT; ++x) vcol[x] = lds_col_frag(Vs, TPV, t0, t1, 16 * ST::col_tile(rg, cp, x), r);
+        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) {
-          const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::row_tile(rg, cp, y), r), wt);
-#pragma unroll
-          for (int x = 0; x < ST::NCT; ++x) sacc[x][y] = mma16_weighted(vcol[x], k, sacc[x][y]);
+        for (int x = 0; x < ST::NCT; ++x) {
+          const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
+          mma16_weighted(vrow, k, [&](int y) -> f32x4& { return sacc[x][y]; });
         }
       }
     }
@@ -317,7 +316,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        store_state_words(out + tiled_state_offset(ST::row_tile(rg, cp, y), ST::col_tile(rg, cp, x), DV / 16, l), racc[x][y]);
+        store_state_words(out + tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l), racc[x][y]);
   }
   ds_lane = group_sum<64>(ds_lane);
   if (l == 0) ds_wave[w] = ds_lane;
@@ -558,8 +557,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
 #pragma unroll
         for (int x = 0; x < ST::NCT; ++x) {
           const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
-#pragma unroll
-          for (int y = 0; y < ST::NRT; ++y) racc[x][y] = mma16_weighted(grow[y], q, racc[x][y]);
+          mma16_weighted(grow, q, [&](int y) -> f32x4& { return racc[x][y]; });
         }
       }
     }

@@ -81,44 +81,52 @@ struct RowFactors {
   }
 };
 
-// An operand fragment whose k slots are tokens, each token's values times a weight: in two parts, the second what rounding the
-// first left over (16 bits and more of the product together), since states are results in fp32 and ds is formed from them.
-// Whole fp32: one.
-struct WeightedFrag {
-  frag8 first;
-#ifndef COTTN_ELEM_F32
-  frag8 rest;
+// An operand fragment whose k slots are tokens, each token's values times a weight, in parts: each the rest that rounding the
+// ones before left over, until fp32 has no more.  States are results in fp32 and ds is formed from them, so bfloat16 takes
+// three (two leave up to 2^-17 of a product, 2.4e-6 of a state in the mean), fp16 two; whole fp32 one.
+#if defined(COTTN_ELEM_F32)
+constexpr int WEIGHTED_PARTS = 1;
+#elif defined(COTTN_ELEM_F16)
+constexpr int WEIGHTED_PARTS = 2;
+#else
+constexpr int WEIGHTED_PARTS = 3;
 #endif
-};
+struct WeightedFrag { frag8 part[WEIGHTED_PARTS]; };
 __device__ __forceinline__ WeightedFrag weighted(const frag8& x, const float (&w)[8]) {
   WeightedFrag f;
 #if defined(COTTN_F32_WHOLE)
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f.first[j] = x[j] * w[j];
+  for (int j = 0; j < 8; ++j) f.part[0][j] = x[j] * w[j];
 #elif !defined(COTTN_ELEM_F32)
   const u32x4 words = __builtin_bit_cast(u32x4, x);
-  u32x4 hi, lo;
+  u32x4 parts[WEIGHTED_PARTS];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a, b, ha, hb;
+    float a, b, pa, pb;
     unpack2(words[i], a, b);
-    hi[i] = pack2(a * w[2 * i], b * w[2 * i + 1]);
-    unpack2(hi[i], ha, hb);
-    lo[i] = pack2(__builtin_fmaf(a, w[2 * i], -ha), __builtin_fmaf(b, w[2 * i + 1], -hb));
+    parts[0][i] = pack2(a * w[2 * i], b * w[2 * i + 1]);
+    unpack2(parts[0][i], pa, pb);
+    a = __builtin_fmaf(a, w[2 * i], -pa);
+    b = __builtin_fmaf(b, w[2 * i + 1], -pb);
+    parts[1][i] = pack2(a, b);
+    if constexpr (WEIGHTED_PARTS > 2) {
+      unpack2(parts[1][i], pa, pb);
+      parts[2][i] = pack2(a - pa, b - pb);
+    }
   }
-  f.first = __builtin_bit_cast(frag8, hi);
-  f.rest = __builtin_bit_cast(frag8, lo);
+#pragma unroll
+  for (int i = 0; i < WEIGHTED_PARTS; ++i) f.part[i] = __builtin_bit_cast(frag8, parts[i]);
 #endif
   return f;
 }
-// sum += a b over 32 tokens, the weighted operand second
-__device__ __forceinline__ f32x4 mma16_weighted(const frag8& a, const WeightedFrag& b, f32x4 sum) {
-#ifndef COTTN_ELEM_F32
-  sum = mma16(a, b.rest, sum);
-  return mma16(a, b.first, sum);
-#else
-  return mma16_add(a, b.first, sum);
-#endif
+// sums[i] += rows[i] w over 32 tokens for the N tiles that share the weighted operand: part by part, the smallest first, so that
+// neighbouring matrix instructions do not wait for each other's sums
+template <int N, class Sum>
+__device__ __forceinline__ void mma16_weighted(const frag8 (&rows)[N], const WeightedFrag& w, Sum sum) {
+#pragma unroll
+  for (int p = WEIGHTED_PARTS - 1; p >= 0; --p)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum(i) = mma16_add(rows[i], w.part[p], sum(i));
 }
 // the weights of the tokens t0 .. t0+3 and t1 .. t1+3
 __device__ __forceinline__ void token_weights(const float* of, int t0, int t1, float (&w)[8]) {

@@ -33,14 +33,13 @@ struct DecayFwdCfg {
 // S[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].
 template <class ST, int TPK>
 __device__ __forceinline__ void add_tokens(f32x4 (&acc)[ST::NCT][ST::NRT], const lds_t* Ks, const float* weights,
-                                           const frag8* vrow, int t0, int t1, int rg, int cp, int r) {
+                                           const frag8 (&vrow)[ST::NRT], int t0, int t1, int rg, int cp, int r) {
   float w[8];
   token_weights(weights, t0, t1, w);
 #pragma unroll
   for (int x = 0; x < ST::NCT; ++x) {
     const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), w);
-#pragma unroll
-    for (int y = 0; y < ST::NRT; ++y) acc[x][y] = mma16_weighted(vrow[y], k, acc[x][y]);
+    mma16_weighted(vrow, k, [&](int y) -> f32x4& { return acc[x][y]; });
   }
 }
 
