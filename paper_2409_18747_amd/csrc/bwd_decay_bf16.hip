@@ -71,7 +71,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const float* __restrict__ state_in, const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units,
     float inv_eps, int carried) {
   using Cfg = DecayBwdCfg<DK, DV, C, CS>;
-  using ST = SplitTiles<DV, DK, Cfg::RG, CS>;   // value rows, key columns
+  using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
   using StageV = TileStage<DV, C, Cfg::NT>;
   constexpr int RG = Cfg::RG, NKT = Cfg::NKT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
@@ -119,12 +119,12 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
   for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
     for (int y = 0; y < ST::NRT; ++y) sacc[x][y] = racc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const bool active = ST::active(rg, cp), with_rev = seg > 0;   // (no workgroup needs the first segment's total)
+  const bool active = ST::active(w), with_rev = seg > 0;   // (no workgroup needs the first segment's total)
   if (active && seg > 0) {
     const float* slots = fwd_states + size_t(unit) * G.n * DK * DV;
     add_decayed_states<false>(sacc, carried ? seg : 0, carried ? seg : seg - 1, g, seg_rows, [&](int slot, int x, int y) {
       return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
-                                             tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l));
+                                             tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l));
     });
   }
   if (active && state_in != nullptr) {
@@ -134,8 +134,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(rg, cp, x) + r) * DV +
-                                                        16 * ST::row_tile(rg, cp, y) + 4 * q4);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(w, x) + r) * DV +
+                                                        16 * ST::row_tile(w, y) + 4 * q4);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sacc[x][y][v] = __builtin_fmaf(since, t[v], sacc[x][y][v]);
       }
@@ -158,7 +158,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
         for (int y = 0; y < ST::NRT; ++y)
-          store4_lds(St + (16 * ST::col_tile(rg, cp, x) + r) * SP + 16 * ST::row_tile(rg, cp, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
+          store4_lds(St + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
                      PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
     }
     {
@@ -193,10 +193,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
         token_weights(qrows + 2 * C, t0, t1, wt);
         frag8 grow[ST::NRT];
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
+        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
 #pragma unroll
         for (int x = 0; x < ST::NCT; ++x) {
-          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
+          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
           mma16_weighted(grow, q, [&](int y) -> f32x4& { return gacc[x][y]; });
         }
       }
@@ -282,10 +282,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
         token_weights(krows + 2 * C, t0, t1, wt);
         frag8 vrow[ST::NRT];
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
+        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
 #pragma unroll
         for (int x = 0; x < ST::NCT; ++x) {
-          const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
+          const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
           mma16_weighted(vrow, k, [&](int y) -> f32x4& { return sacc[x][y]; });
         }
       }
@@ -316,7 +316,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        store_state_words(out + tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l), racc[x][y]);
+        store_state_words(out + tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l), racc[x][y]);
   }
   ds_lane = group_sum<64>(ds_lane);
   if (l == 0) ds_wave[w] = ds_lane;
@@ -341,7 +341,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     const float* __restrict__ rev_in, float* __restrict__ rev_out, const int* __restrict__ lengths, int B, Divisor H, Divisor G,
     int seg_rows, int N, float inv_eps, int carried) {
   using Cfg = DecayBwdCfg<DK, DV, C, CS>;
-  using ST = SplitTiles<DV, DK, Cfg::RG, CS>;   // value rows, key columns
+  using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
   using StageV = TileStage<DV, C, Cfg::NT>;
   constexpr int RG = Cfg::RG, NKT = Cfg::NKT, NVT = Cfg::NVT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
@@ -401,13 +401,13 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
   for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
     for (int y = 0; y < ST::NRT; ++y) racc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const bool active = ST::active(rg, cp);
+  const bool active = ST::active(w);
   if (active && there > piece_end) {
     const float* slots = rev_states + size_t(unit) * G.n * DK * DV;
     const int last = (there - 1) / seg_rows;
     add_decayed_states<true>(racc, carried ? seg : seg + 1, carried ? seg : last, g, seg_rows, [&](int slot, int x, int y) {
       return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
-                                             tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l));
+                                             tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l));
     });
   }
   if (active && rev_in != nullptr) {
@@ -417,8 +417,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(rg, cp, x) + r) * DV +
-                                                        16 * ST::row_tile(rg, cp, y) + 4 * q4);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(w, x) + r) * DV +
+                                                        16 * ST::row_tile(w, y) + 4 * q4);
 #pragma unroll
         for (int v = 0; v < 4; ++v) racc[x][y][v] = __builtin_fmaf(until, t[v], racc[x][y][v]);
       }
@@ -444,7 +444,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
         for (int y = 0; y < ST::NRT; ++y) {
-          store4_lds(Rl + (16 * ST::col_tile(rg, cp, x) + r) * SP + 16 * ST::row_tile(rg, cp, y) + 4 * q4, PER_UNIT * racc[x][y][0],
+          store4_lds(Rl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * racc[x][y][0],
                      PER_UNIT * racc[x][y][1], PER_UNIT * racc[x][y][2], PER_UNIT * racc[x][y][3], un);
           racc[x][y] = kept.of(racc[x][y]);
         }
@@ -553,10 +553,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
         token_weights(qrows + 2 * C, t0, t1, wt);
         frag8 grow[ST::NRT];
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
+        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
 #pragma unroll
         for (int x = 0; x < ST::NCT; ++x) {
-          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), wt);
+          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
           mma16_weighted(grow, q, [&](int y) -> f32x4& { return racc[x][y]; });
         }
       }
@@ -592,7 +592,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(rg, cp, x) + r) * DV + 16 * ST::row_tile(rg, cp, y) + 4 * q4) =
+        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(w, x) + r) * DV + 16 * ST::row_tile(w, y) + 4 * q4) =
             PER_UNIT * racc[x][y];
   }
 }

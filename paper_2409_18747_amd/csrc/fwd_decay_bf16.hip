@@ -33,12 +33,12 @@ struct DecayFwdCfg {
 // S[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].
 template <class ST, int TPK>
 __device__ __forceinline__ void add_tokens(f32x4 (&acc)[ST::NCT][ST::NRT], const lds_t* Ks, const float* weights,
-                                           const frag8 (&vrow)[ST::NRT], int t0, int t1, int rg, int cp, int r) {
-  float w[8];
-  token_weights(weights, t0, t1, w);
+                                           const frag8 (&vrow)[ST::NRT], int t0, int t1, int w, int r) {
+  float wt[8];
+  token_weights(weights, t0, t1, wt);
 #pragma unroll
   for (int x = 0; x < ST::NCT; ++x) {
-    const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(rg, cp, x), r), w);
+    const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
     mma16_weighted(vrow, k, [&](int y) -> f32x4& { return acc[x][y]; });
   }
 }
@@ -65,7 +65,7 @@ COTTN_KERNEL((C * 4), decay_segment_state)
     const float* __restrict__ log_decay, const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N,
     int units, float inv_eps) {
   using Cfg = DecayFwdCfg<DK, DV, C, 1>;
-  using ST = SplitTiles<DV, DK, Cfg::RG, 1>;
+  using ST = AccTiles<DV, DK, Cfg::NW>;
   using StageK = TileStage<DK, C, Cfg::NT>;
   using StageV = TileStage<DV, C, Cfg::NT>;
   COTTN_LDS_ARRAY(lds_t, Ks, Cfg::TILEK, 0)
@@ -103,7 +103,7 @@ COTTN_KERNEL((C * 4), decay_segment_state)
       vst.fetch(Vu, row0 + C, row_end);
     }
     __syncthreads();
-    if (ST::active(w, 0)) {
+    if (ST::active(w)) {
       const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
 #pragma unroll
       for (int x = 0; x < ST::NCT; ++x)
@@ -114,18 +114,18 @@ COTTN_KERNEL((C * 4), decay_segment_state)
         const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
         frag8 vrow[ST::NRT];
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, Cfg::TPV, t0, t1, 16 * ST::row_tile(w, 0, y), r);
-        add_tokens<ST, Cfg::TPK>(acc, Ks, rows + 2 * C, vrow, t0, t1, w, 0, r);
+        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, Cfg::TPV, t0, t1, 16 * ST::row_tile(w, y), r);
+        add_tokens<ST, Cfg::TPK>(acc, Ks, rows + 2 * C, vrow, t0, t1, w, r);
       }
     }
   }
-  if (ST::active(w, 0)) {
+  if (ST::active(w)) {
     float* out = seg_state + (size_t(unit) * G.n + seg) * DK * DV;
 #pragma unroll
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        store_state_words(out + tiled_state_offset(ST::col_tile(w, 0, x), ST::row_tile(w, 0, y), DV / 16, l), acc[x][y]);
+        store_state_words(out + tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l), acc[x][y]);
   }
 }
 
@@ -140,7 +140,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     float* __restrict__ state_out, const float* __restrict__ seg_states, const float* __restrict__ state_in,
     const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units, float inv_eps, int carried) {
   using Cfg = DecayFwdCfg<DK, DV, C, CS>;
-  using ST = SplitTiles<DV, DK, Cfg::RG, CS>;
+  using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
   using StageV = TileStage<DV, C, Cfg::NT>;
   constexpr int RG = Cfg::RG, NOT = Cfg::NOT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
@@ -183,12 +183,12 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
     for (int y = 0; y < ST::NRT; ++y) sacc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const bool active = ST::active(rg, cp);
+  const bool active = ST::active(w);
   if (active && seg > 0) {
     const float* slots = seg_states + size_t(unit) * G.n * DK * DV;
     add_decayed_states<false>(sacc, carried ? seg : 0, carried ? seg : seg - 1, g, seg_rows, [&](int slot, int x, int y) {
       return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
-                                             tiled_state_offset(ST::col_tile(rg, cp, x), ST::row_tile(rg, cp, y), DV / 16, l));
+                                             tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l));
     });
   }
   if (active && state_in != nullptr) {
@@ -198,8 +198,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(rg, cp, x) + r) * DV +
-                                                        16 * ST::row_tile(rg, cp, y) + 4 * q4);
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(w, x) + r) * DV +
+                                                        16 * ST::row_tile(w, y) + 4 * q4);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sacc[x][y][v] = __builtin_fmaf(since, t[v], sacc[x][y][v]);
       }
@@ -224,7 +224,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
         for (int y = 0; y < ST::NRT; ++y) {
-          store4_lds(Sl + (16 * ST::col_tile(rg, cp, x) + r) * SP + 16 * ST::row_tile(rg, cp, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
+          store4_lds(Sl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
                      PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
           sacc[x][y] = kept.of(sacc[x][y]);
         }
@@ -278,7 +278,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
       for (int nt = 0; nt < NOT; ++nt) vc[nt] = lds_col_frag(Vs, TPV, t0, t1, col0 + 16 * nt, r);
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        vrow[y] = ST::ROW_OPERAND_IS_RESULT_COLUMN ? vc[y] : lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(rg, cp, y), r);
+        vrow[y] = CS == 1 && ST::WPC == 1 ? vc[y] : lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
       if (diag_or_below) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -304,7 +304,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
 #pragma unroll
         for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16_add(vc[nt], pf, oacc[nt]);
       }
-      if (active) add_tokens<ST, TPK>(sacc, Ks, rows + 2 * C, vrow, t0, t1, rg, cp, r);
+      if (active) add_tokens<ST, TPK>(sacc, Ks, rows + 2 * C, vrow, t0, t1, w, r);
       __builtin_amdgcn_sched_barrier(0);
     }
     wave_lds_sync();
@@ -320,7 +320,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(rg, cp, x) + r) * DV + 16 * ST::row_tile(rg, cp, y) + 4 * q4) =
+        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(w, x) + r) * DV + 16 * ST::row_tile(w, y) + 4 * q4) =
             PER_UNIT * sacc[x][y];
   }
 }
