@@ -179,44 +179,31 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     if (row0 > row_begin) store_row_pieces<DK, NKT>(finished, dQu, row0 - C + 16 * rg, row_end, l, colk);
     __syncthreads();
 
-    // G of the chunk, ds of the rows before it, and the segment's reverse-time total
+    // G of the chunk, ds of the rows before it, and the segment's reverse-time total, a few value tiles at a time
     if (active) {
-      f32x4 gacc[ST::NCT][ST::NRT];
-#pragma unroll
-      for (int x = 0; x < ST::NCT; ++x)
-#pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) gacc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int p = 0; p < Cfg::NP; ++p) {
-        const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
-        float wt[8];
-        token_weights(qrows + 2 * C, t0, t1, wt);
-        frag8 grow[ST::NRT];
-#pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
-#pragma unroll
-        for (int x = 0; x < ST::NCT; ++x) {
-          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
-          mma16_weighted(grow, q, [&](int y) -> f32x4& { return gacc[x][y]; });
-        }
-      }
+      const WeightedTile<ST, Cfg::NP, TPK> q(Qs, qrows + 2 * C, w, r, q4);
       const float at = g.after(float(row0 - row_begin));
+      constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
       float t = 0.f;
 #pragma unroll
-      for (int x = 0; x < ST::NCT; ++x)
+      for (int y0 = 0; y0 < ST::NRT; y0 += YN) {
+        f32x4 gacc[ST::NCT][YN];
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y)
+        for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            t = __builtin_fmaf(sacc[x][y][v], gacc[x][y][v], t);
-            racc[x][y][v] = __builtin_fmaf(at, gacc[x][y][v], racc[x][y][v]);
-          }
+          for (int y = 0; y < YN; ++y) gacc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+        q.template add<YN, TPV>(Gs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return gacc[x][y]; });
+#pragma unroll
+        for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+          for (int y = 0; y < YN; ++y)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              t = __builtin_fmaf(sacc[x][y0 + y][v], gacc[x][y][v], t);
+              racc[x][y0 + y][v] = __builtin_fmaf(at, gacc[x][y][v], racc[x][y0 + y][v]);
+            }
+      }
       ds_lane += PER_UNIT * PER_UNIT * once * t;
-      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
-#pragma unroll
-      for (int x = 0; x < ST::NCT; ++x)
-#pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) sacc[x][y] = kept.of(sacc[x][y]);
     }
 
     // what the state gives: dqh^T = H dO^T, then the row's factor
@@ -247,47 +234,68 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     float ds_row = 0.f;
 #pragma unroll
     for (int p = 0; p < Cfg::NP; ++p) {
+      if (2 * p > rg) break;   // wave-uniform: every key is masked from here on
       const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
-      if (2 * p <= rg) {
-        frag8 af;
+      f32x4 ta[2], tp[2];
+      {
+        frag8 vr[2][Cfg::KSV];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSV; ++ks) vr[half][ks] = lds_row_frag(Vs + (16 * (2 * p + half) + r) * TPV + 32 * ks, q4);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const int jt = 2 * p + half;
-          f32x4 ta = {0.f, 0.f, 0.f, 0.f}, tp = {0.f, 0.f, 0.f, 0.f};
+          ta[half] = tp[half] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ks = 0; ks < Cfg::KSV; ++ks) ta = mma16(lds_row_frag(Vs + (16 * jt + r) * TPV + 32 * ks, q4), gf[ks], ta);
-          // (one wave of a row group forms the tiles of ds)
-          if (CS == 1 || cp == p % CS) {
-#pragma unroll
-            for (int ks = 0; ks < Cfg::KSK; ++ks) tp = mma16(lds_row_frag(Ks + (16 * jt + r) * TPK + 32 * ks, q4), qf[ks], tp);
-          }
-          // ta[v] = dO_(16 rg + r) . v_(16 jt + 4 q4 + v)
-          const f32x4 kj = *reinterpret_cast<const f32x4*>(krows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
-          const float below = g.after(row - float(16 * jt + 15));   // (jt < rg)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            ta[v] = jt > rg ? 0.f : ta[v] * (kj[v] * (jt == rg ? on_diagonal[v] : below));
-            ds_row = __builtin_fmaf(tp[v], ta[v], ds_row);
-          }
-          put_four(af, half, ta);
+          for (int ks = 0; ks < Cfg::KSV; ++ks) ta[half] = mma16(vr[half][ks], gf[ks], ta[half]);
         }
-        frag8 kc[NKT];
-#pragma unroll
-        for (int nt = 0; nt < NKT; ++nt) kc[nt] = lds_col_frag(Ks, TPK, t0, t1, colk + 16 * nt, r);
-#pragma unroll
-        for (int nt = 0; nt < NKT; ++nt) dq[nt] = mma16_add(kc[nt], af, dq[nt]);
       }
-      if (active) {   // the state after the chunk
-        float wt[8];
-        token_weights(krows + 2 * C, t0, t1, wt);
-        frag8 vrow[ST::NRT];
+      if (CS == 1 || cp == p % CS) {   // (one wave of a row group forms the tiles of ds)
+        frag8 kr[2][Cfg::KSK];
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int x = 0; x < ST::NCT; ++x) {
-          const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
-          mma16_weighted(vrow, k, [&](int y) -> f32x4& { return sacc[x][y]; });
+          for (int ks = 0; ks < Cfg::KSK; ++ks) kr[half][ks] = lds_row_frag(Ks + (16 * (2 * p + half) + r) * TPK + 32 * ks, q4);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSK; ++ks) tp[half] = mma16(kr[half][ks], qf[ks], tp[half]);
+      }
+      frag8 kc[NKT], af;
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) kc[nt] = lds_col_frag(Ks, TPK, t0, t1, colk + 16 * nt, r);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int jt = 2 * p + half;
+        // ta[half][v] = dO_(16 rg + r) . v_(16 jt + 4 q4 + v)
+        const f32x4 kj = *reinterpret_cast<const f32x4*>(krows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
+        const float below = g.after(row - float(16 * jt + 15));   // (jt < rg)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          ta[half][v] = jt > rg ? 0.f : ta[half][v] * (kj[v] * (jt == rg ? on_diagonal[v] : below));
+          ds_row = __builtin_fmaf(tp[half][v], ta[half][v], ds_row);
         }
+        put_four(af, half, ta[half]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) dq[nt] = mma16_add(kc[nt], af, dq[nt]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the state after the chunk
+    if (active) {
+      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
+      const WeightedTile<ST, Cfg::NP, TPK> k(Ks, krows + 2 * C, w, r, q4);
+      constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
+#pragma unroll
+      for (int y0 = 0; y0 < ST::NRT; y0 += YN) {
+#pragma unroll
+        for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+          for (int y = 0; y < YN; ++y) sacc[x][y0 + y] = kept.of(sacc[x][y0 + y]);
+        k.template add<YN, TPV>(Vs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return sacc[x][y0 + y]; });
       }
     }
 
@@ -515,51 +523,71 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     // the chunk itself, 32 queries at a time
 #pragma unroll
     for (int p = 0; p < Cfg::NP; ++p) {
+      if (2 * p + 1 < rg) continue;   // wave-uniform: every query is masked
       const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
-      if (2 * p + 1 >= rg) {
-        frag8 pf, af;
+      f32x4 tp[2], ta[2];
+      {
+        frag8 qr[2][Cfg::KSK];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSK; ++ks) qr[half][ks] = lds_row_frag(Qs + (16 * (2 * p + half) + r) * TPK + 32 * ks, q4);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const int it = 2 * p + half;
-          f32x4 tp = {0.f, 0.f, 0.f, 0.f}, ta = {0.f, 0.f, 0.f, 0.f};
+          tp[half] = ta[half] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ks = 0; ks < Cfg::KSK; ++ks) tp = mma16(lds_row_frag(Qs + (16 * it + r) * TPK + 32 * ks, q4), kf[ks], tp);
-#pragma unroll
-          for (int ks = 0; ks < Cfg::KSV; ++ks) ta = mma16(lds_row_frag(Gs + (16 * it + r) * TPV + 32 * ks, q4), vf[ks], ta);
-          // tp[v] = q_(16 it + 4 q4 + v) . k_(16 rg + r)
-          const f32x4 qi = *reinterpret_cast<const f32x4*>(qrows + (it == rg ? 0 : C) + 16 * it + 4 * q4);
-          const float above = g.after(float(16 * it) - row);   // (it > rg)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float f = it < rg ? 0.f : qi[v] * (it == rg ? on_diagonal[v] : above);
-            tp[v] = it < rg ? 0.f : tp[v] * (f * (1.f / ROW_NORM * left));
-            ta[v] = it < rg ? 0.f : ta[v] * f;
-          }
-          put_four(pf, half, tp);
-          put_four(af, half, ta);
-        }
-        frag8 gc[NVT], qc[NKT];
-#pragma unroll
-        for (int nt = 0; nt < NVT; ++nt) gc[nt] = lds_col_frag(Gs, TPV, t0, t1, colv + 16 * nt, r);
-#pragma unroll
-        for (int nt = 0; nt < NVT; ++nt) dv[nt] = mma16_add(gc[nt], pf, dv[nt]);
-#pragma unroll
-        for (int nt = 0; nt < NKT; ++nt) qc[nt] = lds_col_frag(Qs, TPK, t0, t1, colk + 16 * nt, r);
-#pragma unroll
-        for (int nt = 0; nt < NKT; ++nt) dk[nt] = mma16_add(qc[nt], af, dk[nt]);
-      }
-      if (active) {   // the state before the chunk
-        float wt[8];
-        token_weights(qrows + 2 * C, t0, t1, wt);
-        frag8 grow[ST::NRT];
-#pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) grow[y] = lds_col_frag(Gs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
-#pragma unroll
-        for (int x = 0; x < ST::NCT; ++x) {
-          const WeightedFrag q = weighted(lds_col_frag(Qs, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
-          mma16_weighted(grow, q, [&](int y) -> f32x4& { return racc[x][y]; });
+          for (int ks = 0; ks < Cfg::KSK; ++ks) tp[half] = mma16(qr[half][ks], kf[ks], tp[half]);
         }
       }
+      {
+        frag8 gr[2][Cfg::KSV];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSV; ++ks) gr[half][ks] = lds_row_frag(Gs + (16 * (2 * p + half) + r) * TPV + 32 * ks, q4);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSV; ++ks) ta[half] = mma16(gr[half][ks], vf[ks], ta[half]);
+      }
+      frag8 pf, af, gc[NVT], qc[NKT];
+#pragma unroll
+      for (int nt = 0; nt < NVT; ++nt) gc[nt] = lds_col_frag(Gs, TPV, t0, t1, colv + 16 * nt, r);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int it = 2 * p + half;
+        // tp[half][v] = q_(16 it + 4 q4 + v) . k_(16 rg + r)
+        const f32x4 qi = *reinterpret_cast<const f32x4*>(qrows + (it == rg ? 0 : C) + 16 * it + 4 * q4);
+        const float above = g.after(float(16 * it) - row);   // (it > rg)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float f = it < rg ? 0.f : qi[v] * (it == rg ? on_diagonal[v] : above);
+          tp[half][v] = it < rg ? 0.f : tp[half][v] * (f * (1.f / ROW_NORM * left));
+          ta[half][v] = it < rg ? 0.f : ta[half][v] * f;
+        }
+        put_four(pf, half, tp[half]);
+        put_four(af, half, ta[half]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NVT; ++nt) dv[nt] = mma16_add(gc[nt], pf, dv[nt]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) qc[nt] = lds_col_frag(Qs, TPK, t0, t1, colk + 16 * nt, r);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int nt = 0; nt < NKT; ++nt) dk[nt] = mma16_add(qc[nt], af, dk[nt]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the state before the chunk
+    if (active) {
+      const WeightedTile<ST, Cfg::NP, TPK> q(Qs, qrows + 2 * C, w, r, q4);
+      constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
+#pragma unroll
+      for (int y0 = 0; y0 < ST::NRT; y0 += YN)
+        q.template add<YN, TPV>(Gs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return racc[x][y0 + y]; });
     }
 
     float xv[NKT][4];

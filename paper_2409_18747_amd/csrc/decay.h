@@ -119,15 +119,6 @@ __device__ __forceinline__ WeightedFrag weighted(const frag8& x, const float (&w
 #endif
   return f;
 }
-// sums[i] += rows[i] w over 32 tokens for the N tiles that share the weighted operand: part by part, the smallest first, so that
-// neighbouring matrix instructions do not wait for each other's sums
-template <int N, class Sum>
-__device__ __forceinline__ void mma16_weighted(const frag8 (&rows)[N], const WeightedFrag& w, Sum sum) {
-#pragma unroll
-  for (int p = WEIGHTED_PARTS - 1; p >= 0; --p)
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum(i) = mma16_add(rows[i], w.part[p], sum(i));
-}
 // the weights of the tokens t0 .. t0+3 and t1 .. t1+3
 __device__ __forceinline__ void token_weights(const float* of, int t0, int t1, float (&w)[8]) {
   const f32x4 lo = *reinterpret_cast<const f32x4*>(of + t0), hi = *reinterpret_cast<const f32x4*>(of + t1);
@@ -142,6 +133,42 @@ __device__ __forceinline__ void token_weights(const float* of, int t0, int t1, f
 // fp16 the second part of kh_j g^n, 2^-11 of it, would else lie below the smallest normal number (2^-14) and lose up to 2^-25,
 // whatever the weight.  (|kh| <= 1: no product is over 2^14.)
 constexpr float STATE_UNIT = ELEM_IS_F16 ? 16384.f : 1.f, PER_UNIT = 1.f / STATE_UNIT;
+
+// The weighted fragments of a wave's key tiles (columns of a tile of k or q rows), for all tokens of a chunk.
+template <class ST, int NP, int PITCH>
+struct WeightedTile {
+  WeightedFrag f[NP][ST::NCT];
+  __device__ __forceinline__ WeightedTile(const lds_t* tile, const float* weights, int w, int r, int q4) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+      float wt[8];
+      token_weights(weights, t0, t1, wt);
+#pragma unroll
+      for (int x = 0; x < ST::NCT; ++x) f[p][x] = weighted(lds_col_frag(tile, PITCH, t0, t1, 16 * ST::col_tile(w, x), r), wt);
+    }
+  }
+  // sums(x, y) += (the weighted columns)^T (the value columns of `rows`) for N of the wave's value tiles from y0 on: part by
+  // part, the smallest first, so that neighbouring matrix instructions do not wait for each other's sums
+  template <int N, int PITCH_V, class Sum>
+  __device__ __forceinline__ void add(const lds_t* rows, int y0, int w, int r, int q4, Sum sum) const {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+      frag8 v[N];
+#pragma unroll
+      for (int y = 0; y < N; ++y) v[y] = lds_col_frag(rows, PITCH_V, t0, t1, 16 * ST::row_tile(w, y0 + y), r);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = WEIGHTED_PARTS - 1; i >= 0; --i)
+#pragma unroll
+        for (int x = 0; x < ST::NCT; ++x)
+#pragma unroll
+          for (int y = 0; y < N; ++y) sum(x, y) = mma16_add(v[y], f[p][x].part[i], sum(x, y));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
 
 // Fills half of an operand fragment with four values.
 __device__ __forceinline__ void put_four(frag8& frag, int half, f32x4 x) {

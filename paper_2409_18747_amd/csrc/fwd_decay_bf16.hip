@@ -28,20 +28,9 @@ struct DecayFwdCfg {
   static constexpr int WAVES = decay_waves(LDS_BYTES, NW, CS);
 };
 
-// What a wave does with the keys of a chunk in either kernel: state += (w_j kh_j)^T v_j over the 32 tokens t0.., t1.. (this
-// lane's slots), held with the values down and the keys along: element [v] of lane (r, q4) of tile (x, y) is
-// S[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].
-template <class ST, int TPK>
-__device__ __forceinline__ void add_tokens(f32x4 (&acc)[ST::NCT][ST::NRT], const lds_t* Ks, const float* weights,
-                                           const frag8 (&vrow)[ST::NRT], int t0, int t1, int w, int r) {
-  float wt[8];
-  token_weights(weights, t0, t1, wt);
-#pragma unroll
-  for (int x = 0; x < ST::NCT; ++x) {
-    const WeightedFrag k = weighted(lds_col_frag(Ks, TPK, t0, t1, 16 * ST::col_tile(w, x), r), wt);
-    mma16_weighted(vrow, k, [&](int y) -> f32x4& { return acc[x][y]; });
-  }
-}
+// In either kernel a wave holds tiles of the state with the values down and the keys along: element [v] of lane (r, q4) of tile
+// (x, y) is S[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  It has few key tiles and as many values as that leaves:
+// the fragments of keys are the ones that weights go to, some 50 instructions each.
 
 // The factors of the chunk's key rows, one lane of a row for each: [0] 1 / norm, [1] that times g^(15 - j' mod 16), for tiles
 // below the diagonal, [2] times g^(n-1-j') STATE_UNIT, for the state after the chunk's n rows.
@@ -109,14 +98,11 @@ COTTN_KERNEL((C * 4), decay_segment_state)
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
         for (int y = 0; y < ST::NRT; ++y) acc[x][y] = kept.of(acc[x][y]);
+      const WeightedTile<ST, Cfg::NP, Cfg::TPK> k(Ks, rows + 2 * C, w, r, q4);
+      constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
-      for (int p = 0; p < Cfg::NP; ++p) {
-        const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
-        frag8 vrow[ST::NRT];
-#pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) vrow[y] = lds_col_frag(Vs, Cfg::TPV, t0, t1, 16 * ST::row_tile(w, y), r);
-        add_tokens<ST, Cfg::TPK>(acc, Ks, rows + 2 * C, vrow, t0, t1, w, r);
-      }
+      for (int y0 = 0; y0 < ST::NRT; y0 += YN)
+        k.template add<YN, Cfg::TPV>(Vs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return acc[x][y0 + y]; });
     }
   }
   if (ST::active(w)) {
@@ -271,41 +257,41 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     // the chunk itself, 32 tokens at a time
 #pragma unroll
     for (int p = 0; p < Cfg::NP; ++p) {
-      const bool diag_or_below = 2 * p <= rg;
+      if (2 * p > rg) break;   // wave-uniform: every key is masked from here on
       const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
-      frag8 vc[NOT], vrow[ST::NRT], kr[2][Cfg::KSK];
+      frag8 vc[NOT], kr[2][Cfg::KSK];
 #pragma unroll
       for (int nt = 0; nt < NOT; ++nt) vc[nt] = lds_col_frag(Vs, TPV, t0, t1, col0 + 16 * nt, r);
 #pragma unroll
-      for (int y = 0; y < ST::NRT; ++y)
-        vrow[y] = CS == 1 && ST::WPC == 1 ? vc[y] : lds_col_frag(Vs, TPV, t0, t1, 16 * ST::row_tile(w, y), r);
-      if (diag_or_below) {
+      for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int ks = 0; ks < Cfg::KSK; ++ks) kr[half][ks] = lds_row_frag(Ks + (16 * (2 * p + half) + r) * TPK + 32 * ks, q4);
-      }
+        for (int ks = 0; ks < Cfg::KSK; ++ks) kr[half][ks] = lds_row_frag(Ks + (16 * (2 * p + half) + r) * TPK + 32 * ks, q4);
       __builtin_amdgcn_sched_barrier(0);
-      if (diag_or_below) {
-        frag8 pf;
+      frag8 pf;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int jt = 2 * p + half;
-          f32x4 t = {0.f, 0.f, 0.f, 0.f};
+      for (int half = 0; half < 2; ++half) {
+        const int jt = 2 * p + half;
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ks = 0; ks < Cfg::KSK; ++ks) t = mma16(kr[half][ks], qf[ks], t);
-          // t[v] = q_(16 rg + r) . k_(16 jt + 4 q4 + v)
-          const f32x4 kj = *reinterpret_cast<const f32x4*>(rows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
-          const float below = ri * g.after(row - float(16 * jt + 15));   // (jt < rg)
+        for (int ks = 0; ks < Cfg::KSK; ++ks) t = mma16(kr[half][ks], qf[ks], t);
+        // t[v] = q_(16 rg + r) . k_(16 jt + 4 q4 + v)
+        const f32x4 kj = *reinterpret_cast<const f32x4*>(rows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
+        const float below = ri * g.after(row - float(16 * jt + 15));   // (jt < rg)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) t[v] = jt > rg ? 0.f : t[v] * (kj[v] * (jt == rg ? ri * on_diagonal[v] : below));
-          put_four(pf, half, t);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16_add(vc[nt], pf, oacc[nt]);
+        for (int v = 0; v < 4; ++v) t[v] = jt > rg ? 0.f : t[v] * (kj[v] * (jt == rg ? ri * on_diagonal[v] : below));
+        put_four(pf, half, t);
       }
-      if (active) add_tokens<ST, TPK>(sacc, Ks, rows + 2 * C, vrow, t0, t1, w, r);
+#pragma unroll
+      for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16_add(vc[nt], pf, oacc[nt]);
       __builtin_amdgcn_sched_barrier(0);
+    }
+    // the state after the chunk
+    if (active) {
+      const WeightedTile<ST, Cfg::NP, TPK> k(Ks, rows + 2 * C, w, r, q4);
+      constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
+#pragma unroll
+      for (int y0 = 0; y0 < ST::NRT; y0 += YN)
+        k.template add<YN, TPV>(Vs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return sacc[x][y0 + y]; });
     }
     wave_lds_sync();
     gather_rows_transposed<DV, NOT>(oacc, scale, stage, l, finished, un, col0);
