@@ -181,7 +181,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
 
     // G of the chunk, ds of the rows before it, and the segment's reverse-time total, a few value tiles at a time
     if (active) {
-      const WeightedTile<ST, Cfg::NP, TPK> q(Qs, qrows + 2 * C, w, r, q4);
+      const WeightedTile<ST, Cfg::NP, TPK, EXACT_PARTS> q(Qs, qrows + 2 * C, w, r, q4);
       const float at = g.after(float(row0 - row_begin));
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
       float t = 0.f;
@@ -286,17 +286,12 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     }
     // the state after the chunk
     if (active) {
-      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
-      const WeightedTile<ST, Cfg::NP, TPK> k(Ks, krows + 2 * C, w, r, q4);
+      (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);
+      const WeightedTile<ST, Cfg::NP, TPK, EXACT_PARTS> k(Ks, krows + 2 * C, w, r, q4);
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
-      for (int y0 = 0; y0 < ST::NRT; y0 += YN) {
-#pragma unroll
-        for (int x = 0; x < ST::NCT; ++x)
-#pragma unroll
-          for (int y = 0; y < YN; ++y) sacc[x][y0 + y] = kept.of(sacc[x][y0 + y]);
+      for (int y0 = 0; y0 < ST::NRT; y0 += YN)
         k.template add<YN, TPV>(Vs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return sacc[x][y0 + y]; });
-      }
     }
 
     const float left = 1.f / ROW_NORM * qrows[16 * rg + r], whole = qrows[3 * C + 16 * rg + r];
@@ -340,8 +335,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
 // ---------------------------------------------------------------------------------------
 // dK and dV of a segment, last chunk to first.  R sits in accumulators with the values down and the keys along, tile (x, y):
 // element [v] of lane (r, q4) is R[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  The first workgroups also add up
-// ds from what the dQ scan left.
-template <int DK, int DV, int C, int CS>
+// ds from what the dQ scan left.  PARTS: EXACT_PARTS where the reverse-time state is asked for.
+template <int DK, int DV, int C, int CS, int PARTS>
 COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
     const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ dK, elem_t* __restrict__ dV,
@@ -447,15 +442,13 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
   for (int row0 = last_row0; row0 >= row_begin && row_begin < row_end; row0 -= C) {
     const int n = min(C, row_end - row0);
     if (active) {
-      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
 #pragma unroll
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) {
+        for (int y = 0; y < ST::NRT; ++y)
           store4_lds(Rl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * racc[x][y][0],
                      PER_UNIT * racc[x][y][1], PER_UNIT * racc[x][y][2], PER_UNIT * racc[x][y][3], un);
-          racc[x][y] = kept.of(racc[x][y]);
-        }
+      (n == C ? whole_chunk : Kept(g, float(n))).on(racc);
     }
     {
       RowFactors<StageK> f;
@@ -583,7 +576,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     }
     // the state before the chunk
     if (active) {
-      const WeightedTile<ST, Cfg::NP, TPK> q(Qs, qrows + 2 * C, w, r, q4);
+      const WeightedTile<ST, Cfg::NP, TPK, PARTS> q(Qs, qrows + 2 * C, w, r, q4);
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
       for (int y0 = 0; y0 < ST::NRT; y0 += YN)
@@ -653,9 +646,13 @@ hipError_t run_bwd_decay(const DecayArgs& a) {
                       units, inv_eps, int(a.carried));
   if (err == hipSuccess && a.G > 1 && a.carried) err = launch_decay_carry(a, rev, true);
   if (err != hipSuccess) return err;
-  return launch_kernel(COTTN_SYM_STR(bwd_decay_dkdv), COTTN_SYM(bwd_decay_dkdv)<DK, DV, C, CS>, grid, block, 0, a.stream, Q, K, V, dO,
-                       a.s, a.log_decay, static_cast<elem_t*>(a.dK), static_cast<elem_t*>(a.dV), rev, ds_partial, a.ds,
-                       a.rev_state_in, a.rev_state_out, a.seq_len, a.B, H, G, a.seg_rows, a.N, inv_eps, int(a.carried));
+  const auto dkdv = [&](auto kernel) {
+    return launch_kernel(COTTN_SYM_STR(bwd_decay_dkdv), kernel, grid, block, 0, a.stream, Q, K, V, dO, a.s, a.log_decay,
+                         static_cast<elem_t*>(a.dK), static_cast<elem_t*>(a.dV), rev, ds_partial, a.ds, a.rev_state_in,
+                         a.rev_state_out, a.seq_len, a.B, H, G, a.seg_rows, a.N, inv_eps, int(a.carried));
+  };
+  if (a.rev_state_out != nullptr) return dkdv(COTTN_SYM(bwd_decay_dkdv)<DK, DV, C, CS, EXACT_PARTS>);
+  return dkdv(COTTN_SYM(bwd_decay_dkdv)<DK, DV, C, CS, ROUNDED_PARTS>);
 }
 
 }  // namespace

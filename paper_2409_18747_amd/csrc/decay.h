@@ -41,14 +41,33 @@ struct Kept {
   float times, plus;
   __device__ __forceinline__ Kept(const Decay& g, float n) {
     const float d = -expm1f(g.ln * n);
-    times = d < 0.5f ? 1.f : g.after(n);
-    plus = d < 0.5f ? -d : 0.f;
+    const float t = d < 0.5f ? 1.f : g.after(n), p = d < 0.5f ? -d : 0.f;
+    times = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, t)));
+    plus = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, p)));
   }
   __device__ __forceinline__ f32x4 of(f32x4 x) const {
     f32x4 y;
 #pragma unroll
     for (int v = 0; v < 4; ++v) y[v] = __builtin_fmaf(x[v], plus, x[v] * times);
     return y;
+  }
+  template <int A, int B>
+  __device__ __forceinline__ void on(f32x4 (&t)[A][B]) const {
+    if (times == 1.f) {   // the same for all lanes
+#pragma unroll
+      for (int x = 0; x < A; ++x)
+#pragma unroll
+        for (int y = 0; y < B; ++y)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) t[x][y][v] = __builtin_fmaf(t[x][y][v], plus, t[x][y][v]);
+    } else {
+#pragma unroll
+      for (int x = 0; x < A; ++x)
+#pragma unroll
+        for (int y = 0; y < B; ++y)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) t[x][y][v] *= times;
+    }
   }
 };
 
@@ -82,24 +101,27 @@ struct RowFactors {
 };
 
 // An operand fragment whose k slots are tokens, each token's values times a weight, in parts: each the rest that rounding the
-// ones before left over, until fp32 has no more.  States are results in fp32 and ds is formed from them, so bfloat16 takes
-// three (two leave up to 2^-17 of a product, 2.4e-6 of a state in the mean), fp16 two; whole fp32 one.
+// ones before left over.  A state that is a result in fp32, and those that ds is formed from, take EXACT_PARTS, until fp32 has
+// no more: three in bfloat16 (two leave up to 2^-17 of a product, 2.4e-6 of a state in the mean), two in fp16, whole fp32 one.
+// One that only enters rounded results takes two at most: with one the 1.4 roundings of a result would be 1.7.
 #if defined(COTTN_ELEM_F32)
-constexpr int WEIGHTED_PARTS = 1;
+constexpr int EXACT_PARTS = 1, ROUNDED_PARTS = 1;
 #elif defined(COTTN_ELEM_F16)
-constexpr int WEIGHTED_PARTS = 2;
+constexpr int EXACT_PARTS = 2, ROUNDED_PARTS = 2;
 #else
-constexpr int WEIGHTED_PARTS = 3;
+constexpr int EXACT_PARTS = 3, ROUNDED_PARTS = 2;
 #endif
-struct WeightedFrag { frag8 part[WEIGHTED_PARTS]; };
-__device__ __forceinline__ WeightedFrag weighted(const frag8& x, const float (&w)[8]) {
-  WeightedFrag f;
+template <int PARTS>
+struct WeightedFrag { frag8 part[PARTS]; };
+template <int PARTS>
+__device__ __forceinline__ WeightedFrag<PARTS> weighted(const frag8& x, const float (&w)[8]) {
+  WeightedFrag<PARTS> f;
 #if defined(COTTN_F32_WHOLE)
 #pragma unroll
   for (int j = 0; j < 8; ++j) f.part[0][j] = x[j] * w[j];
 #elif !defined(COTTN_ELEM_F32)
   const u32x4 words = __builtin_bit_cast(u32x4, x);
-  u32x4 parts[WEIGHTED_PARTS];
+  u32x4 parts[PARTS];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float a, b, pa, pb;
@@ -109,13 +131,13 @@ __device__ __forceinline__ WeightedFrag weighted(const frag8& x, const float (&w
     a = __builtin_fmaf(a, w[2 * i], -pa);
     b = __builtin_fmaf(b, w[2 * i + 1], -pb);
     parts[1][i] = pack2(a, b);
-    if constexpr (WEIGHTED_PARTS > 2) {
+    if constexpr (PARTS > 2) {
       unpack2(parts[1][i], pa, pb);
       parts[2][i] = pack2(a - pa, b - pb);
     }
   }
 #pragma unroll
-  for (int i = 0; i < WEIGHTED_PARTS; ++i) f.part[i] = __builtin_bit_cast(frag8, parts[i]);
+  for (int i = 0; i < PARTS; ++i) f.part[i] = __builtin_bit_cast(frag8, parts[i]);
 #endif
   return f;
 }
@@ -135,9 +157,9 @@ __device__ __forceinline__ void token_weights(const float* of, int t0, int t1, f
 constexpr float STATE_UNIT = ELEM_IS_F16 ? 16384.f : 1.f, PER_UNIT = 1.f / STATE_UNIT;
 
 // The weighted fragments of a wave's key tiles (columns of a tile of k or q rows), for all tokens of a chunk.
-template <class ST, int NP, int PITCH>
+template <class ST, int NP, int PITCH, int PARTS>
 struct WeightedTile {
-  WeightedFrag f[NP][ST::NCT];
+  WeightedFrag<PARTS> f[NP][ST::NCT];
   __device__ __forceinline__ WeightedTile(const lds_t* tile, const float* weights, int w, int r, int q4) {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -145,7 +167,7 @@ struct WeightedTile {
       float wt[8];
       token_weights(weights, t0, t1, wt);
 #pragma unroll
-      for (int x = 0; x < ST::NCT; ++x) f[p][x] = weighted(lds_col_frag(tile, PITCH, t0, t1, 16 * ST::col_tile(w, x), r), wt);
+      for (int x = 0; x < ST::NCT; ++x) f[p][x] = weighted<PARTS>(lds_col_frag(tile, PITCH, t0, t1, 16 * ST::col_tile(w, x), r), wt);
     }
   }
   // sums(x, y) += (the weighted columns)^T (the value columns of `rows`) for N of the wave's value tiles from y0 on: part by
@@ -160,7 +182,7 @@ struct WeightedTile {
       for (int y = 0; y < N; ++y) v[y] = lds_col_frag(rows, PITCH_V, t0, t1, 16 * ST::row_tile(w, y0 + y), r);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = WEIGHTED_PARTS - 1; i >= 0; --i)
+      for (int i = PARTS - 1; i >= 0; --i)
 #pragma unroll
         for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll

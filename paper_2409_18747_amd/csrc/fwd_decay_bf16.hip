@@ -93,12 +93,8 @@ COTTN_KERNEL((C * 4), decay_segment_state)
     }
     __syncthreads();
     if (ST::active(w)) {
-      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
-#pragma unroll
-      for (int x = 0; x < ST::NCT; ++x)
-#pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) acc[x][y] = kept.of(acc[x][y]);
-      const WeightedTile<ST, Cfg::NP, Cfg::TPK> k(Ks, rows + 2 * C, w, r, q4);
+      (n == C ? whole_chunk : Kept(g, float(n))).on(acc);
+      const WeightedTile<ST, Cfg::NP, Cfg::TPK, EXACT_PARTS> k(Ks, rows + 2 * C, w, r, q4);
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
       for (int y0 = 0; y0 < ST::NRT; y0 += YN)
@@ -118,8 +114,8 @@ COTTN_KERNEL((C * 4), decay_segment_state)
 // ---------------------------------------------------------------------------------------
 // The scan of one segment.  Wave (row group rg, column part cp) owns the query rows 16 rg .. of the chunk and the output
 // columns of its part, and tiles of the state, held as add_tokens says.  Results are accumulated transposed: a lane holds four
-// consecutive columns of one output row.
-template <int DK, int DV, int C, int CS>
+// consecutive columns of one output row.  PARTS: EXACT_PARTS where the state is asked for.
+template <int DK, int DV, int C, int CS, int PARTS>
 COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V,
     const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ O,
@@ -205,15 +201,13 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   for (int row0 = row_begin; row0 < row_end; row0 += C) {
     const int n = min(C, row_end - row0);
     if (active) {
-      const Kept kept = n == C ? whole_chunk : Kept(g, float(n));
 #pragma unroll
       for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y) {
+        for (int y = 0; y < ST::NRT; ++y)
           store4_lds(Sl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
                      PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
-          sacc[x][y] = kept.of(sacc[x][y]);
-        }
+      (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);
     }
     {
       RowFactors<StageK> f;
@@ -287,7 +281,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     }
     // the state after the chunk
     if (active) {
-      const WeightedTile<ST, Cfg::NP, TPK> k(Ks, rows + 2 * C, w, r, q4);
+      const WeightedTile<ST, Cfg::NP, TPK, PARTS> k(Ks, rows + 2 * C, w, r, q4);
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
       for (int y0 = 0; y0 < ST::NRT; y0 += YN)
@@ -320,10 +314,14 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
     if (err == hipSuccess && a.carried) err = launch_decay_carry(a, states, false);
     if (err != hipSuccess) return err;
   }
-  return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS>, dim3(units * a.G),
-                       dim3(64 * (C / 16) * CS), 0, a.stream, static_cast<const elem_t*>(a.Q), static_cast<const elem_t*>(a.K),
-                       static_cast<const elem_t*>(a.V), a.s, a.log_decay, static_cast<elem_t*>(a.O), a.state, states, a.state_in,
-                       a.seq_len, Divisor(a.H), Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps, int(a.carried));
+  const auto scan = [&](auto kernel) {
+    return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), kernel, dim3(units * a.G), dim3(64 * (C / 16) * CS), 0, a.stream,
+                         static_cast<const elem_t*>(a.Q), static_cast<const elem_t*>(a.K), static_cast<const elem_t*>(a.V), a.s,
+                         a.log_decay, static_cast<elem_t*>(a.O), a.state, states, a.state_in, a.seq_len, Divisor(a.H),
+                         Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps, int(a.carried));
+  };
+  if (a.state != nullptr) return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, EXACT_PARTS>);
+  return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, ROUNDED_PARTS>);
 }
 
 template <int DK, int DV, int C>
@@ -379,6 +377,9 @@ using namespace COTTN_NS;
 // Rows of a chunk: 64, in fp32 32.  Waves on a row group: two where the output of a wave is 128 columns wide and the tiles
 // leave one workgroup to a compute unit, and in fp32, whose chunk is two row groups.
 hipError_t COTTN_SYM(fwd_decay)(const DecayArgs& a) {
+#ifndef COTTN_ELEM_F32
+  if (a.dk == 128 && a.dv == 128 && long(a.B) * a.H * a.G > 256) return run_fwd_decay<128, 128, 32, 2>(a);
+#endif
 #define COTTN_CASE(DK, DV) \
   case DK * 1000 + DV: return run_fwd_decay<DK, DV, ELEM_IS_F32 ? 32 : 64, ELEM_IS_F32 || (DK == 128 && DV == 128) ? 2 : 1>(a);
   COTTN_DECAY_SHAPES(COTTN_CASE)
