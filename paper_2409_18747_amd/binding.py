@@ -28,6 +28,7 @@ class _NoMarshal:
     def fwd(*_):
         return None
     bwd = step = scale_varlen = bind = fwd
+    fwd_decay = bwd_decay = step_decay = tree = tree_accept = fwd
 
 
 def _import_marshal():
@@ -806,6 +807,10 @@ def cottn_fwd_causal_decay(Q, K, V, s, log_decay, seq_len=None, state_in=None, O
     (like V; Q and K may have another width).  With seq_len (int32 [B]) a padded batch, and s float32 [B, H], else [H].
     state_in, if given, is the state before the first row, and `state` receives that after the last one, both float32
     [B, H, d_key, d_value] and not the same memory."""
+    if stream is None:
+        done = _marshal.fwd_decay(Q, K, V, s, log_decay, seq_len, state_in, O, state, workspace, eps)
+        if done is not None:
+            return done
     B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
     if O is None:
         O = torch.empty_like(V)
@@ -831,6 +836,11 @@ def cottn_bwd_causal_decay(Q, K, V, s, log_decay, dO, seq_len=None, state_in=Non
     (dQ, dK, dV, ds), ds float32 [H], or [B, H] with seq_len.  state_in as in the forward call; rev_state_in and rev_state_out
     hand the reverse-time state from one piece of a sequence to the piece before (include/cottn.h).  fwd_workspace: the
     workspace tensor of the matching forward call (untouched since), or None."""
+    if stream is None:
+        done = _marshal.bwd_decay(Q, K, V, s, log_decay, seq_len, dO, state_in, rev_state_in, dQ, dK, dV, ds, rev_state_out,
+                                  fwd_workspace, workspace, eps)
+        if done is not None:
+            return done
     B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
     dQ, dK, dV, ds = _grads_dkdv(Q, V, dQ, dK, dV, ds, H if seq_len is None else (B, H))
     _rows_like(Q, K=K, dQ=dQ, dK=dK)
@@ -873,6 +883,10 @@ def cottn_step_decay(q, k, v, s, log_decay, state, state_in=None, parent=None, o
     [B, H, d_key] and v [B, H, d_value]; log_decay (float32 [H], or None: no decay); states float32 [B, H, d_key, d_value].
     Without state_in, `state` is updated in place; with it, `state` is written (not the same memory).  parent (int32 [B], with
     state_in [B_in, H, d_key, d_value]): whose state each sequence goes on from; a value outside starts from zeros."""
+    if stream is None:
+        done = _marshal.step_decay(q, k, v, s, log_decay, state, state_in, parent, o, eps)
+        if done is not None:
+            return done
     B, H, dk, dv, dt = _token_widths(q, v, 3, "[B, H, d]")
     if o is None:
         o = torch.empty_like(v)
@@ -902,6 +916,10 @@ def cottn_tree(q, k, v, s, state, parent, log_decay=None, o=None, eps=1e-6, stre
     """Outputs of up to 64 drafted tokens for each sequence that form a tree over `state` (float32 [B, H, d_key, d_value],
     left as it is): each token's, as if the tokens on its path had been fed one by one.  q, k are [B, H, T, d_key], v
     [B, H, T, d_value], parent int32 [B, T]: a token before, or anything else for a root; returns o (like v)."""
+    if stream is None:
+        done = _marshal.tree(q, k, v, s, state, parent, log_decay, o, eps)
+        if done is not None:
+            return done
     B, H, T, dk, dv, dt = _token_widths(q, v, 4, "[B, H, T, d]")
     if o is None:
         o = torch.empty_like(v)
@@ -921,6 +939,10 @@ def cottn_tree(q, k, v, s, state, parent, log_decay=None, o=None, eps=1e-6, stre
 def cottn_tree_accept(k, v, state, parent, last, log_decay=None, eps=1e-6, stream=None):
     """Takes `state` on along the path to token last[b] (int32 [B]) of each sequence's tree, in place (k, v, parent as in
     cottn_tree); where last[b] is not a token nothing is accepted.  Returns state."""
+    if stream is None:
+        done = _marshal.tree_accept(k, v, state, parent, last, log_decay, eps)
+        if done is not None:
+            return done
     B, H, T, dk, dv, dt = _token_widths(k, v, 4, "[B, H, T, d]")
     _f32("log_decay", log_decay, H, k.device, optional=True)
     _f32("state", state, B * H * dk * dv, k.device)

@@ -42,6 +42,11 @@ struct Library {
   decltype(&cottn_bwd_bidir_varlen) bwd_bidir_varlen;
   decltype(&cottn_bwd_bidir_dkdv) bwd_bidir_dkdv;
   decltype(&cottn_step_dkdv) step_dkdv;
+  decltype(&cottn_fwd_causal_decay) fwd_causal_decay;
+  decltype(&cottn_bwd_causal_decay) bwd_causal_decay;
+  decltype(&cottn_step_decay) step_decay;
+  decltype(&cottn_tree) tree;
+  decltype(&cottn_tree_accept) tree_accept;
   decltype(&cottn_scale_from_m_varlen) scale_from_m_varlen;
   decltype(&cottn_scale_backward_varlen) scale_backward_varlen;
 } lib;
@@ -136,6 +141,23 @@ struct Call {
     const at::Tensor* t = tensor();
     ok = ok && t->scalar_type() == at::kInt && t->numel() == B && t->device() == device;
     return ok ? static_cast<const int*>(t->data_ptr()) : nullptr;
+  }
+  // int32 of exactly this shape; with `optional` None too
+  const int* indices(at::IntArrayRef shape, bool optional = false) {
+    if (optional && *next == Py_None) {
+      ++next;
+      return nullptr;
+    }
+    const at::Tensor* t = tensor();
+    ok = ok && t->scalar_type() == at::kInt && t->sizes() == shape && t->device() == device;
+    return ok ? static_cast<const int*>(t->data_ptr()) : nullptr;
+  }
+  // rows that differ from `ref` in their last size at most
+  const at::Tensor* rows_beside(const at::Tensor* ref) {
+    const at::Tensor* t = tensor();
+    ok = ok && ref != nullptr && t->dim() == ref->dim() && t->scalar_type() == ref->scalar_type() && t->device() == device &&
+         t->sizes().slice(0, t->dim() - 1) == ref->sizes().slice(0, ref->dim() - 1) && t->size(t->dim() - 1) <= INT_MAX;
+    return t;
   }
   // a workspace and its size
   void* bytes(size_t& size) {
@@ -438,6 +460,232 @@ PyObject* step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// fwd_decay(Q, K, V, s, log_decay, seq_len, state_in, O, state, workspace, eps)
+PyObject* fwd_decay(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11 || modes_on() || lib.fwd_causal_decay == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *Q = c.first(4), *K = c.rows_like(Q), *V = c.rows_beside(Q);
+  if (!c.ok || !sizes_fit(*Q)) Py_RETURN_NONE;
+  const int B = int(Q->size(0)), H = int(Q->size(1)), N = int(Q->size(2)), dk = int(Q->size(3)), dv = int(V->size(3)),
+            dt = dtype_code(*Q);
+  const int64_t units = int64_t(B) * H, states = units * dk * dv;
+  const bool padded = args[5] != Py_None;
+  const float* s = static_cast<const float*>(c.floats(padded ? units : H));
+  const float* log_decay = static_cast<const float*>(c.floats(H));
+  const int* seq_len = padded ? c.lengths(B) : (++c.next, nullptr);
+  const float* state_in = static_cast<const float*>(c.floats(states, true));
+  PyObject* given = *c.next;
+  const at::Tensor* O = c.rows_like(V, true);
+  float* state = static_cast<float*>(c.floats(states, true));
+  const bool given_workspace = *c.next != Py_None;
+  size_t have = 0;
+  void* workspace = c.bytes(have);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  if (!given_workspace) {
+    have = lib.workspace_bytes_dkdv(COTTN_OP_FWD_DECAY, B, H, N, dk, dv, 0, dt);
+    if (have == size_t(-1)) Py_RETURN_NONE;
+  }
+  at::Tensor made, scratch;
+  int st;
+  {
+    const Unlocked unlocked;
+    if (O == nullptr) {
+      made = at::empty(V->sizes(), V->options());
+      O = &made;
+    }
+    if (!given_workspace && have > 0) {
+      scratch = at::empty({int64_t(have)}, Q->options().dtype(at::kByte));
+      workspace = scratch.data_ptr();
+    }
+    st = lib.fwd_causal_decay(Q->data_ptr(), K->data_ptr(), V->data_ptr(), s, log_decay, seq_len, state_in, O->data_ptr(), state,
+                              workspace, have, B, H, N, dk, dv, dt, eps, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_fwd_causal_decay");
+  return result(given, made);
+  END_HANDLE_TH_ERRORS
+}
+
+// bwd_decay(Q, K, V, s, log_decay, seq_len, dO, state_in, rev_state_in, dQ, dK, dV, ds, rev_state_out, fwd_workspace, workspace,
+//           eps)
+PyObject* bwd_decay(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 17 || modes_on() || lib.bwd_causal_decay == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *Q = c.first(4), *K = c.rows_like(Q), *V = c.rows_beside(Q);
+  if (!c.ok || !sizes_fit(*Q)) Py_RETURN_NONE;
+  const int B = int(Q->size(0)), H = int(Q->size(1)), N = int(Q->size(2)), dk = int(Q->size(3)), dv = int(V->size(3)),
+            dt = dtype_code(*Q);
+  const int64_t units = int64_t(B) * H, states = units * dk * dv;
+  const bool padded = args[5] != Py_None;
+  const int64_t scales = padded ? units : H;
+  const float* s = static_cast<const float*>(c.floats(scales));
+  const float* log_decay = static_cast<const float*>(c.floats(H));
+  const int* seq_len = padded ? c.lengths(B) : (++c.next, nullptr);
+  const at::Tensor* dO = c.rows_like(V);
+  const float* state_in = static_cast<const float*>(c.floats(states, true));
+  const float* rev_in = static_cast<const float*>(c.floats(states, true));
+  PyObject* const* given = c.next;   // dQ, dK, dV, ds
+  const at::Tensor* grads[3] = {c.rows_like(Q, true), nullptr, nullptr};
+  grads[1] = c.rows_like(Q, true);
+  grads[2] = c.rows_like(V, true);
+  float* ds = static_cast<float*>(c.floats(scales, true));
+  float* rev_out = static_cast<float*>(c.floats(states, true));
+  size_t fwd_have = 0, have = 0;
+  const void* fwd_workspace = c.bytes(fwd_have);
+  const bool given_workspace = *c.next != Py_None;
+  void* workspace = c.bytes(have);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  if (!given_workspace) {
+    have = lib.workspace_bytes_dkdv(COTTN_OP_BWD_DECAY, B, H, N, dk, dv, 0, dt);
+    if (have == size_t(-1)) Py_RETURN_NONE;
+  }
+  at::Tensor made[4], scratch;
+  int st;
+  {
+    const Unlocked unlocked;
+    for (int i = 0; i < 3; ++i)
+      if (grads[i] == nullptr) {
+        const at::Tensor* ref = i < 2 ? Q : V;
+        made[i] = at::empty(ref->sizes(), ref->options());
+        grads[i] = &made[i];
+      }
+    if (given[3] == Py_None) {
+      made[3] = padded ? at::empty({B, H}, Q->options().dtype(at::kFloat)) : at::empty({H}, Q->options().dtype(at::kFloat));
+      ds = static_cast<float*>(made[3].data_ptr());
+    }
+    if (!given_workspace && have > 0) {
+      scratch = at::empty({int64_t(have)}, Q->options().dtype(at::kByte));
+      workspace = scratch.data_ptr();
+    }
+    st = lib.bwd_causal_decay(Q->data_ptr(), K->data_ptr(), V->data_ptr(), s, log_decay, seq_len, dO->data_ptr(), state_in, rev_in,
+                              grads[0]->data_ptr(), grads[1]->data_ptr(), grads[2]->data_ptr(), ds, rev_out, fwd_workspace, fwd_have,
+                              workspace, have, B, H, N, dk, dv, dt, eps, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_bwd_causal_decay");
+  PyObject* all = PyTuple_New(4);
+  if (all == nullptr) return nullptr;
+  for (int i = 0; i < 4; ++i) {
+    PyObject* o = result(given[i], made[i]);
+    if (o == nullptr) {
+      Py_DECREF(all);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(all, i, o);
+  }
+  return all;
+  END_HANDLE_TH_ERRORS
+}
+
+// step_decay(q, k, v, s, log_decay, state, state_in, parent, o, eps)
+PyObject* step_decay(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 10 || modes_on() || lib.step_decay == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *q = c.first(3), *k = c.rows_like(q), *v = c.rows_beside(q);
+  if (!c.ok || !sizes_fit(*q)) Py_RETURN_NONE;
+  const int B = int(q->size(0)), H = int(q->size(1)), dk = int(q->size(2)), dv = int(v->size(2)), dt = dtype_code(*q);
+  const float* s = static_cast<const float*>(c.floats(H));
+  const float* log_decay = static_cast<const float*>(c.floats(H, true));
+  float* state = static_cast<float*>(c.floats(int64_t(B) * H * dk * dv));
+  int B_in = B;
+  const float* from = state;
+  if (*c.next == Py_None) {
+    ++c.next;
+    if (*c.next != Py_None) Py_RETURN_NONE;   // (a parent without state_in)
+  } else {
+    const at::Tensor* t = c.tensor();
+    if (!c.ok) Py_RETURN_NONE;
+    if (*c.next != Py_None) {
+      if (t->dim() != 4 || t->size(0) > INT_MAX) Py_RETURN_NONE;
+      B_in = int(t->size(0));
+    }
+    if (t->scalar_type() != at::kFloat || t->numel() != int64_t(B_in) * H * dk * dv || t->device() != c.device) Py_RETURN_NONE;
+    from = static_cast<const float*>(t->data_ptr());
+  }
+  const int* parent = c.indices({B}, true);
+  PyObject* given = *c.next;
+  const at::Tensor* o = c.rows_like(v, true);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  at::Tensor made;
+  int st;
+  {
+    const Unlocked unlocked;
+    if (o == nullptr) {
+      made = at::empty(v->sizes(), v->options());
+      o = &made;
+    }
+    st = lib.step_decay(q->data_ptr(), k->data_ptr(), v->data_ptr(), s, log_decay, from, parent, B_in, state, o->data_ptr(), B, H,
+                        dk, dv, dt, eps, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_step_decay");
+  return result(given, made);
+  END_HANDLE_TH_ERRORS
+}
+
+// tree(q, k, v, s, state, parent, log_decay, o, eps)
+PyObject* tree(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 9 || modes_on() || lib.tree == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *q = c.first(4), *k = c.rows_like(q), *v = c.rows_beside(q);
+  if (!c.ok || !sizes_fit(*q)) Py_RETURN_NONE;
+  const int B = int(q->size(0)), H = int(q->size(1)), T = int(q->size(2)), dk = int(q->size(3)), dv = int(v->size(3)),
+            dt = dtype_code(*q);
+  const float* s = static_cast<const float*>(c.floats(H));
+  const float* state = static_cast<const float*>(c.floats(int64_t(B) * H * dk * dv));
+  const int* parent = c.indices({B, T});
+  const float* log_decay = static_cast<const float*>(c.floats(H, true));
+  PyObject* given = *c.next;
+  const at::Tensor* o = c.rows_like(v, true);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  at::Tensor made;
+  int st;
+  {
+    const Unlocked unlocked;
+    if (o == nullptr) {
+      made = at::empty(v->sizes(), v->options());
+      o = &made;
+    }
+    st = lib.tree(q->data_ptr(), k->data_ptr(), v->data_ptr(), s, log_decay, parent, state, o->data_ptr(), B, H, T, dk, dv, dt, eps,
+                  current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_tree");
+  return result(given, made);
+  END_HANDLE_TH_ERRORS
+}
+
+// tree_accept(k, v, state, parent, last, log_decay, eps)
+PyObject* tree_accept(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7 || modes_on() || lib.tree_accept == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *k = c.first(4), *v = c.rows_beside(k);
+  if (!c.ok || !sizes_fit(*k)) Py_RETURN_NONE;
+  const int B = int(k->size(0)), H = int(k->size(1)), T = int(k->size(2)), dk = int(k->size(3)), dv = int(v->size(3)),
+            dt = dtype_code(*k);
+  PyObject* given = *c.next;
+  float* state = static_cast<float*>(c.floats(int64_t(B) * H * dk * dv));
+  const int* parent = c.indices({B, T});
+  const int* last = c.indices({B});
+  const float* log_decay = static_cast<const float*>(c.floats(H, true));
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  int st;
+  {
+    const Unlocked unlocked;
+    st = lib.tree_accept(k->data_ptr(), v->data_ptr(), log_decay, parent, last, state, B, H, T, dk, dv, dt, eps, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_tree_accept");
+  Py_INCREF(given);
+  return given;
+  END_HANDLE_TH_ERRORS
+}
+
 // scale_varlen(m, seq_len, ds or None, result): s from m, or with ds the gradient of m
 PyObject* scale_varlen(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -507,8 +755,15 @@ PyObject* bind(PyObject*, PyObject* args) {
   COTTN_FIND(step_dkdv);
   COTTN_FIND(scale_from_m_varlen);
   COTTN_FIND(scale_backward_varlen);
+  // (a library may lack these: then their calls are binding.py's)
+  const bool needed = all;
+  COTTN_FIND(fwd_causal_decay);
+  COTTN_FIND(bwd_causal_decay);
+  COTTN_FIND(step_decay);
+  COTTN_FIND(tree);
+  COTTN_FIND(tree_accept);
 #undef COTTN_FIND
-  if (!all) {
+  if (!needed) {
     PyErr_Format(PyExc_ImportError, "%s lacks a function of cottn.h", path);
     return nullptr;
   }
@@ -524,6 +779,11 @@ PyMethodDef methods[] = {
     {"fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fwd)), METH_FASTCALL, nullptr},
     {"bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bwd)), METH_FASTCALL, nullptr},
     {"step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(step)), METH_FASTCALL, nullptr},
+    {"fwd_decay", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fwd_decay)), METH_FASTCALL, nullptr},
+    {"bwd_decay", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bwd_decay)), METH_FASTCALL, nullptr},
+    {"step_decay", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(step_decay)), METH_FASTCALL, nullptr},
+    {"tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree)), METH_FASTCALL, nullptr},
+    {"tree_accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_accept)), METH_FASTCALL, nullptr},
     {"scale_varlen", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(scale_varlen)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
