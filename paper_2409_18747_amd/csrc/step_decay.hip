@@ -179,6 +179,10 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(
 // non-temporal loads where the states of a call exceed the L2s (step.hip)
 bool streamed(long units, int dk, int dv) { return double(units) * dk * dv * sizeof(float) > 32.0 * 1024 * 1024; }
 
+// Up to 128 states a workgroup takes 32 value columns instead of all, so that more compute units have one.  Kernels alone, states of
+// 128 x 128, whole / parts: step of 16 states 3.6 / 3.0 us, 128 5.4 / 4.2, 256 6.9 / 7.9; accepting 5.2 / 4.0, 7.5 / 5.2, 8.7 / 8.9.
+bool state_parts(long units, int dv) { return dv > 32 && units <= 128; }
+
 template <typename T, int DK, int DV, int COLS>
 hipError_t step_parts(const StepDecayArgs& a) {
   const int units = a.B * a.H;
@@ -205,14 +209,14 @@ hipError_t accept_parts(const TreeArgs& a) {
 template <typename T>
 hipError_t run_step_decay(const StepDecayArgs& a) {
 #define COTTN_CASE(DK, DV) \
-  case DK * 1000 + DV: return step_parts<T, DK, DV, DV>(a);
+  case DK * 1000 + DV: return state_parts(a.B * a.H, DV) ? step_parts<T, DK, DV, 32>(a) : step_parts<T, DK, DV, DV>(a);
   COTTN_STATE_SHAPES(COTTN_CASE)
 #undef COTTN_CASE
 }
 template <typename T>
 hipError_t run_tree_accept(const TreeArgs& a) {
 #define COTTN_CASE(DK, DV) \
-  case DK * 1000 + DV: return accept_parts<T, DK, DV, DV>(a);
+  case DK * 1000 + DV: return state_parts(a.B * a.H, DV) ? accept_parts<T, DK, DV, 32>(a) : accept_parts<T, DK, DV, DV>(a);
   COTTN_STATE_SHAPES(COTTN_CASE)
 #undef COTTN_CASE
 }
