@@ -81,7 +81,8 @@ typedef enum {
   COTTN_OP_BWD_BIDIR = 3,
   COTTN_OP_STEP = 4,
   COTTN_OP_FWD_DECAY = 5,
-  COTTN_OP_BWD_DECAY = 6
+  COTTN_OP_BWD_DECAY = 6,
+  COTTN_OP_FWD_DECAY_ALONE = 8 /* a forward whose workspace no backward takes over */
 } cottn_op;
 
 /* Bytes of workspace the given operation needs for these arguments (0 for COTTN_OP_STEP).
@@ -295,7 +296,9 @@ int cottn_scale_backward_varlen(const float* m, const int* seq_len, const float*
  * counts as 0).  It is a constant of the head: the backward gives no gradient for it.
  * States are float[B][H][dk][dv], H after the last row, without s; dk and dv are each one of 32, 64, 128.  Chunks are the
  * library's own (64 rows, fp32 32).  All dtypes; states and ds are accurate to fp32 whatever the dtype (16-bit operands
- * enter them in two parts).  Workspaces: cottn_workspace_bytes_dkdv with COTTN_OP_FWD_DECAY and COTTN_OP_BWD_DECAY, chunk 0.
+ * enter them in parts).  Workspaces: cottn_workspace_bytes_dkdv with COTTN_OP_FWD_DECAY and COTTN_OP_BWD_DECAY, chunk 0.  A
+ * forward that no backward follows can do with a workspace of COTTN_OP_FWD_DECAY_ALONE, often none, and is then faster for short
+ * prompts of few sequences: with less than COTTN_OP_FWD_DECAY asks for it takes the split of that smaller size.
  *
  * Forward.  seq_len: NULL, or int[B] as in the *_varlen calls, and then s is float[B][H] (else float[H]); the state is that
  * after a sequence's own last row.  state_in: NULL (zeros) or the state before row 0.  state: NULL or out; the two must not
@@ -306,8 +309,9 @@ int cottn_scale_backward_varlen(const float* m, const int* seq_len, const float*
  *                  rev_state_out of the piece behind;
  *   rev_state_out  the same at this piece's row 0; s g times it is the gradient with respect to state_in.  Must overlap
  *                  neither rev_state_in nor state_in (COTTN_E_ARG).
- * fwd_workspace: NULL, or the workspace of the matching completed cottn_fwd_causal_decay call, untouched since (same K, V,
- * log_decay, seq_len, sizes, dtype and eps, and the same cottn_tune_segments; as in cottn_bwd_causal). */
+ * fwd_workspace: NULL, or the workspace, of COTTN_OP_FWD_DECAY's size or more, of the matching completed
+ * cottn_fwd_causal_decay call, untouched since (same K, V, log_decay, seq_len, sizes, dtype and eps, and the same
+ * cottn_tune_segments; as in cottn_bwd_causal).  A smaller one is refused (COTTN_E_WORKSPACE). */
 int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const float* s, const float* log_decay,
                            const int* seq_len, const float* state_in, void* O, float* state, void* workspace,
                            size_t workspace_bytes, int B, int H, int N, int dk, int dv, int dtype, float eps, void* hip_stream);

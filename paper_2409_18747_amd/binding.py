@@ -52,6 +52,7 @@ library_path = os.path.join(_HERE, "libcottn.so")
 
 COTTN_F32, COTTN_BF16, COTTN_F16 = 0, 1, 2
 OP_FWD_CAUSAL, OP_BWD_CAUSAL, OP_FWD_BIDIR, OP_BWD_BIDIR, OP_STEP, OP_FWD_DECAY, OP_BWD_DECAY = range(7)
+OP_FWD_DECAY_ALONE = 8
 MOST_DRAFTS = 64  # COTTN_MOST_DRAFTS of include/cottn.h
 
 
@@ -806,7 +807,8 @@ def cottn_fwd_causal_decay(Q, K, V, s, log_decay, seq_len=None, state_in=None, O
     """O_i = s_h sum over j <= i of g_h^(i-j) (qhat_i . khat_j) v_j with g = exp(log_decay) (float32 [H], <= 0); returns O
     (like V; Q and K may have another width).  With seq_len (int32 [B]) a padded batch, and s float32 [B, H], else [H].
     state_in, if given, is the state before the first row, and `state` receives that after the last one, both float32
-    [B, H, d_key, d_value] and not the same memory."""
+    [B, H, d_key, d_value] and not the same memory.  workspace: for a backward that takes it over as fwd_workspace, of
+    cottn_workspace_bytes_dkdv(OP_FWD_DECAY, ..) bytes; without one the call allocates what it needs by itself."""
     if stream is None:
         done = _marshal.fwd_decay(Q, K, V, s, log_decay, seq_len, state_in, O, state, workspace, eps)
         if done is not None:
@@ -823,7 +825,7 @@ def cottn_fwd_causal_decay(Q, K, V, s, log_decay, seq_len=None, state_in=None, O
     _f32("state_in", state_in, B * H * dk * dv, Q.device, optional=True)
     _f32("state", state, B * H * dk * dv, Q.device, optional=True)
     _on_gpu(Q)
-    workspace, have = _workspace_dkdv(OP_FWD_DECAY, B, H, N, dk, dv, 0, dt, Q.device, workspace, stream)
+    workspace, have = _workspace_dkdv(OP_FWD_DECAY_ALONE, B, H, N, dk, dv, 0, dt, Q.device, workspace, stream)
     st = lib.cottn_fwd_causal_decay(_ptr(Q), _ptr(K), _ptr(V), _ptr(s), _ptr(log_decay), _ptr(seq_len), _ptr(state_in),
                                     _ptr(O), _ptr(state), _ptr(workspace), have, B, H, N, dk, dv, dt, eps, _stream(stream))
     _check(st, "cottn_fwd_causal_decay")

@@ -242,32 +242,42 @@ bool make_plan(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype
 
 namespace {
 
-// The split of a call with a decay, the same for the forward and its backward.
+// The split of a call with a decay, the same for a forward and its backward; a forward by itself (`alone`) may walk a sequence
+// as one segment where those two take several.
 struct DecayPlan {
-  int G, seg_rows;
+  int G, seg_rows, value_columns;
   bool carried;   // DecayArgs
 };
-bool make_decay_plan(int B, int H, int N, int dk, int dv, int chunk, int dtype, DecayPlan* plan) {
+bool make_decay_plan(bool alone, int B, int H, int N, int dk, int dv, int chunk, int dtype, DecayPlan* plan) {
   if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
-  const int C = dtype == COTTN_F32 ? 32 : 64;
+  const bool f32 = dtype == COTTN_F32;
+  const int C = f32 ? 32 : 64;
   if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != C)) return false;
   const long units = long(B) * H, n_chunks = (long(N) + C - 1) / C;
   long want = g_tuned_segments;
-  if (want <= 0) want = n_chunks > 0 ? causal_segments(units, N, n_chunks, C, dtype, dk, dv) : 1;
+  if (want <= 0) {
+    want = n_chunks > 0 ? causal_segments(units, N, n_chunks, C, dtype, dk, dv) : 1;
+    // Two chunks are two segments up to 128 units: the step that a scan saves is longer than the totals' launch (forward +
+    // backward of 128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 -> 26.5, 32 x 32 18.1 -> 16.8; 128 units 128 x 128
+    // 40.3 -> 39.1; 192 units 128 x 128 43.4 -> 64.6)
+    if (!f32 && n_chunks == 2 && units <= 128) want = 2;
+    if (alone && N <= decay_one_segment_rows(units, dk, dv, f32)) want = 1;
+  }
   if (want > n_chunks) want = n_chunks;
   if (want < 1) want = 1;
   const long steps = n_chunks > 0 ? (n_chunks + want - 1) / want : 1, G = n_chunks > 0 ? (n_chunks + steps - 1) / steps : 1;
   if (!threads_fit(units * G, 512)) return false;
   plan->G = int(G);
   plan->seg_rows = int(steps * C);
-  plan->carried = G > 1 && !causal_totals_in_place(units, int(G), dk, dv, dtype == COTTN_F32) && threads_fit(units, dk * dv / 4);
+  plan->value_columns = G == 1 ? decay_value_columns(units, dk, dv, f32) : dv;
+  plan->carried = G > 1 && !causal_totals_in_place(units, int(G), dk, dv, f32) && threads_fit(units, dk * dv / 4);
   return true;
 }
 // forward: the states of G segments; backward: two such arrays, and the segments' parts of ds
 size_t decay_workspace_bytes(int op, int B, int H, int dk, int dv, const DecayPlan& p) {
   const long units = long(B) * H;
   const size_t states = p.G > 1 ? state_slots_bytes(units * p.G, dk, dv) : 0;
-  return op == COTTN_OP_FWD_DECAY ? states : 2 * states + round_up_256(size_t(units) * p.G * sizeof(float));
+  return op != COTTN_OP_BWD_DECAY ? states : 2 * states + round_up_256(size_t(units) * p.G * sizeof(float));
 }
 
 // whether n floats at p and m floats at q have one in common
@@ -359,9 +369,9 @@ size_t cottn_workspace_bytes_dkdv(int op, int B, int H, int N, int dk, int dv, i
                ? 0
                : size_t(-1);
   }
-  if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY) {
+  if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY || op == COTTN_OP_FWD_DECAY_ALONE) {
     DecayPlan plan;
-    return make_decay_plan(B, H, N, dk, dv, chunk, dtype, &plan) ? decay_workspace_bytes(op, B, H, dk, dv, plan) : size_t(-1);
+    return make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan) ? decay_workspace_bytes(op, B, H, dk, dv, plan) : size_t(-1);
   }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_STEP) return size_t(-1);
   SeqPlan plan;
@@ -374,9 +384,9 @@ size_t cottn_workspace_bytes(int op, int B, int H, int N, int d, int chunk, int 
 }
 
 int cottn_segments_dkdv(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype) {
-  if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY) {
+  if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY || op == COTTN_OP_FWD_DECAY_ALONE) {
     DecayPlan plan;
-    return make_decay_plan(B, H, N, dk, dv, chunk, dtype, &plan) ? plan.G : 0;
+    return make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan) ? plan.G : 0;
   }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_BWD_BIDIR) return 0;
   SeqPlan plan;
@@ -815,7 +825,10 @@ int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   if (overlap(state_in, states, state, states)) return COTTN_E_ARG;
   if ((st = check_lengths(seq_len)) != COTTN_OK) return st;
   DecayPlan plan;
-  if (!make_decay_plan(B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
+  if (!make_decay_plan(false, B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
+  // with room for the states that a backward takes over they are left there, else the call takes the split of a forward alone
+  if (workspace == nullptr || workspace_bytes < decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan))
+    make_decay_plan(true, B, H, N, dk, dv, 0, dtype, &plan);
   st = check_workspace(workspace, workspace_bytes, decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan));
   if (st != COTTN_OK) return st;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -826,7 +839,8 @@ int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   DecayArgs a{};
   a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.O = O; a.state = state; a.state_in = state_in;
   a.seq_len = seq_len; a.workspace = workspace;
-  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows; a.carried = plan.carried;
+  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows;
+  a.value_columns = plan.value_columns; a.carried = plan.carried;
   a.eps = eps; a.stream = stream;
   return map_hip(dtype == COTTN_BF16 ? fwd_decay_bf16(a) : dtype == COTTN_F16 ? fwd_decay_f16(a) : fwd_decay_f32w(a));
 }
@@ -846,7 +860,7 @@ int cottn_bwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   if (overlap(rev_state_in, states, rev_state_out, states) || overlap(state_in, states, rev_state_out, states)) return COTTN_E_ARG;
   if ((st = check_lengths(seq_len)) != COTTN_OK) return st;
   DecayPlan plan;
-  if (!make_decay_plan(B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
+  if (!make_decay_plan(false, B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
   st = check_workspace(workspace, workspace_bytes, decay_workspace_bytes(COTTN_OP_BWD_DECAY, B, H, dk, dv, plan));
   if (st != COTTN_OK) return st;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -861,7 +875,8 @@ int cottn_bwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.ds = ds;
   a.state_in = state_in; a.rev_state_in = rev_state_in; a.rev_state_out = rev_state_out; a.seq_len = seq_len;
   a.workspace = workspace;
-  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows; a.carried = plan.carried;
+  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows;
+  a.value_columns = plan.value_columns; a.carried = plan.carried;
   a.eps = eps; a.stream = stream;
   if (fwd_workspace != nullptr && plan.G > 1) {
     st = check_workspace(fwd_workspace, fwd_workspace_bytes, decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan));

@@ -114,8 +114,9 @@ COTTN_KERNEL((C * 4), decay_segment_state)
 // ---------------------------------------------------------------------------------------
 // The scan of one segment.  Wave (row group rg, column part cp) owns the query rows 16 rg .. of the chunk and the output
 // columns of its part, and tiles of the state, held as add_tokens says.  Results are accumulated transposed: a lane holds four
-// consecutive columns of one output row.  PARTS: EXACT_PARTS where the state is asked for.
-template <int DK, int DV, int C, int CS, int PARTS>
+// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value columns, which the whole
+// computation leaves apart from one another but for the masked tiles; those are formed LDV / DV times.  PARTS: EXACT_PARTS where the state is asked for.
+template <int DK, int DV, int C, int CS, int PARTS, int LDV = DV>
 COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V,
     const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ O,
@@ -124,7 +125,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   using Cfg = DecayFwdCfg<DK, DV, C, CS>;
   using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
-  using StageV = TileStage<DV, C, Cfg::NT>;
+  using StageV = TileStage<DV, C, Cfg::NT, LDV>;
   constexpr int RG = Cfg::RG, NOT = Cfg::NOT, TPK = Cfg::TPK, TPV = Cfg::TPV, SP = Cfg::SP;
   COTTN_LDS_ARRAY(lds_t, Qs, Cfg::TILEK, 0)
   COTTN_LDS_ARRAY(lds_t, Ks, Cfg::TILEK, 1)
@@ -136,19 +137,26 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   Unparted un;
   fetch_argument_now(Q, K, V, s, log_decay, O, state_out, seg_states, state_in, lengths, H, G, seg_rows, N, units, inv_eps,
                      carried);
-  int unit, seg;
-  unit_and_segment(blockIdx.x, units, G, unit, seg);
+  constexpr int VALUE_PARTS = LDV / DV;
+  int unit, seg, part = 0;
+  if constexpr (VALUE_PARTS > 1) {   // (one segment)
+    unit = blockIdx.x / VALUE_PARTS;
+    part = blockIdx.x % VALUE_PARTS;
+    seg = 0;
+  } else {
+    unit_and_segment(blockIdx.x, units, G, unit, seg);
+  }
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
   const int rg = w % RG, cp = w / RG;
   const elem_t* Qu = Q + size_t(unit) * N * DK;
   const elem_t* Ku = K + size_t(unit) * N * DK;
-  const elem_t* Vu = V + size_t(unit) * N * DV;
-  elem_t* Ou = O + size_t(unit) * N * DV;
+  const elem_t* Vu = V + size_t(unit) * N * LDV + part * DV;
+  elem_t* Ou = O + size_t(unit) * N * LDV + part * DV;
   const int there = valid_rows(lengths, unit, H, N), row_begin = seg * seg_rows, piece_end = min(N, row_begin + seg_rows);
   const int row_end = max(row_begin, min(there, piece_end));
   const bool ends_here = there > row_begin ? there <= piece_end : there == 0 && seg == 0;   // the state after the last row
   if (there <= row_begin && !ends_here) {
-    zero_rows<DV>(Ou, row_begin, piece_end);
+    zero_rows<DV, LDV>(Ou, row_begin, piece_end);
     return;
   }
   StageK qst, kst;
@@ -175,12 +183,12 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   }
   if (active && state_in != nullptr) {
     const float since = STATE_UNIT * g.after(float(row_begin));
-    const float* src = state_in + size_t(unit) * DK * DV;
+    const float* src = state_in + size_t(unit) * DK * LDV + part * DV;
 #pragma unroll
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y) {
-        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(w, x) + r) * DV +
+        const f32x4 t = *reinterpret_cast<const f32x4*>(src + (16 * ST::col_tile(w, x) + r) * LDV +
                                                         16 * ST::row_tile(w, y) + 4 * q4);
 #pragma unroll
         for (int v = 0; v < 4; ++v) sacc[x][y][v] = __builtin_fmaf(since, t[v], sacc[x][y][v]);
@@ -222,7 +230,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
       kst.fetch(Ku, row0 + C, row_end);
       vst.fetch(Vu, row0 + C, row_end);
     }
-    if (row0 > row_begin) store_row_pieces<DV, NOT>(finished, Ou, row0 - C + 16 * rg, row_end, l, col0);
+    if (row0 > row_begin) store_row_pieces<DV, NOT, LDV>(finished, Ou, row0 - C + 16 * rg, row_end, l, col0);
     __syncthreads();
 
     // what the state gives: O^T = S^T Q^T, then the row's factor
@@ -292,20 +300,20 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     __syncthreads();   // everything of the chunk is read
   }
   if (row_end > row_begin)
-    store_row_pieces<DV, NOT>(finished, Ou, row_begin + (row_end - row_begin - 1) / C * C + 16 * rg, row_end, l, col0);
-  if (lengths != nullptr) zero_rows<DV>(Ou, row_end, piece_end);
+    store_row_pieces<DV, NOT, LDV>(finished, Ou, row_begin + (row_end - row_begin - 1) / C * C + 16 * rg, row_end, l, col0);
+  if (lengths != nullptr) zero_rows<DV, LDV>(Ou, row_end, piece_end);
   if (state_out != nullptr && ends_here && active) {
-    float* out = state_out + size_t(unit) * DK * DV;
+    float* out = state_out + size_t(unit) * DK * LDV + part * DV;
 #pragma unroll
     for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
       for (int y = 0; y < ST::NRT; ++y)
-        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(w, x) + r) * DV + 16 * ST::row_tile(w, y) + 4 * q4) =
+        *reinterpret_cast<f32x4*>(out + (16 * ST::col_tile(w, x) + r) * LDV + 16 * ST::row_tile(w, y) + 4 * q4) =
             PER_UNIT * sacc[x][y];
   }
 }
 
-template <int DK, int DV, int C, int CS>
+template <int DK, int DV, int C, int CS, int LDV = DV>
 hipError_t run_fwd_decay(const DecayArgs& a) {
   const int units = a.B * a.H;
   float* states = static_cast<float*>(a.workspace);
@@ -315,17 +323,20 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
     if (err != hipSuccess) return err;
   }
   const auto scan = [&](auto kernel) {
-    return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), kernel, dim3(units * a.G), dim3(64 * (C / 16) * CS), 0, a.stream,
+    return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), kernel, dim3(units * a.G * (LDV / DV)), dim3(64 * (C / 16) * CS), 0, a.stream,
                          static_cast<const elem_t*>(a.Q), static_cast<const elem_t*>(a.K), static_cast<const elem_t*>(a.V), a.s,
                          a.log_decay, static_cast<elem_t*>(a.O), a.state, states, a.state_in, a.seq_len, Divisor(a.H),
                          Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps, int(a.carried));
   };
-  if (a.state != nullptr) return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, EXACT_PARTS>);
-  return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, ROUNDED_PARTS>);
+  if (a.state != nullptr) return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, EXACT_PARTS, LDV>);
+  return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, ROUNDED_PARTS, LDV>);
 }
 
 template <int DK, int DV, int C>
 hipError_t run_decay_totals(const DecayArgs& a, float* dst) {
+  // 128 rows at a time where segments are that long and two such workgroups fit a compute unit (TALLER)
+  if constexpr (C == 64 && LDS_ELEM * 128 * (tile_pitch(DK, 128) + tile_pitch(DV, 128)) + 12 * 128 <= 80 * 1024)
+    if (a.seg_rows >= 128) return run_decay_totals<DK, DV, 128>(a, dst);
   const int units = a.B * a.H;
   return launch_kernel(COTTN_SYM_STR(decay_segment_state), COTTN_SYM(decay_segment_state)<DK, DV, C>, dim3(units * a.G),
                        dim3(4 * C), 0, a.stream, static_cast<const elem_t*>(a.K), static_cast<const elem_t*>(a.V), dst,
@@ -377,6 +388,19 @@ using namespace COTTN_NS;
 // Rows of a chunk: 64, in fp32 32.  Waves on a row group: two where the output of a wave is 128 columns wide and the tiles
 // leave one workgroup to a compute unit, and in fp32, whose chunk is two row groups.
 hipError_t COTTN_SYM(fwd_decay)(const DecayArgs& a) {
+  constexpr int C = ELEM_IS_F32 ? 32 : 64, CS = ELEM_IS_F32 ? 2 : 1;
+  switch (a.value_columns != a.dv ? (a.dk * 1000 + a.dv) * 100 + a.value_columns : 0) {
+    case 3206432: return run_fwd_decay<32, 32, C, CS, 64>(a);
+    case 6406432: return run_fwd_decay<64, 32, C, CS, 64>(a);
+    case 12806432: return run_fwd_decay<128, 32, C, CS, 64>(a);
+    case 3212832: return run_fwd_decay<32, 32, C, CS, 128>(a);
+    case 6412832: return run_fwd_decay<64, 32, C, CS, 128>(a);
+    case 12812832: return run_fwd_decay<128, 32, C, CS, 128>(a);
+    case 3212864: return run_fwd_decay<32, 64, C, CS, 128>(a);
+    case 6412864: return run_fwd_decay<64, 64, C, CS, 128>(a);
+    case 12812864: return run_fwd_decay<128, 64, C, CS, 128>(a);
+    default: break;
+  }
 #ifndef COTTN_ELEM_F32
   if (a.dk == 128 && a.dv == 128 && long(a.B) * a.H * a.G > 256) return run_fwd_decay<128, 128, 32, 2>(a);
 #endif

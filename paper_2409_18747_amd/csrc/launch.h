@@ -261,10 +261,31 @@ struct DecayArgs {
   const float* saved_fwd_states;    // backward only: null, or what the forward left in its workspace
   void* workspace;
   int B, H, N, dk, dv, G, seg_rows;
+  int value_columns;                // forward of one segment: value columns of a workgroup
   bool carried;
   float eps;
   hipStream_t stream;
 };
+
+// Value columns of a workgroup in a forward of one segment: parts of them where sequences are few, so that more compute units
+// have a workgroup.  Kernel alone, continued from a state, whole / 64 / 32 columns: 16 units of 64 rows 128 x 128 9.9 / 7.5 / 6.0 us, 64 x 64
+// 5.7 / - / 4.7; 64 units 128 x 128 10.6 / 8.4 / 8.6, 64 x 128 7.6 / 5.8 / 5.1; 128 units 128 x 128 11.9 / 10.7 / 12.4, 64 x 64
+// 6.1 / - / 5.3, of 384 rows 17.2 / - / 14.7; 192 units of 384 rows 64 x 128 25.1 / 24.5 / 29.0, 128 x 128 32.6 / 36.8 / 46.5.
+constexpr int decay_value_columns(long units, int dk, int dv, bool f32) {
+  if (dv == 32 || units <= 64) return 32;
+  if (units <= 128) return dv == 128 ? 64 : 32;
+  return !f32 && units <= 256 && dk <= 64 && dv == 128 ? 64 : dv;
+}
+// Rows up to which a forward by itself, whose states no backward takes over, walks a sequence as one segment in such parts.
+// Kernels alone, segments / one in parts: 16 units of 192 rows 128 x 128 16.2 / 11.7 us, of 384 22.5 / 19.5; 64 x 64 192 9.3 / 8.1, 256
+// 9.3 / 9.9; 64 x 128 256 12.1 / 10.1, 384 12.8 / 14.3; 128 units of 384 rows 128 x 128 34.3 / 27.9, 64 x 64 17.2 / 14.7; fp32 16 units
+// 128 x 128 128 26.9 / 20.7, 256 30.6 / 37.6, 64 x 64 64 11.4 / 7.9, 128 11.8 / 12.5; 128 units of 384 128 x 128 94 / 75.
+constexpr int decay_one_segment_rows(long units, int dk, int dv, bool f32) {
+  if (dv == 32 || units > 128) return 0;
+  if (units > 64) return 384;
+  if (f32) return dk * dv >= 128 * 128 ? 128 : 64;
+  return dk * dv >= 128 * 128 ? 384 : dk * dv >= 64 * 128 ? 256 : 192;
+}
 
 struct StepDecayArgs {
   const void* q; const void* k; const void* v; const float* s; const float* log_decay;   // log_decay may be null: no decay

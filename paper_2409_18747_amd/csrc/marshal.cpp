@@ -484,7 +484,7 @@ PyObject* fwd_decay(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const float eps = c.real();
   if (!c.ok) Py_RETURN_NONE;
   if (!given_workspace) {
-    have = lib.workspace_bytes_dkdv(COTTN_OP_FWD_DECAY, B, H, N, dk, dv, 0, dt);
+    have = lib.workspace_bytes_dkdv(COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, 0, dt);
     if (have == size_t(-1)) Py_RETURN_NONE;
   }
   at::Tensor made, scratch;

@@ -42,9 +42,11 @@ struct TreeCfg {
   static constexpr bool DIRECT = RG > 2;
   // columns of a wave's tile nt: col0 + STRIDE (m / 4) + OFFSET nt + m % 4
   static constexpr int STRIDE = DIRECT ? 4 : 4 * NOT, OFFSET = DIRECT ? 16 : 4;
+  static constexpr int LDS_BYTES = LDS_ELEM * (2 * T * TPK + T * TPV + (DIRECT ? 8 : DK * SP)) + int(sizeof(frag8)) * RG * PAIRS * 64 + 2048;
+  static constexpr int AT_ONCE = LDS_BYTES <= 80 * 1024 ? 2 : 1;
 };
 template <int DK, int DV, int COLS, int RG>
-__global__ __launch_bounds__(256, 2) void COTTN_SYM(tree_kernel)(
+__global__ __launch_bounds__(256, (TreeCfg<DK, DV, COLS, RG>::AT_ONCE)) void COTTN_SYM(tree_kernel)(
     const elem_t* __restrict__ q, const elem_t* __restrict__ k, const elem_t* __restrict__ v, const float* __restrict__ s,
     const float* __restrict__ log_decay, const int* __restrict__ parent, const float* __restrict__ state,
     elem_t* __restrict__ o, Divisor H, int n_tokens, float inv_eps, int stream) {
@@ -243,11 +245,13 @@ hipError_t launch_tree(const TreeArgs& a) {
 template <int DK, int DV>
 hipError_t run_tree(const TreeArgs& a) {
   constexpr int COLS = ELEM_IS_F32 && DV == 128 ? 64 : DV;   // (four fp32 tiles of 128 columns do not fit the LDS)
-  // up to 64 states: 32 value columns to a workgroup, so that more compute units have one
+  // Up to 64 states: parts of the value columns to a workgroup, so that more compute units have one.  Kernel alone, states of
+  // 128 x 128, whole / 64 / 32 columns: 16 states, 13 tokens 4.1 / - / 3.5 us, 64 tokens 5.8 / 5.1 / 5.4; 64 states, 64 tokens 6.5 /
+  // 5.3 / 7.3; 128 states, 13 tokens 4.7 / - / 5.4.
   if (DV > 32 && a.B * a.H <= 64) {
     if (a.n_tokens <= 16) return launch_tree<DK, DV, 32, 1>(a);
     if (a.n_tokens <= 32) return launch_tree<DK, DV, 32, 2>(a);
-    return launch_tree<DK, DV, 32, 4>(a);
+    return launch_tree<DK, DV, DV < 64 ? DV : 64, 4>(a);
   }
   if (a.n_tokens <= 16) return launch_tree<DK, DV, COLS, 1>(a);
   if (a.n_tokens <= 32) return launch_tree<DK, DV, COLS, 2>(a);

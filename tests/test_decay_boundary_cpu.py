@@ -95,4 +95,22 @@ def test_sizes(lib):
         lib.cottn_tune_segments(0)
         assert size(5, 2, 3, 1000, 64, 32, 128, dtype) == NO_SIZE and segments(5, 2, 3, 1000, 64, 32, 128, dtype) == 0
         assert size(5, 2, 3, 0, 64, 32, 0, dtype) == 0
-    assert size(7, 2, 3, 1000, 64, 32, 0, 1) == NO_SIZE
+    assert size(7, 2, 3, 1000, 64, 32, 0, 1) == size(9, 2, 3, 1000, 64, 32, 0, 1) == NO_SIZE
+
+
+def test_a_forward_alone_needs_no_more(lib):
+    """It walks short prompts of few sequences as one segment, without a workspace, and all others as a pair does."""
+    size = lib.cottn_workspace_bytes_dkdv
+    for dtype in (0, 1, 2):
+        for B in (1, 4, 8, 16):
+            for N in (1, 64, 128, 192, 384, 385, 2048):
+                for dk, dv in ((32, 32), (64, 64), (64, 128), (128, 128)):
+                    pair, alone = size(5, B, 16, N, dk, dv, 0, dtype), size(8, B, 16, N, dk, dv, 0, dtype)
+                    assert alone in (0, pair)
+                    assert alone == pair or (N <= 384 and B <= 8 and dv > 32)
+    assert size(5, 1, 16, 192, 128, 128, 0, 1) > 0 and size(8, 1, 16, 192, 128, 128, 0, 1) == 0
+    # without room the forward takes that split; where neither fits it is refused
+    assert refused(lib, "cottn_fwd_causal_decay", {**FWD, "B": 1, "H": 16, "N": 2048}, {"ws": None}, WORKSPACE)
+    lib.cottn_tune_segments(4)
+    assert size(8, 1, 16, 192, 128, 128, 0, 1) == size(5, 1, 16, 192, 128, 128, 0, 1) > 0
+    lib.cottn_tune_segments(0)

@@ -162,6 +162,26 @@ def test_short_and_long_rows(cottn, dtype, dk, dv, tuned):
     check(out, x, dtype, eps=1e-3 if dtype == "f16" else 1e-6, norms=False)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("B,H,N,dk,dv", [(1, 5, 100, 128, 128), (2, 33, 63, 64, 128), (3, 40, 97, 128, 64), (5, 40, 33, 32, 128),
+                                         (1, 3, 190, 32, 64), (2, 50, 380, 64, 64), (1, 16, 5, 128, 128), (2, 8, 380, 128, 128)])
+@pytest.mark.parametrize("padded", [False, True])
+def test_forward_alone(cottn, dtype, B, H, N, dk, dv, padded):
+    """Without a workspace for a backward: one segment in parts of the value columns, from a state and with lengths."""
+    lens = [N - 7 * b if b % 3 else b for b in range(B)] if padded else None
+    x = draw(B, H, N, dk, dv, dtype, N + B, lens=lens, states=True)
+    d = {k: v.cuda() for k, v in x.items()}
+    state = torch.full((B, H, dk, dv), float("nan"), device="cuda")
+    O = cottn.cottn_fwd_causal_decay(d["Q"], d["K"], d["V"], d["s"], d["log_decay"], state_in=d["state_in"], state=state,
+                                     seq_len=None if lens is None else torch.tensor(lens, dtype=torch.int32).cuda(),
+                                     O=torch.full_like(d["V"], float("nan")))
+    f = {k: v.double() for k, v in x.items()}
+    want, S, M, MS = ref.forward(f["Q"], f["K"], f["V"], x["s"], x["log_decay"], lens, f["state_in"])
+    n = N + max(dk, dv) + 40
+    assert worst(O, want, M, U[dtype], n) <= 1.0 and worst(state, S, MS, U[dtype], n, in_fp32=True) <= 1.0
+    assert norm_error(O, want) <= NORM * U[dtype] + 2e-6 and norm_error(state, S) <= 2 * U[dtype] ** 2 + 2e-6
+
+
 def test_no_decay_is_the_call_without(cottn):
     x = draw(2, 3, 300, 64, 64, "bf16", 9)
     x["log_decay"] = torch.zeros(3)
