@@ -334,8 +334,9 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
 
 template <int DK, int DV, int C>
 hipError_t run_decay_totals(const DecayArgs& a, float* dst) {
-  // 128 rows at a time where segments are that long and two such workgroups fit a compute unit (TALLER)
-  if constexpr (C == 64 && LDS_ELEM * 128 * (tile_pitch(DK, 128) + tile_pitch(DV, 128)) + 12 * 128 <= 80 * 1024)
+  // 128 rows at a time where segments are that long: eight waves, a key tile each (96 units of 1024 rows forward + backward 162.5 ->
+  // 156.4 us; not at narrower shapes, 64 x 64 63.6 / 63.9, 32 x 32 35.8 / 37.1, 128 x 64 105.7 / 106.7)
+  if constexpr (C == 64 && !ELEM_IS_F32 && DK == 128 && DV == 128)
     if (a.seg_rows >= 128) return run_decay_totals<DK, DV, 128>(a, dst);
   const int units = a.B * a.H;
   return launch_kernel(COTTN_SYM_STR(decay_segment_state), COTTN_SYM(decay_segment_state)<DK, DV, C>, dim3(units * a.G),
