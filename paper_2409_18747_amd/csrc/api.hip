@@ -242,8 +242,72 @@ bool make_plan(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype
 
 namespace {
 
+// Calls with a decay: the time of g segments by the model of causal_call_us, with constants for a forward and its backward and for a
+// forward alone, whose sequences of one segment may be in parts of the value columns (decay_value_columns), a step of which is
+// shorter by `parts`.  Fitted to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128 x 128, fp32
+// 64 x 64): the split chosen takes 0.4 and 0.5 % longer than the best of up to ten measured; the pair with the constants of
+// causal_call_us 1.5 % (300 units of 2048 rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units
+// of 1024 rows 128 x 128 4 segments 89 us, 1 segment 62).  Farthest off: 128 units of 512 rows 32 x 32 with backward 8 segments 33 us, 4
+// segments 28; 16 units of 8192 rows 64 x 64 forward 16 segments 1.14 times 32 segments.
+struct DecayTimes {
+  double next_narrow_f32, next_f32, next_narrow, next;   // of a step for each further workgroup at once on a compute unit
+  double step_f32, step_widest, step, prologue, row;      // us a column, us a column, us a column, steps, us a MB
+  double launch, totals, add_widest, add;                 // us, of a step, us a KB of a state
+  double parts_64, parts_128, parts_many;
+};
+constexpr DecayTimes kDecayPair = {0.2, 0.434, 0.019, 0.275, 0.123, 0.0667, 0.0573, 0.85, 0.876, 5.56, 0.0538, 0.0259, 0.0402, 1, 1, 1};
+constexpr DecayTimes kDecayAlone = {0.2, 0.266, 0.02, 0.23, 0.05, 0.0245, 0.0287, 1.02, 0.1235, 3.33, 0.3225, 0.0251, 0.0343, 0.8, 0.7, 0.48};
+double decay_call_us(const DecayTimes& t, long units, long N, long n_chunks, long g, bool f32, int dk, int dv) {
+  const bool narrowest = dk == 32 && dv == 32, widest = dk == 128 && dv == 128;
+  const int big = dk > dv ? dk : dv, small = dk > dv ? dv : dk;
+  const long at_once = narrowest ? 4 : (f32 ? big == 128 && small >= 64 : widest) ? 1 : 2;
+  const double next_one = f32 ? (narrowest ? t.next_narrow_f32 : t.next_f32) : narrowest ? t.next_narrow : t.next;
+  double step = (f32 ? t.step_f32 : widest ? t.step_widest : t.step) * (dk + dv);
+  if (g == 1 && decay_value_columns(units, dk, dv, f32) != dv) step *= units > 128 ? t.parts_many : dv == 64 ? t.parts_64 : t.parts_128;
+  const long steps = (n_chunks + g - 1) / g, on_cu = (units * g + kComputeUnits - 1) / kComputeUnits;
+  const auto together = [&](long n) { return n > 0 ? 1.0 + next_one * double(n - 1) : 0.0; };
+  double us = step * (double(steps) + t.prologue) * (double(on_cu / at_once) * together(at_once) + together(on_cu % at_once));
+  const double rows_us = t.row * 1e-6 * double(units) * double(N) * (dk + dv) * (f32 ? 4 : 2);
+  if (us < rows_us) us = rows_us;
+  if (g > 1) {
+    const double state = double(dk) * dv * 4.0 / 1024.0;   // KB
+    us += t.launch + t.totals * step * double(steps * on_cu);
+    const bool wide = widest && !f32;
+    us += causal_totals_in_place(units, int(g), dk, dv, f32)
+              ? (wide ? t.add_widest : t.add) * (state + 7.0) * double(g - 1)
+              : (wide ? 9.0 + 0.2 * double(g) : 8.0 + 0.3 * double(g)) + 0.001 * state * double(units * g);
+  }
+  return us;
+}
+
+// Segments of a call with a decay: the least time by the model among splits of up to 1024 workgroups, or none; a forward alone takes
+// no more than with its backward, so that the size of its workspace says which of the two it is.  With a backward,
+// 16-bit sequences of two chunks are two segments up to 128 units (128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 -> 26.5, 32 x 32
+// 18.1 -> 16.8; 128 units 128 x 128 40.3 -> 39.1; 192 units 43.4 -> 64.6), and longer ones are split where those without a decay are
+// (causal_segments).
+long decay_segments(bool alone, long units, long N, long n_chunks, bool f32, int dk, int dv) {
+  const bool narrowest = dk == 32 && dv == 32, widest = dk == 128 && dv == 128;
+  const bool cut = !f32 && !alone && ((n_chunks == 2 && units <= 128) || (!widest && n_chunks > 4 && units <= 160) ||
+                                      (narrowest && n_chunks > 8 && units < 384));
+  const DecayTimes& t = alone ? kDecayAlone : kDecayPair;
+  const long most = alone ? decay_segments(false, units, N, n_chunks, f32, dk, dv) : n_chunks;
+  double best = decay_call_us(t, units, N, n_chunks, 1, f32, dk, dv);
+  long best_g = 1;
+  for (long steps = n_chunks - 1; steps >= 1; --steps) {
+    const long g = (n_chunks + steps - 1) / steps;
+    steps = (n_chunks + g - 1) / g;
+    if (units * g > 1024 || g > most) break;
+    const double us = decay_call_us(t, units, N, n_chunks, g, f32, dk, dv);
+    if (us < best || (cut && best_g == 1)) {
+      best = us;
+      best_g = g;
+    }
+  }
+  return best_g;
+}
+
 // The split of a call with a decay, the same for a forward and its backward; a forward by itself (`alone`) may walk a sequence
-// as one segment where those two take several.
+// in fewer segments where those two take several.
 struct DecayPlan {
   int G, seg_rows, value_columns;
   bool carried;   // DecayArgs
@@ -255,14 +319,7 @@ bool make_decay_plan(bool alone, int B, int H, int N, int dk, int dv, int chunk,
   if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != C)) return false;
   const long units = long(B) * H, n_chunks = (long(N) + C - 1) / C;
   long want = g_tuned_segments;
-  if (want <= 0) {
-    want = n_chunks > 0 ? causal_segments(units, N, n_chunks, C, dtype, dk, dv) : 1;
-    // Two chunks are two segments up to 128 units: the step that a scan saves is longer than the totals' launch (forward +
-    // backward of 128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 -> 26.5, 32 x 32 18.1 -> 16.8; 128 units 128 x 128
-    // 40.3 -> 39.1; 192 units 128 x 128 43.4 -> 64.6)
-    if (!f32 && n_chunks == 2 && units <= 128) want = 2;
-    if (alone && N <= decay_one_segment_rows(units, dk, dv, f32)) want = 1;
-  }
+  if (want <= 0) want = n_chunks > 0 ? decay_segments(alone, units, N, n_chunks, f32, dk, dv) : 1;
   if (want > n_chunks) want = n_chunks;
   if (want < 1) want = 1;
   const long steps = n_chunks > 0 ? (n_chunks + want - 1) / want : 1, G = n_chunks > 0 ? (n_chunks + steps - 1) / steps : 1;
@@ -827,8 +884,9 @@ int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   DecayPlan plan;
   if (!make_decay_plan(false, B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
   // with room for the states that a backward takes over they are left there, else the call takes the split of a forward alone
-  if (workspace == nullptr || workspace_bytes < decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan))
-    make_decay_plan(true, B, H, N, dk, dv, 0, dtype, &plan);
+  const size_t with_backward = decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan);
+  if (with_backward > 0 && (workspace == nullptr || workspace_bytes < with_backward))
+    if (!make_decay_plan(true, B, H, N, dk, dv, 0, dtype, &plan)) return COTTN_E_SHAPE;
   st = check_workspace(workspace, workspace_bytes, decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan));
   if (st != COTTN_OK) return st;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);

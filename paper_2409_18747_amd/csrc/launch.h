@@ -276,17 +276,6 @@ constexpr int decay_value_columns(long units, int dk, int dv, bool f32) {
   if (units <= 128) return dv == 128 ? 64 : 32;
   return !f32 && units <= 256 && dk <= 64 && dv == 128 ? 64 : dv;
 }
-// Rows up to which a forward by itself, whose states no backward takes over, walks a sequence as one segment in such parts.
-// Kernels alone, segments / one in parts: 16 units of 192 rows 128 x 128 16.2 / 11.7 us, of 384 22.5 / 19.5; 64 x 64 192 9.3 / 8.1, 256
-// 9.3 / 9.9; 64 x 128 256 12.1 / 10.1, 384 12.8 / 14.3; 128 units of 384 rows 128 x 128 34.3 / 27.9, 64 x 64 17.2 / 14.7; fp32 16 units
-// 128 x 128 128 26.9 / 20.7, 256 30.6 / 37.6, 64 x 64 64 11.4 / 7.9, 128 11.8 / 12.5; 128 units of 384 128 x 128 94 / 75.
-constexpr int decay_one_segment_rows(long units, int dk, int dv, bool f32) {
-  if (dv == 32 || units > 128) return 0;
-  if (units > 64) return 384;
-  if (f32) return dk * dv >= 128 * 128 ? 128 : 64;
-  return dk * dv >= 128 * 128 ? 384 : dk * dv >= 64 * 128 ? 256 : 192;
-}
-
 struct StepDecayArgs {
   const void* q; const void* k; const void* v; const float* s; const float* log_decay;   // log_decay may be null: no decay
   const float* from; const int* parent; int n_from;   // states of n_from sequences; parent null or int[B]
