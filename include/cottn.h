@@ -298,7 +298,8 @@ int cottn_scale_backward_varlen(const float* m, const int* seq_len, const float*
  * library's own (64 rows, fp32 32).  All dtypes; states and ds are accurate to fp32 whatever the dtype (16-bit operands
  * enter them in parts).  Workspaces: cottn_workspace_bytes_dkdv with COTTN_OP_FWD_DECAY and COTTN_OP_BWD_DECAY, chunk 0.  A
  * forward that no backward follows can do with a workspace of COTTN_OP_FWD_DECAY_ALONE, often none, and is then faster for short
- * prompts of few sequences: with less than COTTN_OP_FWD_DECAY asks for it takes the split of that smaller size.
+ * prompts of few sequences: with less than COTTN_OP_FWD_DECAY asks for it takes the split of that smaller size.  A row that is
+ * not finite can make results of the rows before it in its chunk not finite, as well as those behind it.
  *
  * Forward.  seq_len: NULL, or int[B] as in the *_varlen calls, and then s is float[B][H] (else float[H]); the state is that
  * after a sequence's own last row.  state_in: NULL (zeros) or the state before row 0.  state: NULL or out; the two must not
@@ -339,7 +340,8 @@ int cottn_step_decay(const void* q, const void* k, const void* v, const float* s
  * state, float[B][H][dk][dv], as it is:
  *   o_i = s [ g^(depth_i + 1) qh_i state + sum over j = i and its ancestors of g^(depth_i - depth_j) (qh_i . kh_j) v_j ]
  * with depth 0 at the roots.  cottn_tree_accept takes state on along the path to token last[b] of each sequence, in place;
- * where last[b] is none of 0 .. T - 1 nothing is accepted and the state stays.  T = 0 does nothing. */
+ * where last[b] is none of 0 .. T - 1 nothing is accepted and the state stays; tokens off the path are not read.  T = 0 does
+ * nothing.  (In cottn_tree a token that is not finite can make outputs of other tokens of its sequence not finite.) */
 #define COTTN_MOST_DRAFTS 64
 int cottn_tree(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const int* parent,
                const float* state, void* o, int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream);

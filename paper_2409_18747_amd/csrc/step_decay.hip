@@ -79,7 +79,8 @@ __global__ __launch_bounds__(256) void step_decay_kernel(
     x.store(w == 0 ? qh : kh, 1.f, eps, l);
   }
   const f32x4 v4 = Element<T>::load4(v + size_t(unit) * DV + col);
-  const float g = Decay(log_decay != nullptr ? log_decay[head] : 0.f).after(1.f), scale = s[head];
+  const float scale = s[head];
+  const Kept kept(Decay(log_decay != nullptr ? log_decay[head] : 0.f), 1.f);
   __syncthreads();
   float* out = to + size_t(unit) * DK * DV;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -88,10 +89,10 @@ __global__ __launch_bounds__(256) void step_decay_kernel(
     const int row = p * R::RPP + row0;
     if (R::WHOLE || row < DK) {
       const float kr = kh[row], qr = qh[row];
-      f32x4 x;
+      f32x4 x = kept.of(rows[p]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] = __builtin_fmaf(g, rows[p][i], kr * v4[i]);
+        x[i] = __builtin_fmaf(kr, v4[i], x[i]);
         acc[i] = __builtin_fmaf(qr, x[i], acc[i]);
       }
       store_state4(out + size_t(row) * DV + col, x);
@@ -135,11 +136,9 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(
   path = (static_cast<unsigned long long>(unsigned(__builtin_amdgcn_readfirstlane(int(path >> 32)))) << 32) |
          unsigned(__builtin_amdgcn_readfirstlane(int(path)));
   const int length = __builtin_popcountll(path);
-  const float kept = g.after(float(length));
+  const Kept kept(g, float(length));
 #pragma unroll
-  for (int p = 0; p < R::PASSES; ++p)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) rows[p][i] *= kept;
+  for (int p = 0; p < R::PASSES; ++p) rows[p] = kept.of(rows[p]);
   for (int first = 0; first < length; first += MOST) {
     const int n = min(MOST, length - first);
     // wave w takes every fourth token of the path

@@ -101,6 +101,45 @@ def test_step_decays(cottn, ld):
     assert worst(o, want, M, U["f32"], 72) <= 1.0 and worst(d["S"], S, MS, U["f32"], 52, in_fp32=True) <= 1.0
 
 
+def hardly_forgetting():
+    """A log_decay near -2e-4 whose exp lies far from every fp32 number."""
+    ld = (-2e-4 * (1 + torch.arange(4096) * 2.0 ** -12)).float()
+    g = torch.exp(ld.double())
+    return ld[torch.argmax(torch.abs(g.float().double() - g))]
+
+
+def test_many_steps_hardly_forget(cottn):
+    """2000 calls without a key: what is left of a state is g^2000.  A factor rounded to fp32 would be off by nearly 2^-25 with
+    the same sign in each, 6e-5 in all; roundings of the products (2^-24 at most, of either sign) stay within four times
+    sqrt(2000) of them, 1.1e-5, and accepting 500 paths of four tokens within half of that."""
+    ld, S = hardly_forgetting(), torch.randn(2, 1, 64, 64, generator=torch.Generator().manual_seed(8))
+    zero = torch.zeros(2, 1, 64).cuda()
+    state, accepted, one, d_ld = S.cuda(), S.cuda(), torch.ones(1).cuda(), ld[None].cuda()
+    parent, last = torch.tensor([[-1, 0, 1, 2]] * 2, dtype=torch.int32).cuda(), torch.full((2,), 3, dtype=torch.int32).cuda()
+    drafts = torch.zeros(2, 1, 4, 64).cuda()
+    for t in range(2000):
+        cottn.cottn_step_decay(zero, zero, zero, one, d_ld, state)
+        if t % 4 == 0:
+            cottn.cottn_tree_accept(drafts, drafts, accepted, parent, last, log_decay=d_ld)
+    want = S.double() * torch.exp(2000 * ld.double())
+    assert norm_error(state, want) <= 1.1e-5 and norm_error(accepted, want) <= 0.6e-5
+
+
+def test_rejected_drafts_are_not_read(cottn):
+    """Tokens off the accepted path may hold anything."""
+    x, parent = draw(2, 3, 6, 64, 128, "bf16", 12), torch.tensor([[-1, 0, 0, 2, 1, 3]] * 2, dtype=torch.int32)
+    last = torch.tensor([5, 4], dtype=torch.int32)   # by 0 2 3 and by 0 1
+    y = dict(x, k=x["k"].clone(), v=x["v"].clone())
+    for b, off in enumerate(([1, 4], [2, 3, 5])):
+        y["k"][b, :, off] = float("nan")
+        y["v"][b, :, off] = float("inf")
+    states = []
+    for z in (x, y):
+        d = cuda(z)
+        states.append(cottn.cottn_tree_accept(d["k"], d["v"], d["S"], parent.cuda(), last.cuda(), log_decay=d["ld"]))
+    assert torch.equal(*states) and torch.isfinite(states[0]).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("dk,dv", WIDTHS)
 @pytest.mark.parametrize("T", [1, 13, 32, 64])
