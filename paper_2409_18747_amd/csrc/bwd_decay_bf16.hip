@@ -69,7 +69,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ dQ,
     const float* __restrict__ fwd_states, float* __restrict__ rev_totals, float* __restrict__ ds_partial,
     const float* __restrict__ state_in, const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units,
-    float inv_eps, int carried) {
+    float inv_eps, int flags) {
   using Cfg = DecayBwdCfg<DK, DV, C, CS>;
   using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
@@ -86,7 +86,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
   COTTN_LDS_ARRAY(float, ds_wave, Cfg::NW, 8)
   Unparted un;
   fetch_argument_now(Q, K, V, dO, s, log_decay, dQ, fwd_states, rev_totals, ds_partial, state_in, lengths, H, G, seg_rows, N,
-                     units, inv_eps, carried);
+                     units, inv_eps, flags);
+  const bool carried = flags & CARRIED;
   int unit, seg;
   unit_and_segment(blockIdx.x, units, G, unit, seg);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
@@ -342,7 +343,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ dK, elem_t* __restrict__ dV,
     const float* __restrict__ rev_states, const float* __restrict__ ds_partial, float* __restrict__ ds,
     const float* __restrict__ rev_in, float* __restrict__ rev_out, const int* __restrict__ lengths, int B, Divisor H, Divisor G,
-    int seg_rows, int N, float inv_eps, int carried) {
+    int seg_rows, int N, float inv_eps, int flags) {
   using Cfg = DecayBwdCfg<DK, DV, C, CS>;
   using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
@@ -358,7 +359,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
   COTTN_LDS_ARRAY(float, xdot, CS > 1 ? CS * C : 1, 7)
   Unparted un;
   fetch_argument_now(Q, K, V, dO, s, log_decay, dK, dV, rev_states, ds_partial, ds, rev_in, rev_out, lengths, B, H, G, seg_rows,
-                     N, inv_eps, carried);
+                     N, inv_eps, flags);
+  const bool carried = flags & CARRIED, stream = flags & STREAM;
   int unit, seg;
   unit_and_segment(blockIdx.x, B * H.n, G, unit, seg);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
@@ -375,10 +377,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
   StageK qst, kst;
   StageV vst, gst;
   if (row_begin < row_end) {
-    qst.fetch(Qu, last_row0, row_end);
-    kst.fetch(Ku, last_row0, row_end);
-    vst.fetch(Vu, last_row0, row_end);
-    gst.fetch(Gu, last_row0, row_end);
+    qst.fetch(Qu, last_row0, row_end, stream);
+    kst.fetch(Ku, last_row0, row_end, stream);
+    vst.fetch(Vu, last_row0, row_end, stream);
+    gst.fetch(Gu, last_row0, row_end, stream);
   }
   // ds[h]: over batches and segments; with lengths ds[b][h], over segments
   if (int(blockIdx.x) < (lengths != nullptr ? B * H.n : H.n) && w == 0) {
@@ -460,10 +462,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
       gst.commit_plain(Gs, un);
     }
     if (row0 > row_begin) {
-      qst.fetch(Qu, row0 - C, row_end);
-      kst.fetch(Ku, row0 - C, row_end);
-      vst.fetch(Vu, row0 - C, row_end);
-      gst.fetch(Gu, row0 - C, row_end);
+      qst.fetch(Qu, row0 - C, row_end, stream);
+      kst.fetch(Ku, row0 - C, row_end, stream);
+      vst.fetch(Vu, row0 - C, row_end, stream);
+      gst.fetch(Gu, row0 - C, row_end, stream);
     }
     if (row0 < last_row0) {
       store_row_pieces<DK, NKT>(done_k, dKu, row0 + C + 16 * rg, row_end, l, colk);
@@ -638,18 +640,23 @@ hipError_t run_bwd_decay(const DecayArgs& a) {
     if (err != hipSuccess) return err;
     fwd = own_fwd;
   }
+  // The second scan is the last to read the rows: past the caches where they hold no call's tensors (768 units of 512 rows 128 x 128,
+  // forward + backward 436 -> 419 us, 16 of 65536 rows 64 x 64 488 -> 473; where they do, 96 of 1024 rows, 63.7 -> 64.8; and the
+  // first scan too, 426 and 478).
+  const double bytes = 2.0 * units * double(a.N) * (DK + DV) * ELEM;
+  const int flags = (a.carried ? CARRIED : 0) | (bytes > 256.0 * 1024 * 1024 ? STREAM : 0);
   const dim3 grid(units * a.G), block(64 * (C / 16) * CS);
   const Divisor H(a.H), G(a.G);
   const float inv_eps = 1.0f / a.eps;
   err = launch_kernel(COTTN_SYM_STR(bwd_decay_dq), COTTN_SYM(bwd_decay_dq)<DK, DV, C, CS>, grid, block, 0, a.stream, Q, K, V, dO, a.s,
                       a.log_decay, static_cast<elem_t*>(a.dQ), fwd, rev, ds_partial, a.state_in, a.seq_len, H, G, a.seg_rows, a.N,
-                      units, inv_eps, int(a.carried));
+                      units, inv_eps, flags);
   if (err == hipSuccess && a.G > 1 && a.carried) err = launch_decay_carry(a, rev, true);
   if (err != hipSuccess) return err;
   const auto dkdv = [&](auto kernel) {
     return launch_kernel(COTTN_SYM_STR(bwd_decay_dkdv), kernel, grid, block, 0, a.stream, Q, K, V, dO, a.s, a.log_decay,
                          static_cast<elem_t*>(a.dK), static_cast<elem_t*>(a.dV), rev, ds_partial, a.ds, a.rev_state_in,
-                         a.rev_state_out, a.seq_len, a.B, H, G, a.seg_rows, a.N, inv_eps, int(a.carried));
+                         a.rev_state_out, a.seq_len, a.B, H, G, a.seg_rows, a.N, inv_eps, flags);
   };
   if (a.rev_state_out != nullptr) return dkdv(COTTN_SYM(bwd_decay_dkdv)<DK, DV, C, CS, EXACT_PARTS>);
   return dkdv(COTTN_SYM(bwd_decay_dkdv)<DK, DV, C, CS, ROUNDED_PARTS>);

@@ -252,6 +252,9 @@ struct TreeNode {
   __device__ __forceinline__ int depth() const { return __builtin_popcountll(path) - 1; }
 };
 
+// Flags of a scan: what the states are (DecayArgs::carried), and rows that nothing will find in a cache again.
+enum : int { CARRIED = 1, STREAM_Q = 2, STREAM_KV = 4, STREAM = 8 };
+
 // waves per SIMD that registers are capped for: two workgroups to a compute unit where the LDS holds them
 constexpr int decay_waves(int lds_bytes, int waves, int waves_per_group) {
   const int own = waves / 4 < 1 ? 1 : waves / 4, at_once = (160 * 1024) / lds_bytes >= 2 ? 2 : 1;

@@ -121,7 +121,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V,
     const float* __restrict__ s, const float* __restrict__ log_decay, elem_t* __restrict__ O,
     float* __restrict__ state_out, const float* __restrict__ seg_states, const float* __restrict__ state_in,
-    const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units, float inv_eps, int carried) {
+    const int* __restrict__ lengths, Divisor H, Divisor G, int seg_rows, int N, int units, float inv_eps, int flags) {
   using Cfg = DecayFwdCfg<DK, DV, C, CS>;
   using ST = AccTiles<DV, DK, Cfg::NW>;   // value rows, key columns
   using StageK = TileStage<DK, C, Cfg::NT>;
@@ -136,8 +136,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   COTTN_LDS_ARRAY(float, rq, C, 6)
   Unparted un;
   fetch_argument_now(Q, K, V, s, log_decay, O, state_out, seg_states, state_in, lengths, H, G, seg_rows, N, units, inv_eps,
-                     carried);
-  constexpr int VALUE_PARTS = LDV / DV;
+                     flags);
+  constexpr int VALUE_PARTS = LDV / DV;   // (several only where sequences are few: nothing past the caches)
+  const bool carried = flags & CARRIED, stream_q = VALUE_PARTS == 1 && (flags & STREAM_Q),
+             stream_kv = VALUE_PARTS == 1 && (flags & STREAM_KV);
   int unit, seg, part = 0;
   if constexpr (VALUE_PARTS > 1) {   // (one segment)
     unit = blockIdx.x / VALUE_PARTS;
@@ -161,9 +163,9 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   }
   StageK qst, kst;
   StageV vst;
-  qst.fetch(Qu, row_begin, row_end);
-  kst.fetch(Ku, row_begin, row_end);
-  vst.fetch(Vu, row_begin, row_end);
+  qst.fetch(Qu, row_begin, row_end, stream_q);
+  kst.fetch(Ku, row_begin, row_end, stream_kv);
+  vst.fetch(Vu, row_begin, row_end, stream_kv);
   const int head = unit - quotient(unit, H) * H.n;
   const Decay g(log_decay[head]);
   const float scale = s[lengths != nullptr ? unit : head];
@@ -226,9 +228,9 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
       vst.commit_plain(Vs, un);
     }
     if (row0 + C < row_end) {
-      qst.fetch(Qu, row0 + C, row_end);
-      kst.fetch(Ku, row0 + C, row_end);
-      vst.fetch(Vu, row0 + C, row_end);
+      qst.fetch(Qu, row0 + C, row_end, stream_q);
+      kst.fetch(Ku, row0 + C, row_end, stream_kv);
+      vst.fetch(Vu, row0 + C, row_end, stream_kv);
     }
     if (row0 > row_begin) store_row_pieces<DV, NOT, LDV>(finished, Ou, row0 - C + 16 * rg, row_end, l, col0);
     __syncthreads();
@@ -322,11 +324,16 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
     if (err == hipSuccess && a.carried) err = launch_decay_carry(a, states, false);
     if (err != hipSuccess) return err;
   }
+  // Rows that nothing finds in a cache again, as without decay (fwd_causal_bf16.hip): 64 x 16 heads of 2048 rows, forward alone, 128 x 128
+  // 561 -> 558 us, 64 x 64 228.5 -> 223.4; where they fit, 96 units of 1024 rows 64 x 64 with backward 63.7 -> 64.1.
+  const double bytes = 2.0 * units * double(a.N) * (DK + LDV) * ELEM;
+  const int flags = (a.carried ? CARRIED : 0) | (bytes > 256.0 * 1024 * 1024 ? STREAM_Q : 0) |
+                    (a.G == 1 && bytes > 1024.0 * 1024 * 1024 ? STREAM_KV : 0);
   const auto scan = [&](auto kernel) {
     return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), kernel, dim3(units * a.G * (LDV / DV)), dim3(64 * (C / 16) * CS), 0, a.stream,
                          static_cast<const elem_t*>(a.Q), static_cast<const elem_t*>(a.K), static_cast<const elem_t*>(a.V), a.s,
                          a.log_decay, static_cast<elem_t*>(a.O), a.state, states, a.state_in, a.seq_len, Divisor(a.H),
-                         Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps, int(a.carried));
+                         Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps, flags);
   };
   if (a.state != nullptr) return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, EXACT_PARTS, LDV>);
   return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, ROUNDED_PARTS, LDV>);

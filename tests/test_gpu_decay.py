@@ -293,3 +293,22 @@ def test_captured(cottn):
         torch.cuda.synchronize()
         for a, b in zip(outs, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B,N,segments", [(5, 16384, 0), (160, 2048, 1)])
+def test_more_than_the_caches_hold(cottn, B, N, segments):
+    """Calls of 0.3 and 1.3 GB: the last sequence's results are those of a call of its own, both within two roundings of the
+    true ones."""
+    H, d = 8, 64
+    g = torch.Generator(device="cuda").manual_seed(21)
+    Q, K, V, dO = (torch.randn(B, H, N, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(4))
+    s, ld = torch.ones(H, device="cuda"), -torch.exp(torch.linspace(-6.0, 0.0, H)).cuda()
+    one = [t[-1:].contiguous() for t in (Q, K, V, dO)]
+    cottn.cottn_tune_segments(segments)
+    try:
+        got = [cottn.cottn_fwd_causal_decay(Q, K, V, s, ld), *cottn.cottn_bwd_causal_decay(Q, K, V, s, ld, dO)[:3]]
+    finally:
+        cottn.cottn_tune_segments(0)
+    want = [cottn.cottn_fwd_causal_decay(*one[:3], s, ld), *cottn.cottn_bwd_causal_decay(*one[:3], s, ld, one[3])[:3]]
+    for a, b in zip(got, want):
+        assert norm_error(a[-1:], b.cpu().double()) <= 2 * NORM * U["bf16"]
