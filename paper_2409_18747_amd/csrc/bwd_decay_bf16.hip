@@ -8,7 +8,7 @@
 //
 // ds = sum_i (sum_j g^(i-j) (qh_i . kh_j) v_j) . dO_i is a result in fp32 and a sum of terms of both signs, so it is not taken from
 // results of rounded operands: the rows before a chunk give g <H, G>, element by element from two fp32 matrices whose operands are
-// carried in two parts, and the chunk itself gives the sum of its two masked fp32 tiles' products before they are rounded.
+// carried in parts (EXACT_PARTS), and the chunk itself gives the sum of its two masked fp32 tiles' products before they are rounded.
 //
 // The chain rule through x / max(|x|, eps): dx = s r (dxh - xh (xh . dxh)) with r = 1 / max(|x|, eps); rows at or below eps have
 // dx = s r dxh.
@@ -62,7 +62,8 @@ __device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stag
 // ---------------------------------------------------------------------------------------
 // dQ of a segment, first chunk to last.  H and G sit in accumulators with the values down and the keys along, tile (x, y):
 // element [v] of lane (r, q4) is H[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  A wave has few key tiles and all
-// values (of its part): fragments of keys and queries are the ones that weights go to, 40 instructions each.
+// values (of its part): fragments of keys and queries are the ones that weights go to, 50 instructions each.  bf16: 96 units
+// of 1024 rows 64 x 64 21.8 us (VALU issue 41 %, matrix instructions 17 %); 16 of 65536 rows 157 us, 4.3 TB/s (53 %, 24 %).
 template <int DK, int DV, int C, int CS>
 COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
@@ -336,7 +337,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
 // ---------------------------------------------------------------------------------------
 // dK and dV of a segment, last chunk to first.  R sits in accumulators with the values down and the keys along, tile (x, y):
 // element [v] of lane (r, q4) is R[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  The first workgroups also add up
-// ds from what the dQ scan left.  PARTS: EXACT_PARTS where the reverse-time state is asked for.
+// ds from what the dQ scan left.  PARTS: EXACT_PARTS where the reverse-time state is asked for.  bf16: 96 units of 1024 rows
+// 64 x 64 19.1 us (VALU issue 34 %, matrix instructions 13 %, LDS 36 %); 16 of 65536 rows 150 us, 5.4 TB/s.
 template <int DK, int DV, int C, int CS, int PARTS>
 COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
@@ -667,7 +669,10 @@ hipError_t run_bwd_decay(const DecayArgs& a) {
 
 using namespace COTTN_NS;
 
-// Rows of a chunk and waves on a row group: as in the backward without decay (bwd_causal_bf16.hip: BwdSplit).
+// Rows of a chunk and waves on a row group, as in the backward without decay (bwd_causal_bf16.hip: BwdSplit).  96 units of 1024 rows,
+// forward + backward, bf16: 64 x 64 one wave / two 63.5 / 103 us, 128 x 128 64 rows / 32 157 / 250, 128 x 64 32 rows / 64 rows, each with two
+// waves, 106 / 264: the others do not fit their registers.  fp32 384 units of 512 rows, two waves / four: 128 x 64 635 / 629, 64 x 128
+// 579 / 596.
 hipError_t COTTN_SYM(bwd_decay)(const DecayArgs& a) {
 #define COTTN_CASE(DK, DV)                                                                                             \
   case DK * 1000 + DV: {                                                                                               \

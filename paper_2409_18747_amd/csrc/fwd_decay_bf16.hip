@@ -6,6 +6,9 @@
 // it forms the masked tiles (Qh Kh^T (.) g^(i-j)) and their product with V, adds what the state gives, and takes the
 // state on to the chunk's end.  Where a sequence is cut into segments, a first kernel leaves the total of every segment
 // but the last, each as seen from the segment's own end; the scans weigh and add those before theirs.
+//
+// What bounds them: vector instructions (the weights of operand fragments, their parts, the masked tiles) and the rows' way through
+// memory, at some 4 to 5.4 TB/s for large calls; matrix instructions take a quarter of the time.
 #include "device_common.h"
 #include "launch.h"
 #include "tile_io.h"
@@ -47,7 +50,8 @@ __device__ __forceinline__ void store_key_factors(float* rows, const RowFactors<
 
 // ---------------------------------------------------------------------------------------
 // T[unit][segment] = sum over the rows j of a segment of g^(end-1-j) kh_j^T v_j, for all segments but the last of a
-// unit (and those that a sequence of a padded batch does not reach), as tiles in accumulator order.
+// unit (and those that a sequence of a padded batch does not reach), as tiles in accumulator order.  96 units of 1024 rows 64 x 64 in
+// bf16, 4 segments, 8.8 us; 16 of 65536 rows, 32 segments, 55.8 us, 4.8 TB/s (VALU issue 57 %, matrix instructions 21 %).
 template <int DK, int DV, int C>
 COTTN_KERNEL((C * 4), decay_segment_state)
     const elem_t* __restrict__ K, const elem_t* __restrict__ V, float* __restrict__ seg_state,
@@ -115,7 +119,9 @@ COTTN_KERNEL((C * 4), decay_segment_state)
 // The scan of one segment.  Wave (row group rg, column part cp) owns the query rows 16 rg .. of the chunk and the output
 // columns of its part, and tiles of the state, held as add_tokens says.  Results are accumulated transposed: a lane holds four
 // consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value columns, which the whole
-// computation leaves apart from one another but for the masked tiles; those are formed LDV / DV times.  PARTS: EXACT_PARTS where the state is asked for.
+// computation leaves apart from one another but for the masked tiles; those are formed LDV / DV times.  PARTS: EXACT_PARTS where the state is asked for.  bf16: 96 units of 1024 rows 64 x 64 in
+// 4 segments 14.8 us; 16 of 65536 rows in 32 segments 99 us, 5.4 TB/s; 1024 of 2048 rows 128 x 128 555 us, 3.9 TB/s (VALU issue 47 %,
+// matrix instructions 28 %, LDS 46 % of the time).
 template <int DK, int DV, int C, int CS, int PARTS, int LDV = DV>
 COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V,
@@ -352,7 +358,8 @@ hipError_t run_decay_totals(const DecayArgs& a, float* dst) {
 }
 
 // In place, for four neighbouring elements: slot k (in walking order) <- what the state at its start is, which is
-// g^seg_rows times that of the slot before, and that slot's total.
+// g^seg_rows times that of the slot before, and that slot's total.  16 units of 32 segments 64 x 64: 7.2 us, two trips to memory a batch
+// of eight slots.
 __global__ __launch_bounds__(256) void decay_carry(float* __restrict__ slots, const float* __restrict__ log_decay,
                                                    const int* __restrict__ lengths, Divisor H, int G, int seg_rows, int N,
                                                    int elems, long total, int reverse) {
@@ -393,8 +400,11 @@ using namespace COTTN_NS;
     default: return hipErrorInvalidValue;                                                                            \
   }
 
-// Rows of a chunk: 64, in fp32 32.  Waves on a row group: two where the output of a wave is 128 columns wide and the tiles
-// leave one workgroup to a compute unit, and in fp32, whose chunk is two row groups.
+// Rows of a chunk: 64, in fp32 32.  Waves on a row group: one; two where the output of a wave would be 128 columns wide and
+// in fp32, whose chunk is two row groups; in fp32 128 x 128, where the LDS holds one workgroup to a compute unit, four (two / four:
+// 384 units of 512 rows 330 / 284 us, 15 of 777 43.0 / 41.4; 64 x 64, 15 units of 777, 128 registers for two workgroups of eight waves, 18.7 / 21.7).
+// 16-bit 128 x 128 with more workgroups than compute units: 32 rows, so that two of them share one (1024 units of 2048 rows, 64 / 32
+// rows 598 / 555 us; 192 workgroups of 512 rows each, with totals and backward, 157 / 163; 32 rows with four waves, spilling, 1187).
 hipError_t COTTN_SYM(fwd_decay)(const DecayArgs& a) {
   constexpr int C = ELEM_IS_F32 ? 32 : 64, CS = ELEM_IS_F32 ? 2 : 1;
   switch (a.value_columns != a.dv ? (a.dk * 1000 + a.dv) * 100 + a.value_columns : 0) {
@@ -413,7 +423,7 @@ hipError_t COTTN_SYM(fwd_decay)(const DecayArgs& a) {
   if (a.dk == 128 && a.dv == 128 && long(a.B) * a.H * a.G > 256) return run_fwd_decay<128, 128, 32, 2>(a);
 #endif
 #define COTTN_CASE(DK, DV) \
-  case DK * 1000 + DV: return run_fwd_decay<DK, DV, ELEM_IS_F32 ? 32 : 64, ELEM_IS_F32 || (DK == 128 && DV == 128) ? 2 : 1>(a);
+  case DK * 1000 + DV: return run_fwd_decay<DK, DV, ELEM_IS_F32 ? 32 : 64, DK == 128 && DV == 128 ? (ELEM_IS_F32 ? 4 : 2) : ELEM_IS_F32 ? 2 : 1>(a);
   COTTN_DECAY_SHAPES(COTTN_CASE)
 #undef COTTN_CASE
 }
