@@ -295,8 +295,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
       for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16_add(vc[nt], pf, oacc[nt]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    // the state after the chunk
-    if (active) {
+    // the state after the chunk, if somebody takes it
+    if (active && (row0 + C < row_end || (state_out != nullptr && ends_here))) {
       const WeightedTile<ST, Cfg::NP, TPK, PARTS> k(Ks, rows + 2 * C, w, r, q4);
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
