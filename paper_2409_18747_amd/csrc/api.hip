@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cstring>
 #include <mutex>
 #include <string>
@@ -244,19 +245,37 @@ namespace {
 
 // Calls with a decay: the time of g segments by the model of causal_call_us, with constants for a forward and its backward and for a
 // forward alone, whose sequences of one segment may be in parts of the value columns (decay_value_columns), a step of which is
-// shorter by `parts`.  Fitted to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128 x 128, fp32
+// shorter by `parts`, and the chunks in row parts, of which the largest counts and rows_again of the whole.  Fitted to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128 x 128, fp32
 // 64 x 64): the split chosen takes 0.4 and 0.5 % longer than the best of up to ten measured; the pair with the constants of
 // causal_call_us 1.5 % (300 units of 2048 rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units
 // of 1024 rows 128 x 128 4 segments 89 us, 1 segment 62).  Farthest off: 128 units of 512 rows 32 x 32 with backward 8 segments 33 us, 4
 // segments 28; 16 units of 8192 rows 64 x 64 forward 16 segments 1.14 times 32 segments.
+struct DecayRowParts { int parts; long most; };   // workgroups that share a sequence's chunks; what the first takes (row_part)
+// A forward whose value columns are in parts: its chunks too, where compute units would be left without a workgroup.  Kernel alone,
+// continued from a state, one / two / four row parts: 16 units 128 x 128 100 rows 9.0 / 8.2 / 8.3 us, 512 rows 24.5 / 20.4 / 19.1; 64 units
+// 64 x 64 of 256 rows 10.5 / 9.1 / 9.6, fp32 22.4 / 16.2 / 17.2; 128 units 64 x 128 of 384 18.1 / 16.9 / 22.3; 128 x 128 in 256 workgroups, 64
+// units of 384 21.4 / 22.0 / 28.5.  (192 units 64 x 128 padded: up to 389 rows 24.0 / 20.8, up to 700 33.3 / 37.6, left whole.)
+DecayRowParts decay_row_parts(long units, long n_chunks, int dk, int dv, bool f32) {
+  const int columns = decay_value_columns(units, dk, dv, f32);
+  const long workgroups = units * (dv / columns);
+  if (columns == dv || n_chunks < 2 || workgroups > (dk == 128 && dv == 128 && !f32 ? 128 : 256)) return {1, n_chunks};
+  const int parts = workgroups <= 64 && n_chunks >= 4 ? 4 : 2;
+  // the least that lets them reach the end; they reach 3/2 and 15/8 of it, but for roundings
+  for (long most = std::max(1L, (parts == 2 ? n_chunks * 2 / 3 : n_chunks * 8 / 15) - 4);; ++most) {
+    long covered = 0;
+    for (int k = 0; k < parts; ++k) covered += most - covered / 2 > 1 ? most - covered / 2 : 1;
+    if (covered >= n_chunks) return {parts, most};
+  }
+}
+
 struct DecayTimes {
   double next_narrow_f32, next_f32, next_narrow, next;   // of a step for each further workgroup at once on a compute unit
   double step_f32, step_widest, step, prologue, row;      // us a column, us a column, us a column, steps, us a MB
   double launch, totals, add_widest, add;                 // us, of a step, us a KB of a state
-  double parts_64, parts_128, parts_many;
+  double parts_64, parts_128, parts_many, rows_again;
 };
-constexpr DecayTimes kDecayPair = {0.2, 0.434, 0.019, 0.275, 0.123, 0.0667, 0.0573, 0.85, 0.876, 5.56, 0.0538, 0.0259, 0.0402, 1, 1, 1};
-constexpr DecayTimes kDecayAlone = {0.2, 0.266, 0.02, 0.23, 0.05, 0.0245, 0.0287, 1.02, 0.1235, 3.33, 0.3225, 0.0251, 0.0343, 0.8, 0.7, 0.48};
+constexpr DecayTimes kDecayPair = {0.2, 0.434, 0.019, 0.275, 0.123, 0.0667, 0.0573, 0.85, 0.876, 5.56, 0.0538, 0.0259, 0.0402, 1, 1, 1, 0};
+constexpr DecayTimes kDecayAlone = {0.2, 0.266, 0.02, 0.23, 0.05, 0.0245, 0.0287, 1.02, 0.1235, 3.33, 0.3225, 0.0251, 0.0343, 0.8, 0.7, 0.48, 0.15};
 double decay_call_us(const DecayTimes& t, long units, long N, long n_chunks, long g, bool f32, int dk, int dv) {
   const bool narrowest = dk == 32 && dv == 32, widest = dk == 128 && dv == 128;
   const int big = dk > dv ? dk : dv, small = dk > dv ? dv : dk;
@@ -266,7 +285,12 @@ double decay_call_us(const DecayTimes& t, long units, long N, long n_chunks, lon
   if (g == 1 && decay_value_columns(units, dk, dv, f32) != dv) step *= units > 128 ? t.parts_many : dv == 64 ? t.parts_64 : t.parts_128;
   const long steps = (n_chunks + g - 1) / g, on_cu = (units * g + kComputeUnits - 1) / kComputeUnits;
   const auto together = [&](long n) { return n > 0 ? 1.0 + next_one * double(n - 1) : 0.0; };
-  double us = step * (double(steps) + t.prologue) * (double(on_cu / at_once) * together(at_once) + together(on_cu % at_once));
+  double walk = double(steps);
+  if (g == 1 && t.rows_again > 0) {
+    const DecayRowParts rows = decay_row_parts(units, n_chunks, dk, dv, f32);
+    if (rows.parts > 1) walk = double(rows.most) + t.rows_again * double(n_chunks);
+  }
+  double us = step * (walk + t.prologue) * (double(on_cu / at_once) * together(at_once) + together(on_cu % at_once));
   const double rows_us = t.row * 1e-6 * double(units) * double(N) * (dk + dv) * (f32 ? 4 : 2);
   if (us < rows_us) us = rows_us;
   if (g > 1) {
@@ -309,7 +333,7 @@ long decay_segments(bool alone, long units, long N, long n_chunks, bool f32, int
 // The split of a call with a decay, the same for a forward and its backward; a forward by itself (`alone`) may walk a sequence
 // in fewer segments where those two take several.
 struct DecayPlan {
-  int G, seg_rows, value_columns;
+  int G, seg_rows, value_columns, row_parts, part_rows;
   bool carried;   // DecayArgs
 };
 bool make_decay_plan(bool alone, int B, int H, int N, int dk, int dv, int chunk, int dtype, DecayPlan* plan) {
@@ -327,6 +351,9 @@ bool make_decay_plan(bool alone, int B, int H, int N, int dk, int dv, int chunk,
   plan->G = int(G);
   plan->seg_rows = int(steps * C);
   plan->value_columns = G == 1 ? decay_value_columns(units, dk, dv, f32) : dv;
+  const DecayRowParts rows = G == 1 ? decay_row_parts(units, n_chunks, dk, dv, f32) : DecayRowParts{1, n_chunks};
+  plan->row_parts = rows.parts;
+  plan->part_rows = int(rows.most * C);
   plan->carried = G > 1 && !causal_totals_in_place(units, int(G), dk, dv, f32) && threads_fit(units, dk * dv / 4);
   return true;
 }
@@ -898,7 +925,7 @@ int cottn_fwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.O = O; a.state = state; a.state_in = state_in;
   a.seq_len = seq_len; a.workspace = workspace;
   a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows;
-  a.value_columns = plan.value_columns; a.carried = plan.carried;
+  a.value_columns = plan.value_columns; a.row_parts = plan.row_parts; a.part_rows = plan.part_rows; a.carried = plan.carried;
   a.eps = eps; a.stream = stream;
   return map_hip(dtype == COTTN_BF16 ? fwd_decay_bf16(a) : dtype == COTTN_F16 ? fwd_decay_f16(a) : fwd_decay_f32w(a));
 }
@@ -934,7 +961,7 @@ int cottn_bwd_causal_decay(const void* Q, const void* K, const void* V, const fl
   a.state_in = state_in; a.rev_state_in = rev_state_in; a.rev_state_out = rev_state_out; a.seq_len = seq_len;
   a.workspace = workspace;
   a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.G = plan.G; a.seg_rows = plan.seg_rows;
-  a.value_columns = plan.value_columns; a.carried = plan.carried;
+  a.carried = plan.carried;
   a.eps = eps; a.stream = stream;
   if (fwd_workspace != nullptr && plan.G > 1) {
     st = check_workspace(fwd_workspace, fwd_workspace_bytes, decay_workspace_bytes(COTTN_OP_FWD_DECAY, B, H, dk, dv, plan));

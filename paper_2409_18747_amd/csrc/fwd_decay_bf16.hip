@@ -116,10 +116,22 @@ COTTN_KERNEL((C * 4), decay_segment_state)
 }
 
 // ---------------------------------------------------------------------------------------
+// Row parts: the chunks of a sequence of one segment, dealt to workgroups that each form the state up to theirs by themselves. A chunk
+// that only makes the state takes about half the time of a whole one, so part k takes `most` chunks less half of those before it.
+__device__ __forceinline__ void row_part(int k, int most, int& begin, int& count) {
+  begin = 0;
+  count = most;
+  for (int i = 0; i < k; ++i) {
+    begin += count;
+    count = max(1, most - begin / 2);
+  }
+}
+
 // The scan of one segment.  Wave (row group rg, column part cp) owns the query rows 16 rg .. of the chunk and the output
 // columns of its part, and tiles of the state, held as add_tokens says.  Results are accumulated transposed: a lane holds four
-// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value columns, which the whole
-// computation leaves apart from one another but for the masked tiles; those are formed LDV / DV times.  PARTS: EXACT_PARTS where the state is asked for.  bf16: 96 units of 1024 rows 64 x 64 in
+// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value
+// columns and a part of the rows (row_part); the whole computation leaves columns apart from one another but for the masked tiles, and
+// those are formed LDV / DV times.  PARTS: EXACT_PARTS where the state is asked for.  bf16: 96 units of 1024 rows 64 x 64 in
 // 4 segments 14.8 us; 16 of 65536 rows in 32 segments 99 us, 5.4 TB/s; 1024 of 2048 rows 128 x 128 555 us, 3.9 TB/s (VALU issue 47 %,
 // matrix instructions 28 %, LDS 46 % of the time).
 template <int DK, int DV, int C, int CS, int PARTS, int LDV = DV>
@@ -146,13 +158,19 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   constexpr int VALUE_PARTS = LDV / DV;   // (several only where sequences are few: nothing past the caches)
   const bool carried = flags & CARRIED, stream_q = VALUE_PARTS == 1 && (flags & STREAM_Q),
              stream_kv = VALUE_PARTS == 1 && (flags & STREAM_KV);
-  int unit, seg, part = 0;
-  if constexpr (VALUE_PARTS > 1) {   // (one segment)
+  int unit, seg, part = 0, row_begin, row_count;
+  if constexpr (VALUE_PARTS > 1) {   // (one segment, whose rows are dealt to workgroups, seg_rows to the first: row_part)
     unit = blockIdx.x / VALUE_PARTS;
     part = blockIdx.x % VALUE_PARTS;
-    seg = 0;
+    seg = unit / units;
+    unit -= seg * units;
+    row_part(seg, seg_rows / C, row_begin, row_count);
+    row_begin *= C;
+    row_count *= C;
   } else {
     unit_and_segment(blockIdx.x, units, G, unit, seg);
+    row_begin = seg * seg_rows;
+    row_count = seg_rows;
   }
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
   const int rg = w % RG, cp = w / RG;
@@ -160,18 +178,19 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   const elem_t* Ku = K + size_t(unit) * N * DK;
   const elem_t* Vu = V + size_t(unit) * N * LDV + part * DV;
   elem_t* Ou = O + size_t(unit) * N * LDV + part * DV;
-  const int there = valid_rows(lengths, unit, H, N), row_begin = seg * seg_rows, piece_end = min(N, row_begin + seg_rows);
+  const int there = valid_rows(lengths, unit, H, N), piece_end = min(N, row_begin + row_count);
   const int row_end = max(row_begin, min(there, piece_end));
   const bool ends_here = there > row_begin ? there <= piece_end : there == 0 && seg == 0;   // the state after the last row
+  const int scan_begin = VALUE_PARTS > 1 ? 0 : row_begin;   // rows before row_begin only make the state
   if (there <= row_begin && !ends_here) {
     zero_rows<DV, LDV>(Ou, row_begin, piece_end);
     return;
   }
   StageK qst, kst;
   StageV vst;
-  qst.fetch(Qu, row_begin, row_end, stream_q);
-  kst.fetch(Ku, row_begin, row_end, stream_kv);
-  vst.fetch(Vu, row_begin, row_end, stream_kv);
+  if (scan_begin == row_begin) qst.fetch(Qu, row_begin, row_end, stream_q);
+  kst.fetch(Ku, scan_begin, row_end, stream_kv);
+  vst.fetch(Vu, scan_begin, row_end, stream_kv);
   const int head = unit - quotient(unit, H) * H.n;
   const Decay g(log_decay[head]);
   const float scale = s[lengths != nullptr ? unit : head];
@@ -182,7 +201,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
 #pragma unroll
     for (int y = 0; y < ST::NRT; ++y) sacc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bool active = ST::active(w);
-  if (active && seg > 0) {
+  if (VALUE_PARTS == 1 && active && seg > 0) {
     const float* slots = seg_states + size_t(unit) * G.n * DK * DV;
     add_decayed_states<false>(sacc, carried ? seg : 0, carried ? seg : seg - 1, g, seg_rows, [&](int slot, int x, int y) {
       return *reinterpret_cast<const f32x4*>(slots + size_t(slot) * DK * DV +
@@ -190,7 +209,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     });
   }
   if (active && state_in != nullptr) {
-    const float since = STATE_UNIT * g.after(float(row_begin));
+    const float since = STATE_UNIT * g.after(float(scan_begin));
     const float* src = state_in + size_t(unit) * DK * LDV + part * DV;
 #pragma unroll
     for (int x = 0; x < ST::NCT; ++x)
@@ -214,86 +233,93 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
   for (int j = 0; j < RowPieces<DV, NOT>::PER_LANE; ++j) finished.v[j] = uint4{0u, 0u, 0u, 0u};
   void* stage = Cfg::OWN_STAGE ? static_cast<void*>(Os + 16 * rg * Cfg::OP) : static_cast<void*>(Qs + 16 * rg * TPK);
   const int col0 = 16 * NOT * cp;
-  for (int row0 = row_begin; row0 < row_end; row0 += C) {
+  for (int row0 = scan_begin; row0 < row_end; row0 += C) {
     const int n = min(C, row_end - row0);
+    const bool mine = VALUE_PARTS == 1 || row0 >= row_begin;
     if (active) {
+      if (mine) {
 #pragma unroll
-      for (int x = 0; x < ST::NCT; ++x)
+        for (int x = 0; x < ST::NCT; ++x)
 #pragma unroll
-        for (int y = 0; y < ST::NRT; ++y)
-          store4_lds(Sl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
-                     PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
+          for (int y = 0; y < ST::NRT; ++y)
+            store4_lds(Sl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
+                       PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
+      }
       (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);
     }
     {
       RowFactors<StageK> f;
-      f.commit(qst, Qs, inv_eps, un);
-      qst.store_rinv(rq, f.left);
+      if (mine) {
+        f.commit(qst, Qs, inv_eps, un);
+        qst.store_rinv(rq, f.left);
+      }
       f.commit(kst, Ks, inv_eps, un);
       store_key_factors<StageK, C>(rows, f, g, n);
       vst.commit_plain(Vs, un);
     }
     if (row0 + C < row_end) {
-      qst.fetch(Qu, row0 + C, row_end, stream_q);
+      if (VALUE_PARTS == 1 || row0 + C >= row_begin) qst.fetch(Qu, row0 + C, row_end, stream_q);
       kst.fetch(Ku, row0 + C, row_end, stream_kv);
       vst.fetch(Vu, row0 + C, row_end, stream_kv);
     }
     if (row0 > row_begin) store_row_pieces<DV, NOT, LDV>(finished, Ou, row0 - C + 16 * rg, row_end, l, col0);
     __syncthreads();
 
-    // what the state gives: O^T = S^T Q^T, then the row's factor
-    frag8 qf[Cfg::KSK];
-#pragma unroll
-    for (int ks = 0; ks < Cfg::KSK; ++ks) qf[ks] = lds_row_frag(Qs + (16 * rg + r) * TPK + 32 * ks, q4);
-    const float ri = rq[16 * rg + r];
     f32x4 oacc[NOT];
+    if (mine) {
+      // what the state gives: O^T = S^T Q^T, then the row's factor
+      frag8 qf[Cfg::KSK];
 #pragma unroll
-    for (int nt = 0; nt < NOT; ++nt) oacc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int ks = 0; ks < Cfg::KSK; ++ks) qf[ks] = lds_row_frag(Qs + (16 * rg + r) * TPK + 32 * ks, q4);
+      const float ri = rq[16 * rg + r];
 #pragma unroll
-    for (int ks = 0; ks < Cfg::KSK; ++ks) {
-      frag8 sf[NOT];
+      for (int nt = 0; nt < NOT; ++nt) oacc[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int nt = 0; nt < NOT; ++nt) sf[nt] = lds_col_frag_ks(Sl, SP, ks, q4, col0 + 16 * nt, r);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int ks = 0; ks < Cfg::KSK; ++ks) {
+        frag8 sf[NOT];
 #pragma unroll
-      for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16(sf[nt], qf[ks], oacc[nt]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+        for (int nt = 0; nt < NOT; ++nt) sf[nt] = lds_col_frag_ks(Sl, SP, ks, q4, col0 + 16 * nt, r);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int nt = 0; nt < NOT; ++nt)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) oacc[nt][v] *= ri * to_row;
-
-    // the chunk itself, 32 tokens at a time
-#pragma unroll
-    for (int p = 0; p < Cfg::NP; ++p) {
-      if (2 * p > rg) break;   // wave-uniform: every key is masked from here on
-      const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
-      frag8 vc[NOT], kr[2][Cfg::KSK];
-#pragma unroll
-      for (int nt = 0; nt < NOT; ++nt) vc[nt] = lds_col_frag(Vs, TPV, t0, t1, col0 + 16 * nt, r);
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int ks = 0; ks < Cfg::KSK; ++ks) kr[half][ks] = lds_row_frag(Ks + (16 * (2 * p + half) + r) * TPK + 32 * ks, q4);
-      __builtin_amdgcn_sched_barrier(0);
-      frag8 pf;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int jt = 2 * p + half;
-        f32x4 t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < Cfg::KSK; ++ks) t = mma16(kr[half][ks], qf[ks], t);
-        // t[v] = q_(16 rg + r) . k_(16 jt + 4 q4 + v)
-        const f32x4 kj = *reinterpret_cast<const f32x4*>(rows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
-        const float below = ri * g.after(row - float(16 * jt + 15));   // (jt < rg)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) t[v] = jt > rg ? 0.f : t[v] * (kj[v] * (jt == rg ? ri * on_diagonal[v] : below));
-        put_four(pf, half, t);
+        for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16(sf[nt], qf[ks], oacc[nt]);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16_add(vc[nt], pf, oacc[nt]);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int nt = 0; nt < NOT; ++nt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) oacc[nt][v] *= ri * to_row;
+
+      // the chunk itself, 32 tokens at a time
+#pragma unroll
+      for (int p = 0; p < Cfg::NP; ++p) {
+        if (2 * p > rg) break;   // wave-uniform: every key is masked from here on
+        const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+        frag8 vc[NOT], kr[2][Cfg::KSK];
+#pragma unroll
+        for (int nt = 0; nt < NOT; ++nt) vc[nt] = lds_col_frag(Vs, TPV, t0, t1, col0 + 16 * nt, r);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSK; ++ks) kr[half][ks] = lds_row_frag(Ks + (16 * (2 * p + half) + r) * TPK + 32 * ks, q4);
+        __builtin_amdgcn_sched_barrier(0);
+        frag8 pf;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int jt = 2 * p + half;
+          f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < Cfg::KSK; ++ks) t = mma16(kr[half][ks], qf[ks], t);
+          // t[v] = q_(16 rg + r) . k_(16 jt + 4 q4 + v)
+          const f32x4 kj = *reinterpret_cast<const f32x4*>(rows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
+          const float below = ri * g.after(row - float(16 * jt + 15));   // (jt < rg)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) t[v] = jt > rg ? 0.f : t[v] * (kj[v] * (jt == rg ? ri * on_diagonal[v] : below));
+          put_four(pf, half, t);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NOT; ++nt) oacc[nt] = mma16_add(vc[nt], pf, oacc[nt]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     // the state after the chunk, if somebody takes it
     if (active && (row0 + C < row_end || (state_out != nullptr && ends_here))) {
@@ -303,8 +329,10 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
       for (int y0 = 0; y0 < ST::NRT; y0 += YN)
         k.template add<YN, TPV>(Vs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return sacc[x][y0 + y]; });
     }
-    wave_lds_sync();
-    gather_rows_transposed<DV, NOT>(oacc, scale, stage, l, finished, un, col0);
+    if (mine) {
+      wave_lds_sync();
+      gather_rows_transposed<DV, NOT>(oacc, scale, stage, l, finished, un, col0);
+    }
     __syncthreads();   // everything of the chunk is read
   }
   if (row_end > row_begin)
@@ -336,10 +364,11 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
   const int flags = (a.carried ? CARRIED : 0) | (bytes > 256.0 * 1024 * 1024 ? STREAM_Q : 0) |
                     (a.G == 1 && bytes > 1024.0 * 1024 * 1024 ? STREAM_KV : 0);
   const auto scan = [&](auto kernel) {
-    return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), kernel, dim3(units * a.G * (LDV / DV)), dim3(64 * (C / 16) * CS), 0, a.stream,
+    return launch_kernel(COTTN_SYM_STR(fwd_decay_scan), kernel, dim3(units * (LDV > DV ? LDV / DV * a.row_parts : a.G)),
+                         dim3(64 * (C / 16) * CS), 0, a.stream,
                          static_cast<const elem_t*>(a.Q), static_cast<const elem_t*>(a.K), static_cast<const elem_t*>(a.V), a.s,
                          a.log_decay, static_cast<elem_t*>(a.O), a.state, states, a.state_in, a.seq_len, Divisor(a.H),
-                         Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps, flags);
+                         Divisor(a.G), LDV > DV ? a.part_rows : a.seg_rows, a.N, units, 1.0f / a.eps, flags);
   };
   if (a.state != nullptr) return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, EXACT_PARTS, LDV>);
   return scan(COTTN_SYM(fwd_decay_scan)<DK, DV, C, CS, ROUNDED_PARTS, LDV>);

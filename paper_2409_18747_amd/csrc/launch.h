@@ -262,6 +262,7 @@ struct DecayArgs {
   void* workspace;
   int B, H, N, dk, dv, G, seg_rows;
   int value_columns;                // forward of one segment: value columns of a workgroup
+  int row_parts, part_rows;         // and, where those are not all, workgroups that its rows are dealt to, rows of the first (row_part)
   bool carried;
   float eps;
   hipStream_t stream;
