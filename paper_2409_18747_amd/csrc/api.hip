@@ -243,13 +243,6 @@ bool make_plan(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype
 
 namespace {
 
-// Calls with a decay: the time of g segments by the model of causal_call_us, with constants for a forward and its backward and for a
-// forward alone, whose sequences of one segment may be in parts of the value columns (decay_value_columns), a step of which is
-// shorter by `parts`, and the chunks in row parts, of which the largest counts and rows_again of the whole.  Fitted to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128 x 128, fp32
-// 64 x 64): the split chosen takes 0.4 and 0.5 % longer than the best of up to ten measured; the pair with the constants of
-// causal_call_us 1.5 % (300 units of 2048 rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units
-// of 1024 rows 128 x 128 4 segments 89 us, 1 segment 62).  Farthest off: 128 units of 512 rows 32 x 32 with backward 8 segments 33 us, 4
-// segments 28; 16 units of 8192 rows 64 x 64 forward 16 segments 1.14 times 32 segments.
 struct DecayRowParts { int parts; long most; };   // workgroups that share a sequence's chunks; what the first takes (row_part)
 // A forward whose value columns are in parts: its chunks too, where compute units would be left without a workgroup.  Kernel alone,
 // continued from a state, one / two / four row parts: 16 units 128 x 128 100 rows 9.0 / 8.2 / 8.3 us, 512 rows 24.5 / 20.4 / 19.1; 64 units
@@ -268,6 +261,15 @@ DecayRowParts decay_row_parts(long units, long n_chunks, int dk, int dv, bool f3
   }
 }
 
+// Calls with a decay: the time of g segments by the model of causal_call_us, with constants for a forward and its backward and for a
+// forward alone, whose sequences of one segment may be in parts of the value columns (decay_value_columns), a step of which is
+// shorter by `parts`, and the rows in parts (decay_row_parts), of which the first counts, and rows_again of all chunks.  Fitted, but for
+// rows_again, to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128 x 128, fp32 64 x 64): the split chosen takes 0.4 and 0.5 % longer than the best of up to ten measured; the pair with the constants of
+// causal_call_us 1.5 % (300 units of 2048 rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units
+// of 1024 rows 128 x 128 4 segments 89 us, 1 segment 62).  Farthest off: 128 units of 512 rows 32 x 32 with backward 8 segments 33 us, 4
+// segments 28; 16 units of 8192 rows 64 x 64 forward 16 segments 1.14 times 32 segments.
+// With row parts, of 60 shapes of 16 to 128 units: 64 units 64 x 128 of 384 rows 2 segments 17.9 us, 1 segment 14.4; at worst 16 units
+// 64 x 64 of 512 rows 4 segments 10.1, 1 segment 10.6.
 struct DecayTimes {
   double next_narrow_f32, next_f32, next_narrow, next;   // of a step for each further workgroup at once on a compute unit
   double step_f32, step_widest, step, prologue, row;      // us a column, us a column, us a column, steps, us a MB

@@ -63,7 +63,7 @@ __device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stag
 // dQ of a segment, first chunk to last.  H and G sit in accumulators with the values down and the keys along, tile (x, y):
 // element [v] of lane (r, q4) is H[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  A wave has few key tiles and all
 // values (of its part): fragments of keys and queries are the ones that weights go to, 50 instructions each.  bf16: 96 units
-// of 1024 rows 64 x 64 21.8 us (VALU issue 41 %, matrix instructions 17 %); 16 of 65536 rows 157 us, 4.3 TB/s (53 %, 24 %).
+// of 1024 rows 64 x 64 20.9 us (VALU issue 40 %, matrix instructions 16 %); 16 of 65536 rows 155 us, 4.3 TB/s (54 %, 25 %).
 template <int DK, int DV, int C, int CS>
 COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,
@@ -339,7 +339,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
 // dK and dV of a segment, last chunk to first.  R sits in accumulators with the values down and the keys along, tile (x, y):
 // element [v] of lane (r, q4) is R[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  The first workgroups also add up
 // ds from what the dQ scan left.  PARTS: EXACT_PARTS where the reverse-time state is asked for.  bf16: 96 units of 1024 rows
-// 64 x 64 19.1 us (VALU issue 34 %, matrix instructions 13 %, LDS 36 %); 16 of 65536 rows 150 us, 5.4 TB/s.
+// 64 x 64 18.5 us (VALU issue 34 %, matrix instructions 13 %, LDS 37 %); 16 of 65536 rows 151 us, 5.3 TB/s.
 template <int DK, int DV, int C, int CS, int PARTS>
 COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V, const elem_t* __restrict__ dO,

@@ -128,12 +128,12 @@ __device__ __forceinline__ void row_part(int k, int most, int& begin, int& count
 }
 
 // The scan of one segment.  Wave (row group rg, column part cp) owns the query rows 16 rg .. of the chunk and the output
-// columns of its part, and tiles of the state, held as add_tokens says.  Results are accumulated transposed: a lane holds four
-// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value
-// columns and a part of the rows (row_part); the whole computation leaves columns apart from one another but for the masked tiles, and
-// those are formed LDV / DV times.  PARTS: EXACT_PARTS where the state is asked for.  bf16: 96 units of 1024 rows 64 x 64 in
-// 4 segments 14.8 us; 16 of 65536 rows in 32 segments 99 us, 5.4 TB/s; 1024 of 2048 rows 128 x 128 555 us, 3.9 TB/s (VALU issue 47 %,
-// matrix instructions 28 %, LDS 46 % of the time).
+// columns of its part, and tiles of the state, held as said above.  Results are accumulated transposed: a lane holds four
+// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value columns, which the whole
+// computation leaves apart from one another but for the masked tiles, formed LDV / DV times, and a part of the rows (row_part).
+// PARTS: EXACT_PARTS where the state is asked for.
+//   bf16: 96 units of 1024 rows 64 x 64 in 4 segments 14.4 us; 16 of 65536 rows in 32 segments 99 us, 5.4 TB/s; 1024 of 2048 rows 128 x 128
+// 558 us, 3.8 TB/s (VALU issue 47 %, matrix instructions 28 %, LDS 46 % of the time).
 template <int DK, int DV, int C, int CS, int PARTS, int LDV = DV>
 COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V,
