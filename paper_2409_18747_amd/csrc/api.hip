@@ -268,8 +268,8 @@ DecayRowParts decay_row_parts(long units, long n_chunks, int dk, int dv, bool f3
 // causal_call_us 1.5 % (300 units of 2048 rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units
 // of 1024 rows 128 x 128 4 segments 89 us, 1 segment 62).  Farthest off: 128 units of 512 rows 32 x 32 with backward 8 segments 33 us, 4
 // segments 28; 16 units of 8192 rows 64 x 64 forward 16 segments 1.14 times 32 segments.
-// With row parts, of 60 shapes of 16 to 128 units: 64 units 64 x 128 of 384 rows 2 segments 17.9 us, 1 segment 14.4; at worst 16 units
-// 64 x 64 of 512 rows 4 segments 10.1, 1 segment 10.6.
+// With row parts, of 60 shapes of 16 to 128 units: 64 units 64 x 128 of 384 rows in segments 17.9 us, in row parts 14.4; at worst 16
+// units 64 x 64 of 512 rows 10.1 and 10.6.
 struct DecayTimes {
   double next_narrow_f32, next_f32, next_narrow, next;   // of a step for each further workgroup at once on a compute unit
   double step_f32, step_widest, step, prologue, row;      // us a column, us a column, us a column, steps, us a MB

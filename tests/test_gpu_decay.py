@@ -312,3 +312,29 @@ def test_more_than_the_caches_hold(cottn, B, N, segments):
     want = [cottn.cottn_fwd_causal_decay(*one[:3], s, ld), *cottn.cottn_bwd_causal_decay(*one[:3], s, ld, one[3])[:3]]
     for a, b in zip(got, want):
         assert norm_error(a[-1:], b.cpu().double()) <= 2 * NORM * U["bf16"]
+
+
+@pytest.mark.parametrize("dtype,dk,dv", [("bf16", 128, 128), ("f16", 64, 128), ("f32", 64, 64), ("bf16", 32, 64)])
+@pytest.mark.parametrize("N", [64, 65, 160, 257, 449, 1100])
+def test_rows_dealt_to_workgroups(cottn, dtype, dk, dv, N):
+    """One segment of few sequences, whose rows several workgroups share: lengths that end in each of them, and none."""
+    lens = [N, N // 2 + 1, N // 4, 1, 0]
+    x = draw(5, 2, N, dk, dv, dtype, N, lens=lens, states=True)
+    d = {k: v.cuda() for k, v in x.items()}
+    f = {k: v.double() for k, v in x.items()}
+    n = N + max(dk, dv) + 40
+    cottn.cottn_tune_segments(1)
+    try:
+        for some in (None, lens):
+            state = torch.full((5, 2, dk, dv), float("nan"), device="cuda")
+            s = x["s"] if some is not None else x["s"][0].contiguous()
+            O = cottn.cottn_fwd_causal_decay(d["Q"], d["K"], d["V"], s.cuda(), d["log_decay"], state_in=d["state_in"], state=state,
+                                             seq_len=None if some is None else torch.tensor(some, dtype=torch.int32).cuda(),
+                                             O=torch.full_like(d["V"], float("nan")))
+            want, S, M, MS = ref.forward(f["Q"], f["K"], f["V"], s, x["log_decay"], some, f["state_in"])
+            assert worst(O, want, M, U[dtype], n) <= 1.0 and worst(state, S, MS, U[dtype], n, in_fp32=True) <= 1.0
+            assert norm_error(O, want) <= NORM * U[dtype] + 2e-6 and norm_error(state, S) <= 2 * U[dtype] ** 2 + 2e-6
+            if some is not None:
+                assert all(not O[b, :, m:].any() for b, m in enumerate(some))
+    finally:
+        cottn.cottn_tune_segments(0)
