@@ -289,7 +289,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     // the state after the chunk, but for the last (with the same in the other scans, 96 units of 1024 rows 64 x 64 63.7 -> 62.0 us,
     // 128 x 128 156.6 -> 155.2 where this scan forms it all the same and 157.9 where not)
     if (active && ((DK == 128 && DV == 128) || row0 + C < row_end)) {
-      (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);
+      (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);   // (the gradients of a state with an infinite element are not finite)
       const WeightedTile<ST, Cfg::NP, TPK, EXACT_PARTS> k(Ks, krows + 2 * C, w, r, q4);
       constexpr int YN = ST::NRT < 4 ? ST::NRT : 4;
 #pragma unroll
@@ -418,6 +418,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
                                              tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l));
     });
   }
+  bool infinite = false;
   if (active && rev_in != nullptr) {
     const float until = STATE_UNIT * g.after(float(there - row_end));
     const float* src = rev_in + size_t(unit) * DK * DV;
@@ -430,6 +431,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
 #pragma unroll
         for (int v = 0; v < 4; ++v) racc[x][y][v] = __builtin_fmaf(until, t[v], racc[x][y][v]);
       }
+    infinite = any_infinite(racc);
   }
 
   const float row = float(16 * rg + r);   // of the chunk: this lane's key
@@ -453,7 +455,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
         for (int y = 0; y < ST::NRT; ++y)
           store4_lds(Rl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * racc[x][y][0],
                      PER_UNIT * racc[x][y][1], PER_UNIT * racc[x][y][2], PER_UNIT * racc[x][y][3], un);
-      (n == C ? whole_chunk : Kept(g, float(n))).on(racc);
+      (n == C ? whole_chunk : Kept(g, float(n))).on(racc, infinite);
     }
     {
       RowFactors<StageK> f;

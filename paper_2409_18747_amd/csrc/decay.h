@@ -36,7 +36,11 @@ struct Decay {
 
 // What a state is multiplied by n rows later: x * times + x * plus.  A factor just below 1 is 1 - d with a d of its own, whose
 // relative error is that of fp32: as one rounded number, g^64 of a head that hardly forgets would be off by up to 2^-25
-// with the same sign in every chunk, 3e-5 of what is oldest after 1024 chunks.
+// with the same sign in every chunk, 3e-5 of what is oldest after 1024 chunks.  x * plus is formed of a finite number in place of an
+// infinite x, which then stays x: inf - inf d would be NaN.
+__device__ __forceinline__ float made_finite(float x) {
+  return __builtin_amdgcn_fmed3f(x, -3.402823466e38f, 3.402823466e38f);   // (of NaN some number: the other term is NaN)
+}
 struct Kept {
   float times, plus;
   __device__ __forceinline__ Kept(const Decay& g, float n) {
@@ -48,7 +52,7 @@ struct Kept {
   __device__ __forceinline__ f32x4 of(f32x4 x) const {
     f32x4 y;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) y[v] = __builtin_fmaf(x[v], plus, x[v] * times);
+    for (int v = 0; v < 4; ++v) y[v] = __builtin_fmaf(made_finite(x[v]), plus, x[v] * times);
     return y;
   }
   template <int A, int B>
@@ -69,7 +73,33 @@ struct Kept {
           for (int v = 0; v < 4; ++v) t[x][y][v] *= times;
     }
   }
+  // the same, where some element is `infinite` (any_infinite): made_finite for every state of 64 x 16 heads of 2048 rows 128 x 128 took
+  // 562 us instead of 547, and 96 units of 1024 rows forward + backward 162 instead of 155
+  template <int A, int B>
+  __device__ __forceinline__ void on(f32x4 (&t)[A][B], bool infinite) const {
+    if (infinite) {
+#pragma unroll
+      for (int x = 0; x < A; ++x)
+#pragma unroll
+        for (int y = 0; y < B; ++y) t[x][y] = of(t[x][y]);
+    } else {
+      on(t);
+    }
+  }
 };
+// Whether a wave's part of a state has an infinite element, the same for all lanes.  Only one that a caller hands over is
+// looked at: finite rows make none below fp32's largest number.
+template <int A, int B>
+__device__ __forceinline__ bool any_infinite(const f32x4 (&t)[A][B]) {
+  float most = 0.f;
+#pragma unroll
+  for (int x = 0; x < A; ++x)
+#pragma unroll
+    for (int y = 0; y < B; ++y)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) most = fmaxf(most, fabsf(t[x][y][v]));
+  return __any(most > 3.402823466e38f);
+}
 
 // Rows are raw in LDS and every factor of a row (1 / norm, decay) goes to fp32 results, to the masked tiles before they are
 // rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.

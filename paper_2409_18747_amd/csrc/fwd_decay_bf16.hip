@@ -208,6 +208,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
                                              tiled_state_offset(ST::col_tile(w, x), ST::row_tile(w, y), DV / 16, l));
     });
   }
+  bool infinite = false;
   if (active && state_in != nullptr) {
     const float since = STATE_UNIT * g.after(float(scan_begin));
     const float* src = state_in + size_t(unit) * DK * LDV + part * DV;
@@ -220,6 +221,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
 #pragma unroll
         for (int v = 0; v < 4; ++v) sacc[x][y][v] = __builtin_fmaf(since, t[v], sacc[x][y][v]);
       }
+    infinite = any_infinite(sacc);
   }
 
   const float row = float(16 * rg + r);            // of the chunk: this lane's query
@@ -245,7 +247,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
             store4_lds(Sl + (16 * ST::col_tile(w, x) + r) * SP + 16 * ST::row_tile(w, y) + 4 * q4, PER_UNIT * sacc[x][y][0],
                        PER_UNIT * sacc[x][y][1], PER_UNIT * sacc[x][y][2], PER_UNIT * sacc[x][y][3], un);
       }
-      (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);
+      (n == C ? whole_chunk : Kept(g, float(n))).on(sacc, infinite);
     }
     {
       RowFactors<StageK> f;
