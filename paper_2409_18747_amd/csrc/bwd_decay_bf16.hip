@@ -45,7 +45,7 @@ __device__ __forceinline__ void take_out_row(f32x4* acc, const float (&xv)[NTILE
     for (int v = 0; v < 4; ++v) acc[nt][v] -= xv[nt][v] * c;
 }
 
-// Factors of rows, which of them by the lane of the row: [0] ROW_NORM `left`, [1] that times g^e1(row), [2] STATE_UNIT
+// Factors of rows, which of them by the lane of the row: [0] TILE_UNIT `left`, [1] that times g^e1(row), [2] STATE_UNIT
 // left g^e2(row), [3] `whole`.
 template <class Stage, int C, class E1, class E2>
 __device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stage>& f, const Decay& g, E1 e1, E2 e2) {
@@ -55,7 +55,7 @@ __device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stag
     const int lr = p * Stage::RPP + threadIdx.x / Stage::LPR;
     const int e = which == 1 ? e1(lr) : which == 2 ? e2(lr) : 0;
     if ((C % Stage::RPP == 0 || lr < C) && which < 4) rows[which * C + lr] = (which == 3 ? f.whole[p] : f.left[p]) * g.after(float(e)) *
-                                                         (which == 2 ? STATE_UNIT : which == 3 ? 1.f : ROW_NORM);
+                                                         (which == 2 ? STATE_UNIT : which == 3 ? 1.f : TILE_UNIT);
   }
 }
 
@@ -143,7 +143,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
       }
   }
 
-  const float row = float(16 * rg + r), to_row = ROW_NORM * g.after(row + 1.f), once = g.after(1.f);
+  const float row = float(16 * rg + r), to_row = TILE_UNIT * g.after(row + 1.f), once = g.after(1.f);
   float on_diagonal[4];
 #pragma unroll
   for (int v = 0; v < 4; ++v) on_diagonal[v] = 4 * q4 + v <= r ? g.after(float(r - 4 * q4 - v)) : 0.f;
@@ -297,8 +297,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
         k.template add<YN, TPV>(Vs, y0, w, r, q4, [&](int x, int y) -> f32x4& { return sacc[x][y0 + y]; });
     }
 
-    const float left = 1.f / ROW_NORM * qrows[16 * rg + r], whole = qrows[3 * C + 16 * rg + r];
-    ds_lane += 1.f / ROW_NORM * left * ds_row;
+    const float left = 1.f / TILE_UNIT * qrows[16 * rg + r], whole = qrows[3 * C + 16 * rg + r];
+    ds_lane += 1.f / TILE_UNIT * left * ds_row;
     float xv[NKT][4];
     float t = dot_with_row<NKT, TPK>(dq, Qs + 16 * rg * TPK, colk, xv, r, q4);
     if (CS > 1) {   // the row's dot product over the columns of all its waves
@@ -311,7 +311,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
     take_out_row<NKT>(dq, xv, t, left, whole, inv_eps);
     // every wave has read all query rows for G: they take the finished ones
     if (CS == 1) __syncthreads();
-    gather_rows_transposed<DK, NKT>(dq, 1.f / ROW_NORM * scale * whole, Qs + 16 * rg * TPK, l, finished, un, colk);
+    gather_rows_transposed<DK, NKT>(dq, 1.f / TILE_UNIT * scale * whole, Qs + 16 * rg * TPK, l, finished, un, colk);
     __syncthreads();
   }
   store_row_pieces<DK, NKT>(finished, dQu, row_begin + (row_end - row_begin - 1) / C * C + 16 * rg, row_end, l, colk);
@@ -484,7 +484,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     for (int ks = 0; ks < Cfg::KSK; ++ks) kf[ks] = lds_row_frag(Ks + (16 * rg + r) * TPK + 32 * ks, q4);
 #pragma unroll
     for (int ks = 0; ks < Cfg::KSV; ++ks) vf[ks] = lds_row_frag(Vs + (16 * rg + r) * TPV + 32 * ks, q4);
-    const float left = 1.f / ROW_NORM * krows[16 * rg + r], whole = krows[3 * C + 16 * rg + r];
+    const float left = 1.f / TILE_UNIT * krows[16 * rg + r], whole = krows[3 * C + 16 * rg + r];
     f32x4 dk[NKT], dv[NVT];
 #pragma unroll
     for (int nt = 0; nt < NKT; ++nt) dk[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -518,7 +518,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
 #pragma unroll
     for (int nt = 0; nt < NKT; ++nt)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) dk[nt][v] *= ROW_NORM * to_end;
+      for (int v = 0; v < 4; ++v) dk[nt][v] *= TILE_UNIT * to_end;
 
     // the chunk itself, 32 queries at a time
 #pragma unroll
@@ -564,7 +564,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const float f = it < rg ? 0.f : qi[v] * (it == rg ? on_diagonal[v] : above);
-          tp[half][v] = it < rg ? 0.f : tp[half][v] * (f * (1.f / ROW_NORM * left));
+          tp[half][v] = it < rg ? 0.f : tp[half][v] * (f * (1.f / TILE_UNIT * left));
           ta[half][v] = it < rg ? 0.f : ta[half][v] * f;
         }
         put_four(pf, half, tp[half]);
@@ -602,7 +602,7 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
     take_out_row<NKT>(dk, xv, t, left, whole, inv_eps);
     // (the row group's own rows of Ks and Vs are read by its own waves only)
     if (CS == 1) wave_lds_sync();
-    gather_rows_transposed<DK, NKT>(dk, 1.f / ROW_NORM * scale * whole, Ks + 16 * rg * TPK, l, done_k, un, colk);
+    gather_rows_transposed<DK, NKT>(dk, 1.f / TILE_UNIT * scale * whole, Ks + 16 * rg * TPK, l, done_k, un, colk);
     gather_rows_transposed<DV, NVT>(dv, scale, Vs + 16 * rg * TPV, l, done_v, un, colv);
     __syncthreads();
   }

@@ -103,10 +103,11 @@ __device__ __forceinline__ bool any_infinite(const f32x4 (&t)[A][B]) {
 
 // Rows are raw in LDS and every factor of a row (1 / norm, decay) goes to fp32 results, to the masked tiles before they are
 // rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.
-//   fp16: rows of q and k times the power of two that brings their norm to 32 .. 64 (exact but for elements 2^-20 below the
-// norm), so that the factors left are alike for short and long rows.  The tiles of dO . v take them ROW_NORM times larger and
-// leave fp16 for none of them, neither for the 1 / eps of a short row nor for the small ones of a long one.
-constexpr float ROW_NORM = ELEM_IS_F16 ? 64.f : 1.f;
+//   fp16: rows of q and k times the power of two that brings their norm to 16 .. 32 (exact but for elements 2^-18 below the
+// norm), so that the factors left, 1/32 .. 1/16, are alike for short and long rows.  The tiles of dO . v take them TILE_UNIT times
+// larger, 1/2 .. 1, so that what is rounded is never above the product, nor less than half of it: they leave fp16 for no row
+// norm, neither for the 1 / eps of a short row nor for the small ones of a long one, and for no product that fp16 holds.
+constexpr float TILE_UNIT = ELEM_IS_F16 ? 16.f : 1.f;
 template <class Stage>
 struct RowFactors {
   float left[Stage::PASSES];    // what the row in the tile is to be multiplied by
@@ -118,8 +119,8 @@ struct RowFactors {
 #pragma unroll
       for (int p = 0; p < Stage::PASSES; ++p) {
         const uint32_t bits = __builtin_bit_cast(uint32_t, whole[p]);
-        power[p] = 0.5f * ROW_NORM * __builtin_bit_cast(float, bits & 0x7F800000u);
-        left[p] = 2.f / ROW_NORM * __builtin_bit_cast(float, (bits & 0x007FFFFFu) | 0x3F800000u);
+        power[p] = 32.f * __builtin_bit_cast(float, bits & 0x7F800000u);
+        left[p] = 1.f / 32.f * __builtin_bit_cast(float, (bits & 0x007FFFFFu) | 0x3F800000u);
       }
       stage.commit_scaled(tile, power, un);
     } else {
