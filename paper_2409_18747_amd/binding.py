@@ -133,16 +133,15 @@ def _load():
     lib.cottn_scale_from_m.argtypes = [fp, fp, i, f, vp]
     lib.cottn_scale_backward.restype = i
     lib.cottn_scale_backward.argtypes = [fp, fp, fp, i, f, vp]
-    lib.cottn_fwd_causal_decay.restype = i
-    lib.cottn_fwd_causal_decay.argtypes = [vp] * 10 + [sz] + [i] * 6 + [f, vp]
-    lib.cottn_bwd_causal_decay.restype = i
-    lib.cottn_bwd_causal_decay.argtypes = [vp] * 15 + [sz, vp, sz] + [i] * 6 + [f, vp]
-    lib.cottn_step_decay.restype = i
-    lib.cottn_step_decay.argtypes = [vp] * 7 + [i, vp, vp] + [i] * 5 + [f, vp]
-    lib.cottn_tree.restype = i
-    lib.cottn_tree.argtypes = [vp] * 8 + [i] * 6 + [f, vp]
-    lib.cottn_tree_accept.restype = i
-    lib.cottn_tree_accept.argtypes = [vp] * 6 + [i] * 6 + [f, vp]
+    # a library that was built before these makes all other calls; one of these then raises and names its function
+    for name, argtypes in (("cottn_fwd_causal_decay", [vp] * 10 + [sz] + [i] * 6 + [f, vp]),
+                           ("cottn_bwd_causal_decay", [vp] * 15 + [sz, vp, sz] + [i] * 6 + [f, vp]),
+                           ("cottn_step_decay", [vp] * 7 + [i, vp, vp] + [i] * 5 + [f, vp]),
+                           ("cottn_tree", [vp] * 8 + [i] * 6 + [f, vp]),
+                           ("cottn_tree_accept", [vp] * 6 + [i] * 6 + [f, vp])):
+        call = getattr(lib, name, None)
+        if call is not None:
+            call.restype, call.argtypes = i, argtypes
     lib.cottn_profile_start.restype = i
     lib.cottn_profile_stop.restype = i
     lib.cottn_profile_count.restype = i

@@ -755,7 +755,7 @@ PyObject* bind(PyObject*, PyObject* args) {
   COTTN_FIND(step_dkdv);
   COTTN_FIND(scale_from_m_varlen);
   COTTN_FIND(scale_backward_varlen);
-  // (a library may lack these: then their calls are binding.py's)
+  // (one that was built before these lacks them: then their calls are binding.py's, which raises)
   const bool needed = all;
   COTTN_FIND(fwd_causal_decay);
   COTTN_FIND(bwd_causal_decay);
