@@ -558,13 +558,13 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dkdv)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int it = 2 * p + half;
-        // tp[half][v] = q_(16 it + 4 q4 + v) . k_(16 rg + r)
+        // tp[half][v] = q_(16 it + 4 q4 + v) . k_(16 rg + r), a row's factor at a time (decay.h: RowFactors)
         const f32x4 qi = *reinterpret_cast<const f32x4*>(qrows + (it == rg ? 0 : C) + 16 * it + 4 * q4);
         const float above = g.after(float(16 * it) - row);   // (it > rg)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const float f = it < rg ? 0.f : qi[v] * (it == rg ? on_diagonal[v] : above);
-          tp[half][v] = it < rg ? 0.f : tp[half][v] * (f * (1.f / TILE_UNIT * left));
+          tp[half][v] = it < rg ? 0.f : tp[half][v] * f * (1.f / TILE_UNIT * left);
           ta[half][v] = it < rg ? 0.f : ta[half][v] * f;
         }
         put_four(pf, half, tp[half]);

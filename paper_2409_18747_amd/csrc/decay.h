@@ -102,7 +102,8 @@ __device__ __forceinline__ bool any_infinite(const f32x4 (&t)[A][B]) {
 }
 
 // Rows are raw in LDS and every factor of a row (1 / norm, decay) goes to fp32 results, to the masked tiles before they are
-// rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.
+// rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.  A product of two
+// rows takes their factors one after the other: the two, each up to 1 / eps, may leave fp32 when the product is small, or 0.
 //   fp16: rows of q and k times the power of two that brings their norm to 16 .. 32 (exact but for elements 2^-18 below the
 // norm), so that the factors left, 1/32 .. 1/16, are alike for short and long rows.  The tiles of dO . v take them TILE_UNIT times
 // larger, 1/2 .. 1, so that what is rounded is never above the product, nor less than half of it: they leave fp16 for no row

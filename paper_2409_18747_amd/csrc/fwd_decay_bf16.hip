@@ -311,11 +311,11 @@ COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
           f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int ks = 0; ks < Cfg::KSK; ++ks) t = mma16(kr[half][ks], qf[ks], t);
-          // t[v] = q_(16 rg + r) . k_(16 jt + 4 q4 + v)
+          // t[v] = q_(16 rg + r) . k_(16 jt + 4 q4 + v), a row's factor at a time (decay.h: RowFactors)
           const f32x4 kj = *reinterpret_cast<const f32x4*>(rows + (jt == rg ? 0 : C) + 16 * jt + 4 * q4);
           const float below = ri * g.after(row - float(16 * jt + 15));   // (jt < rg)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) t[v] = jt > rg ? 0.f : t[v] * (kj[v] * (jt == rg ? ri * on_diagonal[v] : below));
+          for (int v = 0; v < 4; ++v) t[v] = jt > rg ? 0.f : t[v] * kj[v] * (jt == rg ? ri * on_diagonal[v] : below);
           put_four(pf, half, t);
         }
 #pragma unroll

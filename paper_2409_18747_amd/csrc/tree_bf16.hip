@@ -146,9 +146,10 @@ __global__ __launch_bounds__(256, (TreeCfg<DK, DV, COLS, RG>::AT_ONCE)) void COT
           const int j = 32 * p + 16 * half + 4 * q4;   // this lane's keys j .. j + 3
 #pragma unroll
           for (int ks = 0; ks < KSK; ++ks) t = mma16(kf[half][ks], qf[ks], t);
+          // (a row's factor at a time: decay.h, RowFactors)
           const f32x4 rj = *reinterpret_cast<const f32x4*>(rk + j), dj = *reinterpret_cast<const f32x4*>(depth + j);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) t[i] = (path >> (j + i)) & 1 ? t[i] * (ri * rj[i] * g.after(mine - dj[i])) : 0.f;
+          for (int i = 0; i < 4; ++i) t[i] = (path >> (j + i)) & 1 ? t[i] * rj[i] * (ri * g.after(mine - dj[i])) : 0.f;
         }
         put_four(pf, half, t);
       }
