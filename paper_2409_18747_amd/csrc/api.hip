@@ -308,13 +308,10 @@ double decay_call_us(const DecayTimes& t, long units, long N, long n_chunks, lon
 
 // Segments of a call with a decay: the least time by the model among splits of up to 1024 workgroups, or none; a forward alone takes
 // no more than with its backward, so that the size of its workspace says which of the two it is.  With a backward,
-// 16-bit sequences of two chunks are two segments up to 128 units (128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 -> 26.5, 32 x 32
-// 18.1 -> 16.8; 128 units 128 x 128 40.3 -> 39.1; 192 units 43.4 -> 64.6), and longer ones are split where those without a decay are
-// (causal_segments).
+// 16-bit sequences of two chunks are two segments up to 128 units (128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 -> 26.5,
+// 32 x 32 18.1 -> 16.8; 128 units 128 x 128 40.3 -> 39.1; 192 units 43.4 -> 64.6).
 long decay_segments(bool alone, long units, long N, long n_chunks, bool f32, int dk, int dv) {
-  const bool narrowest = dk == 32 && dv == 32, widest = dk == 128 && dv == 128;
-  const bool cut = !f32 && !alone && ((n_chunks == 2 && units <= 128) || (!widest && n_chunks > 4 && units <= 160) ||
-                                      (narrowest && n_chunks > 8 && units < 384));
+  const bool cut = !f32 && !alone && n_chunks == 2 && units <= 128;
   const DecayTimes& t = alone ? kDecayAlone : kDecayPair;
   const long most = alone ? decay_segments(false, units, N, n_chunks, f32, dk, dv) : n_chunks;
   double best = decay_call_us(t, units, N, n_chunks, 1, f32, dk, dv);
