@@ -300,6 +300,8 @@ int cottn_scale_backward_varlen(const float* m, const int* seq_len, const float*
  * forward that no backward follows can do with a workspace of COTTN_OP_FWD_DECAY_ALONE, often none, and is then faster for short
  * prompts of few sequences: with less than COTTN_OP_FWD_DECAY asks for it takes the split of that smaller size.  A row that is
  * not finite can make results of the rows before it in its chunk not finite, as well as those behind it.
+ * B H is below 8 388 608 here and in cottn_tree, below 16 777 216 in cottn_step_decay and cottn_tree_accept; more is
+ * refused (COTTN_E_SHAPE).
  * In the calls of this section and the next an infinite element of a state that is handed over stays as it is, but where g^n, one
  * fp32 number for n rows, is 0: there it becomes NaN.  Results that its column, or its row, enters are not finite.
  *
