@@ -5,8 +5,8 @@ PyTorch supplies device memory and the stream handle, nothing else.
 The marshalling is here, over ctypes, for every call, and once more in C++ (csrc/marshal.cpp, module _marshal) for
 plain tensors on the current stream, which the attention, step and tree calls try first: it does the whole call, or nothing and
 answers None.  Decode step of 16 states 7.4 -> 3.7 us a call, of which the launch is 3.1; five drafted tokens of 128
-states 7.9 -> 6.6, a forward of 2 x 256 rows of 32 fp32 with its two allocations 9.9 -> 7.5 (the kernels from there on); with a decay a step of 16
-states 8.8 -> 5.4, a tree over them 9.0 -> 5.4, accepting 7.0 -> 5.0.
+states 7.9 -> 6.6, a forward of 2 x 256 rows of 32 fp32 with its two allocations 9.9 -> 7.5 (the kernels from there on);
+with a decay a step of 16 states 8.8 -> 5.4, a tree over them 9.0 -> 5.4, accepting 7.0 -> 5.0.
 
 The library must have been built (``python -m paper_2409_18747_amd.build``); there is no
 fallback: a missing library raises at first use.  Without _marshal the calls are the same and take those few us longer:

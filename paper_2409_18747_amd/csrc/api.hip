@@ -244,10 +244,11 @@ bool make_plan(int op, int B, int H, int N, int dk, int dv, int chunk, int dtype
 namespace {
 
 struct DecayRowParts { int parts; long most; };   // workgroups that share a sequence's chunks; what the first takes (row_part)
-// A forward whose value columns are in parts: its chunks too, where compute units would be left without a workgroup.  Kernel alone,
-// continued from a state, one / two / four row parts: 16 units 128 x 128 100 rows 9.0 / 8.2 / 8.3 us, 512 rows 24.5 / 20.4 / 19.1; 64 units
-// 64 x 64 of 256 rows 10.5 / 9.1 / 9.6, fp32 22.4 / 16.2 / 17.2; 128 units 64 x 128 of 384 18.1 / 16.9 / 22.3; 128 x 128 in 256 workgroups, 64
-// units of 384 21.4 / 22.0 / 28.5.  (192 units 64 x 128 padded: up to 389 rows 24.0 / 20.8, up to 700 33.3 / 37.6, left whole.)
+// A forward whose value columns are in parts: its chunks too, where compute units would be left without a workgroup.  Kernel
+// alone, continued from a state, one / two / four row parts: 16 units 128 x 128 100 rows 9.0 / 8.2 / 8.3 us, 512 rows 24.5 /
+// 20.4 / 19.1; 64 units 64 x 64 of 256 rows 10.5 / 9.1 / 9.6, fp32 22.4 / 16.2 / 17.2; 128 units 64 x 128 of 384 18.1 / 16.9 /
+// 22.3; 128 x 128 in 256 workgroups, 64 units of 384 21.4 / 22.0 / 28.5.  (192 units 64 x 128 padded: up to 389 rows 24.0 /
+// 20.8, up to 700 33.3 / 37.6, left whole.)
 DecayRowParts decay_row_parts(long units, long n_chunks, int dk, int dv, bool f32) {
   const int columns = decay_value_columns(units, dk, dv, f32);
   const long workgroups = units * (dv / columns);
@@ -261,23 +262,29 @@ DecayRowParts decay_row_parts(long units, long n_chunks, int dk, int dv, bool f3
   }
 }
 
-// Calls with a decay: the time of g segments by the model of causal_call_us, with constants for a forward and its backward and for a
-// forward alone, whose sequences of one segment may be in parts of the value columns (decay_value_columns), a step of which is
-// shorter by `parts`, and the rows in parts (decay_row_parts), of which the first counts, and rows_again of all chunks.  Fitted, but for
-// rows_again, to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128 x 128, fp32 64 x 64): the split chosen takes 0.4 and 0.5 % longer than the best of up to ten measured; the pair with the constants of
-// causal_call_us 1.5 % (300 units of 2048 rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units
-// of 1024 rows 128 x 128 4 segments 89 us, 1 segment 62).  Farthest off: 128 units of 512 rows 32 x 32 with backward 8 segments 33 us, 4
-// segments 28; 16 units of 8192 rows 64 x 64 forward 16 segments 1.14 times 32 segments.
-// With row parts, of 60 shapes of 16 to 128 units: 64 units 64 x 128 of 384 rows in segments 17.9 us, in row parts 14.4; at worst 16
-// units 64 x 64 of 512 rows 10.1 and 10.6.
+// Calls with a decay: the time of g segments by the model of causal_call_us, with constants for a forward and its backward and
+// for a forward alone, whose sequences of one segment may be in parts of the value columns (decay_value_columns), a step of
+// which is shorter by `parts`, and the rows in parts (decay_row_parts), of which the first counts, and rows_again of all
+// chunks.
+//   Fitted, but for rows_again, to 240 shapes each (5 to 512 units of 128 to 8192 rows, 16-bit 32 x 32, 64 x 64, 64 x 128, 128
+// x 128, fp32 64 x 64).  Measured again over those, the split chosen takes 0.4 % longer with a backward and 0.8 % alone than
+// the best of up to ten; the pair with the constants of causal_call_us 1.5 % (300 units of 2048
+// rows 64 x 64 1 segment 342 us, 3 segments 291), the forward with those of the pair 12 % (192 units of 1024 rows 128 x 128 4
+// segments 89 us, 1 segment 62).  Farthest off: 40 units of 8192 rows 32 x 32 with backward 16 segments 95 us, 19 segments 83;
+// 64 units of 128 rows 64 x 64 fp32 forward 4 segments 12.0 us, 1 segment 10.5.  fp32 128 x 128 was not fitted: 0.7 % over 40
+// shapes with a backward, but 6 % alone (96 units of 1024 rows 1 segment 238 us, 8 segments 168).
+//   With row parts, of 60 shapes of 16 to 128 units: 64 units 64 x 128 of 384 rows in segments 17.9 us, in row parts 14.4; at
+// worst 16 units 64 x 64 of 512 rows 10.1 and 10.6.
 struct DecayTimes {
   double next_narrow_f32, next_f32, next_narrow, next;   // of a step for each further workgroup at once on a compute unit
   double step_f32, step_widest, step, prologue, row;      // us a column, us a column, us a column, steps, us a MB
   double launch, totals, add_widest, add;                 // us, of a step, us a KB of a state
   double parts_64, parts_128, parts_many, rows_again;
 };
-constexpr DecayTimes kDecayPair = {0.2, 0.434, 0.019, 0.275, 0.123, 0.0667, 0.0573, 0.85, 0.876, 5.56, 0.0538, 0.0259, 0.0402, 1, 1, 1, 0};
-constexpr DecayTimes kDecayAlone = {0.2, 0.266, 0.02, 0.23, 0.05, 0.0245, 0.0287, 1.02, 0.1235, 3.33, 0.3225, 0.0251, 0.0343, 0.8, 0.7, 0.48, 0.15};
+constexpr DecayTimes kDecayPair = {0.2,  0.434, 0.019,  0.275,  0.123,  0.0667, 0.0573, 0.85, 0.876,
+                                   5.56, 0.0538, 0.0259, 0.0402, 1, 1, 1, 0};
+constexpr DecayTimes kDecayAlone = {0.2,  0.266, 0.02,   0.23,   0.05, 0.0245, 0.0287, 1.02, 0.1235,
+                                    3.33, 0.3225, 0.0251, 0.0343, 0.8,  0.7,    0.48,   0.15};
 double decay_call_us(const DecayTimes& t, long units, long N, long n_chunks, long g, bool f32, int dk, int dv) {
   const bool narrowest = dk == 32 && dv == 32, widest = dk == 128 && dv == 128;
   const int big = dk > dv ? dk : dv, small = dk > dv ? dv : dk;
@@ -306,10 +313,10 @@ double decay_call_us(const DecayTimes& t, long units, long N, long n_chunks, lon
   return us;
 }
 
-// Segments of a call with a decay: the least time by the model among splits of up to 1024 workgroups, or none; a forward alone takes
-// no more than with its backward, so that the size of its workspace says which of the two it is.  With a backward,
-// 16-bit sequences of two chunks are two segments up to 128 units (128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 -> 26.5,
-// 32 x 32 18.1 -> 16.8; 128 units 128 x 128 40.3 -> 39.1; 192 units 43.4 -> 64.6).
+// Segments of a call with a decay: the least time by the model among splits of up to 1024 workgroups, or none; a forward alone
+// takes no more than with its backward, so that the size of its workspace says which of the two it is.  With a backward, 16-bit
+// sequences of two chunks are two segments up to 128 units (128 rows: 16 units 128 x 128 37.9 -> 31.1 us, 64 x 128 34.2 ->
+// 26.5, 32 x 32 18.1 -> 16.8; 128 units 128 x 128 40.3 -> 39.1; 192 units 43.4 -> 64.6).
 long decay_segments(bool alone, long units, long N, long n_chunks, bool f32, int dk, int dv) {
   const bool cut = !f32 && !alone && n_chunks == 2 && units <= 128;
   const DecayTimes& t = alone ? kDecayAlone : kDecayPair;
@@ -454,7 +461,8 @@ size_t cottn_workspace_bytes_dkdv(int op, int B, int H, int N, int dk, int dv, i
   }
   if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY || op == COTTN_OP_FWD_DECAY_ALONE) {
     DecayPlan plan;
-    return make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan) ? decay_workspace_bytes(op, B, H, dk, dv, plan) : size_t(-1);
+    if (!make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan)) return size_t(-1);
+    return decay_workspace_bytes(op, B, H, dk, dv, plan);
   }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_STEP) return size_t(-1);
   SeqPlan plan;

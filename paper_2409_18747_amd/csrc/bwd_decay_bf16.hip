@@ -6,12 +6,13 @@
 // g^i' qh_i^T dO_i, from which it leaves the segment's reverse-time total for the second, and ds.  The second walks backward in
 // time with R and gives dK and dV.
 //
-// ds = sum_i (sum_j g^(i-j) (qh_i . kh_j) v_j) . dO_i is a result in fp32 and a sum of terms of both signs, so it is not taken from
-// results of rounded operands: the rows before a chunk give g <H, G>, element by element from two fp32 matrices whose operands are
-// carried in parts (EXACT_PARTS), and the chunk itself gives the sum of its two masked fp32 tiles' products before they are rounded.
+// ds = sum_i (sum_j g^(i-j) (qh_i . kh_j) v_j) . dO_i is a result in fp32 and a sum of terms of both signs, so it is not taken
+// from results of rounded operands: the rows before a chunk give g <H, G>, element by element from two fp32 matrices whose
+// operands are carried in parts (EXACT_PARTS), and the chunk itself gives the sum of its two masked fp32 tiles' products before
+// they are rounded.
 //
-// The chain rule through x / max(|x|, eps): dx = s r (dxh - xh (xh . dxh)) with r = 1 / max(|x|, eps); rows at or below eps have
-// dx = s r dxh.
+// The chain rule through x / max(|x|, eps): dx = s r (dxh - xh (xh . dxh)) with r = 1 / max(|x|, eps); rows at or below eps
+// have dx = s r dxh.
 #include "device_common.h"
 #include "launch.h"
 #include "tile_io.h"
@@ -54,8 +55,9 @@ __device__ __forceinline__ void store_factors(float* rows, const RowFactors<Stag
   for (int p = 0; p < Stage::PASSES; ++p) {
     const int lr = p * Stage::RPP + threadIdx.x / Stage::LPR;
     const int e = which == 1 ? e1(lr) : which == 2 ? e2(lr) : 0;
-    if ((C % Stage::RPP == 0 || lr < C) && which < 4) rows[which * C + lr] = (which == 3 ? f.whole[p] : f.left[p]) * g.after(float(e)) *
-                                                         (which == 2 ? STATE_UNIT : which == 3 ? 1.f : TILE_UNIT);
+    if ((C % Stage::RPP == 0 || lr < C) && which < 4)
+      rows[which * C + lr] = (which == 3 ? f.whole[p] : f.left[p]) * g.after(float(e)) *
+                             (which == 2 ? STATE_UNIT : which == 3 ? 1.f : TILE_UNIT);
   }
 }
 
@@ -286,8 +288,8 @@ COTTN_KERNEL((C * 4 * CS, (DecayBwdCfg<DK, DV, C, CS>::WAVES)), bwd_decay_dq)
       for (int nt = 0; nt < NKT; ++nt) dq[nt] = mma16_add(kc[nt], af, dq[nt]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    // the state after the chunk, but for the last (with the same in the other scans, 96 units of 1024 rows 64 x 64 63.7 -> 62.0 us,
-    // 128 x 128 156.6 -> 155.2 where this scan forms it all the same and 157.9 where not)
+    // the state after the chunk, but for the last (with the same in the other scans, 96 units of 1024 rows 64 x 64 63.7 -> 62.0
+    // us, 128 x 128 156.6 -> 155.2 where this scan forms it all the same and 157.9 where not)
     if (active && ((DK == 128 && DV == 128) || row0 + C < row_end)) {
       (n == C ? whole_chunk : Kept(g, float(n))).on(sacc);   // (the gradients of a state with an infinite element are not finite)
       const WeightedTile<ST, Cfg::NP, TPK, EXACT_PARTS> k(Ks, krows + 2 * C, w, r, q4);
@@ -645,9 +647,9 @@ hipError_t run_bwd_decay(const DecayArgs& a) {
     if (err != hipSuccess) return err;
     fwd = own_fwd;
   }
-  // The second scan is the last to read the rows: past the caches where they hold no call's tensors (768 units of 512 rows 128 x 128,
-  // forward + backward 436 -> 419 us, 16 of 65536 rows 64 x 64 488 -> 473; where they do, 96 of 1024 rows, 63.7 -> 64.8; and the
-  // first scan too, 426 and 478).
+  // The second scan is the last to read the rows: past the caches where they hold no call's tensors (768 units of 512 rows 128
+  // x 128, forward + backward 436 -> 419 us, 16 of 65536 rows 64 x 64 488 -> 473; where they do, 96 of 1024 rows, 63.7 -> 64.8;
+  // and the first scan too, 426 and 478).
   const double bytes = 2.0 * units * double(a.N) * (DK + DV) * ELEM;
   const int flags = (a.carried ? CARRIED : 0) | (bytes > 256.0 * 1024 * 1024 ? STREAM : 0);
   const dim3 grid(units * a.G), block(64 * (C / 16) * CS);
@@ -672,10 +674,10 @@ hipError_t run_bwd_decay(const DecayArgs& a) {
 
 using namespace COTTN_NS;
 
-// Rows of a chunk and waves on a row group, as in the backward without decay (bwd_causal_bf16.hip: BwdSplit).  96 units of 1024 rows,
-// forward + backward, bf16: 64 x 64 one wave / two 63.5 / 103 us, 128 x 128 64 rows / 32 157 / 250, 128 x 64 32 rows / 64 rows, each with two
-// waves, 106 / 264: the others do not fit their registers.  fp32 384 units of 512 rows, two waves / four: 128 x 64 635 / 629, 64 x 128
-// 579 / 596.
+// Rows of a chunk and waves on a row group, as in the backward without decay (bwd_causal_bf16.hip: BwdSplit).  96 units of 1024
+// rows, forward + backward, bf16: 64 x 64 one wave / two 63.5 / 103 us, 128 x 128 64 rows / 32 157 / 250, 128 x 64 32 rows / 64
+// rows, each with two waves, 106 / 264: the others do not fit their registers.  fp32 384 units of 512 rows, two waves / four:
+// 128 x 64 635 / 629, 64 x 128 579 / 596.
 hipError_t COTTN_SYM(bwd_decay)(const DecayArgs& a) {
 #define COTTN_CASE(DK, DV)                                                                                             \
   case DK * 1000 + DV: {                                                                                               \

@@ -35,8 +35,8 @@ struct Decay {
 };
 
 // What a state is multiplied by n rows later: x * times + x * plus.  A factor just below 1 is 1 - d with a d of its own, whose
-// relative error is that of fp32: as one rounded number, g^64 of a head that hardly forgets would be off by up to 2^-25
-// with the same sign in every chunk, 3e-5 of what is oldest after 1024 chunks.  x * plus is formed of a finite number in place of an
+// relative error is that of fp32: as one rounded number, g^64 of a head that hardly forgets would be off by up to 2^-25 with
+// the same sign in every chunk, 3e-5 of what is oldest after 1024 chunks.  x * plus is formed of a finite number in place of an
 // infinite x, which then stays x: inf - inf d would be NaN.
 __device__ __forceinline__ float made_finite(float x) {
   return __builtin_amdgcn_fmed3f(x, -3.402823466e38f, 3.402823466e38f);   // (of NaN some number: the other term is NaN)
@@ -73,8 +73,8 @@ struct Kept {
           for (int v = 0; v < 4; ++v) t[x][y][v] *= times;
     }
   }
-  // the same, where some element is `infinite` (any_infinite): made_finite for every state of 64 x 16 heads of 2048 rows 128 x 128 took
-  // 562 us instead of 547, and 96 units of 1024 rows forward + backward 162 instead of 155
+  // the same, where some element is `infinite` (any_infinite): made_finite for every state of 64 x 16 heads of 2048 rows 128 x
+  // 128 took 562 us instead of 547, and 96 units of 1024 rows forward + backward 162 instead of 155
   template <int A, int B>
   __device__ __forceinline__ void on(f32x4 (&t)[A][B], bool infinite) const {
     if (infinite) {
@@ -102,12 +102,13 @@ __device__ __forceinline__ bool any_infinite(const f32x4 (&t)[A][B]) {
 }
 
 // Rows are raw in LDS and every factor of a row (1 / norm, decay) goes to fp32 results, to the masked tiles before they are
-// rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.  A product of two
-// rows takes their factors one after the other: the two, each up to 1 / eps, may leave fp32 when the product is small, or 0.
+// rounded, or to operand fragments below: an element of a result has met one rounding to 16 bits but for its own.  A product of
+// two rows takes their factors one after the other: the two, each up to 1 / eps, may leave fp32 when the product is small, or
+// 0.
 //   fp16: rows of q and k times the power of two that brings their norm to 16 .. 32 (exact but for elements 2^-18 below the
-// norm), so that the factors left, 1/32 .. 1/16, are alike for short and long rows.  The tiles of dO . v take them TILE_UNIT times
-// larger, 1/2 .. 1, so that what is rounded is never above the product, nor less than half of it: they leave fp16 for no row
-// norm, neither for the 1 / eps of a short row nor for the small ones of a long one, and for no product that fp16 holds.
+// norm), so that the factors left, 1/32 .. 1/16, are alike for short and long rows.  The tiles of dO . v take them TILE_UNIT
+// times larger, 1/2 .. 1, so that what is rounded is never above the product, nor less than half of it: they leave fp16 for no
+// row norm, neither for the 1 / eps of a short row nor for the small ones of a long one, and for no product that fp16 holds.
 constexpr float TILE_UNIT = ELEM_IS_F16 ? 16.f : 1.f;
 template <class Stage>
 struct RowFactors {

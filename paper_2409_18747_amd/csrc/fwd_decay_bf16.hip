@@ -2,13 +2,13 @@
 // bfloat16 kernels, the IEEE half ones when it is included with COTTN_ELEM_F16 defined and the fp32 ones with
 // COTTN_ELEM_F32 and COTTN_F32_WHOLE.
 //
-// A workgroup walks a segment of a (batch, head) chunk by chunk with the d_key x d_value state in fp32 accumulators.  Of a chunk
-// it forms the masked tiles (Qh Kh^T (.) g^(i-j)) and their product with V, adds what the state gives, and takes the
-// state on to the chunk's end.  Where a sequence is cut into segments, a first kernel leaves the total of every segment
-// but the last, each as seen from the segment's own end; the scans weigh and add those before theirs.
+// A workgroup walks a segment of a (batch, head) chunk by chunk with the d_key x d_value state in fp32 accumulators.  Of a
+// chunk it forms the masked tiles (Qh Kh^T (.) g^(i-j)) and their product with V, adds what the state gives, and takes the
+// state on to the chunk's end.  Where a sequence is cut into segments, a first kernel leaves the total of every segment but the
+// last, each as seen from the segment's own end; the scans weigh and add those before theirs.
 //
-// What bounds them: vector instructions (the weights of operand fragments, their parts, the masked tiles) and the rows' way through
-// memory, at some 4 to 5.4 TB/s for large calls; matrix instructions take a quarter of the time.
+// What bounds them: vector instructions (the weights of operand fragments, their parts, the masked tiles) and the rows' way
+// through memory, at some 4 to 5.4 TB/s for large calls; matrix instructions take a quarter of the time.
 #include "device_common.h"
 #include "launch.h"
 #include "tile_io.h"
@@ -32,8 +32,8 @@ struct DecayFwdCfg {
 };
 
 // In either kernel a wave holds tiles of the state with the values down and the keys along: element [v] of lane (r, q4) of tile
-// (x, y) is S[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  It has few key tiles and as many values as that leaves:
-// the fragments of keys are the ones that weights go to, some 50 instructions each.
+// (x, y) is S[key 16 col_tile(x) + r][value 16 row_tile(y) + 4 q4 + v].  It has few key tiles and as many values as that
+// leaves: the fragments of keys are the ones that weights go to, some 50 instructions each.
 
 // The factors of the chunk's key rows, one lane of a row for each: [0] 1 / norm, [1] that times g^(15 - j' mod 16), for tiles
 // below the diagonal, [2] times g^(n-1-j') STATE_UNIT, for the state after the chunk's n rows.
@@ -44,13 +44,14 @@ __device__ __forceinline__ void store_key_factors(float* rows, const RowFactors<
   for (int p = 0; p < Stage::PASSES; ++p) {
     const int lr = p * Stage::RPP + threadIdx.x / Stage::LPR;
     const int e = which == 0 ? 0 : which == 1 ? 15 - lr % 16 : max(n - 1 - lr, 0);
-    if ((C % Stage::RPP == 0 || lr < C) && which < 3) rows[which * C + lr] = f.left[p] * g.after(float(e)) * (which == 2 ? STATE_UNIT : 1.f);
+    if ((C % Stage::RPP == 0 || lr < C) && which < 3)
+      rows[which * C + lr] = f.left[p] * g.after(float(e)) * (which == 2 ? STATE_UNIT : 1.f);
   }
 }
 
 // ---------------------------------------------------------------------------------------
-// T[unit][segment] = sum over the rows j of a segment of g^(end-1-j) kh_j^T v_j, for all segments but the last of a
-// unit (and those that a sequence of a padded batch does not reach), as tiles in accumulator order.  96 units of 1024 rows 64 x 64 in
+// T[unit][segment] = sum over the rows j of a segment of g^(end-1-j) kh_j^T v_j, for all segments but the last of a unit (and
+// those that a sequence of a padded batch does not reach), as tiles in accumulator order.  96 units of 1024 rows 64 x 64 in
 // bf16, 4 segments, 8.8 us; 16 of 65536 rows, 32 segments, 55.8 us, 4.8 TB/s (VALU issue 57 %, matrix instructions 21 %).
 template <int DK, int DV, int C>
 COTTN_KERNEL((C * 4), decay_segment_state)
@@ -116,8 +117,9 @@ COTTN_KERNEL((C * 4), decay_segment_state)
 }
 
 // ---------------------------------------------------------------------------------------
-// Row parts: the chunks of a sequence of one segment, dealt to workgroups that each form the state up to theirs by themselves. A chunk
-// that only makes the state takes about half the time of a whole one, so part k takes `most` chunks less half of those before it.
+// Row parts: the chunks of a sequence of one segment, dealt to workgroups that each form the state up to theirs by themselves.
+// A chunk that only makes the state takes about half the time of a whole one, so part k takes `most` chunks less half of those
+// before it.
 __device__ __forceinline__ void row_part(int k, int most, int& begin, int& count) {
   begin = 0;
   count = most;
@@ -129,11 +131,11 @@ __device__ __forceinline__ void row_part(int k, int most, int& begin, int& count
 
 // The scan of one segment.  Wave (row group rg, column part cp) owns the query rows 16 rg .. of the chunk and the output
 // columns of its part, and tiles of the state, held as said above.  Results are accumulated transposed: a lane holds four
-// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value columns, which the whole
-// computation leaves apart from one another but for the masked tiles, formed LDV / DV times, and a part of the rows (row_part).
-// PARTS: EXACT_PARTS where the state is asked for.
-//   bf16: 96 units of 1024 rows 64 x 64 in 4 segments 14.4 us; 16 of 65536 rows in 32 segments 99 us, 5.4 TB/s; 1024 of 2048 rows 128 x 128
-// 558 us, 3.8 TB/s (VALU issue 47 %, matrix instructions 28 %, LDS 46 % of the time).
+// consecutive columns of one output row.  LDV > DV (one segment): a workgroup takes DV of the LDV value columns, which the
+// whole computation leaves apart from one another but for the masked tiles, formed LDV / DV times, and a part of the rows
+// (row_part). PARTS: EXACT_PARTS where the state is asked for.
+//   bf16: 96 units of 1024 rows 64 x 64 in 4 segments 14.4 us; 16 of 65536 rows in 32 segments 99 us, 5.4 TB/s; 1024 of 2048
+// rows 128 x 128 558 us, 3.8 TB/s (VALU issue 47 %, matrix instructions 28 %, LDS 46 % of the time).
 template <int DK, int DV, int C, int CS, int PARTS, int LDV = DV>
 COTTN_KERNEL((C * 4 * CS, (DecayFwdCfg<DK, DV, C, CS>::WAVES)), fwd_decay_scan)
     const elem_t* __restrict__ Q, const elem_t* __restrict__ K, const elem_t* __restrict__ V,
@@ -360,8 +362,9 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
     if (err == hipSuccess && a.carried) err = launch_decay_carry(a, states, false);
     if (err != hipSuccess) return err;
   }
-  // Rows that nothing finds in a cache again, as without decay (fwd_causal_bf16.hip): 64 x 16 heads of 2048 rows, forward alone, 128 x 128
-  // 561 -> 558 us, 64 x 64 228.5 -> 223.4; where they fit, 96 units of 1024 rows 64 x 64 with backward 63.7 -> 64.1.
+  // Rows that nothing finds in a cache again, as without decay (fwd_causal_bf16.hip): 64 x 16 heads of 2048 rows, forward
+  // alone, 128 x 128 561 -> 558 us, 64 x 64 228.5 -> 223.4; where they fit, 96 units of 1024 rows 64 x 64 with backward 63.7 ->
+  // 64.1.
   const double bytes = 2.0 * units * double(a.N) * (DK + LDV) * ELEM;
   const int flags = (a.carried ? CARRIED : 0) | (bytes > 256.0 * 1024 * 1024 ? STREAM_Q : 0) |
                     (a.G == 1 && bytes > 1024.0 * 1024 * 1024 ? STREAM_KV : 0);
@@ -378,8 +381,8 @@ hipError_t run_fwd_decay(const DecayArgs& a) {
 
 template <int DK, int DV, int C>
 hipError_t run_decay_totals(const DecayArgs& a, float* dst) {
-  // 128 rows at a time where segments are that long: eight waves, a key tile each (96 units of 1024 rows forward + backward 162.5 ->
-  // 156.4 us; not at narrower shapes, 64 x 64 63.6 / 63.9, 32 x 32 35.8 / 37.1, 128 x 64 105.7 / 106.7)
+  // 128 rows at a time where segments are that long: eight waves, a key tile each (96 units of 1024 rows forward + backward
+  // 162.5 -> 156.4 us; not at narrower shapes, 64 x 64 63.6 / 63.9, 32 x 32 35.8 / 37.1, 128 x 64 105.7 / 106.7)
   if constexpr (C == 64 && !ELEM_IS_F32 && DK == 128 && DV == 128)
     if (a.seg_rows >= 128) return run_decay_totals<DK, DV, 128>(a, dst);
   const int units = a.B * a.H;
@@ -388,8 +391,8 @@ hipError_t run_decay_totals(const DecayArgs& a, float* dst) {
                        a.log_decay, a.seq_len, Divisor(a.H), Divisor(a.G), a.seg_rows, a.N, units, 1.0f / a.eps);
 }
 
-// In place, for four neighbouring elements: slot k (in walking order) <- what the state at its start is, which is
-// g^seg_rows times that of the slot before, and that slot's total.  16 units of 32 segments 64 x 64: 7.2 us, two trips to memory a batch
+// In place, for four neighbouring elements: slot k (in walking order) <- what the state at its start is, which is g^seg_rows
+// times that of the slot before, and that slot's total.  16 units of 32 segments 64 x 64: 7.2 us, two trips to memory a batch
 // of eight slots.
 __global__ __launch_bounds__(256) void decay_carry(float* __restrict__ slots, const float* __restrict__ log_decay,
                                                    const int* __restrict__ lengths, Divisor H, int G, int seg_rows, int N,
@@ -431,11 +434,12 @@ using namespace COTTN_NS;
     default: return hipErrorInvalidValue;                                                                            \
   }
 
-// Rows of a chunk: 64, in fp32 32.  Waves on a row group: one; two where the output of a wave would be 128 columns wide and
-// in fp32, whose chunk is two row groups; in fp32 128 x 128, where the LDS holds one workgroup to a compute unit, four (two / four:
-// 384 units of 512 rows 330 / 284 us, 15 of 777 43.0 / 41.4; 64 x 64, 15 units of 777, 128 registers for two workgroups of eight waves, 18.7 / 21.7).
-// 16-bit 128 x 128 with more workgroups than compute units: 32 rows, so that two of them share one (1024 units of 2048 rows, 64 / 32
-// rows 598 / 555 us; 192 workgroups of 512 rows each, with totals and backward, 157 / 163; 32 rows with four waves, spilling, 1187).
+// Rows of a chunk: 64, in fp32 32.  Waves on a row group: one; two where the output of a wave would be 128 columns wide and in
+// fp32, whose chunk is two row groups; in fp32 128 x 128, where the LDS holds one workgroup to a compute unit, four (two /
+// four: 384 units of 512 rows 330 / 284 us, 15 of 777 43.0 / 41.4; 64 x 64, 15 units of 777, 128 registers for two workgroups
+// of eight waves, 18.7 / 21.7). 16-bit 128 x 128 with more workgroups than compute units: 32 rows, so that two of them share
+// one (1024 units of 2048 rows, 64 / 32 rows 598 / 555 us; 192 workgroups of 512 rows each, with totals and backward, 157 /
+// 163; 32 rows with four waves, spilling, 1187).
 hipError_t COTTN_SYM(fwd_decay)(const DecayArgs& a) {
   constexpr int C = ELEM_IS_F32 ? 32 : 64, CS = ELEM_IS_F32 ? 2 : 1;
   switch (a.value_columns != a.dv ? (a.dk * 1000 + a.dv) * 100 + a.value_columns : 0) {

@@ -269,12 +269,13 @@ struct DecayArgs {
 };
 
 // Value columns of a workgroup in a forward of one segment: parts of them where sequences are few, so that more compute units
-// have a workgroup.  Kernel alone, continued from a state, whole / 64 / 32 columns: 16 units of 64 rows 128 x 128 9.9 / 7.5 / 6.0 us,
-// 64 x 64 5.7 / - / 4.7; 64 units 128 x 128 10.6 / 8.4 / 8.6, 64 x 128 7.6 / 5.8 / 5.1; 128 units 128 x 128 11.9 / 10.7 / 12.4, 64 x 64
-// 6.1 / - / 5.3, of 384 rows 17.2 / - / 14.7; 192 units of 384 rows 64 x 128 25.1 / 24.5 / 29.0, 128 x 128 32.6 / 36.8 / 46.5.
-//   129 to 256 units, bf16, whole / 64 columns, of 5, 128, 256, 384 and 700 rows: 64 x 128, 130 units 8.2 / 7.5, 11.9 / 11.6, 17.9 / 16.6,
-// 24.0 / 22.1, 39.7 / 35.2; 256 units 9.4 / 8.4, 13.4 / 13.5, 19.8 / 18.7, 25.9 / 25.5, 47.0 / 43.5; 32 x 128, 192 units 6.5 / 6.2, 9.5 / 9.4,
-// 14.6 / 13.6, 19.0 / 18.1, 31.2 / 28.4; at worst 256 units of 512 rows 24.4 / 24.7.
+// have a workgroup.  Kernel alone, continued from a state, whole / 64 / 32 columns: 16 units of 64 rows 128 x 128 9.9 / 7.5 /
+// 6.0 us, 64 x 64 5.7 / - / 4.7; 64 units 128 x 128 10.6 / 8.4 / 8.6, 64 x 128 7.6 / 5.8 / 5.1; 128 units 128 x 128 11.9 / 10.7
+// / 12.4, 64 x 64 6.1 / - / 5.3, of 384 rows 17.2 / - / 14.7; 192 units of 384 rows 64 x 128 25.1 / 24.5 / 29.0, 128 x 128 32.6
+// / 36.8 / 46.5.
+//   129 to 256 units, bf16, whole / 64 columns, of 5, 128, 256, 384 and 700 rows: 64 x 128, 130 units 8.2 / 7.5, 11.9 / 11.6,
+// 17.9 / 16.6, 24.0 / 22.1, 39.7 / 35.2; 256 units 9.4 / 8.4, 13.4 / 13.5, 19.8 / 18.7, 25.9 / 25.5, 47.0 / 43.5; 32 x 128, 192
+// units 6.5 / 6.2, 9.5 / 9.4, 14.6 / 13.6, 19.0 / 18.1, 31.2 / 28.4; at worst 256 units of 512 rows 24.4 / 24.7.
 constexpr int decay_value_columns(long units, int dk, int dv, bool f32) {
   if (dv == 32 || units <= 64) return 32;
   if (units <= 128) return dv == 128 ? 64 : 32;

@@ -2,9 +2,10 @@
 // from another one's state (beams), and the accepted path of a tree of drafted tokens.
 //
 // Both are a stream of the states through the chip; the arithmetic is fp32 on the vector ALU.  A workgroup owns COLS value
-// columns of one state: a row is covered by COLS / 4 lanes with four columns each, and all rows are requested before any is used.  128 x 128, bf16 rows: 4096 states with beams 79 us (268 MB written,
-// at most as much read), the same accepted of trees of 13 tokens, one sequence in eight rejecting all, 86 us, 5.5 TB/s; 16 states 3.0 and 4.0
-// us, of which an empty kernel takes 2.4.
+// columns of one state: a row is covered by COLS / 4 lanes with four columns each, and all rows are requested before any is
+// used.  128 x 128, bf16 rows: 4096 states with beams 81 us (268 MB written, at most as much read), the same accepted of trees
+// of 32 tokens, one sequence in eight rejecting all, 88 us, 5.4 TB/s; 16 states 3.0 and 4.0 us, of which an empty kernel takes
+// 2.4.
 #include "device_common.h"
 #include "launch.h"
 #include "tile_io.h"
@@ -110,7 +111,8 @@ __global__ __launch_bounds__(256) void step_decay_kernel(
   }
 }
 
-// S <- g^L S + sum over the L tokens j of the path to node `last` of g^(L-1-depth_j) kh_j^T v_j; last outside the tree: S stays.
+// S <- g^L S + sum over the L tokens j of the path to node `last` of g^(L-1-depth_j) kh_j^T v_j; last outside the tree: S
+// stays.
 template <typename T, int DK, int DV, int COLS>
 __global__ __launch_bounds__(256) void tree_accept_kernel(
     const T* __restrict__ k, const T* __restrict__ v, const float* __restrict__ log_decay, const int* __restrict__ parent,
@@ -180,8 +182,9 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(
 // non-temporal loads where the states of a call exceed the L2s (step.hip)
 bool streamed(long units, int dk, int dv) { return double(units) * dk * dv * sizeof(float) > 32.0 * 1024 * 1024; }
 
-// Up to 128 states a workgroup takes 32 value columns instead of all, so that more compute units have one.  Kernels alone, states of
-// 128 x 128, whole / parts: step of 16 states 3.6 / 3.0 us, 128 5.4 / 4.2, 256 6.9 / 7.9; accepting 5.2 / 4.0, 7.5 / 5.2, 8.7 / 8.9.
+// Up to 128 states a workgroup takes 32 value columns instead of all, so that more compute units have one.  Kernels alone,
+// states of 128 x 128, whole / parts: step of 16 states 3.6 / 3.0 us, 128 5.4 / 4.2, 256 6.9 / 7.9; accepting 5.2 / 4.0, 7.5 /
+// 5.2, 8.7 / 8.9.
 bool state_parts(long units, int dv) { return dv > 32 && units <= 128; }
 
 template <typename T, int DK, int DV, int COLS>

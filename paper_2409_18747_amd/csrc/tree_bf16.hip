@@ -29,10 +29,12 @@ __device__ __forceinline__ frag8 lds_spread_frag(const lds_t* tile, int pitch, i
 // of the columns (NOT tiles) of every one, or of every RW-th where there are fewer than four column tiles.  Each masked tile is
 // formed by one wave and handed on as the fragment that it enters the next product as.  The columns of a wave's two tiles are
 // interleaved by fours, so that a lane ends with eight consecutive columns of a row, a whole 16-byte store.
-//   The state is most of what is read, and what bounds a call of many sequences.  It is requested first.  Up to 32 tokens its rows
-// go through the LDS; beyond, where the tiles of the rows would then leave a compute unit one workgroup, every wave reads its
-// columns straight into operand fragments (DIRECT), 64-byte pieces of rows.  1024 states of 128 x 128, kernel alone, through the LDS /
-// direct: 13 tokens 15.1 / 17.1 us, 64 tokens 30.3 / 28.5 (one workgroup to a compute unit 35.5): 134 MB, 4.8 TB/s.
+//   The state is most of what is read, and what bounds a call of many sequences.  It is requested first.  Up to 32 tokens its
+// rows go through the LDS; beyond, where the tiles of the rows would then leave a compute unit one workgroup, every wave reads
+// its columns straight into operand fragments (DIRECT), 64-byte pieces of rows.  1024 states of 128 x 128, through the LDS /
+// direct, when that was chosen: 13 tokens 15.1 / 17.1 us, 64 tokens 30.3 / 28.5 (one workgroup to a compute unit 35.5).  As it
+// is, 64 tokens 27.0 us for 134 MB, 5.0 TB/s; fp32, whose 128 columns are two workgroups that each read the rows and form the
+// masked tiles, 13 tokens 28.6 us for 94 MB, 64 tokens 95.7 for 201 MB.
 template <int DK, int DV, int COLS, int RG>
 struct TreeCfg {
   static constexpr int T = 16 * RG < 32 ? 32 : 16 * RG, PAIRS = T / 32;   // rows of the tiles: a product takes 32 tokens
@@ -247,8 +249,8 @@ template <int DK, int DV>
 hipError_t run_tree(const TreeArgs& a) {
   constexpr int COLS = ELEM_IS_F32 && DV == 128 ? 64 : DV;   // (four fp32 tiles of 128 columns do not fit the LDS)
   // Up to 64 states: parts of the value columns to a workgroup, so that more compute units have one.  Kernel alone, states of
-  // 128 x 128, whole / 64 / 32 columns: 16 states, 13 tokens 4.1 / - / 3.5 us, 64 tokens 5.8 / 5.1 / 5.4; 64 states, 64 tokens 6.5 /
-  // 5.3 / 7.3; 128 states, 13 tokens 4.7 / - / 5.4.
+  // 128 x 128, whole / 64 / 32 columns: 16 states, 13 tokens 4.1 / - / 3.5 us, 64 tokens 5.8 / 5.1 / 5.4; 64 states, 64 tokens
+  // 6.5 / 5.3 / 7.3; 128 states, 13 tokens 4.7 / - / 5.4.
   if (DV > 32 && a.B * a.H <= 64) {
     if (a.n_tokens <= 16) return launch_tree<DK, DV, 32, 1>(a);
     if (a.n_tokens <= 32) return launch_tree<DK, DV, 32, 2>(a);
