@@ -82,7 +82,11 @@ typedef enum {
   COTTN_OP_STEP = 4,
   COTTN_OP_FWD_DECAY = 5,
   COTTN_OP_BWD_DECAY = 6,
-  COTTN_OP_FWD_DECAY_ALONE = 8 /* a forward whose workspace no backward takes over */
+  COTTN_OP_FWD_DECAY_ALONE = 8, /* a forward whose workspace no backward takes over */
+  COTTN_OP_FWD_DELTA = 16,
+  COTTN_OP_FWD_DELTA_ALONE = 17, /* likewise */
+  COTTN_OP_BWD_DELTA = 18,
+  COTTN_OP_BWD_DELTA_SAVED = 19  /* a backward that is handed its forward's workspace */
 } cottn_op;
 
 /* Bytes of workspace the given operation needs for these arguments (0 for COTTN_OP_STEP).
@@ -351,6 +355,64 @@ int cottn_tree(const void* q, const void* k, const void* v, const float* s, cons
                const float* state, void* o, int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream);
 int cottn_tree_accept(const void* k, const void* v, const float* log_decay, const int* parent, const int* last, float* state,
                       int B, int H, int T, int dk, int dv, int dtype, float eps, void* hip_stream);
+
+/* ---- the gated delta rule ---------------------------------------------------------------------
+ * The recurrence of Sec. 5 with a state that replaces what it held for a key instead of adding to it: with
+ * g_t = exp(log_decay[b][h][t]) and beta_t = beta[b][h][t]
+ *   H_t = g_t (I - beta_t kh_t^T kh_t) H_(t-1) + beta_t kh_t^T v_t,   o_t = s_h qh_t H_t,   that is
+ *   e_t = v_t - kh_t g_t H_(t-1),   H_t = g_t H_(t-1) + beta_t kh_t^T e_t.
+ * log_decay and beta: float[B][H][N] device pointers.  log_decay may be NULL (no decay); values are <= 0, one above 0 counts as
+ * 0, one below -128 (-inf among them) keeps nothing.  beta is usually in 0 .. 1, and any finite number: between 0 and 2 no state
+ * grows but by its values.  States are float[B][H][dk][dv], without s; dk and dv are each one of 32, 64, 128.  Chunks
+ * are of 64 rows.  All dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them
+ * in bfloat16 parts).  Workspaces: cottn_workspace_bytes_dkdv with the COTTN_OP_*_DELTA* operations, chunk 0; always needed.
+ * A value that is not finite, in a row, a gate or a state, can make results of its sequence and head not finite, those of
+ * earlier rows of its chunk among them.  B H (N + 63) / 64 and B H dv / 16 are below 16 777 216; more is refused
+ * (COTTN_E_SHAPE).
+ *
+ * Forward.  seq_len, s, N = 0 and the state as in cottn_fwd_causal_decay; rows and gates at or beyond a sequence's end are not
+ * read.  state may be state_in (in place), else the two must not overlap (COTTN_E_ARG).  With a workspace of
+ * COTTN_OP_FWD_DELTA's size or more the call leaves there what a backward takes over; COTTN_OP_FWD_DELTA_ALONE's is enough
+ * without one, and then a 16-bit call without state is the faster one.
+ * Backward, of the same call: gradients with respect to the raw Q, K, V, to s (float[H], with seq_len float[B][H]), to
+ * log_decay and to beta (float[B][H][N], zeros at or beyond a sequence's end; dlog_decay may be NULL, and must be where log_decay
+ * is; it is 0 where log_decay is above 0 or below -128).  For a sequence in pieces, last piece first (both optional):
+ *   dstate      the gradient with respect to the forward call's `state`: the dstate_in of the piece behind;
+ *   dstate_in   that with respect to its state_in.  May be dstate, else must overlap neither dstate nor state_in (COTTN_E_ARG).
+ * fwd_workspace: NULL, or the workspace, of COTTN_OP_FWD_DELTA's size or more, of the matching completed cottn_fwd_causal_delta
+ * call, untouched since; a smaller one is refused (COTTN_E_WORKSPACE).  With it `workspace` is of COTTN_OP_BWD_DELTA_SAVED's
+ * size, without it of COTTN_OP_BWD_DELTA's. */
+int cottn_fwd_causal_delta(const void* Q, const void* K, const void* V, const float* s, const float* log_decay, const float* beta,
+                           const int* seq_len, const float* state_in, void* O, float* state, void* workspace,
+                           size_t workspace_bytes, int B, int H, int N, int dk, int dv, int dtype, float eps, void* hip_stream);
+int cottn_bwd_causal_delta(const void* Q, const void* K, const void* V, const float* s, const float* log_decay, const float* beta,
+                           const int* seq_len, const void* dO, const float* state_in, const float* dstate, void* dQ, void* dK,
+                           void* dV, float* ds, float* dlog_decay, float* dbeta, float* dstate_in, const void* fwd_workspace,
+                           size_t fwd_workspace_bytes, void* workspace, size_t workspace_bytes, int B, int H, int N, int dk,
+                           int dv, int dtype, float eps, void* hip_stream);
+
+/* One token: e = v - kh g state_in[parent[b]], state[b] = g state_in[parent[b]] + beta kh^T e, o[b] = s qh state[b].
+ * log_decay (may be NULL) and beta are float[B][H], s is float[H]; state_in, parent, B_in, state, q, k, v, o as in
+ * cottn_step_decay. */
+int cottn_step_delta(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const float* beta,
+                     const float* state_in, const int* parent, int B_in, float* state, void* o, int B, int H, int dk, int dv,
+                     int dtype, float eps, void* hip_stream);
+
+/* ---- rotary positions -------------------------------------------------------------------------
+ * Rows of Q and K, before any of the calls above, turned by where they stand: the operations of this library see no positions
+ * but the causal order, and the bidirectional ones none.  A rotation keeps a row's norm.  Pair p of a row's features, (x_a,
+ * x_b), becomes
+ *   y_a = x_a cos phi - x_b sin phi,   y_b = x_b cos phi + x_a sin phi,   phi = positions[b][n][axis[p]] freq[p],
+ * with (a, b) = (2 p, 2 p + 1) if `neighbours`, else (p, p + pairs); features from 2 pairs on are copied.
+ *   Q, K, Qr, Kr [B][H][N][d], K and Kr both NULL for Q alone; Qr may be Q and Kr may be K (in place), else no output overlaps
+ *   an input or the other output (COTTN_E_ARG).  For single tokens N is 1.
+ *   positions: int[B][N][axes], any values; freq: float[pairs], radians to a position; axis: int[pairs], the axis (time, row,
+ *   column, ...) that a pair is turned by, NULL for 0; a pair whose axis is none of 0 .. axes - 1 is not turned.
+ *   pairs: 1 .. d / 2; d one of 32, 64, 128; axes >= 1.
+ *   inverse: turned by - phi, which is the gradient of the call without.
+ * Angles are formed in 64 bits.  N = 0 does nothing. */
+int cottn_rotary(const void* Q, const void* K, const int* positions, const float* freq, const int* axis, void* Qr, void* Kr,
+                 int B, int H, int N, int d, int pairs, int axes, int neighbours, int inverse, int dtype, void* hip_stream);
 
 /* Per-kernel timing for benchmarks.  After cottn_profile_start(), every kernel the library
  * launches carries two HIP events of its own (attached to the dispatch, so they mark the

@@ -54,6 +54,7 @@ library_path = os.path.join(_HERE, "libcottn.so")
 COTTN_F32, COTTN_BF16, COTTN_F16 = 0, 1, 2
 OP_FWD_CAUSAL, OP_BWD_CAUSAL, OP_FWD_BIDIR, OP_BWD_BIDIR, OP_STEP, OP_FWD_DECAY, OP_BWD_DECAY = range(7)
 OP_FWD_DECAY_ALONE = 8
+OP_FWD_DELTA, OP_FWD_DELTA_ALONE, OP_BWD_DELTA, OP_BWD_DELTA_SAVED = range(16, 20)
 MOST_DRAFTS = 64  # COTTN_MOST_DRAFTS of include/cottn.h
 
 
@@ -138,7 +139,11 @@ def _load():
                            ("cottn_bwd_causal_decay", [vp] * 15 + [sz, vp, sz] + [i] * 6 + [f, vp]),
                            ("cottn_step_decay", [vp] * 7 + [i, vp, vp] + [i] * 5 + [f, vp]),
                            ("cottn_tree", [vp] * 8 + [i] * 6 + [f, vp]),
-                           ("cottn_tree_accept", [vp] * 6 + [i] * 6 + [f, vp])):
+                           ("cottn_tree_accept", [vp] * 6 + [i] * 6 + [f, vp]),
+                           ("cottn_fwd_causal_delta", [vp] * 11 + [sz] + [i] * 6 + [f, vp]),
+                           ("cottn_bwd_causal_delta", [vp] * 18 + [sz, vp, sz] + [i] * 6 + [f, vp]),
+                           ("cottn_step_delta", [vp] * 8 + [i, vp, vp] + [i] * 5 + [f, vp]),
+                           ("cottn_rotary", [vp] * 7 + [i] * 9 + [vp])):
         call = getattr(lib, name, None)
         if call is not None:
             call.restype, call.argtypes = i, argtypes
@@ -955,6 +960,137 @@ def cottn_tree_accept(k, v, state, parent, last, log_decay=None, eps=1e-6, strea
                                _stream(stream))
     _check(st, "cottn_tree_accept")
     return state
+
+
+def cottn_fwd_causal_delta(Q, K, V, s, log_decay, beta, seq_len=None, state_in=None, O=None, state=None, workspace=None,
+                           eps=1e-6, stream=None):
+    """Attention by the gated delta rule: H_t = g_t (I - beta_t khat_t^T khat_t) H_(t-1) + beta_t khat_t^T v_t, o_t = s_h qhat_t
+    H_t, with g = exp(log_decay); returns O (like V; Q and K may have another width).  log_decay (<= 0, or None: no decay) and
+    beta are float32 [B, H, N].  With seq_len (int32 [B]) a padded batch, and s float32 [B, H], else [H].  state_in, if given, is
+    the state before the first row, and `state` receives that after the last one, both float32 [B, H, d_key, d_value]; they may be
+    one tensor.  workspace: for a backward that takes it over as fwd_workspace, of cottn_workspace_bytes_dkdv(OP_FWD_DELTA, ..)
+    bytes; without one the call allocates what it needs by itself."""
+    B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
+    if O is None:
+        O = torch.empty_like(V)
+    _rows_like(Q, K=K)
+    _rows_like(V, O=O)
+    if seq_len is not None:
+        _check_lengths(seq_len, B, Q.device)
+    _f32("s", s, H if seq_len is None else B * H, Q.device)
+    _f32("log_decay", log_decay, B * H * N, Q.device, optional=True)
+    _f32("beta", beta, B * H * N, Q.device)
+    _f32("state_in", state_in, B * H * dk * dv, Q.device, optional=True)
+    _f32("state", state, B * H * dk * dv, Q.device, optional=True)
+    _on_gpu(Q)
+    workspace, have = _workspace_dkdv(OP_FWD_DELTA_ALONE, B, H, N, dk, dv, 0, dt, Q.device, workspace, stream)
+    st = lib.cottn_fwd_causal_delta(_ptr(Q), _ptr(K), _ptr(V), _ptr(s), _ptr(log_decay), _ptr(beta), _ptr(seq_len),
+                                    _ptr(state_in), _ptr(O), _ptr(state), _ptr(workspace), have, B, H, N, dk, dv, dt, eps,
+                                    _stream(stream))
+    _check(st, "cottn_fwd_causal_delta")
+    return O
+
+
+def cottn_bwd_causal_delta(Q, K, V, s, log_decay, beta, dO, seq_len=None, state_in=None, dstate=None, dQ=None, dK=None, dV=None,
+                           ds=None, dlog_decay=None, dbeta=None, dstate_in=None, workspace=None, eps=1e-6, stream=None,
+                           fwd_workspace=None):
+    """Gradients of cottn_fwd_causal_delta wrt raw Q, K, V, s, log_decay and beta; returns (dQ, dK, dV, ds, dlog_decay, dbeta), ds
+    float32 [H], or [B, H] with seq_len, dlog_decay (None where log_decay is) and dbeta float32 [B, H, N].  state_in as in the
+    forward call; dstate, if given, is the gradient wrt its `state`, and dstate_in receives that wrt its state_in (one tensor is
+    allowed).  fwd_workspace: the workspace tensor of the matching forward call (untouched since), or None."""
+    B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
+    dQ, dK, dV, ds = _grads_dkdv(Q, V, dQ, dK, dV, ds, H if seq_len is None else (B, H))
+    if dbeta is None:
+        dbeta = torch.empty((B, H, N), dtype=torch.float32, device=Q.device)
+    if dlog_decay is None and log_decay is not None:
+        dlog_decay = torch.empty((B, H, N), dtype=torch.float32, device=Q.device)
+    _rows_like(Q, K=K, dQ=dQ, dK=dK)
+    _rows_like(V, dO=dO, dV=dV)
+    if seq_len is not None:
+        _check_lengths(seq_len, B, Q.device)
+    scales = H if seq_len is None else B * H
+    _f32("s", s, scales, Q.device)
+    _f32("ds", ds, scales, Q.device)
+    for name, t in (("log_decay", log_decay), ("dlog_decay", dlog_decay)):
+        _f32(name, t, B * H * N, Q.device, optional=True)
+    _f32("beta", beta, B * H * N, Q.device)
+    _f32("dbeta", dbeta, B * H * N, Q.device)
+    for name, t in (("state_in", state_in), ("dstate", dstate), ("dstate_in", dstate_in)):
+        _f32(name, t, B * H * dk * dv, Q.device, optional=True)
+    _on_gpu(Q)
+    op = OP_BWD_DELTA if fwd_workspace is None else OP_BWD_DELTA_SAVED
+    workspace, have = _workspace_dkdv(op, B, H, N, dk, dv, 0, dt, Q.device, workspace, stream)
+    st = lib.cottn_bwd_causal_delta(_ptr(Q), _ptr(K), _ptr(V), _ptr(s), _ptr(log_decay), _ptr(beta), _ptr(seq_len), _ptr(dO),
+                                    _ptr(state_in), _ptr(dstate), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ds), _ptr(dlog_decay),
+                                    _ptr(dbeta), _ptr(dstate_in), _ptr(fwd_workspace), _bytes(fwd_workspace, Q.device),
+                                    _ptr(workspace), have, B, H, N, dk, dv, dt, eps, _stream(stream))
+    _check(st, "cottn_bwd_causal_delta")
+    return dQ, dK, dV, ds, dlog_decay, dbeta
+
+
+def cottn_step_delta(q, k, v, s, log_decay, beta, state, state_in=None, parent=None, o=None, eps=1e-6, stream=None):
+    """One token of B sequences by the gated delta rule (cottn_fwd_causal_delta); returns o = s_h qhat state (like v).  q, k are
+    [B, H, d_key] and v [B, H, d_value]; log_decay (or None: no decay) and beta float32 [B, H]; state, state_in and parent as in
+    cottn_step_decay."""
+    B, H, dk, dv, dt = _token_widths(q, v, 3, "[B, H, d]")
+    if o is None:
+        o = torch.empty_like(v)
+    _tokens_like(q, k=k)
+    _tokens_like(v, o=o)
+    _f32("s", s, H, q.device)
+    _f32("log_decay", log_decay, B * H, q.device, optional=True)
+    _f32("beta", beta, B * H, q.device)
+    _f32("state", state, B * H * dk * dv, q.device)
+    B_in = B
+    if parent is not None:
+        _indices("parent", parent, (B,), q.device)
+        if state_in is None:
+            raise ValueError("parent needs state_in")
+        if state_in.dim() != 4:
+            raise ValueError("state_in must be [B_in, H, d_key, d_value], got shape %s" % (tuple(state_in.shape),))
+        B_in = state_in.shape[0]
+    if state_in is not None:
+        _f32("state_in", state_in, B_in * H * dk * dv, q.device)
+    _on_gpu(q)
+    st = lib.cottn_step_delta(_ptr(q), _ptr(k), _ptr(v), _ptr(s), _ptr(log_decay), _ptr(beta),
+                              _ptr(state if state_in is None else state_in), _ptr(parent), B_in, _ptr(state), _ptr(o), B, H, dk,
+                              dv, dt, eps, _stream(stream))
+    _check(st, "cottn_step_delta")
+    return o
+
+
+def cottn_rotary(Q, K, positions, freq, axis=None, neighbours=False, inverse=False, Qr=None, Kr=None, stream=None):
+    """Rows of Q and K ([B, H, N, d]; K may be None) turned by where they stand: pair p of a row's features by the angle
+    positions[b, n, axis[p]] * freq[p]; returns (Qr, Kr).  positions: int32 [B, N, axes] (or [B, N]: one axis); freq: float32
+    [pairs], radians to a position; axis: int32 [pairs], or None for the first.  A pair is features 2 p and 2 p + 1 with
+    `neighbours`, else p and p + pairs; features behind 2 pairs are copied.  inverse: turned back, which is the gradient.  Qr may
+    be Q and Kr may be K."""
+    if Q.dim() != 4:
+        raise ValueError("rows must be [B, H, N, d], got shape %s" % (tuple(Q.shape),))
+    B, H, N, d = Q.shape
+    dt = _dtype_code(Q)
+    if K is None and Kr is not None:
+        raise ValueError("Kr needs K")
+    Qr = torch.empty_like(Q) if Qr is None else Qr
+    _rows_like(Q, Qr=Qr)
+    if K is not None:
+        Kr = torch.empty_like(K) if Kr is None else Kr
+        _rows_like(Q, K=K, Kr=Kr)
+    if positions.dim() not in (2, 3):
+        raise ValueError("positions must be [B, N, axes] or [B, N], got shape %s" % (tuple(positions.shape),))
+    axes = 1 if positions.dim() == 2 else positions.shape[2]
+    _indices("positions", positions, (B, N) if positions.dim() == 2 else (B, N, axes), Q.device)
+    if freq.dim() != 1:
+        raise ValueError("freq must be [pairs], got shape %s" % (tuple(freq.shape),))
+    pairs = freq.shape[0]
+    _f32("freq", freq, pairs, Q.device)
+    if axis is not None:
+        _indices("axis", axis, (pairs,), Q.device)
+    _on_gpu(Q)
+    st = lib.cottn_rotary(_ptr(Q), _ptr(K), _ptr(positions), _ptr(freq), _ptr(axis), _ptr(Qr), _ptr(Kr), B, H, N, d, pairs, axes,
+                          int(bool(neighbours)), int(bool(inverse)), dt, _stream(stream))
+    _check(st, "cottn_rotary")
+    return Qr, Kr
 
 
 def profile_start():

@@ -370,6 +370,44 @@ size_t decay_workspace_bytes(int op, int B, int H, int dk, int dv, const DecayPl
   return op != COTTN_OP_BWD_DECAY ? states : 2 * states + round_up_256(size_t(units) * p.G * sizeof(float));
 }
 
+// ---- the gated delta rule: what a workspace holds (launch.h: DeltaArgs), one array after the other
+struct DeltaSpace {
+  size_t W, decays, factors, alone, errors, states, forward;          // a forward's; `alone`, `forward`: bytes of the two kinds
+  size_t zs, dstates, ds_parts, saved;                                // a backward's that is handed one; `saved`: its bytes
+};
+bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, DeltaSpace* p) {
+  if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
+  if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != 64)) return false;
+  const long units = long(B) * H, chunks = (long(N) + 63) / 64;
+  if (!threads_fit(units * std::max<long>(chunks, dv / 16), 256)) return false;
+  const size_t all = size_t(units) * chunks, state = round_up_256(all * dk * dv * 4), rows = round_up_256(all * 64 * dv * 4);
+  p->W = 0;
+  p->decays = p->W + round_up_256(all * 64 * 64 * 4);
+  p->factors = p->decays + round_up_256(all * 64 * 8);
+  p->errors = p->alone = p->factors + round_up_256(all * 64 * 4);
+  p->states = p->errors + rows;
+  p->forward = p->states + state;
+  p->zs = 0;
+  p->dstates = rows;
+  p->ds_parts = p->dstates + state;
+  p->saved = p->ds_parts + round_up_256(all * 4);
+  return true;
+}
+size_t delta_workspace_bytes(int op, const DeltaSpace& p) {
+  return op == COTTN_OP_FWD_DELTA ? p.forward : op == COTTN_OP_FWD_DELTA_ALONE ? p.alone : op == COTTN_OP_BWD_DELTA_SAVED ? p.saved
+                                                                                                         : p.forward + p.saved;
+}
+bool is_delta(int op) { return op >= COTTN_OP_FWD_DELTA && op <= COTTN_OP_BWD_DELTA_SAVED; }
+// the arrays of a forward's workspace at `base`
+void place_delta(DeltaArgs* a, const void* base, const DeltaSpace& p, bool with_states) {
+  char* at = static_cast<char*>(const_cast<void*>(base));
+  a->W = reinterpret_cast<float*>(at + p.W);
+  a->decays = reinterpret_cast<double*>(at + p.decays);
+  a->factors = reinterpret_cast<float*>(at + p.factors);
+  a->errors = with_states ? reinterpret_cast<float*>(at + p.errors) : nullptr;
+  a->states = with_states ? reinterpret_cast<float*>(at + p.states) : nullptr;
+}
+
 // whether n floats at p and m floats at q have one in common
 bool overlap(const float* p, double n, const float* q, double m) {
   const double a = double(reinterpret_cast<uintptr_t>(p)), b = double(reinterpret_cast<uintptr_t>(q));
@@ -464,6 +502,10 @@ size_t cottn_workspace_bytes_dkdv(int op, int B, int H, int N, int dk, int dv, i
     if (!make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan)) return size_t(-1);
     return decay_workspace_bytes(op, B, H, dk, dv, plan);
   }
+  if (is_delta(op)) {
+    DeltaSpace space;
+    return delta_space(B, H, N, dk, dv, chunk, dtype, &space) ? delta_workspace_bytes(op, space) : size_t(-1);
+  }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_STEP) return size_t(-1);
   SeqPlan plan;
   if (!make_plan(op, B, H, N, dk, dv, chunk, dtype, &plan)) return size_t(-1);
@@ -478,6 +520,10 @@ int cottn_segments_dkdv(int op, int B, int H, int N, int dk, int dv, int chunk, 
   if (op == COTTN_OP_FWD_DECAY || op == COTTN_OP_BWD_DECAY || op == COTTN_OP_FWD_DECAY_ALONE) {
     DecayPlan plan;
     return make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan) ? plan.G : 0;
+  }
+  if (is_delta(op)) {   // a sequence is walked from one end to the other
+    DeltaSpace space;
+    return delta_space(B, H, N, dk, dv, chunk, dtype, &space) ? 1 : 0;
   }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_BWD_BIDIR) return 0;
   SeqPlan plan;
@@ -1024,6 +1070,124 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
   a.k = k; a.v = v; a.log_decay = log_decay; a.parent = parent; a.last = last; a.state = state;
   a.B = B; a.H = H; a.n_tokens = T; a.dk = dk; a.dv = dv; a.eps = eps; a.stream = static_cast<hipStream_t>(hip_stream);
   return map_hip(tree_accept_any(a, dtype));
+}
+
+// ---- the gated delta rule -------------------------------------------------------------------------
+int cottn_fwd_causal_delta(const void* Q, const void* K, const void* V, const float* s, const float* log_decay, const float* beta,
+                           const int* seq_len, const float* state_in, void* O, float* state, void* workspace,
+                           size_t workspace_bytes, int B, int H, int N, int dk, int dv, int dtype, float eps, void* hip_stream) {
+  const void* req[] = {s, Q, K, V, O};
+  int st = check_common(req, N == 0 ? 1 : 5, B, H, N, dk, dv, dtype, eps);   // (no rows: tensors without memory)
+  if (st != COTTN_OK) return st;
+  if (beta == nullptr && N > 0) return COTTN_E_NULL;
+  if (!is_aligned(log_decay, 4) || !is_aligned(beta, 4) || !is_aligned(state, 16) || !is_aligned(state_in, 16)) return COTTN_E_ALIGN;
+  const double states = double(B) * H * dk * dv;
+  if (state_in != state && overlap(state_in, states, state, states)) return COTTN_E_ARG;
+  if ((st = check_lengths(seq_len)) != COTTN_OK) return st;
+  DeltaSpace space;
+  if (!delta_space(B, H, N, dk, dv, 0, dtype, &space)) return COTTN_E_SHAPE;
+  if ((st = check_workspace(workspace, workspace_bytes, space.alone)) != COTTN_OK) return st;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (N == 0) {
+    if (state == nullptr || state == state_in) return COTTN_OK;
+    return map_hip(state_in == nullptr ? zero_f32(state, long(states), stream) : copy_state(state, state_in, long(states), stream));
+  }
+  DeltaArgs a{};
+  a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.beta = beta; a.seq_len = seq_len; a.state_in = state_in;
+  a.O = O; a.state = state;
+  place_delta(&a, workspace, space, workspace_bytes >= space.forward);
+  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.eps = eps; a.stream = stream;
+  return map_hip(dtype == COTTN_BF16 ? delta_fwd_bf16(a) : dtype == COTTN_F16 ? delta_fwd_f16(a) : delta_fwd_f32(a));
+}
+
+int cottn_bwd_causal_delta(const void* Q, const void* K, const void* V, const float* s, const float* log_decay, const float* beta,
+                           const int* seq_len, const void* dO, const float* state_in, const float* dstate, void* dQ, void* dK,
+                           void* dV, float* ds, float* dlog_decay, float* dbeta, float* dstate_in, const void* fwd_workspace,
+                           size_t fwd_workspace_bytes, void* workspace, size_t workspace_bytes, int B, int H, int N, int dk,
+                           int dv, int dtype, float eps, void* hip_stream) {
+  const void* req[] = {s, ds, Q, K, V, dO, dQ, dK, dV};
+  int st = check_common(req, N == 0 ? 2 : 9, B, H, N, dk, dv, dtype, eps);
+  if (st != COTTN_OK) return st;
+  if ((beta == nullptr || dbeta == nullptr) && N > 0) return COTTN_E_NULL;
+  if (log_decay == nullptr && dlog_decay != nullptr) return COTTN_E_ARG;
+  if (!is_aligned(log_decay, 4) || !is_aligned(beta, 4) || !is_aligned(dlog_decay, 4) || !is_aligned(dbeta, 4) ||
+      !is_aligned(state_in, 16) || !is_aligned(dstate, 16) || !is_aligned(dstate_in, 16))
+    return COTTN_E_ALIGN;
+  const double states = double(B) * H * dk * dv;
+  if (dstate != dstate_in && overlap(dstate, states, dstate_in, states)) return COTTN_E_ARG;
+  if (overlap(state_in, states, dstate_in, states)) return COTTN_E_ARG;
+  if ((st = check_lengths(seq_len)) != COTTN_OK) return st;
+  DeltaSpace space;
+  if (!delta_space(B, H, N, dk, dv, 0, dtype, &space)) return COTTN_E_SHAPE;
+  const bool saved = fwd_workspace != nullptr;
+  if (saved && (st = check_workspace(fwd_workspace, fwd_workspace_bytes, space.forward)) != COTTN_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, delta_workspace_bytes(saved ? COTTN_OP_BWD_DELTA_SAVED : COTTN_OP_BWD_DELTA, space));
+  if (st != COTTN_OK) return st;
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (N == 0) {
+    hipError_t e = zero_f32(ds, seq_len != nullptr ? long(B) * H : H, stream);
+    if (e == hipSuccess && dstate_in != nullptr && dstate_in != dstate)
+      e = dstate != nullptr ? copy_state(dstate_in, dstate, long(states), stream) : zero_f32(dstate_in, long(states), stream);
+    return map_hip(e);
+  }
+  DeltaArgs a{};
+  a.Q = Q; a.K = K; a.V = V; a.s = s; a.log_decay = log_decay; a.beta = beta; a.seq_len = seq_len; a.state_in = state_in;
+  a.dO = dO; a.dstate = dstate; a.dstate_in = dstate_in;
+  a.dQ = dQ; a.dK = dK; a.dV = dV; a.ds = ds; a.dlog_decay = dlog_decay; a.dbeta = dbeta;
+  a.saved = saved;
+  char* own = static_cast<char*>(workspace);
+  a.zs = reinterpret_cast<float*>(own + space.zs);
+  a.dstates = reinterpret_cast<float*>(own + space.dstates);
+  a.ds_parts = reinterpret_cast<float*>(own + space.ds_parts);
+  place_delta(&a, saved ? fwd_workspace : own + space.saved, space, true);
+  a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.eps = eps; a.stream = stream;
+  return map_hip(dtype == COTTN_BF16 ? delta_bwd_bf16(a) : dtype == COTTN_F16 ? delta_bwd_f16(a) : delta_bwd_f32(a));
+}
+
+int cottn_step_delta(const void* q, const void* k, const void* v, const float* s, const float* log_decay, const float* beta,
+                     const float* state_in, const int* parent, int B_in, float* state, void* o, int B, int H, int dk, int dv,
+                     int dtype, float eps, void* hip_stream) {
+  const void* req[] = {q, k, v, s, state_in, state, o};
+  int st = check_common(req, 7, B, H, 1, dk, dv, dtype, eps);
+  if (st != COTTN_OK) return st;
+  if (beta == nullptr) return COTTN_E_NULL;
+  if (!is_aligned(log_decay, 4) || !is_aligned(beta, 4) || !is_aligned(parent, 4)) return COTTN_E_ALIGN;
+  if (B_in < 1 || (parent == nullptr && B_in != B) || !threads_fit(long(B) * H, 256)) return COTTN_E_SHAPE;
+  const double one = double(H) * dk * dv;
+  if (!(parent == nullptr && state_in == state) && overlap(state_in, B_in * one, state, B * one)) return COTTN_E_ARG;
+  StepDeltaArgs a{};
+  a.step.q = q; a.step.k = k; a.step.v = v; a.step.s = s; a.step.log_decay = log_decay; a.step.from = state_in;
+  a.step.parent = parent; a.step.n_from = B_in; a.step.to = state; a.step.o = o;
+  a.step.B = B; a.step.H = H; a.step.dk = dk; a.step.dv = dv; a.step.eps = eps;
+  a.step.stream = static_cast<hipStream_t>(hip_stream);
+  a.beta = beta;
+  return map_hip(step_delta_any(a, dtype));
+}
+
+// ---- rotary positions -----------------------------------------------------------------------------
+int cottn_rotary(const void* Q, const void* K, const int* positions, const float* freq, const int* axis, void* Qr, void* Kr,
+                 int B, int H, int N, int d, int pairs, int axes, int neighbours, int inverse, int dtype, void* hip_stream) {
+  const void* req[] = {Q, Qr, K, Kr};
+  const bool both = K != nullptr || Kr != nullptr;
+  int st = check_common(req, N == 0 ? 0 : both ? 4 : 2, B, H, N, d, d, dtype, 1.f);
+  if (st != COTTN_OK) return st;
+  if (pairs < 1 || pairs > d / 2 || axes < 1) return COTTN_E_SHAPE;
+  if (freq == nullptr || (positions == nullptr && N > 0)) return COTTN_E_NULL;
+  if (!is_aligned(positions, 4) || !is_aligned(freq, 4) || !is_aligned(axis, 4)) return COTTN_E_ALIGN;
+  if (double(B) * N * d >= 4294967296.0) return COTTN_E_SHAPE;   // threads of a launch: one to a pair of a token at most
+  if (N == 0) return COTTN_OK;
+  const double floats = double(B) * H * N * d * (dtype == COTTN_F32 ? 1.0 : 0.5);
+  const float* in[] = {static_cast<const float*>(Q), static_cast<const float*>(K)};
+  const float* out[] = {static_cast<const float*>(Qr), static_cast<const float*>(Kr)};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j)
+      if (!(i == j && in[i] == out[j]) && overlap(in[i], floats, out[j], floats)) return COTTN_E_ARG;
+  if (overlap(out[0], floats, out[1], floats)) return COTTN_E_ARG;
+  RotaryArgs a{};
+  a.Q = Q; a.K = K; a.positions = positions; a.freq = freq; a.axis = axis; a.Qr = Qr; a.Kr = Kr;
+  a.B = B; a.H = H; a.N = N; a.d = d; a.pairs = pairs; a.axes = axes; a.neighbours = neighbours != 0; a.inverse = inverse != 0;
+  a.stream = static_cast<hipStream_t>(hip_stream);
+  return map_hip(rotary_any(a, dtype));
 }
 
 int cottn_profile_start(void) {

@@ -1,0 +1,249 @@
+// What the kernels of the gated delta rule share.  With qh, kh the normalised rows, g_t = exp(log_decay_t) and b_t = beta_t
+//     H_t = g_t (I - b_t kh_t^T kh_t) H_(t-1) + b_t kh_t^T v_t,    o_t = s qh_t H_t.
+//
+// A chunk takes 64 rows; G_i is the product of the decays from its first row to row i, H the state before it and
+//     A_ij = (G_i / G_j) kh_i . kh_j  for j < i, else 0,      P_ij = (G_i / G_j) qh_i . kh_j  for j <= i, else 0,
+//     W = A (I + b A)^-1, strictly lower: what row j's value leaves in row i's prediction after the rows between took theirs
+// With the rows' factors b as diagonal matrices and D the gradient with respect to the state behind the chunk:
+//     Y = V - G Kh H,  E = Y - W b Y,  U = b E,  O = s (G Qh H + P U),  H <- G_n H + (G_n/G Kh)^T U
+//     dO' = s dO,  F = P^T dO' + (G_n/G) Kh D,  Z = F - W^T b F,  X = b Z,  D <- G_n D + (G Qh)^T dO' - (G Kh)^T X
+//     dV = X,  db_i = z_i . e_i,  p_ij = (G_i/G_j) dO'_i . u_j (j <= i),  a_ij = -(G_i/G_j) x_i . u_j (j < i)
+//     dQh = G dO' H^T + p Kh,   dKh = (G_n/G) U D^T - G X H^T + p^T Qh + (a + a^T) Kh
+//     d log g_t = <D, H behind the chunk> + sum over i >= t of (qh_i . dqh_i - x_i . v_i),   ds = sum of qh_i . dqh_i / s
+// (E is the error of a row's prediction; neither b nor a decay is ever divided by.)  W's entries are products of rows with
+// contractions, at most 1 in magnitude for 0 <= b <= 2.  Every decay that is formed has an exponent that is not positive.
+//
+// Precision.  Products take bfloat16 parts of their operands, each part the rest that rounding the ones before left over:
+// bfloat16 rows are one part, fp16 rows two and fp32 rows three, exactly; what is computed takes as many parts as its results
+// need.  Of the products of parts those i + j < LEVEL are formed: LEVEL 3 leaves out less than 2^-24 of a product, LEVEL 2 less
+// than 2^-15.  States, the error rows and gradients of gates are fp32 results and take 3; results in 16 bits alone take 2, so
+// that an element has met one rounding that counts, its own.
+//
+// Included behind device_common.h.
+#pragma once
+
+namespace cottn {
+namespace {
+
+using namespace COTTN_NS;
+
+constexpr int CHUNK = 64;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+
+template <typename T> struct Rows;
+template <> struct Rows<__bf16> { static constexpr int PARTS = 1; };
+template <> struct Rows<_Float16> { static constexpr int PARTS = 2; };
+template <> struct Rows<float> { static constexpr int PARTS = 3; };
+// parts of operands that only enter results of the rows' type
+template <typename T> constexpr int RESULT_LEVEL = sizeof(T) == 4 ? 3 : 2;
+
+// Four values as N parts, two to a word.
+template <int N>
+__device__ __forceinline__ void split4(f32x4 x, uint2 (&parts)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    parts[i] = uint2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    if (i + 1 < N) {
+      float p[4];
+      unpack2(parts[i].x, p[0], p[1]);
+      unpack2(parts[i].y, p[2], p[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] -= p[e];
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void split8(f32x4 lo, f32x4 hi, bf16x8 (&parts)[N]) {
+  uint2 a[N], b[N];
+  split4<N>(lo, a);
+  split4<N>(hi, b);
+#pragma unroll
+  for (int i = 0; i < N; ++i) parts[i] = __builtin_bit_cast(bf16x8, u32x4{a[i].x, a[i].y, b[i].x, b[i].y});
+}
+
+// The values that parts stand for.
+template <int N>
+__device__ __forceinline__ void join8(const bf16x8 (&parts)[N], f32x4& lo, f32x4& hi) {
+  lo = hi = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = N - 1; i >= 0; --i) {
+    const u32x4 w = __builtin_bit_cast(u32x4, parts[i]);
+    float a, b;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      unpack2(w[e], a, b);
+      lo[2 * e] += a;
+      lo[2 * e + 1] += b;
+      unpack2(w[2 + e], a, b);
+      hi[2 * e] += a;
+      hi[2 * e + 1] += b;
+    }
+  }
+}
+
+// acc (16 x 16) += a (16 x 32) b (32 x 16), the smallest products of parts first.
+template <int LEVEL, int NA, int NB>
+__device__ __forceinline__ f32x4 mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB], f32x4 acc) {
+#pragma unroll
+  for (int sum = LEVEL - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      const int j = sum - i;
+      if (j >= 0 && j < NB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc, 0, 0, 0);
+    }
+  return acc;
+}
+
+// Eight consecutive elements of a row as they lie in memory, as fp32 and as parts.
+template <typename T>
+struct Raw8 {
+  static constexpr int PIECES = sizeof(T) / 2, PARTS = Rows<T>::PARTS;
+  u32x4 w[PIECES];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
+  }
+  __device__ __forceinline__ void values(f32x4& lo, f32x4& hi) const {
+    if constexpr (sizeof(T) == 4) {
+      lo = __builtin_bit_cast(f32x4, w[0]);
+      hi = __builtin_bit_cast(f32x4, w[PIECES - 1]);
+    } else {
+      typedef __attribute__((ext_vector_type(8))) T vec8;
+      const vec8 x = __builtin_bit_cast(vec8, w[0]);
+      lo = f32x4{float(x[0]), float(x[1]), float(x[2]), float(x[3])};
+      hi = f32x4{float(x[4]), float(x[5]), float(x[6]), float(x[7])};
+    }
+  }
+  __device__ __forceinline__ void parts(bf16x8 (&p)[PARTS]) const {
+    if constexpr (PARTS == 1) {
+      p[0] = __builtin_bit_cast(bf16x8, w[0]);
+    } else {
+      f32x4 lo, hi;
+      values(lo, hi);
+      split8<PARTS>(lo, hi, p);
+    }
+  }
+  __device__ __forceinline__ float sum_sq() const {
+    f32x4 lo, hi;
+    values(lo, hi);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_fmaf(lo[i], lo[i], __builtin_fmaf(hi[i], hi[i], s));
+    return s;
+  }
+};
+
+// A tile of 16-bit parts in LDS: plane after plane of ROWS rows, each PITCH wide.
+// (Rows 16 apart from a multiple of 32 are read fastest, device_common.h; 8 where the LDS has no room for that.)
+template <int ROWS, int COLS, int PARTS, int PAD = 16>
+struct PartTile {
+  static constexpr int PITCH = COLS + PAD, PLANE = ROWS * PITCH, SIZE = PARTS * PLANE;
+  // operand fragment whose k slots are columns c .. c + 7 of a row
+  template <int N = PARTS>
+  static __device__ __forceinline__ void row_frag(const uint16_t* tile, int row, int c, bf16x8 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(tile + i * PLANE + row * PITCH + c));
+  }
+  // columns c .. c + 3 and c + 16 .. c + 19 of a row: the slot order of two accumulator tiles side by side
+  template <int N = PARTS>
+  static __device__ __forceinline__ void row_frag_pairs(const uint16_t* tile, int row, int c, bf16x8 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint16_t* p = tile + i * PLANE + row * PITCH + c;
+      const uint2 lo = *reinterpret_cast<const uint2*>(p), hi = *reinterpret_cast<const uint2*>(p + 16);
+      f[i] = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+    }
+  }
+  // operand fragment whose k slots are rows r0 .. r0 + 3 and r1 .. r1 + 3 of column col0 + r
+  template <int N = PARTS>
+  static __device__ __forceinline__ void col_frag(const uint16_t* tile, int r0, int r1, int col0, int r, bf16x8 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = __builtin_bit_cast(bf16x8, lds_col_frag(tile + i * PLANE, PITCH, r0, r1, col0, r));
+  }
+  template <int N = PARTS>
+  static __device__ __forceinline__ void store4(uint16_t* tile, int row, int c, f32x4 x) {
+    uint2 p[N];
+    split4<N>(x, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<uint2*>(tile + i * PLANE + row * PITCH + c) = p[i];
+  }
+  template <int N>
+  static __device__ __forceinline__ void store8(uint16_t* tile, int row, int c, const bf16x8 (&p)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(tile + i * PLANE + row * PITCH + c) = __builtin_bit_cast(u32x4, p[i]);
+  }
+};
+
+// 64 rows of D elements on their way from memory to LDS, 256 threads: D / 8 neighbouring lanes share a row.
+template <typename T, int D, int PAD = 16>
+struct RowTile {
+  static constexpr int LPR = D / 8, RPP = 256 / LPR, PASSES = RPP < CHUNK ? CHUNK / RPP : 1, PARTS = Rows<T>::PARTS;
+  using Tile = PartTile<CHUNK, D, PARTS, PAD>;
+  Raw8<T> raw[PASSES];
+  static __device__ __forceinline__ int row(int p) { return p * RPP + int(threadIdx.x) / LPR; }
+  static __device__ __forceinline__ int col() { return int(threadIdx.x) % LPR * 8; }
+  static __device__ __forceinline__ bool in(int p) { return RPP <= CHUNK || row(p) < CHUNK; }   // (all threads take part)
+  // rows from row0 on, LD elements apart; those from `end` on are zeros
+  __device__ __forceinline__ void fetch(const T* base, int row0, int end, int ld = D) {
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      raw[p].zero();
+      if (in(p) && row0 + row(p) < end) raw[p].load(base + size_t(row0 + row(p)) * ld + col());
+    }
+  }
+  __device__ __forceinline__ void commit(uint16_t* tile) const {
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      bf16x8 x[PARTS];
+      raw[p].parts(x);
+      if (in(p)) Tile::store8(tile, row(p), col(), x);
+    }
+  }
+  // out[row] = 1 / max(|row|, eps)
+  __device__ __forceinline__ void store_factors(float* out, float eps) const {
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const float f = inv_norm(group_sum<LPR>(raw[p].sum_sq()), eps);
+      if (in(p) && threadIdx.x % LPR == 0) out[row(p)] = f;
+    }
+  }
+};
+
+// Decays as logarithms to base 2, in 64 bits: 64 of them are added up and differences of those sums taken, and a token that
+// forgets everything must not cost the ones behind it their accuracy.  What is below fp32's least number counts as 2^-256.
+__device__ __forceinline__ double log2_decay(float log_decay) {
+  return log_decay > 0.f ? 0.0 : log_decay < -128.f ? -256.0 : 1.4426950408889634 * double(log_decay);
+}
+__device__ __forceinline__ float decay_between(double later, double earlier) {
+  return __builtin_amdgcn_exp2f(float(later - earlier));
+}
+// What a state is multiplied by: x times + x plus, with a factor just below 1 as 1 - d and d's own fp32 accuracy.
+struct StateFactor {
+  float times, plus;
+  __device__ __forceinline__ explicit StateFactor(double l2) {
+    const float d = -expm1f(float(0.6931471805599453 * l2));
+    times = d < 0.5f ? 1.f : __builtin_amdgcn_exp2f(float(l2));
+    plus = d < 0.5f ? -d : 0.f;
+  }
+  __device__ __forceinline__ float of(float x) const { return __builtin_fmaf(x, plus, x * times); }
+};
+
+// The 16 x 16 tiles of a DK x VC part of a state that each of four waves holds: keys down, values along.
+template <int DK, int VC>
+struct StateTiles {
+  static constexpr int RT = DK / 16, CT = VC / 16;
+  static constexpr int NR = RT >= 4 ? RT / 4 : 1, NC = RT >= 4 ? CT : CT >= 2 ? CT / 2 : 1;
+  static __device__ __forceinline__ bool active(int w) { return RT >= 4 || CT >= 2 || w < 2; }
+  static __device__ __forceinline__ int row_tile(int w, int x) { return RT >= 4 ? w * NR + x : w % 2; }
+  static __device__ __forceinline__ int col_tile(int w, int y) { return RT >= 4 ? y : w / 2 * NC + y; }
+};
+
+// Chunks of a unit in the workspace.
+__host__ __device__ constexpr int delta_chunks(int N) { return (N + CHUNK - 1) / CHUNK; }
+
+}  // namespace
+}  // namespace cottn

@@ -1,0 +1,3 @@
+// The kernels of delta_prepare_bf16.hip for rows in fp32.
+#define COTTN_DELTA_F32
+#include "delta_prepare_bf16.hip"

@@ -290,6 +290,12 @@ struct StepDecayArgs {
   hipStream_t stream;
 };
 
+// One token by the gated delta rule: log_decay (null: none) and beta [B][H].
+struct StepDeltaArgs {
+  StepDecayArgs step;
+  const float* beta;
+};
+
 // A tree of n_tokens <= 64 drafted tokens for each sequence: q, k [B][H][n_tokens][dk], v, o [B][H][n_tokens][dv], parent
 // int[B][n_tokens]; accepting takes last int[B] and no q, s, o.
 struct TreeArgs {
@@ -297,6 +303,36 @@ struct TreeArgs {
   const int* parent; const int* last; float* state; void* o;
   int B, H, n_tokens, dk, dv;
   float eps;
+  hipStream_t stream;
+};
+
+// The gated delta rule (delta.h), forward and backward.  Chunks are of 64 rows; per (batch, head) and chunk the workspace has
+// W [64][64], decays (from the chunk's start, logarithms to base 2) and factors (1 / norm of K's rows) [64]; for a backward
+// errors E [64][dv] and the state before the chunk [dk][dv]; and of the backward itself Z [64][dv] and the gradient with respect
+// to the state behind the chunk [dk][dv].
+struct DeltaArgs {
+  const void* Q; const void* K; const void* V; const float* s; const float* log_decay; const float* beta;   // log_decay may be null
+  const int* seq_len;               // null, or int[B] row counts: then s and ds are [B][H]
+  const float* state_in;            // may be null
+  void* O; float* state;            // forward: results (state may be null); backward: no O, and only errors and states are formed
+  float* W; double* decays; float* factors;
+  float* errors; float* states;     // forward: may be null
+  // backward
+  const void* dO; const float* dstate; float* dstate_in;   // the two states may be null
+  void* dQ; void* dK; void* dV; float* ds; float* dlog_decay; float* dbeta;   // dlog_decay may be null
+  float* zs; float* dstates; float* ds_parts;   // workspace
+  bool saved;                       // W, decays, factors, errors and states are a forward's
+  int B, H, N, dk, dv;
+  float eps;
+  hipStream_t stream;
+};
+
+// Rows turned by their positions (rotary.hip): of Q and, where there is one, of K.
+struct RotaryArgs {
+  const void* Q; const void* K; const int* positions; const float* freq; const int* axis;   // K, axis may be null
+  void* Qr; void* Kr;
+  int B, H, N, d, pairs, axes;
+  bool neighbours, inverse;
   hipStream_t stream;
 };
 
@@ -335,6 +371,17 @@ hipError_t tree_bf16(const TreeArgs& a);
 hipError_t tree_f16(const TreeArgs& a);
 hipError_t tree_f32w(const TreeArgs& a);
 hipError_t tree_accept_any(const TreeArgs& a, int dtype);
+hipError_t delta_prepare_bf16(const DeltaArgs& a);
+hipError_t delta_prepare_f16(const DeltaArgs& a);
+hipError_t delta_prepare_f32(const DeltaArgs& a);
+hipError_t delta_fwd_bf16(const DeltaArgs& a);
+hipError_t delta_fwd_f16(const DeltaArgs& a);
+hipError_t delta_fwd_f32(const DeltaArgs& a);
+hipError_t delta_bwd_bf16(const DeltaArgs& a);
+hipError_t delta_bwd_f16(const DeltaArgs& a);
+hipError_t delta_bwd_f32(const DeltaArgs& a);
+hipError_t step_delta_any(const StepDeltaArgs& a, int dtype);
+hipError_t rotary_any(const RotaryArgs& a, int dtype);
 
 // small fp32 state kernels shared by all element types (defined next to their kernels)
 hipError_t launch_fwd_state_carry(float* seg_state, int units, int G, int elems, hipStream_t st);

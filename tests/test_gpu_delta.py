@@ -1,0 +1,233 @@
+"""GPU parity of the gated delta rule, forward and backward, against 64 bits."""
+import itertools
+
+import pytest
+import torch
+
+import delta_reference as ref
+from delta_reference import TYPES, check
+
+pytestmark = pytest.mark.gpu
+WIDTHS = list(itertools.product((32, 64, 128), repeat=2))
+
+
+@pytest.fixture(scope="module")
+def cottn():
+    import paper_2409_18747_amd.binding as b
+    yield b
+
+
+def draw(B, H, N, dk, dv, dtype, seed, per_unit=False, strong=False):
+    """Inputs as a model has them: keys with a mean of their own, gates between nothing and all; fp32 and `dtype` as stored."""
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g)   # noqa: E731
+    x = {"Q": r(B, H, N, dk), "K": r(B, H, N, dk) + 0.5 * r(1, H, 1, dk), "V": r(B, H, N, dv)}
+    x = {k: v.to(TYPES[dtype]) for k, v in x.items()}
+    x["s"] = (r(B, H) if per_unit else r(H)).abs() + 0.5
+    x["log_decay"] = -torch.exp(torch.linspace(-6.0, 2.5 if strong else 0.0, H))[None, :, None] * r(B, H, N).abs()
+    x["beta"] = torch.sigmoid(2 * r(B, H, N))
+    more = {"dO": r(B, H, N, dv).to(TYPES[dtype]), "state_in": r(B, H, dk, dv), "dstate": r(B, H, dk, dv)}
+    return x, more
+
+
+def double(x):
+    return {k: v.double() for k, v in x.items()}
+
+
+def cuda(x):
+    return {k: v.cuda() for k, v in x.items()}
+
+
+def train_workspace(cottn, x):
+    B, H, N, dk = x["Q"].shape
+    code = {torch.bfloat16: cottn.COTTN_BF16, torch.float16: cottn.COTTN_F16, torch.float32: cottn.COTTN_F32}[x["Q"].dtype]
+    n = cottn.cottn_workspace_bytes_dkdv(cottn.OP_FWD_DELTA, B, H, N, dk, x["V"].shape[-1], 0, code)
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def run_both(cottn, x, more, dtype, lens=None, states=True, off=0.0):
+    want_O, want_S = ref.forward(**double(x), lens=lens, state_in=more["state_in"].double() if states else None)
+    want = ref.gradients(**double(x), dO=more["dO"].double(), lens=lens, state_in=more["state_in"].double() if states else None,
+                         dstate=more["dstate"].double() if states else None)
+    d, m = cuda(x), cuda(more)
+    seq_len = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = train_workspace(cottn, d)
+    state = torch.empty_like(m["state_in"]) if states else None
+    dstate_in = torch.empty_like(m["state_in"]) if states else None
+    O = cottn.cottn_fwd_causal_delta(**d, seq_len=seq_len, state_in=m["state_in"] if states else None, state=state, workspace=ws)
+    got = cottn.cottn_bwd_causal_delta(**d, dO=m["dO"], seq_len=seq_len, state_in=m["state_in"] if states else None,
+                                       dstate=m["dstate"] if states else None, dstate_in=dstate_in, fwd_workspace=ws)
+    torch.cuda.synchronize()
+    check("O", O, want_O, dtype, more=off)
+    if states:
+        check("state", state, want_S, None, more=off)
+        check("dstate_in", dstate_in, want["dstate_in"], None, more=off)
+    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
+        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None, more=off)
+    return d, m, O, state, got
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dk,dv", WIDTHS)
+def test_forward_and_backward(cottn, dtype, dk, dv):
+    x, more = draw(2, 3, 150, dk, dv, dtype, dk + dv)
+    run_both(cottn, x, more, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 33, 63, 64, 65, 128, 191, 300])
+def test_lengths_of_a_sequence(cottn, dtype, N):
+    x, more = draw(1, 2, N, 64, 32, dtype, N)
+    run_both(cottn, x, more, dtype, states=N % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_padded_batch(cottn, dtype):
+    lens = [0, 1, 64, 65, 130, 129]
+    x, more = draw(6, 2, 130, 64, 64, dtype, 5, per_unit=True)
+    for b, n in enumerate(lens):   # what stands behind a sequence is not read
+        for t in (x["Q"], x["K"], x["V"], more["dO"], x["log_decay"], x["beta"]):
+            t[b, :, n:] = float("nan")
+    d, m, O, state, got = run_both_padded(cottn, x, more, dtype, lens)
+    for t in (O,) + tuple(got[:3]) + tuple(got[4:]):
+        for b, n in enumerate(lens):
+            assert not t[b, :, n:].any()
+
+
+def run_both_padded(cottn, x, more, dtype, lens):
+    clean = {k: torch.nan_to_num(v) for k, v in x.items()}
+    more_clean = {k: torch.nan_to_num(v) for k, v in more.items()}
+    want_O, want_S = ref.forward(**double(clean), lens=lens, state_in=more["state_in"].double())
+    want = ref.gradients(**double(clean), dO=more_clean["dO"].double(), lens=lens, state_in=more["state_in"].double(),
+                         dstate=more["dstate"].double())
+    d, m = cuda(x), cuda(more)
+    seq_len = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = train_workspace(cottn, d)
+    state, dstate_in = torch.empty_like(m["state_in"]), torch.empty_like(m["state_in"])
+    O = cottn.cottn_fwd_causal_delta(**d, seq_len=seq_len, state_in=m["state_in"], state=state, workspace=ws)
+    got = cottn.cottn_bwd_causal_delta(**d, dO=m["dO"], seq_len=seq_len, state_in=m["state_in"], dstate=m["dstate"],
+                                       dstate_in=dstate_in, fwd_workspace=ws)
+    check("O", O, want_O, dtype)
+    check("state", state, want_S, None)
+    check("dstate_in", dstate_in, want["dstate_in"], None)
+    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
+        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None)
+    return d, m, O, state, got
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(32, 32), (64, 64), (128, 128), (128, 64)])
+def test_forward_alone(cottn, dtype, dk, dv):
+    x, _ = draw(2, 2, 200, dk, dv, dtype, 7)
+    want, _ = ref.forward(**double(x))
+    check("O", cottn.cottn_fwd_causal_delta(**cuda(x)), want, dtype, two_parts=dtype != "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_decay(cottn, dtype):
+    x, more = draw(2, 3, 100, 64, 64, dtype, 8)
+    none = {**double(x), "log_decay": torch.zeros_like(x["log_decay"]).double()}
+    want_O, _ = ref.forward(**none)
+    want = ref.gradients(**none, dO=more["dO"].double())
+    d = {**cuda(x), "log_decay": None}
+    O = cottn.cottn_fwd_causal_delta(**d)
+    got = cottn.cottn_bwd_causal_delta(**d, dO=more["dO"].cuda())
+    assert got[4] is None
+    check("O", O, want_O, dtype, two_parts=True)
+    for name, t in zip(("dQ", "dK", "dV", "ds"), got):
+        check(name, t, want[name], dtype if name != "ds" else None)
+    check("dbeta", got[5], want["dbeta"], None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strong_decays(cottn, dtype):
+    """Tokens that forget everything, -inf among them, between ones that forget little; above 0 counts as 0."""
+    x, more = draw(2, 4, 140, 64, 32, dtype, 9, strong=True)
+    x["log_decay"][0, 1, 5::17] = -float("inf")
+    x["log_decay"][0, 2, 3::11] = -1000.0
+    x["log_decay"][1, 3, ::7] = 0.5
+    clean = dict(x)
+    clean["log_decay"] = x["log_decay"].clamp(min=-500.0, max=0.0)   # (exp(-500) is 0 beside anything here)
+    want_O, want_S = ref.forward(**double(clean), state_in=more["state_in"].double())
+    want = ref.gradients(**double(clean), dO=more["dO"].double(), state_in=more["state_in"].double())
+    want["dlog_decay"] = torch.where((x["log_decay"] > 0.0) | (x["log_decay"] < -128.0), 0.0, want["dlog_decay"])
+    d, m = cuda(x), cuda(more)
+    state = torch.empty_like(m["state_in"])
+    O = cottn.cottn_fwd_causal_delta(**d, state_in=m["state_in"], state=state)
+    got = cottn.cottn_bwd_causal_delta(**d, dO=m["dO"], state_in=m["state_in"])
+    check("O", O, want_O, dtype)
+    check("state", state, want_S, None)
+    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
+        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None)
+
+
+@pytest.mark.parametrize("beta", [0.0, 1.0, 2.0])
+def test_keys_alike(cottn, beta):
+    """The same key for all tokens, the hardest case for the triangular system: with beta 1 a token replaces the one before, with
+    beta 2 it is reflected.
+    With beta 2 nothing contracts: a token multiplies what the state holds along the key by 1 - 2 |kh|^2.  The key's factor is
+    off by a square root and a division, 2^-24 of it, and a sum's last roundings, half of that again, the same for all tokens, so
+    that |kh|^2 is 1 + 3 2^-24 at worst, the factor -(1 + 6 2^-24), and after 130 tokens 780 2^-24 are added up."""
+    x, more = draw(1, 2, 130, 64, 64, "f32", 10)
+    x["K"][:] = x["K"][:, :, :1]
+    x["beta"].fill_(beta)
+    x["log_decay"].zero_()
+    run_both(cottn, x, more, "f32", off=780 * 2.0 ** -24 if beta == 2.0 else 0.0)
+
+
+def test_rows_of_zeros_and_short_rows(cottn):
+    x, more = draw(1, 2, 70, 32, 64, "f32", 11)
+    x["K"][:, :, 3] = 0.0
+    x["Q"][:, :, 4] = 0.0
+    x["K"][:, :, 5] *= 1e-8
+    x["Q"][:, :, 6] *= 1e-8
+    d, m = cuda(x), cuda(more)
+    want_O, _ = ref.forward(**double(x))
+    want = ref.gradients(**double(x), dO=more["dO"].double())
+    O = cottn.cottn_fwd_causal_delta(**d)
+    dQ, dK = cottn.cottn_bwd_causal_delta(**d, dO=m["dO"])[:2]
+    check("O", O, want_O, "f32")
+    for got, w, rows in ((dQ, want["dQ"], (4, 6)), (dK, want["dK"], (3, 5))):   # rows below eps: gradients over eps
+        far = torch.zeros(70, dtype=torch.bool)
+        far[list(rows)] = True
+        check("below eps", got[:, :, far], w[:, :, far], "f32")
+        check("the others", got[:, :, ~far], w[:, :, ~far], "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pieces_are_the_whole(cottn, dtype):
+    """A sequence in three pieces, forward first to last in place of its state, backward last to first."""
+    x, more = draw(2, 2, 210, 64, 64, dtype, 12)
+    want_O, want_S = ref.forward(**double(x), state_in=more["state_in"].double())
+    want = ref.gradients(**double(x), dO=more["dO"].double(), state_in=more["state_in"].double(), dstate=more["dstate"].double())
+    d, m = cuda(x), cuda(more)
+    cuts = [(0, 100), (100, 101), (101, 210)]
+    part = lambda t, c: t[:, :, c[0]:c[1]].contiguous()   # noqa: E731
+    pieces = [{k: part(v, c) if k != "s" else v for k, v in d.items()} for c in cuts]
+    state, before, O, spaces = m["state_in"].clone(), [], [], []
+    for p in pieces:
+        before.append(state.clone())
+        spaces.append(train_workspace(cottn, p))
+        O.append(cottn.cottn_fwd_causal_delta(**p, state_in=state, state=state, workspace=spaces[-1]))
+    check("O", torch.cat(O, 2), want_O, dtype)
+    check("state", state, want_S, None)
+    D, grads = m["dstate"].clone(), []
+    for i in (2, 1, 0):
+        grads.insert(0, cottn.cottn_bwd_causal_delta(**pieces[i], dO=part(m["dO"], cuts[i]), state_in=before[i], dstate=D, dstate_in=D,
+                                                     fwd_workspace=spaces[i] if i != 1 else None))
+    check("dstate_in", D, want["dstate_in"], None)
+    check("ds", sum(g[3] for g in grads), want["ds"], None)
+    for i, name in ((0, "dQ"), (1, "dK"), (2, "dV"), (4, "dlog_decay"), (5, "dbeta")):
+        check(name, torch.cat([g[i] for g in grads], 2), want[name], dtype if i < 3 else None)
+
+
+def test_no_rows(cottn):
+    S = torch.randn(2, 3, 32, 64, device="cuda")
+    rows = lambda d: torch.empty(2, 3, 0, d, device="cuda")   # noqa: E731
+    gates = torch.empty(2, 3, 0, device="cuda")
+    s, state = torch.ones(3, device="cuda"), torch.empty_like(S)
+    O = cottn.cottn_fwd_causal_delta(rows(32), rows(32), rows(64), s, gates, gates, state_in=S, state=state)
+    assert O.shape == (2, 3, 0, 64) and torch.equal(state, S)
+    D = torch.empty_like(S)
+    got = cottn.cottn_bwd_causal_delta(rows(32), rows(32), rows(64), s, gates, gates, rows(64), state_in=S, dstate=S, dstate_in=D)
+    assert torch.equal(D, S) and not got[3].any() and got[5].shape == (2, 3, 0)
