@@ -372,7 +372,7 @@ size_t decay_workspace_bytes(int op, int B, int H, int dk, int dv, const DecayPl
 
 // ---- the gated delta rule: what a workspace holds (launch.h: DeltaArgs), one array after the other
 struct DeltaSpace {
-  size_t W, decays, factors, alone, errors, states, forward;          // a forward's; `alone`, `forward`: bytes of the two kinds
+  size_t records, w_rows, alone, w_cols, errors, states, forward;      // a forward's; `alone`, `forward`: bytes of the two kinds
   size_t zs, dstates, ds_parts, saved;                                // a backward's that is handed one; `saved`: its bytes
 };
 bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, DeltaSpace* p) {
@@ -381,10 +381,10 @@ bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, Delt
   const long units = long(B) * H, chunks = (long(N) + 63) / 64;
   if (!threads_fit(units * std::max<long>(chunks, dv / 16), 256)) return false;
   const size_t all = size_t(units) * chunks, state = round_up_256(all * dk * dv * 4), rows = round_up_256(all * 64 * dv * 4);
-  p->W = 0;
-  p->decays = p->W + round_up_256(all * 64 * 64 * 4);
-  p->factors = p->decays + round_up_256(all * 64 * 8);
-  p->errors = p->alone = p->factors + round_up_256(all * 64 * 4);
+  p->records = 0;
+  p->w_rows = round_up_256(all * DELTA_RECORD_BYTES);
+  p->w_cols = p->alone = p->w_rows + all * DELTA_W_BYTES;
+  p->errors = p->w_cols + all * DELTA_W_BYTES;
   p->states = p->errors + rows;
   p->forward = p->states + state;
   p->zs = 0;
@@ -401,9 +401,9 @@ bool is_delta(int op) { return op >= COTTN_OP_FWD_DELTA && op <= COTTN_OP_BWD_DE
 // the arrays of a forward's workspace at `base`
 void place_delta(DeltaArgs* a, const void* base, const DeltaSpace& p, bool with_states) {
   char* at = static_cast<char*>(const_cast<void*>(base));
-  a->W = reinterpret_cast<float*>(at + p.W);
-  a->decays = reinterpret_cast<double*>(at + p.decays);
-  a->factors = reinterpret_cast<float*>(at + p.factors);
+  a->records = at + p.records;
+  a->w_rows = reinterpret_cast<unsigned short*>(at + p.w_rows);
+  a->w_cols = with_states ? reinterpret_cast<unsigned short*>(at + p.w_cols) : nullptr;
   a->errors = with_states ? reinterpret_cast<float*>(at + p.errors) : nullptr;
   a->states = with_states ? reinterpret_cast<float*>(at + p.states) : nullptr;
 }

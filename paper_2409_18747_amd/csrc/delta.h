@@ -178,6 +178,9 @@ struct PartTile {
   }
 };
 
+// 1 / max(norm, eps) of a row from its sum of squares, to a unit of fp32.
+__device__ __forceinline__ float row_factor(float sum_sq, float inv_eps) { return fminf(__builtin_amdgcn_rsqf(sum_sq), inv_eps); }
+
 // 64 rows of D elements on their way from memory to LDS, 256 threads: D / 8 neighbouring lanes share a row.
 template <typename T, int D, int PAD = 16>
 struct RowTile {
@@ -187,12 +190,18 @@ struct RowTile {
   static __device__ __forceinline__ int row(int p) { return p * RPP + int(threadIdx.x) / LPR; }
   static __device__ __forceinline__ int col() { return int(threadIdx.x) % LPR * 8; }
   static __device__ __forceinline__ bool in(int p) { return RPP <= CHUNK || row(p) < CHUNK; }   // (all threads take part)
-  // rows from row0 on, LD elements apart; those from `end` on are zeros
-  __device__ __forceinline__ void fetch(const T* base, int row0, int end, int ld = D) {
+  // the first `rows` rows from `base` on, LD elements apart; zeros behind them
+  __device__ __forceinline__ void fetch(const T* base, int rows, int ld = D) {
+    const unsigned lane = unsigned((int(threadIdx.x) / LPR) * ld + col());
+    if (RPP <= CHUNK && rows >= CHUNK) {
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) raw[p].load(base + p * RPP * ld + lane);
+      return;
+    }
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       raw[p].zero();
-      if (in(p) && row0 + row(p) < end) raw[p].load(base + size_t(row0 + row(p)) * ld + col());
+      if (in(p) && row(p) < rows) raw[p].load(base + p * RPP * ld + lane);
     }
   }
   __device__ __forceinline__ void commit(uint16_t* tile) const {
@@ -204,10 +213,10 @@ struct RowTile {
     }
   }
   // out[row] = 1 / max(|row|, eps)
-  __device__ __forceinline__ void store_factors(float* out, float eps) const {
+  __device__ __forceinline__ void store_factors(float* out, float inv_eps) const {
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-      const float f = inv_norm(group_sum<LPR>(raw[p].sum_sq()), eps);
+      const float f = row_factor(group_sum<LPR>(raw[p].sum_sq()), inv_eps);
       if (in(p) && threadIdx.x % LPR == 0) out[row(p)] = f;
     }
   }
@@ -222,24 +231,47 @@ __device__ __forceinline__ float decay_between(double later, double earlier) {
   return __builtin_amdgcn_exp2f(float(later - earlier));
 }
 // What a state is multiplied by: x times + x plus, with a factor just below 1 as 1 - d and d's own fp32 accuracy.
-struct StateFactor {
-  float times, plus;
-  __device__ __forceinline__ explicit StateFactor(double l2) {
-    const float d = -expm1f(float(0.6931471805599453 * l2));
-    times = d < 0.5f ? 1.f : __builtin_amdgcn_exp2f(float(l2));
-    plus = d < 0.5f ? -d : 0.f;
-  }
-  __device__ __forceinline__ float of(float x) const { return __builtin_fmaf(x, plus, x * times); }
-};
+__device__ __forceinline__ void state_factor(double l2, float& times, float& plus) {
+  const float d = -expm1f(float(0.6931471805599453 * l2));
+  times = d < 0.5f ? 1.f : __builtin_amdgcn_exp2f(float(l2));
+  plus = d < 0.5f ? -d : 0.f;
+}
 
-// The 16 x 16 tiles of a DK x VC part of a state that each of four waves holds: keys down, values along.
+// What a chunk's gates and keys come to, as it lies in the workspace and in LDS.  A decay from row j to a later row i is
+// in_tile[i] between[it][jt] to_tile[j] for rows of different tiles of 16, so that tiles below the diagonal take no exponentials
+// of their own; none of the three is above 1.
+struct alignas(16) ChunkRecord {
+  double decay[CHUNK];    // logarithm to base 2 of the decay from the chunk's start to a row, its own included
+  float rk[CHUNK];        // 1 / |k|
+  float rk_to_tile[CHUNK];   // times the decay behind the row to the end of its tile
+  float rk_to_end[CHUNK];    // ... to the end of the chunk
+  float rk_since[CHUNK];     // times `since`
+  float since[CHUNK];     // the decay from the chunk's start
+  float in_tile[CHUNK];   // ... from the start of the row's tile
+  float beta[CHUNK];      // 0 where there is no row
+  float between[4][4];    // from the end of tile [second] to the start of tile [first]
+  float times, plus, unused[2];   // state_factor of the whole chunk
+};
+constexpr int RECORD_PIECES = sizeof(ChunkRecord) / 16;
+static_assert(sizeof(ChunkRecord) == DELTA_RECORD_BYTES && RECORD_PIECES <= 256, "a piece to a thread");
+
+// W as operand fragments of three parts, [fragment][part][lane][8 elements]: of the row (column) tiles 0 .. 3 and the 32 columns
+// (rows) ks the ones that are not all zeros.
+constexpr int W_FRAGS = 6, W_ELEMS = W_FRAGS * 3 * 64 * 8;
+static_assert(2 * W_ELEMS == DELTA_W_BYTES, "workspace");
+__host__ __device__ constexpr bool w_row_there(int tile, int ks) { return 2 * ks <= tile; }
+__host__ __device__ constexpr int w_row_frag(int tile, int ks) { return (tile < 2 ? tile : 2 * tile - 2) + ks; }
+__host__ __device__ constexpr bool w_col_there(int tile, int ks) { return 2 * ks + 1 >= tile; }
+__host__ __device__ constexpr int w_col_frag(int tile, int ks) { return tile < 2 ? 2 * tile + ks : tile + 2; }
+
+// The 16 x 16 tiles of a VC x DK part of a state that each of four waves holds: values down, keys along.
 template <int DK, int VC>
 struct StateTiles {
-  static constexpr int RT = DK / 16, CT = VC / 16;
-  static constexpr int NR = RT >= 4 ? RT / 4 : 1, NC = RT >= 4 ? CT : CT >= 2 ? CT / 2 : 1;
-  static __device__ __forceinline__ bool active(int w) { return RT >= 4 || CT >= 2 || w < 2; }
-  static __device__ __forceinline__ int row_tile(int w, int x) { return RT >= 4 ? w * NR + x : w % 2; }
-  static __device__ __forceinline__ int col_tile(int w, int y) { return RT >= 4 ? y : w / 2 * NC + y; }
+  static constexpr int KT = DK / 16, VT = VC / 16;
+  static constexpr int NK = KT >= 4 ? KT / 4 : 1, NV = KT >= 4 ? VT : VT >= 2 ? VT / 2 : 1;
+  static __device__ __forceinline__ bool active(int w) { return KT >= 4 || VT >= 2 || w < 2; }
+  static __device__ __forceinline__ int key_tile(int w, int y) { return KT >= 4 ? w * NK + y : w % 2; }
+  static __device__ __forceinline__ int value_tile(int w, int x) { return KT >= 4 ? x : w / 2 * NV + x; }
 };
 
 // Chunks of a unit in the workspace.

@@ -14,20 +14,21 @@ template <typename T, int DK, int VC>
 struct DeltaRevCfg {
   static constexpr int IN = Rows<T>::PARTS, LEVEL = 3;
   using KTile = PartTile<CHUNK, DK, IN>;
-  using GTile = PartTile<CHUNK, VC, IN>;     // rows of dO
-  using State = PartTile<VC, DK, LEVEL>;     // [value][key]
-  using Errors = PartTile<VC, CHUNK, LEVEL>; // [value][token]
-  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + State::SIZE + 2 * Errors::SIZE) + CHUNK * 20;
+  using GTile = PartTile<CHUNK, VC, IN>;      // rows of dO
+  using State = PartTile<DK, VC, LEVEL>;      // [key][value]
+  using Errors = PartTile<CHUNK, VC, LEVEL>;  // [token][value]
+  // the gradient behind the chunk, and when it is read X
+  static constexpr int ROOM = State::SIZE > Errors::SIZE ? State::SIZE : Errors::SIZE;
+  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + ROOM + Errors::SIZE) + int(sizeof(ChunkRecord)) + 8 * CHUNK;
   static constexpr int GROUPS = (160 * 1024) / LDS_BYTES >= 3 ? 3 : (160 * 1024) / LDS_BYTES >= 2 ? 2 : 1;
 };
 
 template <typename T, int DK, int VC>
 __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
-    const float* __restrict__ beta, const int* __restrict__ lengths, const float* dstate,
-    float* dstate_in, const float* __restrict__ W, const double* __restrict__ decays,
-    const float* __restrict__ factors, float* __restrict__ zs, float* __restrict__ dstates, Divisor H, Divisor parts, int N,
-    int units, int DV, float eps) {
+    const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
+    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, Divisor H, Divisor parts, int N,
+    int units, int DV, float inv_eps) {
   using Cfg = DeltaRevCfg<T, DK, VC>;
   using KTile = typename Cfg::KTile;
   using GTile = typename Cfg::GTile;
@@ -38,12 +39,13 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Os[GTile::SIZE];
-  __shared__ __attribute__((aligned(16))) uint16_t Ds[State::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t room[Cfg::ROOM];
   __shared__ __attribute__((aligned(16))) uint16_t Fs[Errors::SIZE];   // b F
-  __shared__ __attribute__((aligned(16))) uint16_t Xs[Errors::SIZE];   // - G X / |k|
-  __shared__ __attribute__((aligned(16))) double Gs[CHUNK];
-  __shared__ __attribute__((aligned(16))) float rk[CHUNK], rq[CHUNK], bs[CHUNK];
-  fetch_argument_now(Q, K, dO, s, beta, lengths, dstate, dstate_in, W, decays, factors, zs, dstates, H, parts, N, units, DV, eps);
+  __shared__ ChunkRecord rec;
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK], rq_since[CHUNK];
+  uint16_t* const Ds = room;
+  uint16_t* const Xs = room;   // - G X / |k|
+  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, H, parts, N, units, DV, inv_eps);
   int unit, part;
   unit_and_segment(blockIdx.x, units, parts, unit, part);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
@@ -52,76 +54,66 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
   const T* Ku = K + size_t(unit) * N * DK;
   const T* dOu = dO + size_t(unit) * N * DV + col0;
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
-  const int own = 16 * w + r;
+  const int own = 16 * w + r;   // this lane's token of the chunk
+  const bool active = ST::active(w);
 
-  f32x4 D[ST::NR][ST::NC];
+  const auto state_at = [&](int x, int y) {
+    return unsigned((16 * ST::key_tile(w, y) + r) * DV + col0 + 16 * ST::value_tile(w, x) + 4 * q4);
+  };
+  f32x4 D[ST::NV][ST::NK];
 #pragma unroll
-  for (int x = 0; x < ST::NR; ++x)
+  for (int x = 0; x < ST::NV; ++x)
 #pragma unroll
-    for (int y = 0; y < ST::NC; ++y) {
+    for (int y = 0; y < ST::NK; ++y) {
       D[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (dstate != nullptr && ST::active(w)) {
-        const float* from = dstate + size_t(unit) * DK * DV + size_t(16 * ST::row_tile(w, x) + 4 * q4) * DV + col0 + 16 * ST::col_tile(w, y) + r;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) D[x][y][v] = from[v * DV];
-      }
+      if (dstate != nullptr && active) D[x][y] = *reinterpret_cast<const f32x4*>(dstate + size_t(unit) * DK * DV + state_at(x, y));
     }
 
   RowTile<T, DK> kt, qt;
   RowTile<T, VC> gt;
-  float wraw[2][8];
-  double g_next = 0.0;
-  float rk_next = 0.f, b_next = 0.f;
+  u32x4 rec_next = {0u, 0u, 0u, 0u};
+  bf16x8 wf[2][LEVEL];
   const auto fetch_rows = [&](int c) {
     const int row0 = c * CHUNK;
-    kt.fetch(Ku, row0, there);
-    qt.fetch(Qu, row0, there);
-    gt.fetch(dOu, row0, there, DV);
-    if (tid < CHUNK) {
-      const size_t at = (size_t(unit) * chunks + c) * CHUNK + tid;
-      g_next = decays[at];
-      rk_next = factors[at];
-      b_next = row0 + tid < there ? beta[size_t(unit) * N + row0 + tid] : 0.f;
-    }
+    kt.fetch(Ku + size_t(row0) * DK, there - row0);
+    qt.fetch(Qu + size_t(row0) * DK, there - row0);
+    gt.fetch(dOu + size_t(row0) * DV, there - row0, DV);
+    if (tid < RECORD_PIECES) rec_next = reinterpret_cast<const u32x4*>(records + size_t(unit) * chunks + c)[tid];
   };
-  const auto fetch_W = [&](int c) {   // column `own` of W
-    const float* from = W + (size_t(unit) * chunks + c) * CHUNK * CHUNK + 8 * q4 * CHUNK + own;
+  const auto fetch_W = [&](int c) {
+    const uint16_t* from = w_cols + (size_t(unit) * chunks + c) * W_ELEMS;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (2 * ks + 1 >= w) wraw[ks][i] = from[(32 * ks + i) * CHUNK];
+      for (int i = 0; i < LEVEL; ++i)
+        if (w_col_there(w, ks))
+          wf[ks][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(from + w_col_frag(w, ks) * 3 * 512 + i * 512 + l * 8));
   };
   if (steps > 0) {
     fetch_rows(steps - 1);
     fetch_W(steps - 1);
   }
   for (int c = steps - 1; c >= 0; --c) {
-    if (ST::active(w)) {
-      float* to = dstates + (size_t(unit) * chunks + c) * DK * DV + col0;
+    if (active) {
+      float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
 #pragma unroll
-      for (int x = 0; x < ST::NR; ++x)
+      for (int x = 0; x < ST::NV; ++x)
 #pragma unroll
-        for (int y = 0; y < ST::NC; ++y) {
-          State::store4(Ds, 16 * ST::col_tile(w, y) + r, 16 * ST::row_tile(w, x) + 4 * q4, D[x][y]);
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            to[size_t(16 * ST::row_tile(w, x) + 4 * q4 + v) * DV + 16 * ST::col_tile(w, y) + r] = D[x][y][v];
+        for (int y = 0; y < ST::NK; ++y) {
+          State::store4(Ds, 16 * ST::key_tile(w, y) + r, 16 * ST::value_tile(w, x) + 4 * q4, D[x][y]);
+          *reinterpret_cast<f32x4*>(to + state_at(x, y)) = D[x][y];
         }
     }
     kt.commit(Ks);
     qt.commit(Qs);
-    qt.store_factors(rq, eps);
+    qt.store_factors(rq, inv_eps);
     gt.commit(Os);
-    if (tid < CHUNK) {
-      Gs[tid] = g_next;
-      rk[tid] = rk_next;
-      bs[tid] = b_next;
-    }
+    if (tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[tid] = rec_next;
     __syncthreads();
 
     // F: what D gives, and the chunk's own rows
     f32x4 f[NT];
+    if (tid < CHUNK) rq_since[tid] = scale * rec.since[tid] * rq[tid];
     {
       bf16x8 kf[KS][IN];
 #pragma unroll
@@ -132,19 +124,13 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           bf16x8 df[LEVEL];
-          State::row_frag(Ds, 16 * t + r, 32 * ks + 8 * q4, df);
-          f[t] = mm<LEVEL>(kf[ks], df, f[t]);
+          State::col_frag(Ds, 32 * ks + 8 * q4, 32 * ks + 8 * q4 + 4, 16 * t, r, df);
+          f[t] = mm<LEVEL>(df, kf[ks], f[t]);
         }
       }
+      const float to_end = rec.rk_to_end[own], to_tile = scale * rec.rk_to_tile[own];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int j = 16 * w + 4 * q4 + v;
-        const float to_end = rk[j] * decay_between(Gs[CHUNK - 1], Gs[j]);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) f[t][v] *= to_end;
-      }
-      const double g_own = Gs[own];
-      const float rk_own = rk[own];
+      for (int t = 0; t < NT; ++t) f[t] *= to_end;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         if (2 * p + 1 < w) continue;   // queries before the wave's keys
@@ -160,10 +146,17 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
               KTile::row_frag(Qs, 16 * it + r, 32 * ks + 8 * q4, qf);
               t = mm<LEVEL>(qf, kf[ks], t);
             }
+            const f32x4 rq4 = *reinterpret_cast<const f32x4*>(rq + 16 * it + 4 * q4);
+            if (it > w) {
+              half[h] = t * rq4 * (*reinterpret_cast<const f32x4*>(rec.in_tile + 16 * it + 4 * q4) * (to_tile * rec.between[it][w]));
+            } else {
+              const double g_own = rec.decay[own];
+              const float rk_own = scale * rec.rk[own];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const int i = 16 * it + 4 * q4 + v;
-              half[h][v] = i >= own ? t[v] * rq[i] * rk_own * (scale * decay_between(Gs[i], g_own)) : 0.f;
+              for (int v = 0; v < 4; ++v) {
+                const int i = 16 * it + 4 * q4 + v;
+                half[h][v] = i >= own ? t[v] * rq4[v] * (rk_own * decay_between(rec.decay[i], g_own)) : 0.f;
+              }
             }
           }
         }
@@ -173,14 +166,13 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
         for (int t = 0; t < NT; ++t) {
           bf16x8 gf[IN];
           GTile::col_frag(Os, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * t, r, gf);
-          f[t] = mm<LEVEL>(pf, gf, f[t]);
+          f[t] = mm<LEVEL>(gf, pf, f[t]);
         }
       }
     }
-    const f32x4 b4 = *reinterpret_cast<const f32x4*>(bs + 16 * w + 4 * q4);
+    const float b = rec.beta[own], x_since = -b * rec.rk_since[own], times = rec.times, plus = rec.plus;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) Errors::store4(Fs, 16 * t + r, 16 * w + 4 * q4, b4 * f[t]);
-    const StateFactor kept(Gs[CHUNK - 1]);
+    for (int t = 0; t < NT; ++t) Errors::store4(Fs, own, 16 * t + 4 * q4, b * f[t]);
     if (c > 0) fetch_rows(c - 1);
     __syncthreads();
 
@@ -190,86 +182,66 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
       for (int t = 0; t < NT; ++t) z[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
-        if (2 * ks + 1 >= w) {
-          bf16x8 wf[LEVEL];
-          split8<LEVEL>(f32x4{wraw[ks][0], wraw[ks][1], wraw[ks][2], wraw[ks][3]},
-                        f32x4{wraw[ks][4], wraw[ks][5], wraw[ks][6], wraw[ks][7]}, wf);
+        if (w_col_there(w, ks)) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             bf16x8 ff[LEVEL];
-            Errors::row_frag(Fs, 16 * t + r, 32 * ks + 8 * q4, ff);
-            z[t] = mm<LEVEL>(wf, ff, z[t]);
+            Errors::col_frag(Fs, 32 * ks + 8 * q4, 32 * ks + 8 * q4 + 4, 16 * t, r, ff);
+            z[t] = mm<LEVEL>(ff, wf[ks], z[t]);
           }
         }
-      float since[4];
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int j = 16 * w + 4 * q4 + v;
-        since[v] = -rk[j] * decay_between(Gs[j], 0.0);
-      }
-      float* to = zs + ((size_t(unit) * chunks + c) * CHUNK + 16 * w + 4 * q4) * DV + col0 + r;
+      float* to = zs + ((size_t(unit) * chunks + c) * CHUNK + own) * DV + col0 + 4 * q4;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         z[t] = f[t] - z[t];
-        const f32x4 x = b4 * z[t];
-        Errors::store4(Xs, 16 * t + r, 16 * w + 4 * q4, f32x4{x[0] * since[0], x[1] * since[1], x[2] * since[2], x[3] * since[3]});
-#pragma unroll
-        for (int v = 0; v < 4; ++v) to[size_t(v) * DV + 16 * t] = z[t][v];
+        Errors::store4(Xs, own, 16 * t + 4 * q4, x_since * z[t]);
+        *reinterpret_cast<f32x4*>(to + 16 * t) = z[t];
       }
       if (c > 0) fetch_W(c - 1);
     }
     __syncthreads();
 
-    if (ST::active(w)) {
+    if (active) {
 #pragma unroll
-      for (int x = 0; x < ST::NR; ++x)
+      for (int x = 0; x < ST::NV; ++x)
 #pragma unroll
-        for (int y = 0; y < ST::NC; ++y)
+        for (int y = 0; y < ST::NK; ++y)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) D[x][y][v] = kept.of(D[x][y][v]);
+          for (int v = 0; v < 4; ++v) D[x][y][v] = __builtin_fmaf(D[x][y][v], plus, D[x][y][v] * times);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const int t0 = 32 * ks + 8 * q4;
-        f32x4 lo, hi;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(rq_since + t0), hi = *reinterpret_cast<const f32x4*>(rq_since + t0 + 4);
+        bf16x8 gf[ST::NV][LEVEL], xf[ST::NV][LEVEL];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          lo[v] = rq[t0 + v] * (scale * decay_between(Gs[t0 + v], 0.0));
-          hi[v] = rq[t0 + 4 + v] * (scale * decay_between(Gs[t0 + 4 + v], 0.0));
-        }
-        bf16x8 gf[ST::NC][LEVEL], xf[ST::NC][LEVEL];
-#pragma unroll
-        for (int y = 0; y < ST::NC; ++y) {
+        for (int x = 0; x < ST::NV; ++x) {
           bf16x8 raw[IN];
-          GTile::col_frag(Os, t0, t0 + 4, 16 * ST::col_tile(w, y), r, raw);
-          f32x4 a, b;
-          join8<IN>(raw, a, b);
-          split8<LEVEL>(a * lo, b * hi, gf[y]);
-          Errors::row_frag(Xs, 16 * ST::col_tile(w, y) + r, t0, xf[y]);
+          GTile::col_frag(Os, t0, t0 + 4, 16 * ST::value_tile(w, x), r, raw);
+          f32x4 a, b_;
+          join8<IN>(raw, a, b_);
+          split8<LEVEL>(a * lo, b_ * hi, gf[x]);
+          Errors::col_frag(Xs, t0, t0 + 4, 16 * ST::value_tile(w, x), r, xf[x]);
         }
 #pragma unroll
-        for (int x = 0; x < ST::NR; ++x) {
+        for (int y = 0; y < ST::NK; ++y) {
           bf16x8 kf[IN], qf[IN];
-          KTile::col_frag(Ks, t0, t0 + 4, 16 * ST::row_tile(w, x), r, kf);
-          KTile::col_frag(Qs, t0, t0 + 4, 16 * ST::row_tile(w, x), r, qf);
+          KTile::col_frag(Ks, t0, t0 + 4, 16 * ST::key_tile(w, y), r, kf);
+          KTile::col_frag(Qs, t0, t0 + 4, 16 * ST::key_tile(w, y), r, qf);
 #pragma unroll
-          for (int y = 0; y < ST::NC; ++y) {
-            D[x][y] = mm<LEVEL>(kf, xf[y], D[x][y]);
-            D[x][y] = mm<LEVEL>(qf, gf[y], D[x][y]);
+          for (int x = 0; x < ST::NV; ++x) {
+            D[x][y] = mm<LEVEL>(xf[x], kf, D[x][y]);
+            D[x][y] = mm<LEVEL>(gf[x], qf, D[x][y]);
           }
         }
       }
     }
     __syncthreads();
   }
-  if (dstate_in != nullptr && ST::active(w)) {
-    float* to = dstate_in + size_t(unit) * DK * DV + col0;
+  if (dstate_in != nullptr && active) {
 #pragma unroll
-    for (int x = 0; x < ST::NR; ++x)
+    for (int x = 0; x < ST::NV; ++x)
 #pragma unroll
-      for (int y = 0; y < ST::NC; ++y)
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          to[size_t(16 * ST::row_tile(w, x) + 4 * q4 + v) * DV + 16 * ST::col_tile(w, y) + r] = D[x][y][v];
+      for (int y = 0; y < ST::NK; ++y) *reinterpret_cast<f32x4*>(dstate_in + size_t(unit) * DK * DV + state_at(x, y)) = D[x][y];
   }
 }
 
@@ -286,7 +258,7 @@ struct DeltaGradCfg {
   // first the rows of dO, E and Z, then two masked tiles and the rows of K and Q
   static constexpr int FIRST = GTile::SIZE + 2 * ETile::SIZE, SECOND = 2 * MTile::SIZE + 2 * KTile::SIZE;
   static constexpr int SIZE = FIRST > SECOND ? FIRST : SECOND;
-  static constexpr int LDS_BYTES = 2 * SIZE + CHUNK * 56;
+  static constexpr int LDS_BYTES = 2 * SIZE + CHUNK * 8 + 16 + int(sizeof(ChunkRecord));
   static constexpr int GROUPS = (160 * 1024) / LDS_BYTES >= 2 ? 2 : 1;
   // key tiles of a wave and token tiles that it forms of them
   static constexpr int KT = DK / 16, NK = KT >= 4 ? KT / 4 : 1, NTOK = KT >= 4 ? 4 : 2;
@@ -304,10 +276,10 @@ template <typename T, int DK, int DV>
 __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_gradients(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
     const float* __restrict__ s, const float* __restrict__ log_decay, const float* __restrict__ beta,
-    const int* __restrict__ lengths, const double* __restrict__ decays, const float* __restrict__ errors,
+    const int* __restrict__ lengths, const ChunkRecord* __restrict__ records, const float* __restrict__ errors,
     const float* __restrict__ states, const float* __restrict__ zs, const float* __restrict__ dstates, T* __restrict__ dQ,
     T* __restrict__ dK, T* __restrict__ dV, float* __restrict__ dlog_decay, float* __restrict__ dbeta,
-    float* __restrict__ ds_parts, Divisor H, Divisor chunks, int N, float eps, int from_state) {
+    float* __restrict__ ds_parts, Divisor H, Divisor chunks, int N, float inv_eps, int from_state) {
   using Cfg = DeltaGradCfg<T, DK, DV>;
   using KTile = typename Cfg::KTile;
   using GTile = typename Cfg::GTile;
@@ -315,9 +287,12 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
   using MTile = typename Cfg::MTile;
   constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, NK = Cfg::NK, NTOK = Cfg::NTOK, VS = DV / 32;
   __shared__ __attribute__((aligned(16))) uint16_t room[Cfg::SIZE];
-  __shared__ __attribute__((aligned(16))) double Gs[CHUNK];
-  __shared__ __attribute__((aligned(16))) float rk[CHUNK], rq[CHUNK], bs[CHUNK], xv[CHUNK];
-  __shared__ float qdot[4][CHUNK], kdot[4][CHUNK], tail[4];
+  __shared__ ChunkRecord rec;
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK], xv[CHUNK];
+  __shared__ float tail[4];
+  typedef float Dots[4][CHUNK];
+  Dots& qdot = *reinterpret_cast<Dots*>(room);   // when nothing else is there any more
+  Dots& kdot = *(&qdot + 1);
   uint16_t* const Os = room;
   uint16_t* const Es = Os + GTile::SIZE;
   uint16_t* const Zs = Es + ETile::SIZE;
@@ -355,14 +330,11 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
   {
     using RT = RowTile<T, DV, Cfg::PAD>;
     RT gt, vt;
-    gt.fetch(dO + row_at * DV, row0, there);
-    vt.fetch(V + row_at * DV, row0, there);
-    kt.fetch(K + row_at * DK, row0, there);
-    qt.fetch(Q + row_at * DK, row0, there);
-    if (tid < CHUNK) {
-      Gs[tid] = decays[size_t(blockIdx.x) * CHUNK + tid];
-      bs[tid] = row0 + tid < there ? beta[row_at + row0 + tid] : 0.f;
-    }
+    gt.fetch(dO + (row_at + row0) * DV, there - row0);
+    vt.fetch(V + (row_at + row0) * DV, there - row0);
+    kt.fetch(K + (row_at + row0) * DK, there - row0);
+    qt.fetch(Q + (row_at + row0) * DK, there - row0);
+    if (tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[tid] = reinterpret_cast<const u32x4*>(records + blockIdx.x)[tid];
     gt.commit(Os);
 #pragma unroll
     for (int p = 0; p < RT::PASSES; ++p) {
@@ -396,8 +368,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
         to[1] = vec4{T(b * z1[0]), T(b * z1[1]), T(b * z1[2]), T(b * z1[3])};
       }
     }
-    kt.store_factors(rk, eps);
-    qt.store_factors(rq, eps);
+    qt.store_factors(rq, inv_eps);
   }
   __syncthreads();
 
@@ -439,11 +410,11 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     }
     // each token's factors; and what the updates of the chunk give to <D, H behind the chunk>
     if (Cfg::KT < 4 && w >= 2) through = 0.f;
-    through *= decay_between(Gs[CHUNK - 1], 0.0);
+    through *= rec.since[CHUNK - 1];
 #pragma unroll
     for (int t = 0; t < NTOK; ++t) {
       const int i = 16 * (tt0 + t) + r;
-      const float since = decay_between(Gs[i], 0.0), to_end = bs[i] * decay_between(Gs[CHUNK - 1], Gs[i]);
+      const float since = rec.since[i], to_end = rec.beta[i] * decay_between(rec.decay[CHUNK - 1], rec.decay[i]);
       float dot = 0.f;
 #pragma unroll
       for (int x = 0; x < NK; ++x) {
@@ -454,10 +425,10 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
           aq[x][t][v] *= since;
           ak[x][t][v] *= to_end;
           dot = __builtin_fmaf(k[v], ak[x][t][v], dot);
-          ak[x][t][v] = __builtin_fmaf(-bs[i] * since, az[x][t][v], ak[x][t][v]);
+          ak[x][t][v] = __builtin_fmaf(-rec.beta[i] * since, az[x][t][v], ak[x][t][v]);
         }
       }
-      through = __builtin_fmaf(rk[i], dot, through);
+      through = __builtin_fmaf(rec.rk[i], dot, through);
     }
     through = group_sum<64>(through);
     if (l == 0) tail[w] = through;
@@ -466,8 +437,8 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
   // the masked tiles: rows i of wave w's tile, columns j; lanes hold four columns of a row
   f32x4 pt[4], at[4];
   const int own = 16 * w + r;
-  const double g_own = Gs[own];
-  const float b_own = bs[own];
+  const double g_own = rec.decay[own];
+  const float b_own = rec.beta[own];
   {
     bf16x8 gf[VS][IN], zf[VS][LEVEL];
 #pragma unroll
@@ -489,20 +460,20 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const int j = 16 * jt + 4 * q4 + v;
-          const float f = bs[j] * decay_between(g_own, Gs[j]);
+          const float f = rec.beta[j] * decay_between(g_own, rec.decay[j]);
           pt[jt][v] = j <= own ? pt[jt][v] * f : 0.f;
           at[jt][v] = j < own ? -b_own * at[jt][v] * f : 0.f;
         }
       }
     }
   }
-  const float rq_own = rq[own], rk_own = rk[own];
+  const float rq_own = rq[own], rk_own = rec.rk[own];
   __syncthreads();   // the rows of dO, E and Z are read
   kt.commit(Ks);
   qt.commit(Qs);
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt) {
-    const f32x4 k4 = *reinterpret_cast<const f32x4*>(rk + 16 * jt + 4 * q4);
+    const f32x4 k4 = *reinterpret_cast<const f32x4*>(rec.rk + 16 * jt + 4 * q4);
     MTile::store4(Ms, own, 16 * jt + 4 * q4, pt[jt] * k4);
     MTile::store4(Mt, own, 16 * jt + 4 * q4, pt[jt] * (scale * rq_own));
   }
@@ -541,7 +512,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
       __syncthreads();
 #pragma unroll
       for (int jt = 0; jt < 4; ++jt) {
-        const f32x4 k4 = *reinterpret_cast<const f32x4*>(rk + 16 * jt + 4 * q4);
+        const f32x4 k4 = *reinterpret_cast<const f32x4*>(rec.rk + 16 * jt + 4 * q4);
         MTile::store4(Ms, own, 16 * jt + 4 * q4, at[jt] * k4);
         MTile::store4(Mt, own, 16 * jt + 4 * q4, at[jt] * rk_own);
       }
@@ -549,6 +520,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     }
   }
 
+  __syncthreads();
   // through the normalisation: dq = (dqh - qh (qh . dqh)) / |q|; a row below eps was divided by eps alone
 #pragma unroll
   for (int t = 0; t < NTOK; ++t) {
@@ -587,7 +559,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
       dq += qdot[n][i];
       dk += kdot[n][i];
     }
-    const float fq = rq[i], fk = rk[i], inv_eps = 1.0f / eps;
+    const float fq = rq[i], fk = rec.rk[i];
     const float cq = fq == inv_eps ? 0.f : fq * (fq * dq), ck = fk == inv_eps ? 0.f : fk * (fk * dk);
     if (row0 + i < there) {
 #pragma unroll
@@ -650,9 +622,9 @@ hipError_t run_rev(const DeltaArgs& a) {
   constexpr int VC = sizeof(T) == 4 && DK == 128 ? 16 : 32;   // (what the LDS holds)
   const int units = a.B * a.H, parts = a.dv / VC;
   return launch_kernel("delta_rev_scan", delta_rev_scan<T, DK, VC>, dim3(unsigned(units * parts)), dim3(256), 0, a.stream,
-                       static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.beta,
-                       a.seq_len, a.dstate, a.dstate_in, a.W, a.decays, a.factors, a.zs, a.dstates, Divisor(a.H), Divisor(parts),
-                       a.N, units, a.dv, a.eps);
+                       static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.seq_len,
+                       a.dstate, a.dstate_in, static_cast<const ChunkRecord*>(a.records), a.w_cols, a.zs, a.dstates, Divisor(a.H),
+                       Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
 }
 
 template <typename T, int DK, int DV>
@@ -660,9 +632,10 @@ hipError_t run_gradients(const DeltaArgs& a) {
   const int chunks = delta_chunks(a.N);
   return launch_kernel("delta_gradients", delta_gradients<T, DK, DV>, dim3(unsigned(a.B * a.H * chunks)), dim3(256), 0, a.stream,
                        static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V),
-                       static_cast<const T*>(a.dO), a.s, a.log_decay, a.beta, a.seq_len, a.decays, a.errors, a.states, a.zs,
+                       static_cast<const T*>(a.dO), a.s, a.log_decay, a.beta, a.seq_len,
+                       static_cast<const ChunkRecord*>(a.records), a.errors, a.states, a.zs,
                        a.dstates, static_cast<T*>(a.dQ), static_cast<T*>(a.dK), static_cast<T*>(a.dV), a.dlog_decay, a.dbeta,
-                       a.ds_parts, Divisor(a.H), Divisor(chunks), a.N, a.eps, int(a.state_in != nullptr));
+                       a.ds_parts, Divisor(a.H), Divisor(chunks), a.N, 1.0f / a.eps, int(a.state_in != nullptr));
 }
 
 template <typename T, int DK>

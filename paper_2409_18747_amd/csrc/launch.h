@@ -307,21 +307,21 @@ struct TreeArgs {
 };
 
 // The gated delta rule (delta.h), forward and backward.  Chunks are of 64 rows; per (batch, head) and chunk the workspace has
-// W [64][64], decays (from the chunk's start, logarithms to base 2) and factors (1 / norm of K's rows) [64]; for a backward
-// errors E [64][dv] and the state before the chunk [dk][dv]; and of the backward itself Z [64][dv] and the gradient with respect
-// to the state behind the chunk [dk][dv].
+// a ChunkRecord and W's fragments by rows; for a backward those by columns, errors E [64][dv] and the state before the chunk
+// [dk][dv]; and of the backward itself Z [64][dv] and the gradient with respect to the state behind the chunk [dk][dv].
+constexpr size_t DELTA_RECORD_BYTES = 2384, DELTA_W_BYTES = 6 * 3 * 1024;
 struct DeltaArgs {
   const void* Q; const void* K; const void* V; const float* s; const float* log_decay; const float* beta;   // log_decay may be null
   const int* seq_len;               // null, or int[B] row counts: then s and ds are [B][H]
   const float* state_in;            // may be null
   void* O; float* state;            // forward: results (state may be null); backward: no O, and only errors and states are formed
-  float* W; double* decays; float* factors;
-  float* errors; float* states;     // forward: may be null
+  void* records; unsigned short* w_rows;
+  unsigned short* w_cols; float* errors; float* states;     // forward: may be null
   // backward
   const void* dO; const float* dstate; float* dstate_in;   // the two states may be null
   void* dQ; void* dK; void* dV; float* ds; float* dlog_decay; float* dbeta;   // dlog_decay may be null
   float* zs; float* dstates; float* ds_parts;   // workspace
-  bool saved;                       // W, decays, factors, errors and states are a forward's
+  bool saved;                       // records, w_rows, w_cols, errors and states are a forward's
   int B, H, N, dk, dv;
   float eps;
   hipStream_t stream;

@@ -55,7 +55,8 @@ __global__ __launch_bounds__(256) void step_delta_kernel(
   typedef __attribute__((ext_vector_type(4))) T vec4;
   const vec4 vt = *reinterpret_cast<const vec4*>(v + size_t(unit) * DV + col);
   const float scale = s[head], b1 = beta[unit];
-  const StateFactor kept(log_decay != nullptr ? log2_decay(log_decay[unit]) : 0.0);
+  float times, plus;
+  state_factor(log_decay != nullptr ? log2_decay(log_decay[unit]) : 0.0, times, plus);
   const float rq = inv_norm(group_sum<64>(__builtin_fmaf(q0, q0, q1 * q1)), eps);
   const float rk = inv_norm(group_sum<64>(__builtin_fmaf(k0, k0, k1 * k1)), eps);
   q0 *= rq; q1 *= rq; k0 *= rk; k1 *= rk;
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(256) void step_delta_kernel(
       const float kr = kh[row], qr = qh[row];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        rows[p][i] = kept.of(rows[p][i]);
+        rows[p][i] = __builtin_fmaf(rows[p][i], plus, rows[p][i] * times);
         by_k[i] = __builtin_fmaf(kr, rows[p][i], by_k[i]);
         by_q[i] = __builtin_fmaf(qr, rows[p][i], by_q[i]);
       }
