@@ -137,8 +137,12 @@ struct Raw8 {
   }
 };
 
-// A tile of 16-bit parts in LDS: plane after plane of ROWS rows, each PITCH wide.
-// (Rows 16 apart from a multiple of 32 are read fastest, device_common.h; 8 where the LDS has no room for that.)
+// Slots of operand fragments.  Lane row q = lane / 16 of a fragment of 32 k indices has the slots 8 q .. 8 q + 7 where it is read
+// from rows in LDS or memory, and 4 q .. 4 q + 3 and 16 + 4 q .. 16 + 4 q + 3 where it is two accumulator tiles side by side (or
+// is to meet one that is): those tiles become operands without leaving their lanes.
+
+// A tile of 16-bit parts in LDS: plane after plane of ROWS rows, each PITCH wide.  (Rows 16 apart from a multiple of 32 are read
+// fastest, device_common.h; 8 where the LDS has no room for that.)
 template <int ROWS, int COLS, int PARTS, int PAD = 16>
 struct PartTile {
   static constexpr int PITCH = COLS + PAD, PLANE = ROWS * PITCH, SIZE = PARTS * PLANE;
@@ -148,21 +152,35 @@ struct PartTile {
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(tile + i * PLANE + row * PITCH + c));
   }
-  // columns c .. c + 3 and c + 16 .. c + 19 of a row: the slot order of two accumulator tiles side by side
-  template <int N = PARTS>
-  static __device__ __forceinline__ void row_frag_pairs(const uint16_t* tile, int row, int c, bf16x8 (&f)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint16_t* p = tile + i * PLANE + row * PITCH + c;
-      const uint2 lo = *reinterpret_cast<const uint2*>(p), hi = *reinterpret_cast<const uint2*>(p + 16);
-      f[i] = __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
-    }
-  }
   // operand fragment whose k slots are rows r0 .. r0 + 3 and r1 .. r1 + 3 of column col0 + r
   template <int N = PARTS>
   static __device__ __forceinline__ void col_frag(const uint16_t* tile, int r0, int r1, int col0, int r, bf16x8 (&f)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = __builtin_bit_cast(bf16x8, lds_col_frag(tile + i * PLANE, PITCH, r0, r1, col0, r));
+  }
+  // the same of 16 columns that are four from `first` on, four from first + 8 on and so forth: lane r has first + 8 (r / 4) + r % 4
+  template <int N = PARTS>
+  static __device__ __forceinline__ void spread_col_frag(const uint16_t* tile, int r0, int r1, int first, int r, bf16x8 (&f)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint16_t* p = tile + i * PLANE + (r >> 2) * PITCH + first + 8 * (r & 3);
+      const s16x4 lo = lds_read_tr(p + r0 * PITCH), hi = lds_read_tr(p + r1 * PITCH);
+      f[i] = __builtin_bit_cast(bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+    }
+  }
+  // rows row0 .. row0 + 3 of column col0 + r as fp32
+  static __device__ __forceinline__ f32x4 col4(const uint16_t* tile, int row0, int col0, int r) {
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = PARTS - 1; i >= 0; --i) {
+      const uint2 w = __builtin_bit_cast(uint2, lds_read_tr(tile + i * PLANE + (row0 + (r >> 2)) * PITCH + col0 + (r & 3) * 4));
+      float t[4];
+      unpack2(w.x, t[0], t[1]);
+      unpack2(w.y, t[2], t[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += t[e];
+    }
+    return x;
   }
   template <int N = PARTS>
   static __device__ __forceinline__ void store4(uint16_t* tile, int row, int c, f32x4 x) {
@@ -181,18 +199,19 @@ struct PartTile {
 // 1 / max(norm, eps) of a row from its sum of squares, to a unit of fp32.
 __device__ __forceinline__ float row_factor(float sum_sq, float inv_eps) { return fminf(__builtin_amdgcn_rsqf(sum_sq), inv_eps); }
 
-// 64 rows of D elements on their way from memory to LDS, 256 threads: D / 8 neighbouring lanes share a row.
-template <typename T, int D, int PAD = 16>
+// 64 rows of D elements on their way from memory to LDS: D / 8 neighbouring lanes share a row.
+template <typename T, int D, int PAD = 16, int THREADS = 256>
 struct RowTile {
-  static constexpr int LPR = D / 8, RPP = 256 / LPR, PASSES = RPP < CHUNK ? CHUNK / RPP : 1, PARTS = Rows<T>::PARTS;
+  static constexpr int LPR = D / 8, RPP = THREADS / LPR, PASSES = RPP < CHUNK ? CHUNK / RPP : 1, PARTS = Rows<T>::PARTS;
   using Tile = PartTile<CHUNK, D, PARTS, PAD>;
   Raw8<T> raw[PASSES];
-  static __device__ __forceinline__ int row(int p) { return p * RPP + int(threadIdx.x) / LPR; }
-  static __device__ __forceinline__ int col() { return int(threadIdx.x) % LPR * 8; }
+  static __device__ __forceinline__ int thread() { return int(threadIdx.x) % THREADS; }   // (of one half of a workgroup's waves)
+  static __device__ __forceinline__ int row(int p) { return p * RPP + thread() / LPR; }
+  static __device__ __forceinline__ int col() { return thread() % LPR * 8; }
   static __device__ __forceinline__ bool in(int p) { return RPP <= CHUNK || row(p) < CHUNK; }   // (all threads take part)
   // the first `rows` rows from `base` on, LD elements apart; zeros behind them
   __device__ __forceinline__ void fetch(const T* base, int rows, int ld = D) {
-    const unsigned lane = unsigned((int(threadIdx.x) / LPR) * ld + col());
+    const unsigned lane = unsigned((thread() / LPR) * ld + col());
     if (RPP <= CHUNK && rows >= CHUNK) {
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) raw[p].load(base + p * RPP * ld + lane);
@@ -217,7 +236,7 @@ struct RowTile {
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const float f = row_factor(group_sum<LPR>(raw[p].sum_sq()), inv_eps);
-      if (in(p) && threadIdx.x % LPR == 0) out[row(p)] = f;
+      if (in(p) && thread() % LPR == 0) out[row(p)] = f;
     }
   }
 };
@@ -264,15 +283,28 @@ __host__ __device__ constexpr int w_row_frag(int tile, int ks) { return (tile < 
 __host__ __device__ constexpr bool w_col_there(int tile, int ks) { return 2 * ks + 1 >= tile; }
 __host__ __device__ constexpr int w_col_frag(int tile, int ks) { return tile < 2 ? 2 * tile + ks : tile + 2; }
 
-// The 16 x 16 tiles of a VC x DK part of a state that each of four waves holds: values down, keys along.
-template <int DK, int VC>
-struct StateTiles {
-  static constexpr int KT = DK / 16, VT = VC / 16;
-  static constexpr int NK = KT >= 4 ? KT / 4 : 1, NV = KT >= 4 ? VT : VT >= 2 ? VT / 2 : 1;
-  static __device__ __forceinline__ bool active(int w) { return KT >= 4 || VT >= 2 || w < 2; }
-  static __device__ __forceinline__ int key_tile(int w, int y) { return KT >= 4 ? w * NK + y : w % 2; }
-  static __device__ __forceinline__ int value_tile(int w, int x) { return KT >= 4 ? x : w / 2 * NV + x; }
-};
+// The scans' state: a wave holds 16 value columns of it in DK / 16 tiles, keys down, [2 ks + h] with the keys key_of(ks, h, q, v)
+// in element v of lane row q: next to each other two tiles are an operand whose slots are 32 consecutive keys, eight to a lane row.
+__device__ __forceinline__ constexpr int key_of(int ks, int h, int q, int v) { return 32 * ks + 8 * q + 4 * h + v; }
+
+// A barrier of all waves of a workgroup that orders their LDS accesses, for code that the waves do not share.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+// Fragment `at` of an array of fragments of N parts, [fragment][part][lane].
+template <int N>
+__device__ __forceinline__ void load_frag(const uint16_t* from, int at, int l, bf16x8 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = __builtin_bit_cast(bf16x8, reinterpret_cast<const u32x4*>(from)[(at * N + i) * 64 + l]);
+}
+template <int N, int M>
+__device__ __forceinline__ void store_frag(uint16_t* to, int at, int l, const bf16x8 (&f)[M]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) reinterpret_cast<u32x4*>(to)[(at * N + i) * 64 + l] = __builtin_bit_cast(u32x4, f[i]);
+}
+__device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
 // Chunks of a unit in the workspace.
 __host__ __device__ constexpr int delta_chunks(int N) { return (N + CHUNK - 1) / CHUNK; }

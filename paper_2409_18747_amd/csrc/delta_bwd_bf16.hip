@@ -8,43 +8,307 @@ namespace cottn {
 namespace {
 
 // ---------------------------------------------------------------------------------------
-// As the forward scan, a workgroup takes VC of the value columns: F = P^T dO' + (G_n/G) Kh D, Z = F - W^T (b F), and D in front
-// of the chunk, one after the other.
-template <typename T, int DK, int VC>
+// As in the forward scan a wave has 16 value columns, whose D, F and X never leave its registers: F = P^T dO' + (G_n/G) Kh D, Z =
+// F - W^T (b F), and D in front of the chunk, one after the other.  Beside those as many waves more fetch the rows, form P, and
+// hand over what does not depend on D: P^T dO' and, where the LDS has room for it, (G Qh)^T dO'.
+template <typename T, int DK, int NW>
 struct DeltaRevCfg {
-  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3;
-  using KTile = PartTile<CHUNK, DK, IN>;
-  using GTile = PartTile<CHUNK, VC, IN>;      // rows of dO
-  using State = PartTile<DK, VC, LEVEL>;      // [key][value]
-  using Errors = PartTile<CHUNK, VC, LEVEL>;  // [token][value]
-  // the gradient behind the chunk, and when it is read X
-  static constexpr int ROOM = State::SIZE > Errors::SIZE ? State::SIZE : Errors::SIZE;
-  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + ROOM + Errors::SIZE) + int(sizeof(ChunkRecord)) + 8 * CHUNK;
-  static constexpr int GROUPS = (160 * 1024) / LDS_BYTES >= 3 ? 3 : (160 * 1024) / LDS_BYTES >= 2 ? 2 : 1;
+  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, KS = DK / 32, PAD = sizeof(T) == 4 ? 8 : 16;
+  using KTile = PartTile<CHUNK, DK, IN, PAD>;
+  using GTile = PartTile<CHUNK, VC, IN, PAD>;      // rows of dO
+  static constexpr int W_SIZE = W_FRAGS * LEVEL * 512;
+  static constexpr int BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + 2 * W_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK + NW * 4 * 1024;
+  static constexpr bool HANDS_R = BYTES + NW * 2 * KS * 1024 <= 160 * 1024;
+  static constexpr bool FITS = BYTES <= 160 * 1024;
 };
 
-template <typename T, int DK, int VC>
-__global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_rev_scan(
+// Parts of s (G Qh)'s factors times rows of dO, slots of two accumulator tiles: the tokens 32 p + 4 q .., 32 p + 16 + 4 q ...
+template <int LEVEL, int IN>
+__device__ __forceinline__ void weighted_rows(const bf16x8 (&g)[IN], const float* rq, const float* since, float scale, int t0,
+                                              bf16x8 (&out)[LEVEL]) {
+  f32x4 lo, hi;
+  join8<IN>(g, lo, hi);
+  split8<LEVEL>(lo * (four(rq + t0) * (scale * four(since + t0))), hi * (four(rq + t0 + 16) * (scale * four(since + t0 + 16))), out);
+}
+
+template <typename T, int DK, int NW>
+__global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
     const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, Divisor H, Divisor parts, int N,
     int units, int DV, float inv_eps) {
-  using Cfg = DeltaRevCfg<T, DK, VC>;
+  using Cfg = DeltaRevCfg<T, DK, NW>;
   using KTile = typename Cfg::KTile;
   using GTile = typename Cfg::GTile;
-  using State = typename Cfg::State;
-  using Errors = typename Cfg::Errors;
-  using ST = StateTiles<DK, VC>;
-  constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, KS = DK / 32, NT = VC / 16;
+  constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, KS = Cfg::KS, NT = 64 * NW, VC = Cfg::VC;
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Os[GTile::SIZE];
-  __shared__ __attribute__((aligned(16))) uint16_t room[Cfg::ROOM];
-  __shared__ __attribute__((aligned(16))) uint16_t Fs[Errors::SIZE];   // b F
+  __shared__ __attribute__((aligned(16))) uint16_t Ws[Cfg::W_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::W_SIZE];
+  __shared__ f32x4 Fs[NW * 4 * 64];                            // P^T dO', tiles in accumulator order
+  __shared__ f32x4 Rs[Cfg::HANDS_R ? NW * 2 * KS * 64 : 1];    // (G Qh)^T dO'
   __shared__ ChunkRecord rec;
-  __shared__ __attribute__((aligned(16))) float rq[CHUNK], rq_since[CHUNK];
-  uint16_t* const Ds = room;
-  uint16_t* const Xs = room;   // - G X / |k|
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK];
+  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, H, parts, N, units, DV, inv_eps);
+  int unit, part;
+  unit_and_segment(blockIdx.x, units, parts, unit, part);
+  const int tid = threadIdx.x % NT, role = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / NT);
+  const int w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), steps = delta_chunks(there), col0 = part * VC;
+  const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
+
+  if (role == 0) {
+    // ---- the gradients with respect to the states
+    // this lane's value column in the first key row, and in the first token row, that it holds
+    const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
+    f32x4 D[2 * KS];
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        D[t][v] = dstate != nullptr ? (dstate + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+    for (int c = steps - 1; c >= 0; --c) {
+      bf16x8 df[KS][LEVEL];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) split8<LEVEL>(D[2 * ks], D[2 * ks + 1], df[ks]);
+      {
+        float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+      }
+      lds_barrier();   // the chunk is there
+      f32x4 f[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf[4][IN];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) KTile::row_frag(Ks, 16 * t + r, 32 * ks + 8 * q4, kf[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) f[t] = mm<LEVEL>(kf[t], df[ks], f[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] *= four(rec.rk_to_end + 16 * t + 4 * q4);
+      lds_barrier();   // P is there
+      lds_barrier();   // P^T dO' is there
+      bf16x8 ff[2][LEVEL], xf[2][LEVEL];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] += Fs[(w * 4 + t) * 64 + l];
+      f32x4 b[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) b[t] = four(rec.beta + 16 * t + 4 * q4);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) split8<LEVEL>(b[2 * p] * f[2 * p], b[2 * p + 1] * f[2 * p + 1], ff[p]);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        f32x4 x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = 2 * p + h;
+          f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            if (w_col_there(t, k)) {
+              bf16x8 wf[LEVEL];
+              load_frag(Ws, w_col_frag(t, k), l, wf);
+              z = mm<LEVEL>(wf, ff[k], z);
+            }
+          z = f[t] - z;
+          float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+          x[h] = -(b[t] * z) * four(rec.rk_since + 16 * t + 4 * q4);
+        }
+        split8<LEVEL>(x[0], x[1], xf[p]);
+      }
+      const float times = rec.times, plus = rec.plus;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) D[t][v] = __builtin_fmaf(D[t][v], plus, D[t][v] * times);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        bf16x8 wg[LEVEL];
+        if constexpr (!Cfg::HANDS_R) {
+          bf16x8 gf[IN];
+          GTile::col_frag(Os, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * w, r, gf);
+          weighted_rows<LEVEL>(gf, rq, rec.since, scale, 32 * p + 4 * q4, wg);
+        }
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) {
+          bf16x8 kf[IN];
+          KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, kf);
+          D[t] = mm<LEVEL>(kf, xf[p], D[t]);
+          if constexpr (!Cfg::HANDS_R) {
+            bf16x8 qf[IN];
+            KTile::spread_col_frag(Qs, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, qf);
+            D[t] = mm<LEVEL>(qf, wg, D[t]);
+          }
+        }
+      }
+      lds_barrier();   // everything of the chunk is read, and (G Qh)^T dO' is there
+      if constexpr (Cfg::HANDS_R) {
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) D[t] += Rs[(w * 2 * KS + t) * 64 + l];
+      }
+    }
+    if (dstate_in != nullptr) {
+      float* to = dstate_in + size_t(unit) * DK * DV;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+    }
+    return;
+  }
+
+  // ---- the chunks' rows and what they come to by themselves
+  constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
+  const T* Qu = Q + size_t(unit) * N * DK;
+  const T* Ku = K + size_t(unit) * N * DK;
+  const T* dOu = dO + size_t(unit) * N * DV + col0;
+  RowTile<T, DK, Cfg::PAD, NT> kt, qt;
+  RowTile<T, VC, Cfg::PAD, NT> gt;
+  u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
+  const auto fetch = [&](int c) {
+    const int row0 = c * CHUNK;
+    kt.fetch(Ku + size_t(row0) * DK, there - row0);
+    qt.fetch(Qu + size_t(row0) * DK, there - row0);
+    gt.fetch(dOu + size_t(row0) * DV, there - row0, DV);
+    const size_t at = size_t(unit) * chunks + c;
+#pragma unroll
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
+#pragma unroll
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
+        w_next[i] = reinterpret_cast<const u32x4*>(w_cols + at * W_ELEMS)[i * NT + tid];
+  };
+  if (steps > 0) fetch(steps - 1);
+  for (int c = steps - 1; c >= 0; --c) {
+    kt.commit(Ks);
+    qt.commit(Qs);
+    qt.store_factors(rq, inv_eps);
+    gt.commit(Os);
+#pragma unroll
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
+#pragma unroll
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
+    lds_barrier();   // the chunk is there
+    if (c > 0) fetch(c - 1);
+
+    // s P, a tile of columns to a wave (two where there are two waves), queries down: an operand as it stands
+#pragma unroll
+    for (int turn = 0; turn < 4 / NW; ++turn) {
+      const int jt = turn == 0 ? w : 3 - w, own = 16 * jt + r;
+      bf16x8 kf[KS][IN];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf[ks]);
+      for (int p = 0; p < 2; ++p) {
+        if (!w_col_there(jt, p)) continue;
+        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int it = 2 * p + h;
+          if (it < jt) continue;
+          f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            bf16x8 qf[IN];
+            KTile::row_frag(Qs, 16 * it + r, 32 * ks + 8 * q4, qf);
+            t = mm<LEVEL>(qf, kf[ks], t);
+          }
+          t *= four(rq + 16 * it + 4 * q4);
+          if (it > jt) {
+            half[h] = t * (four(rec.in_tile + 16 * it + 4 * q4) * (scale * rec.rk_to_tile[own] * rec.between[it][jt]));
+          } else {
+            const double g_own = rec.decay[own];
+            const float rk_own = scale * rec.rk[own];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int i = 16 * it + 4 * q4 + v;
+              half[h][v] = i >= own ? t[v] * (rk_own * decay_between(rec.decay[i], g_own)) : 0.f;
+            }
+          }
+        }
+        bf16x8 pf[LEVEL];
+        split8<LEVEL>(half[0], half[1], pf);
+        store_frag<LEVEL>(Ps, w_col_frag(jt, p), l, pf);
+      }
+    }
+    bf16x8 gf[2][IN];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) GTile::col_frag(Os, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * w, r, gf[p]);
+    lds_barrier();   // P is there
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 f = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        if (w_col_there(t, p)) {
+          bf16x8 pf[LEVEL];
+          load_frag(Ps, w_col_frag(t, p), l, pf);
+          f = mm<LEVEL>(pf, gf[p], f);
+        }
+      Fs[(w * 4 + t) * 64 + l] = f;
+    }
+    lds_barrier();   // P^T dO' is there
+    if constexpr (Cfg::HANDS_R) {
+      bf16x8 wg[2][LEVEL];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) weighted_rows<LEVEL>(gf[p], rq, rec.since, scale, 32 * p + 4 * q4, wg[p]);
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          bf16x8 qf[IN];
+          KTile::spread_col_frag(Qs, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, qf);
+          x = mm<LEVEL>(qf, wg[p], x);
+        }
+        Rs[(w * 2 * KS + t) * 64 + l] = x;
+      }
+    }
+    lds_barrier();   // everything of the chunk is read, and (G Qh)^T dO' is there
+  }
+}
+
+// The same by waves that do all of it, where the LDS has no room for what one half of the waves hands the other.
+template <typename T, int DK, int NW>
+struct DeltaWideRevCfg {
+  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, PAD = sizeof(T) == 4 && DK == 128 ? 8 : 16;
+  using KTile = PartTile<CHUNK, DK, IN, PAD>;
+  using GTile = PartTile<CHUNK, VC, IN, PAD>;      // rows of dO
+  static constexpr int W_SIZE = W_FRAGS * LEVEL * 512;
+  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + 2 * W_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK;
+  static constexpr int AT_ONCE = (160 * 1024) / LDS_BYTES, MOST = NW <= 4 ? 2 : 1;
+  static constexpr int WAVES = (AT_ONCE < MOST ? AT_ONCE : MOST) * (NW <= 4 ? 1 : 2);   // to a SIMD
+};
+
+template <typename T, int DK, int NW>
+__global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void delta_wide_rev_scan(
+    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
+    const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
+    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, Divisor H, Divisor parts, int N,
+    int units, int DV, float inv_eps) {
+  using Cfg = DeltaWideRevCfg<T, DK, NW>;
+  using KTile = typename Cfg::KTile;
+  using GTile = typename Cfg::GTile;
+  constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, KS = DK / 32, NT = 64 * NW, VC = Cfg::VC;
+  constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
+  __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Os[GTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ws[Cfg::W_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::W_SIZE];
+  __shared__ ChunkRecord rec;
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK];
   fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, H, parts, N, units, DV, inv_eps);
   int unit, part;
   unit_and_segment(blockIdx.x, units, parts, unit, part);
@@ -54,91 +318,71 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
   const T* Ku = K + size_t(unit) * N * DK;
   const T* dOu = dO + size_t(unit) * N * DV + col0;
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
-  const int own = 16 * w + r;   // this lane's token of the chunk
-  const bool active = ST::active(w);
+  // this lane's value column in the first key row, and in the first token row, that it holds
+  const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
 
-  const auto state_at = [&](int x, int y) {
-    return unsigned((16 * ST::key_tile(w, y) + r) * DV + col0 + 16 * ST::value_tile(w, x) + 4 * q4);
-  };
-  f32x4 D[ST::NV][ST::NK];
+  f32x4 D[2 * KS];
 #pragma unroll
-  for (int x = 0; x < ST::NV; ++x)
+  for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-    for (int y = 0; y < ST::NK; ++y) {
-      D[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (dstate != nullptr && active) D[x][y] = *reinterpret_cast<const f32x4*>(dstate + size_t(unit) * DK * DV + state_at(x, y));
-    }
+    for (int v = 0; v < 4; ++v)
+      D[t][v] = dstate != nullptr ? (dstate + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
 
-  RowTile<T, DK> kt, qt;
-  RowTile<T, VC> gt;
-  u32x4 rec_next = {0u, 0u, 0u, 0u};
-  bf16x8 wf[2][LEVEL];
-  const auto fetch_rows = [&](int c) {
+  RowTile<T, DK, Cfg::PAD, NT> kt, qt;
+  RowTile<T, VC, Cfg::PAD, NT> gt;
+  u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
+  const auto fetch = [&](int c) {
     const int row0 = c * CHUNK;
     kt.fetch(Ku + size_t(row0) * DK, there - row0);
     qt.fetch(Qu + size_t(row0) * DK, there - row0);
     gt.fetch(dOu + size_t(row0) * DV, there - row0, DV);
-    if (tid < RECORD_PIECES) rec_next = reinterpret_cast<const u32x4*>(records + size_t(unit) * chunks + c)[tid];
-  };
-  const auto fetch_W = [&](int c) {
-    const uint16_t* from = w_cols + (size_t(unit) * chunks + c) * W_ELEMS;
+    const size_t at = size_t(unit) * chunks + c;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
 #pragma unroll
-      for (int i = 0; i < LEVEL; ++i)
-        if (w_col_there(w, ks))
-          wf[ks][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(from + w_col_frag(w, ks) * 3 * 512 + i * 512 + l * 8));
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
+        w_next[i] = reinterpret_cast<const u32x4*>(w_cols + at * W_ELEMS)[i * NT + tid];
   };
-  if (steps > 0) {
-    fetch_rows(steps - 1);
-    fetch_W(steps - 1);
-  }
+  if (steps > 0) fetch(steps - 1);
   for (int c = steps - 1; c >= 0; --c) {
-    if (active) {
-      float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
-#pragma unroll
-      for (int x = 0; x < ST::NV; ++x)
-#pragma unroll
-        for (int y = 0; y < ST::NK; ++y) {
-          State::store4(Ds, 16 * ST::key_tile(w, y) + r, 16 * ST::value_tile(w, x) + 4 * q4, D[x][y]);
-          *reinterpret_cast<f32x4*>(to + state_at(x, y)) = D[x][y];
-        }
-    }
     kt.commit(Ks);
     qt.commit(Qs);
     qt.store_factors(rq, inv_eps);
     gt.commit(Os);
-    if (tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[tid] = rec_next;
+#pragma unroll
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
+#pragma unroll
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
     __syncthreads();
-
-    // F: what D gives, and the chunk's own rows
-    f32x4 f[NT];
-    if (tid < CHUNK) rq_since[tid] = scale * rec.since[tid] * rq[tid];
+    if (c > 0) fetch(c - 1);
     {
-      bf16x8 kf[KS][IN];
+      float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) f[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf[ks]);
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+    }
+
+    // s P, a tile of columns to a wave (two where there are two waves), queries down: an operand as it stands
+    if (NW <= 4 || w < 4) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          bf16x8 df[LEVEL];
-          State::col_frag(Ds, 32 * ks + 8 * q4, 32 * ks + 8 * q4 + 4, 16 * t, r, df);
-          f[t] = mm<LEVEL>(df, kf[ks], f[t]);
-        }
-      }
-      const float to_end = rec.rk_to_end[own], to_tile = scale * rec.rk_to_tile[own];
+      for (int turn = 0; turn < (NW >= 4 ? 1 : 4 / NW); ++turn) {
+        const int jt = turn == 0 ? w : 3 - w, own = 16 * jt + r;
+        bf16x8 kf[KS][IN];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) f[t] *= to_end;
+        for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf[ks]);
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        if (2 * p + 1 < w) continue;   // queries before the wave's keys
-        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (int p = 0; p < 2; ++p) {
+          if (!w_col_there(jt, p)) continue;
+          f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int it = 2 * p + h;
-          if (it >= w) {
+          for (int h = 0; h < 2; ++h) {
+            const int it = 2 * p + h;
+            if (it < jt) continue;
             f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -146,102 +390,126 @@ __global__ __launch_bounds__(256, (DeltaRevCfg<T, DK, VC>::GROUPS)) void delta_r
               KTile::row_frag(Qs, 16 * it + r, 32 * ks + 8 * q4, qf);
               t = mm<LEVEL>(qf, kf[ks], t);
             }
-            const f32x4 rq4 = *reinterpret_cast<const f32x4*>(rq + 16 * it + 4 * q4);
-            if (it > w) {
-              half[h] = t * rq4 * (*reinterpret_cast<const f32x4*>(rec.in_tile + 16 * it + 4 * q4) * (to_tile * rec.between[it][w]));
+            t *= *reinterpret_cast<const f32x4*>(rq + 16 * it + 4 * q4);
+            if (it > jt) {
+              half[h] = t * (*reinterpret_cast<const f32x4*>(rec.in_tile + 16 * it + 4 * q4) *
+                             (scale * rec.rk_to_tile[own] * rec.between[it][jt]));
             } else {
               const double g_own = rec.decay[own];
               const float rk_own = scale * rec.rk[own];
 #pragma unroll
               for (int v = 0; v < 4; ++v) {
                 const int i = 16 * it + 4 * q4 + v;
-                half[h][v] = i >= own ? t[v] * rq4[v] * (rk_own * decay_between(rec.decay[i], g_own)) : 0.f;
+                half[h][v] = i >= own ? t[v] * (rk_own * decay_between(rec.decay[i], g_own)) : 0.f;
               }
             }
           }
-        }
-        bf16x8 pf[LEVEL];
-        split8<LEVEL>(half[0], half[1], pf);
+          bf16x8 pf[LEVEL];
+          split8<LEVEL>(half[0], half[1], pf);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          bf16x8 gf[IN];
-          GTile::col_frag(Os, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * t, r, gf);
-          f[t] = mm<LEVEL>(gf, pf, f[t]);
+          for (int i = 0; i < LEVEL; ++i)
+            reinterpret_cast<u32x4*>(Ps)[(w_col_frag(jt, p) * LEVEL + i) * 64 + l] = __builtin_bit_cast(u32x4, pf[i]);
         }
       }
     }
-    const float b = rec.beta[own], x_since = -b * rec.rk_since[own], times = rec.times, plus = rec.plus;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) Errors::store4(Fs, own, 16 * t + 4 * q4, b * f[t]);
-    if (c > 0) fetch_rows(c - 1);
-    __syncthreads();
 
-    {
-      f32x4 z[NT];
+    // F: what D gives, and the chunk's own rows
+    f32x4 f[4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) z[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 4; ++t) f[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-        if (w_col_there(w, ks)) {
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 df[LEVEL];
+      split8<LEVEL>(D[2 * ks], D[2 * ks + 1], df);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            bf16x8 ff[LEVEL];
-            Errors::col_frag(Fs, 32 * ks + 8 * q4, 32 * ks + 8 * q4 + 4, 16 * t, r, ff);
-            z[t] = mm<LEVEL>(ff, wf[ks], z[t]);
-          }
-        }
-      float* to = zs + ((size_t(unit) * chunks + c) * CHUNK + own) * DV + col0 + 4 * q4;
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        z[t] = f[t] - z[t];
-        Errors::store4(Xs, own, 16 * t + 4 * q4, x_since * z[t]);
-        *reinterpret_cast<f32x4*>(to + 16 * t) = z[t];
+      for (int t = 0; t < 4; ++t) {
+        bf16x8 kf[IN];
+        KTile::row_frag(Ks, 16 * t + r, 32 * ks + 8 * q4, kf);
+        f[t] = mm<LEVEL>(kf, df, f[t]);
       }
-      if (c > 0) fetch_W(c - 1);
     }
-    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) f[t] *= *reinterpret_cast<const f32x4*>(rec.rk_to_end + 16 * t + 4 * q4);
+    bf16x8 gf[2][IN];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) GTile::col_frag(Os, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * w, r, gf[p]);
+    __syncthreads();   // P is there
+    const auto fragment = [&](const uint16_t* from, int tile, int p, bf16x8 (&x)[LEVEL]) {
+#pragma unroll
+      for (int i = 0; i < LEVEL; ++i)
+        x[i] = __builtin_bit_cast(bf16x8, reinterpret_cast<const u32x4*>(from)[(w_col_frag(tile, p) * LEVEL + i) * 64 + l]);
+    };
+    bf16x8 ff[2][LEVEL], xf[2][LEVEL];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        if (w_col_there(t, p)) {
+          bf16x8 pf[LEVEL];
+          fragment(Ps, t, p, pf);
+          f[t] = mm<LEVEL>(pf, gf[p], f[t]);
+        }
+    f32x4 b[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) b[t] = *reinterpret_cast<const f32x4*>(rec.beta + 16 * t + 4 * q4);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) split8<LEVEL>(b[2 * p] * f[2 * p], b[2 * p + 1] * f[2 * p + 1], ff[p]);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      f32x4 x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int t = 2 * p + h;
+        f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          if (w_col_there(t, k)) {
+            bf16x8 wf[LEVEL];
+            fragment(Ws, t, k, wf);
+            z = mm<LEVEL>(wf, ff[k], z);
+          }
+        z = f[t] - z;
+        float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+        x[h] = -(b[t] * z) * *reinterpret_cast<const f32x4*>(rec.rk_since + 16 * t + 4 * q4);
+      }
+      split8<LEVEL>(x[0], x[1], xf[p]);
+    }
 
-    if (active) {
+    // D in front of the chunk
+    bf16x8 wg[2][LEVEL];
 #pragma unroll
-      for (int x = 0; x < ST::NV; ++x)
+    for (int p = 0; p < 2; ++p) {
+      f32x4 lo, hi;
+      join8<IN>(gf[p], lo, hi);
+      const int t0 = 32 * p + 4 * q4, t1 = t0 + 16;
+      lo *= *reinterpret_cast<const f32x4*>(rq + t0) * (scale * *reinterpret_cast<const f32x4*>(rec.since + t0));
+      hi *= *reinterpret_cast<const f32x4*>(rq + t1) * (scale * *reinterpret_cast<const f32x4*>(rec.since + t1));
+      split8<LEVEL>(lo, hi, wg[p]);
+    }
+    const float times = rec.times, plus = rec.plus;
 #pragma unroll
-        for (int y = 0; y < ST::NK; ++y)
+    for (int t = 0; t < 2 * KS; ++t) {
 #pragma unroll
-          for (int v = 0; v < 4; ++v) D[x][y][v] = __builtin_fmaf(D[x][y][v], plus, D[x][y][v] * times);
+      for (int v = 0; v < 4; ++v) D[t][v] = __builtin_fmaf(D[t][v], plus, D[t][v] * times);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const int t0 = 32 * ks + 8 * q4;
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(rq_since + t0), hi = *reinterpret_cast<const f32x4*>(rq_since + t0 + 4);
-        bf16x8 gf[ST::NV][LEVEL], xf[ST::NV][LEVEL];
-#pragma unroll
-        for (int x = 0; x < ST::NV; ++x) {
-          bf16x8 raw[IN];
-          GTile::col_frag(Os, t0, t0 + 4, 16 * ST::value_tile(w, x), r, raw);
-          f32x4 a, b_;
-          join8<IN>(raw, a, b_);
-          split8<LEVEL>(a * lo, b_ * hi, gf[x]);
-          Errors::col_frag(Xs, t0, t0 + 4, 16 * ST::value_tile(w, x), r, xf[x]);
-        }
-#pragma unroll
-        for (int y = 0; y < ST::NK; ++y) {
-          bf16x8 kf[IN], qf[IN];
-          KTile::col_frag(Ks, t0, t0 + 4, 16 * ST::key_tile(w, y), r, kf);
-          KTile::col_frag(Qs, t0, t0 + 4, 16 * ST::key_tile(w, y), r, qf);
-#pragma unroll
-          for (int x = 0; x < ST::NV; ++x) {
-            D[x][y] = mm<LEVEL>(xf[x], kf, D[x][y]);
-            D[x][y] = mm<LEVEL>(gf[x], qf, D[x][y]);
-          }
-        }
+      for (int p = 0; p < 2; ++p) {
+        bf16x8 kf[IN], qf[IN];
+        KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, kf);
+        KTile::spread_col_frag(Qs, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, qf);
+        D[t] = mm<LEVEL>(kf, xf[p], D[t]);
+        D[t] = mm<LEVEL>(qf, wg[p], D[t]);
       }
     }
-    __syncthreads();
+    __syncthreads();   // everything of the chunk is read
   }
-  if (dstate_in != nullptr && active) {
+  if (dstate_in != nullptr) {
+    float* to = dstate_in + size_t(unit) * DK * DV;
 #pragma unroll
-    for (int x = 0; x < ST::NV; ++x)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-      for (int y = 0; y < ST::NK; ++y) *reinterpret_cast<f32x4*>(dstate_in + size_t(unit) * DK * DV + state_at(x, y)) = D[x][y];
+      for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
   }
 }
 
@@ -617,14 +885,17 @@ __global__ __launch_bounds__(256) void delta_sum_ds(const float* __restrict__ pa
   if (l == 0) ds[out] = float(sum);
 }
 
-template <typename T, int DK>
+template <typename T, int DK, int NW>
 hipError_t run_rev(const DeltaArgs& a) {
-  constexpr int VC = sizeof(T) == 4 && DK == 128 ? 16 : 32;   // (what the LDS holds)
-  const int units = a.B * a.H, parts = a.dv / VC;
-  return launch_kernel("delta_rev_scan", delta_rev_scan<T, DK, VC>, dim3(unsigned(units * parts)), dim3(256), 0, a.stream,
-                       static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.seq_len,
-                       a.dstate, a.dstate_in, static_cast<const ChunkRecord*>(a.records), a.w_cols, a.zs, a.dstates, Divisor(a.H),
-                       Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
+  const int units = a.B * a.H, parts = a.dv / (16 * NW);
+  const auto run = [&](auto kernel, int threads) {
+    return launch_kernel("delta_rev_scan", kernel, dim3(unsigned(units * parts)), dim3(threads), 0, a.stream,
+                         static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.seq_len,
+                         a.dstate, a.dstate_in, static_cast<const ChunkRecord*>(a.records), a.w_cols, a.zs, a.dstates, Divisor(a.H),
+                         Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
+  };
+  if constexpr (DeltaRevCfg<T, DK, NW>::FITS) return run(delta_rev_scan<T, DK, NW>, 128 * NW);
+  else return run(delta_wide_rev_scan<T, DK, NW>, 64 * NW);
 }
 
 template <typename T, int DK, int DV>
@@ -640,7 +911,8 @@ hipError_t run_gradients(const DeltaArgs& a) {
 
 template <typename T, int DK>
 hipError_t run_backward(const DeltaArgs& a) {
-  hipError_t err = run_rev<T, DK>(a);
+  constexpr int MOST = sizeof(T) == 4 && DK == 128 ? 2 : 4;   // waves that the LDS holds the rows of dO for
+  hipError_t err = a.dv == 32 ? run_rev<T, DK, 2>(a) : run_rev<T, DK, MOST>(a);
   if (err != hipSuccess) return err;
   err = a.dv == 32 ? run_gradients<T, DK, 32>(a) : a.dv == 64 ? run_gradients<T, DK, 64>(a) : run_gradients<T, DK, 128>(a);
   if (err != hipSuccess) return err;

@@ -1,9 +1,14 @@
 // The gated delta rule, forward scan (formulas, precision: delta.h).
 //
-// A workgroup walks a (batch, head) chunk by chunk with VC of its value columns: those do not meet one another, the matrices W
-// and P are the same for all.  The state is held in fp32 accumulators, values down, and as parts in LDS for the products that
-// read it.  A step is three products that wait for one another, Kh H, W b Y and Kh^T U, a barrier after each.  Results lie
-// transposed in the accumulators: a lane has four consecutive value columns of one token, whose factors it holds.
+// A workgroup walks a (batch, head) chunk by chunk, a wave for every 16 of its value columns: those do not meet one another, the
+// rows of K and Q and the matrices W and P are the same for all.  A step is three products that wait for one another, Kh H, W b Y
+// and Kh^T U.  Each is formed for the wave's columns with the tokens (or keys) down, and so is the next one's operand in the
+// lanes that it is needed in: the state, Y and U never leave the wave's registers.
+//   What nothing waits for is done beside that by as many waves more: they fetch the rows of the next chunk, form P, and of the
+// parts of the state and of U that the others leave in LDS the results, Q H + P U, transposed, so that four consecutive columns
+// of a token are in a lane.
+//   With rows of tokens to a wave instead, and states and errors handed round through LDS, prompts of 32 x 16 heads of 2048 rows
+// at 128 x 128 took 811 us, the LDS busy in 64 % of the cycles.
 #include "device_common.h"
 #include "delta.h"
 #include "delta_elem.h"
@@ -11,40 +16,312 @@
 namespace cottn {
 namespace {
 
-template <typename T, int DK, int VC, int LEVEL>
+template <typename T, int DK, int NW, int LEVEL>
 struct DeltaFwdCfg {
-  static constexpr int IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>;
+  static constexpr int IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW, KS = DK / 32;
   using KTile = PartTile<CHUNK, DK, IN>;
-  using State = PartTile<DK, VC, LEVEL>;      // [key][value]
-  using Errors = PartTile<CHUNK, VC, LEVEL>;  // [token][value]
-  using Updates = PartTile<CHUNK, VC, OUT>;
-  // the state before the chunk, and when it is read the updates
-  static constexpr int ROOM = State::SIZE > Errors::SIZE + Updates::SIZE ? State::SIZE : Errors::SIZE + Updates::SIZE;
-  static constexpr int LDS_BYTES = 2 * (KTile::SIZE + ROOM + Errors::SIZE) + int(sizeof(ChunkRecord));
-  static constexpr int GROUPS = (160 * 1024) / LDS_BYTES >= 3 ? 3 : (160 * 1024) / LDS_BYTES >= 2 ? 2 : 1;
+  using VTile = PartTile<CHUNK, VC, IN>;
+  static constexpr int W_SIZE = W_FRAGS * LEVEL * 512, P_SIZE = W_FRAGS * OUT * 512, S_SIZE = NW * KS * OUT * 512, U_SIZE = NW * 2 * OUT * 512;
+  static constexpr int BYTES = 2 * (2 * KTile::SIZE + W_SIZE + P_SIZE + S_SIZE + U_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK;
+  // rows of V by way of the LDS (transposed on the way out), where it has room for them
+  static constexpr bool V_IN_LDS = BYTES + 2 * VTile::SIZE <= 160 * 1024;
+  static constexpr bool FITS = BYTES <= 160 * 1024;
 };
 
-template <typename T, int DK, int VC, int LEVEL>
-__global__ __launch_bounds__(256, (DeltaFwdCfg<T, DK, VC, LEVEL>::GROUPS)) void delta_fwd_scan(
+template <typename T, int DK, int NW, int LEVEL>
+__global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
     float* __restrict__ states, Divisor H, Divisor parts, int N, int units, int DV, float inv_eps) {
-  using Cfg = DeltaFwdCfg<T, DK, VC, LEVEL>;
+  using Cfg = DeltaFwdCfg<T, DK, NW, LEVEL>;
   using KTile = typename Cfg::KTile;
-  using State = typename Cfg::State;
-  using Errors = typename Cfg::Errors;
-  using Updates = typename Cfg::Updates;
-  using ST = StateTiles<DK, VC>;
-  constexpr int IN = Cfg::IN, OUT = Cfg::OUT, KS = DK / 32, NT = VC / 16;
+  using VTile = typename Cfg::VTile;
+  constexpr int IN = Cfg::IN, OUT = Cfg::OUT, KS = Cfg::KS, NT = 64 * NW, VC = Cfg::VC;
   typedef __attribute__((ext_vector_type(4))) T vec4;
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
-  __shared__ __attribute__((aligned(16))) uint16_t room[Cfg::ROOM];
-  __shared__ __attribute__((aligned(16))) uint16_t Ys[Errors::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[Cfg::V_IN_LDS ? VTile::SIZE : 8];
+  __shared__ __attribute__((aligned(16))) uint16_t Ws[Cfg::W_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::P_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ss[Cfg::S_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Us[Cfg::U_SIZE];
   __shared__ ChunkRecord rec;
-  uint16_t* const Ss = room;
-  uint16_t* const Ts = room;                  // U as it reaches the chunk's end
-  uint16_t* const Us = room + Errors::SIZE;   // U
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK];
+  fetch_argument_now(Q, K, V, s, lengths, state_in, O, state_out, records, w_rows, errors, states, H, parts, N, units, DV, inv_eps);
+  int unit, part;
+  unit_and_segment(blockIdx.x, units, parts, unit, part);
+  const int tid = threadIdx.x % NT, role = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / NT);
+  const int w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), steps = delta_chunks(there), col0 = part * VC;
+
+  if (role == 0) {
+    // ---- the states
+    const T* Vu = V + size_t(unit) * N * DV + col0;
+    // this lane's value column in the first key row, and in the first token row, that it holds
+    const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
+    f32x4 S[2 * KS];
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        S[t][v] = state_in != nullptr ? (state_in + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+    for (int c = 0; c < steps; ++c) {
+      bf16x8 sf[KS][LEVEL];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        split8<LEVEL>(S[2 * ks], S[2 * ks + 1], sf[ks]);
+        store_frag<OUT>(Ss, w * KS + ks, l, sf[ks]);
+      }
+      if (states != nullptr) {
+        float* to = states + (size_t(unit) * chunks + c) * DK * DV;
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
+      }
+      f32x4 y[4];
+      if constexpr (!Cfg::V_IN_LDS) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int row = c * CHUNK + 16 * t + v;
+            y[t][v] = row + 4 * q4 < there ? float((Vu + size_t(row) * DV)[unsigned(4 * q4 * DV + 16 * w + r)]) : 0.f;
+          }
+      }
+      lds_barrier();   // the chunk is there
+      f32x4 kh[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) kh[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf[4][IN];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) KTile::row_frag(Ks, 16 * t + r, 32 * ks + 8 * q4, kf[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) kh[t] = mm<LEVEL>(kf[t], sf[ks], kh[t]);
+      }
+      bf16x8 yf[2][LEVEL];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if constexpr (Cfg::V_IN_LDS) y[t] = VTile::col4(Vs, 16 * t + 4 * q4, 16 * w, r);
+        const f32x4 since = four(rec.rk_since + 16 * t + 4 * q4);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[t][v] = __builtin_fmaf(-since[v], kh[t][v], y[t][v]);
+      }
+      split8<LEVEL>(y[0], y[1], yf[0]);
+      split8<LEVEL>(y[2], y[3], yf[1]);
+      bf16x8 tf[2][LEVEL];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        f32x4 u[2], t[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int it = 2 * p + h;
+          f32x4 e = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k <= p; ++k) {
+            bf16x8 wf[LEVEL];
+            load_frag(Ws, w_row_frag(it, k), l, wf);
+            e = mm<LEVEL>(wf, yf[k], e);
+          }
+          e = y[it] - e;
+          u[h] = e * four(rec.beta + 16 * it + 4 * q4);
+          t[h] = u[h] * four(rec.rk_to_end + 16 * it + 4 * q4);
+          if (errors != nullptr) {
+            float* to = errors + (size_t(unit) * chunks + c) * CHUNK * DV;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) (to + (16 * it + v) * DV)[at_token] = e[v];
+          }
+        }
+        bf16x8 uf[OUT];
+        split8<OUT>(u[0], u[1], uf);
+        store_frag<OUT>(Us, w * 2 + p, l, uf);
+        split8<LEVEL>(t[0], t[1], tf[p]);
+      }
+      const float times = rec.times, plus = rec.plus;
+      lds_barrier();   // U and P are there
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) S[t][v] = __builtin_fmaf(S[t][v], plus, S[t][v] * times);
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t) {
+          bf16x8 kf[IN];
+          KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, kf);
+          S[t] = mm<LEVEL>(kf, tf[p], S[t]);
+        }
+      lds_barrier();   // everything of the chunk is read
+    }
+    if (state_out != nullptr) {
+      float* to = state_out + size_t(unit) * DK * DV;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
+    }
+    return;
+  }
+
+  // ---- the chunks' rows and the results
+  constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
+  const T* Qu = Q + size_t(unit) * N * DK;
+  const T* Ku = K + size_t(unit) * N * DK;
+  const T* Vu = V + size_t(unit) * N * DV + col0;
+  T* Ou = O + size_t(unit) * N * DV + col0;
+  const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
+  RowTile<T, DK, 16, NT> kt, qt;
+  RowTile<T, VC, 16, NT> vt;
+  u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
+  const auto fetch = [&](int c) {
+    const int row0 = c * CHUNK;
+    kt.fetch(Ku + size_t(row0) * DK, there - row0);
+    qt.fetch(Qu + size_t(row0) * DK, there - row0);
+    if constexpr (Cfg::V_IN_LDS) vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
+    const size_t at = size_t(unit) * chunks + c;
+#pragma unroll
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
+#pragma unroll
+    for (int i = 0; i < W_PIECES; ++i) {   // [fragment][part][lane]: the first LEVEL of three parts
+      const int piece = i * NT + tid;
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || piece < W_FRAGS * LEVEL * 64)
+        w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
+    }
+  };
+  if (steps > 0) fetch(0);
+  for (int c = 0; c < steps; ++c) {
+    const int row0 = c * CHUNK;
+    kt.commit(Ks);
+    qt.commit(Qs);
+    qt.store_factors(rq, inv_eps);
+    if constexpr (Cfg::V_IN_LDS) vt.commit(Vs);
+#pragma unroll
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
+#pragma unroll
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
+    lds_barrier();   // the chunk is there
+    if (c + 1 < steps) fetch(c + 1);
+
+    // P, a tile of rows to a wave (two where there are two waves), keys down: an operand as it stands
+#pragma unroll
+    for (int turn = 0; turn < 4 / NW; ++turn) {
+      const int it = turn == 0 ? w : 3 - w, own = 16 * it + r;
+      const float rq_own = rq[own];
+      bf16x8 qf[KS][IN];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Qs, own, 32 * ks + 8 * q4, qf[ks]);
+      for (int p = 0; w_row_there(it, p) && p < 2; ++p) {
+        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int jt = 2 * p + h;
+          if (jt > it) continue;
+          f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            bf16x8 kf[IN];
+            KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf);
+            t = mm<OUT>(kf, qf[ks], t);
+          }
+          if (jt < it) {
+            half[h] = t * four(rec.rk_to_tile + 16 * jt + 4 * q4) * (rq_own * rec.in_tile[own] * rec.between[it][jt]);
+          } else {
+            const double g_own = rec.decay[own];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int j = 16 * jt + 4 * q4 + v;
+              half[h][v] = j <= own ? t[v] * rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
+            }
+          }
+        }
+        bf16x8 pf[OUT];
+        split8<OUT>(half[0], half[1], pf);
+        store_frag<OUT>(Ps, w_row_frag(it, p), l, pf);
+      }
+    }
+    f32x4 o[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 sf[OUT];
+      load_frag(Ss, w * KS + ks, l, sf);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        bf16x8 qf[IN];
+        KTile::row_frag(Qs, 16 * t + r, 32 * ks + 8 * q4, qf);
+        o[t] = mm<OUT>(sf, qf, o[t]);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] *= rq[16 * t + r] * rec.since[16 * t + r];
+    lds_barrier();   // U and P are there
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      bf16x8 uf[OUT];
+      load_frag(Us, w * 2 + p, l, uf);
+#pragma unroll
+      for (int it = 2 * p; it < 4; ++it) {
+        bf16x8 pf[OUT];
+        load_frag(Ps, w_row_frag(it, p), l, pf);
+        o[it] = mm<OUT>(uf, pf, o[it]);
+      }
+    }
+    if (O != nullptr) {
+#pragma unroll
+      for (int it = 0; it < 4; ++it)
+        if (row0 + 16 * it + r < there)
+          *reinterpret_cast<vec4*>(Ou + (size_t(row0) + 16 * it) * DV + unsigned(r * DV + 16 * w + 4 * q4)) =
+              vec4{T(scale * o[it][0]), T(scale * o[it][1]), T(scale * o[it][2]), T(scale * o[it][3])};
+    }
+    lds_barrier();   // everything of the chunk is read
+  }
+  // rows that do not exist
+  if (O == nullptr) return;
+  for (long i = tid; i < long(N - there) * (VC / 4); i += NT)
+    *reinterpret_cast<vec4*>(Ou + size_t(there + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
+}
+
+// The same by waves that do all of it, for rows of 128 in fp32, whose three parts leave the LDS no room for what one half of the
+// waves hands the other.
+template <typename T, int DK, int NW, int LEVEL>
+struct DeltaWideFwdCfg {
+  static constexpr int IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW;
+  static constexpr bool V_IN_LDS = sizeof(T) == 2;
+  using KTile = PartTile<CHUNK, DK, IN>;
+  using VTile = PartTile<CHUNK, VC, IN>;
+  static constexpr int W_SIZE = W_FRAGS * LEVEL * 512, P_SIZE = W_FRAGS * OUT * 512;
+  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + (V_IN_LDS ? VTile::SIZE : 0) + W_SIZE + P_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK;
+  static constexpr int AT_ONCE = (160 * 1024) / LDS_BYTES, MOST = NW <= 4 ? 2 : 1;
+  static constexpr int WAVES = (AT_ONCE < MOST ? AT_ONCE : MOST) * (NW <= 4 ? 1 : 2);   // to a SIMD
+};
+
+template <typename T, int DK, int NW, int LEVEL>
+__global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)) void delta_wide_fwd_scan(
+    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
+    const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
+    const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
+    float* __restrict__ states, Divisor H, Divisor parts, int N, int units, int DV, float inv_eps) {
+  using Cfg = DeltaWideFwdCfg<T, DK, NW, LEVEL>;
+  using KTile = typename Cfg::KTile;
+  using VTile = typename Cfg::VTile;
+  constexpr int IN = Cfg::IN, OUT = Cfg::OUT, KS = DK / 32, NT = 64 * NW, VC = Cfg::VC;
+  constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
+  typedef __attribute__((ext_vector_type(4))) T vec4;
+  __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[Cfg::V_IN_LDS ? VTile::SIZE : 8];
+  __shared__ __attribute__((aligned(16))) uint16_t Ws[Cfg::W_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::P_SIZE];
+  __shared__ ChunkRecord rec;
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK];
   fetch_argument_now(Q, K, V, s, lengths, state_in, O, state_out, records, w_rows, errors, states, H, parts, N, units, DV, inv_eps);
   int unit, part;
   unit_and_segment(blockIdx.x, units, parts, unit, part);
@@ -55,122 +332,123 @@ __global__ __launch_bounds__(256, (DeltaFwdCfg<T, DK, VC, LEVEL>::GROUPS)) void 
   const T* Vu = V + size_t(unit) * N * DV + col0;
   T* Ou = O + size_t(unit) * N * DV + col0;
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
-  const int own = 16 * w + r;   // this lane's token of the chunk
-  const unsigned own_q = unsigned(own * DK + 8 * q4), own_v = unsigned(own * DV + 4 * q4);
-  const bool active = ST::active(w);
+  // this lane's value column in the first key row, and in the first token row, that it holds
+  const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
 
-  const auto state_at = [&](int x, int y) {
-    return unsigned((16 * ST::key_tile(w, y) + r) * DV + col0 + 16 * ST::value_tile(w, x) + 4 * q4);
-  };
-  f32x4 S[ST::NV][ST::NK];
+  f32x4 S[2 * KS];
 #pragma unroll
-  for (int x = 0; x < ST::NV; ++x)
+  for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-    for (int y = 0; y < ST::NK; ++y) {
-      S[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (state_in != nullptr && active) S[x][y] = *reinterpret_cast<const f32x4*>(state_in + size_t(unit) * DK * DV + state_at(x, y));
-    }
+    for (int v = 0; v < 4; ++v)
+      S[t][v] = state_in != nullptr ? (state_in + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
 
-  RowTile<T, DK> kt;
-  Raw8<T> qraw[KS];
-  vec4 vraw[NT];
-  u32x4 rec_next = {0u, 0u, 0u, 0u};
-  bf16x8 wf[2][LEVEL];
-  const auto fetch_rows = [&](int c) {
+  RowTile<T, DK, 16, NT> kt, qt;
+  RowTile<T, VC, 16, NT> vt;
+  T vraw[4][4];
+  u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
+  const auto fetch = [&](int c) {
     const int row0 = c * CHUNK;
     kt.fetch(Ku + size_t(row0) * DK, there - row0);
-    const T* Qc = Qu + size_t(row0) * DK;
-    const T* Vc = Vu + size_t(row0) * DV;
-    if (row0 + own < there) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qraw[ks].load(Qc + own_q + 32 * ks);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) vraw[t] = *reinterpret_cast<const vec4*>(Vc + own_v + 16 * t);
+    qt.fetch(Qu + size_t(row0) * DK, there - row0);
+    if constexpr (Cfg::V_IN_LDS) {
+      vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
     } else {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qraw[ks].zero();
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) vraw[t] = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
+        for (int v = 0; v < 4; ++v) {
+          const int row = 16 * t + 4 * q4 + v;
+          vraw[t][v] = T(0.f);
+          if (row0 + row < there) vraw[t][v] = (Vu + (size_t(row0) + 16 * t + v) * DV)[unsigned(4 * q4 * DV + 16 * w + r)];
+        }
     }
-    if (tid < RECORD_PIECES) rec_next = reinterpret_cast<const u32x4*>(records + size_t(unit) * chunks + c)[tid];
-  };
-  const auto fetch_W = [&](int c) {
-    const uint16_t* from = w_rows + (size_t(unit) * chunks + c) * W_ELEMS;
+    const size_t at = size_t(unit) * chunks + c;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
 #pragma unroll
-      for (int i = 0; i < LEVEL; ++i)
-        if (w_row_there(w, ks))
-          wf[ks][i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(from + w_row_frag(w, ks) * 3 * 512 + i * 512 + l * 8));
+    for (int i = 0; i < W_PIECES; ++i) {   // [fragment][part][lane]: the first LEVEL of three parts
+      const int piece = i * NT + tid;
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || piece < W_FRAGS * LEVEL * 64)
+        w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
+    }
   };
-  if (steps > 0) {
-    fetch_rows(0);
-    fetch_W(0);
-  }
+  if (steps > 0) fetch(0);
   for (int c = 0; c < steps; ++c) {
     const int row0 = c * CHUNK;
-    if (active) {
-#pragma unroll
-      for (int x = 0; x < ST::NV; ++x)
-#pragma unroll
-        for (int y = 0; y < ST::NK; ++y)
-          State::store4(Ss, 16 * ST::key_tile(w, y) + r, 16 * ST::value_tile(w, x) + 4 * q4, S[x][y]);
-      if (states != nullptr) {
-        float* to = states + (size_t(unit) * chunks + c) * DK * DV;
-#pragma unroll
-        for (int x = 0; x < ST::NV; ++x)
-#pragma unroll
-          for (int y = 0; y < ST::NK; ++y) *reinterpret_cast<f32x4*>(to + state_at(x, y)) = S[x][y];
-      }
-    }
     kt.commit(Ks);
-    if (tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[tid] = rec_next;
+    qt.commit(Qs);
+    qt.store_factors(rq, inv_eps);
+    if constexpr (Cfg::V_IN_LDS) vt.commit(Vs);
+#pragma unroll
+    for (int i = 0; i < REC_PIECES; ++i)
+      if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
+#pragma unroll
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
+    f32x4 y[4];
+    if constexpr (!Cfg::V_IN_LDS) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) y[t] = f32x4{float(vraw[t][0]), float(vraw[t][1]), float(vraw[t][2]), float(vraw[t][3])};
+    }
     __syncthreads();
+    if (c + 1 < steps) fetch(c + 1);
+    if (states != nullptr) {
+      float* to = states + (size_t(unit) * chunks + c) * DK * DV;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
+    }
 
-    // what the state before the chunk gives: Kh H and Qh H; and P, keys down
-    f32x4 y[NT], o[NT];
-    bf16x8 pf[2][OUT];
-    {
-      bf16x8 qf[KS][IN];
-      float rq = 0.f;
+    // what the state before the chunk gives: Kh H, and Qh H
+    f32x4 kh[4], o[4];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qraw[ks].parts(qf[ks]);
-        rq += qraw[ks].sum_sq();
-      }
-      rq += __shfl_xor(rq, 16, 64);
-      rq = row_factor(rq + __shfl_xor(rq, 32, 64), inv_eps);
+    for (int t = 0; t < 4; ++t) kh[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < NT; ++t) y[t] = o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 sf[LEVEL], kf[4][IN], qf[4][IN];
+      split8<LEVEL>(S[2 * ks], S[2 * ks + 1], sf);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        bf16x8 kf[IN], sf[NT][LEVEL];
-        KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf);
+      for (int t = 0; t < 4; ++t) KTile::row_frag(Ks, 16 * t + r, 32 * ks + 8 * q4, kf[t]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) State::col_frag(Ss, 32 * ks + 8 * q4, 32 * ks + 8 * q4 + 4, 16 * t, r, sf[t]);
+      for (int t = 0; t < 4; ++t) KTile::row_frag(Qs, 16 * t + r, 32 * ks + 8 * q4, qf[t]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) y[t] = mm<LEVEL>(sf[t], kf, y[t]);
+      for (int t = 0; t < 4; ++t) kh[t] = mm<LEVEL>(kf[t], sf, kh[t]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) o[t] = mm<OUT>(sf[t], qf[ks], o[t]);
-      }
-      const float before = -rec.rk_since[own];
+      for (int t = 0; t < 4; ++t) o[t] = mm<OUT>(sf, qf[t], o[t]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 yf[2][LEVEL];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < 4; ++t) {
+      if constexpr (Cfg::V_IN_LDS) y[t] = VTile::col4(Vs, 16 * t + 4 * q4, 16 * w, r);
+      const f32x4 since = *reinterpret_cast<const f32x4*>(rec.rk_since + 16 * t + 4 * q4);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) y[t][v] = __builtin_fmaf(before, y[t][v], float(vraw[t][v]));
-        Errors::store4(Ys, own, 16 * t + 4 * q4, y[t]);
-      }
-      const float since = rq * rec.since[own];
+      for (int v = 0; v < 4; ++v) y[t][v] = __builtin_fmaf(-since[v], kh[t][v], y[t][v]);
+    }
+    split8<LEVEL>(y[0], y[1], yf[0]);
+    split8<LEVEL>(y[2], y[3], yf[1]);
+
+    __builtin_amdgcn_sched_barrier(0);
+    // P, a tile of rows to a wave (two where there are two waves), keys down: an operand as it stands
+    if (NW <= 4 || w < 4) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) o[t] *= since;
-      const float in_tile = rq * rec.in_tile[own];
+      for (int turn = 0; turn < (NW >= 4 ? 1 : 4 / NW); ++turn) {
+        const int it = turn == 0 ? w : 3 - w, own = 16 * it + r;
+        const float rq_own = rq[own];
+        bf16x8 qf[KS][IN];
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Qs, own, 32 * ks + 8 * q4, qf[ks]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int jt = 2 * p + h;
-          if (jt <= w) {
+        for (int p = 0; p < 2; ++p) {
+          if (!w_row_there(it, p)) break;
+          f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int jt = 2 * p + h;
+            if (jt > it) break;
             f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -178,123 +456,128 @@ __global__ __launch_bounds__(256, (DeltaFwdCfg<T, DK, VC, LEVEL>::GROUPS)) void 
               KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf);
               t = mm<OUT>(kf, qf[ks], t);
             }
-            if (jt < w) {
-              half[h] = t * *reinterpret_cast<const f32x4*>(rec.rk_to_tile + 16 * jt + 4 * q4) * (in_tile * rec.between[w][jt]);
+            if (jt < it) {
+              half[h] = t * *reinterpret_cast<const f32x4*>(rec.rk_to_tile + 16 * jt + 4 * q4) *
+                        (rq_own * rec.in_tile[own] * rec.between[it][jt]);
             } else {
               const double g_own = rec.decay[own];
 #pragma unroll
               for (int v = 0; v < 4; ++v) {
                 const int j = 16 * jt + 4 * q4 + v;
-                half[h][v] = j <= own ? t[v] * rec.rk[j] * (rq * decay_between(g_own, rec.decay[j])) : 0.f;
+                half[h][v] = j <= own ? t[v] * rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
               }
             }
           }
+          bf16x8 pf[OUT];
+          split8<OUT>(half[0], half[1], pf);
+#pragma unroll
+          for (int i = 0; i < OUT; ++i)
+            reinterpret_cast<u32x4*>(Ps)[(w_row_frag(it, p) * OUT + i) * 64 + l] = __builtin_bit_cast(u32x4, pf[i]);
         }
-        split8<OUT>(half[0], half[1], pf[p]);
       }
     }
-    const float b = rec.beta[own], b_to_end = b * rec.rk_to_end[own], times = rec.times, plus = rec.plus;
-    if (c + 1 < steps) fetch_rows(c + 1);
-    __syncthreads();
 
+    __builtin_amdgcn_sched_barrier(0);
     // the errors and the updates
-    {
-      f32x4 e[NT];
+    bf16x8 uf[2][OUT], tf[2][LEVEL];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) e[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < 2; ++p) {
+      f32x4 e[2], u[2], t[2];
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-        if (w_row_there(w, ks)) {
+      for (int h = 0; h < 2; ++h) {
+        const int it = 2 * p + h;
+        e[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            bf16x8 yf[LEVEL];
-            Errors::col_frag(Ys, 32 * ks + 8 * q4, 32 * ks + 8 * q4 + 4, 16 * t, r, yf);
-            e[t] = mm<LEVEL>(yf, wf[ks], e[t]);
-          }
+        for (int k = 0; k <= p; ++k) {
+          bf16x8 wf[LEVEL];
+#pragma unroll
+          for (int i = 0; i < LEVEL; ++i)
+            wf[i] = __builtin_bit_cast(bf16x8, reinterpret_cast<const u32x4*>(Ws)[(w_row_frag(it, k) * LEVEL + i) * 64 + l]);
+          e[h] = mm<LEVEL>(wf, yf[k], e[h]);
         }
+        e[h] = y[it] - e[h];
+        u[h] = e[h] * *reinterpret_cast<const f32x4*>(rec.beta + 16 * it + 4 * q4);
+        t[h] = u[h] * *reinterpret_cast<const f32x4*>(rec.rk_to_end + 16 * it + 4 * q4);
+        if (errors != nullptr) {
+          float* to = errors + (size_t(unit) * chunks + c) * CHUNK * DV;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        e[t] = y[t] - e[t];
-        Errors::store4(Ts, own, 16 * t + 4 * q4, b_to_end * e[t]);
-        Updates::store4(Us, own, 16 * t + 4 * q4, b * e[t]);
+          for (int v = 0; v < 4; ++v) (to + (16 * it + v) * DV)[at_token] = e[h][v];
+        }
       }
-      if (errors != nullptr) {
-        float* to = errors + (size_t(unit) * chunks + c) * CHUNK * DV + col0 + own_v;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4*>(to + 16 * t) = e[t];
-      }
-      if (c + 1 < steps) fetch_W(c + 1);
+      split8<OUT>(u[0], u[1], uf[p]);
+      split8<LEVEL>(t[0], t[1], tf[p]);
     }
-    __syncthreads();
 
-    // the state behind the chunk, and the rows' results
-    if (active) {
+    __builtin_amdgcn_sched_barrier(0);
+    // the state behind the chunk
+    const float times = rec.times, plus = rec.plus;
 #pragma unroll
-      for (int x = 0; x < ST::NV; ++x)
+    for (int t = 0; t < 2 * KS; ++t) {
 #pragma unroll
-        for (int k = 0; k < ST::NK; ++k)
+      for (int v = 0; v < 4; ++v) S[t][v] = __builtin_fmaf(S[t][v], plus, S[t][v] * times);
 #pragma unroll
-          for (int v = 0; v < 4; ++v) S[x][k][v] = __builtin_fmaf(S[x][k][v], plus, S[x][k][v] * times);
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const int t0 = 32 * ks + 8 * q4;
-        bf16x8 uf[ST::NV][LEVEL];
-#pragma unroll
-        for (int x = 0; x < ST::NV; ++x) Errors::col_frag(Ts, t0, t0 + 4, 16 * ST::value_tile(w, x), r, uf[x]);
-#pragma unroll
-        for (int k = 0; k < ST::NK; ++k) {
-          bf16x8 kf[IN];
-          KTile::col_frag(Ks, t0, t0 + 4, 16 * ST::key_tile(w, k), r, kf);
-#pragma unroll
-          for (int x = 0; x < ST::NV; ++x) S[x][k] = mm<LEVEL>(uf[x], kf, S[x][k]);
-        }
+      for (int p = 0; p < 2; ++p) {
+        bf16x8 kf[IN];
+        KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, kf);
+        S[t] = mm<LEVEL>(kf, tf[p], S[t]);
       }
     }
+    __syncthreads();   // P is there
+
+    // the rows' results
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
-      if (2 * p <= w) {
+    for (int it = 0; it < 4; ++it) {
+      o[it] *= rq[16 * it + r] * rec.since[16 * it + r];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          bf16x8 uf[OUT];
-          Updates::col_frag(Us, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * t, r, uf);
-          o[t] = mm<OUT>(uf, pf[p], o[t]);
+      for (int p = 0; p < 2; ++p)
+        if (w_row_there(it, p)) {
+          bf16x8 pf[OUT];
+#pragma unroll
+          for (int i = 0; i < OUT; ++i)
+            pf[i] = __builtin_bit_cast(bf16x8, reinterpret_cast<const u32x4*>(Ps)[(w_row_frag(it, p) * OUT + i) * 64 + l]);
+          o[it] = mm<OUT>(uf[p], pf, o[it]);
         }
-      }
-    if (O != nullptr && row0 + own < there) {
-      T* to = Ou + size_t(row0) * DV + own_v;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        *reinterpret_cast<vec4*>(to + 16 * t) = vec4{T(scale * o[t][0]), T(scale * o[t][1]), T(scale * o[t][2]), T(scale * o[t][3])};
+      if (O != nullptr && row0 + 16 * it + r < there)
+        *reinterpret_cast<vec4*>(Ou + (size_t(row0) + 16 * it) * DV + unsigned(r * DV + 16 * w + 4 * q4)) =
+            vec4{T(scale * o[it][0]), T(scale * o[it][1]), T(scale * o[it][2]), T(scale * o[it][3])};
     }
     __syncthreads();   // everything of the chunk is read
   }
-  if (state_out != nullptr && active) {
+  if (state_out != nullptr) {
+    float* to = state_out + size_t(unit) * DK * DV;
 #pragma unroll
-    for (int x = 0; x < ST::NV; ++x)
+    for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-      for (int y = 0; y < ST::NK; ++y) *reinterpret_cast<f32x4*>(state_out + size_t(unit) * DK * DV + state_at(x, y)) = S[x][y];
+      for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
   }
   // rows that do not exist
   if (O == nullptr) return;
-  for (long i = tid; i < long(N - there) * (VC / 4); i += 256)
+  for (long i = tid; i < long(N - there) * (VC / 4); i += NT)
     *reinterpret_cast<vec4*>(Ou + size_t(there + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
 }
 
-template <typename T, int DK, int VC, int LEVEL>
+template <typename T, int DK, int NW, int LEVEL>
 hipError_t run_scan(const DeltaArgs& a) {
-  const int units = a.B * a.H, parts = a.dv / VC;
-  return launch_kernel("delta_fwd_scan", delta_fwd_scan<T, DK, VC, LEVEL>, dim3(unsigned(units * parts)), dim3(256), 0, a.stream,
-                       static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len,
-                       a.state_in, static_cast<T*>(a.O), a.state, static_cast<const ChunkRecord*>(a.records), a.w_rows, a.errors,
-                       a.states, Divisor(a.H), Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
+  const int units = a.B * a.H, parts = a.dv / (16 * NW);
+  const auto run = [&](auto kernel, int threads) {
+    return launch_kernel("delta_fwd_scan", kernel, dim3(unsigned(units * parts)), dim3(threads), 0, a.stream,
+                         static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len,
+                         a.state_in, static_cast<T*>(a.O), a.state, static_cast<const ChunkRecord*>(a.records), a.w_rows, a.errors,
+                         a.states, Divisor(a.H), Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
+  };
+  if constexpr (DeltaFwdCfg<T, DK, NW, LEVEL>::FITS) return run(delta_fwd_scan<T, DK, NW, LEVEL>, 128 * NW);
+  else return run(delta_wide_fwd_scan<T, DK, NW, LEVEL>, 64 * NW);
 }
 
+template <typename T, int DK, int LEVEL>
+hipError_t run_level(const DeltaArgs& a) {
+  return a.dv == 32 ? run_scan<T, DK, 2, LEVEL>(a) : run_scan<T, DK, 4, LEVEL>(a);
+}
 template <typename T, int DK>
 hipError_t run_shape(const DeltaArgs& a) {
-  constexpr int MOST = 3;
   // without fp32 results two parts do
-  if (sizeof(T) == 2 && a.state == nullptr && a.errors == nullptr) return run_scan<T, DK, 32, RESULT_LEVEL<T>>(a);
-  return run_scan<T, DK, 32, MOST>(a);
+  if (sizeof(T) == 2 && a.state == nullptr && a.errors == nullptr) return run_level<T, DK, RESULT_LEVEL<T>>(a);
+  return run_level<T, DK, 3>(a);
 }
 
 }  // namespace

@@ -160,21 +160,21 @@ __global__ __launch_bounds__(256, 3) void delta_prepare(const T* __restrict__ K,
     bf16x8 f[3];
     if (w_row_there(w, ks)) {
       // W b: its columns take the factors of the rows that they are multiplied by
-      const float* from = As + (16 * w + r) * WP + 32 * ks + 8 * q4;
-      const float* b = rec.beta + 32 * ks + 8 * q4;
+      const float* from = As + (16 * w + r) * WP + 32 * ks + 4 * q4;
+      const float* b = rec.beta + 32 * ks + 4 * q4;
       split8<3>(*reinterpret_cast<const f32x4*>(from) * *reinterpret_cast<const f32x4*>(b),
-                *reinterpret_cast<const f32x4*>(from + 4) * *reinterpret_cast<const f32x4*>(b + 4), f);
+                *reinterpret_cast<const f32x4*>(from + 16) * *reinterpret_cast<const f32x4*>(b + 16), f);
       uint16_t* to = w_rows + size_t(blockIdx.x) * W_ELEMS + w_row_frag(w, ks) * 3 * 512 + l * 8;
 #pragma unroll
       for (int i = 0; i < 3; ++i) *reinterpret_cast<u32x4*>(to + i * 512) = __builtin_bit_cast(u32x4, f[i]);
     }
     if (w_cols != nullptr && w_col_there(w, ks)) {
-      const float* from = As + (32 * ks + 8 * q4) * WP + 16 * w + r;
+      const float* from = As + (32 * ks + 4 * q4) * WP + 16 * w + r;
       f32x4 lo, hi;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         lo[i] = from[i * WP];
-        hi[i] = from[(4 + i) * WP];
+        hi[i] = from[(16 + i) * WP];
       }
       split8<3>(lo, hi, f);
       uint16_t* to = w_cols + size_t(blockIdx.x) * W_ELEMS + w_col_frag(w, ks) * 3 * 512 + l * 8;

@@ -10,6 +10,8 @@ contractions: five chunks, the longest sequences here, add up to sqrt(5) times t
 products in two parts 2^-14.
   Elements.  The same with all signs alike, 5 x 768 of 2^-24 = 2^-12, of the largest value of the sequence and head; in two parts
 2^-14 sqrt(192) more, 2^-10.
+  ds is the sum of a token's dO . o / s over all tokens, each off by as much of itself: by as much of the root of the sum of their
+squares (ds_terms), which the sum itself may be far below.
 """
 import torch
 
@@ -67,19 +69,30 @@ def gradients(Q, K, V, s, log_decay, beta, dO, lens=None, state_in=None, dstate=
     return {n: torch.zeros_like(t) if g is None else g for n, t, g in zip(names, x + [S], got)}
 
 
-def check(name, got, want, dtype, two_parts=False, more=0.0):
-    """got: a result in fp32 or in `dtype`; want: float64, [B, H, ..] or [H]; more: added to either bound, relative."""
+def ds_terms(O, dO, s, lens=None):
+    """The root of the sum of the squares of what ds adds up, [H], or with lens [B, H]."""
+    there = torch.ones(dO.shape[:3], dtype=torch.bool)
+    if lens is not None:
+        there = (torch.arange(dO.shape[2]) < torch.as_tensor(lens)[:, None])[:, None].expand(dO.shape[:3])
+    t = torch.where(there, (O * dO.double()).sum(-1) / s.double().view(-1, O.shape[1], 1), torch.zeros(1, dtype=torch.float64))
+    return torch.sqrt((t * t).sum((0, 2) if lens is None else 2))
+
+
+def check(name, got, want, dtype, two_parts=False, more=0.0, terms=None):
+    """got: a result in fp32 or in `dtype`; want: float64, [B, H, ..] or [H]; more: added to either bound, relative; terms: what
+    the result's own magnitude is replaced by where that is less."""
     got = got.detach().double().cpu()
     assert got.shape == want.shape, name
     assert bool(torch.isfinite(got).all()), name
     u = U["f32"] if dtype is None else U[dtype]
-    norm, off = float(want.norm()), float((got - want).norm())
+    size = want.abs() if terms is None else torch.maximum(want.abs(), terms)
+    norm, off = float(size.norm()), float((got - want).norm())
     if norm == 0.0:
         assert off == 0.0, name
         return
     rel = 0.58 * u + 63 * U["f32"] + (2.0 ** -14 if two_parts else 0.0) + more
     assert off <= rel * norm, "%s: norm error %.3g of %.3g" % (name, off / norm, rel)
-    most = want.abs().flatten(2).amax(2).view(want.shape[:2] + (1,) * (want.dim() - 2)) if want.dim() > 2 else want.abs().max()
+    most = want.abs().flatten(2).amax(2).view(want.shape[:2] + (1,) * (want.dim() - 2)) if want.dim() > 2 else size.max()
     bound = u * want.abs() + (2.0 ** -12 + (2.0 ** -10 if two_parts else 0.0) + more) * most
     worst = float(((got - want).abs() / torch.where(bound > 0, bound, torch.full_like(bound, 1e-300))).max())
     assert worst <= 1.0, "%s: %.3g of the bound" % (name, worst)

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import delta_reference as ref
-from delta_reference import TYPES, check
+from delta_reference import TYPES, check, ds_terms
 
 pytestmark = pytest.mark.gpu
 WIDTHS = list(itertools.product((32, 64, 128), repeat=2))
@@ -45,6 +45,11 @@ def train_workspace(cottn, x):
     return torch.empty(n, dtype=torch.uint8, device="cuda")
 
 
+def check_gradients(got, want, dtype, terms, off=0.0):
+    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
+        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None, more=off, terms=terms if name == "ds" else None)
+
+
 def run_both(cottn, x, more, dtype, lens=None, states=True, off=0.0):
     want_O, want_S = ref.forward(**double(x), lens=lens, state_in=more["state_in"].double() if states else None)
     want = ref.gradients(**double(x), dO=more["dO"].double(), lens=lens, state_in=more["state_in"].double() if states else None,
@@ -62,8 +67,7 @@ def run_both(cottn, x, more, dtype, lens=None, states=True, off=0.0):
     if states:
         check("state", state, want_S, None, more=off)
         check("dstate_in", dstate_in, want["dstate_in"], None, more=off)
-    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
-        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None, more=off)
+    check_gradients(got, want, dtype, ds_terms(want_O, more["dO"], x["s"], lens), off)
     return d, m, O, state, got
 
 
@@ -110,8 +114,7 @@ def run_both_padded(cottn, x, more, dtype, lens):
     check("O", O, want_O, dtype)
     check("state", state, want_S, None)
     check("dstate_in", dstate_in, want["dstate_in"], None)
-    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
-        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None)
+    check_gradients(got, want, dtype, ds_terms(want_O, more_clean["dO"], clean["s"], lens))
     return d, m, O, state, got
 
 
@@ -134,8 +137,9 @@ def test_no_decay(cottn, dtype):
     got = cottn.cottn_bwd_causal_delta(**d, dO=more["dO"].cuda())
     assert got[4] is None
     check("O", O, want_O, dtype, two_parts=True)
+    terms = ds_terms(want_O, more["dO"], x["s"])
     for name, t in zip(("dQ", "dK", "dV", "ds"), got):
-        check(name, t, want[name], dtype if name != "ds" else None)
+        check(name, t, want[name], dtype if name != "ds" else None, terms=terms if name == "ds" else None)
     check("dbeta", got[5], want["dbeta"], None)
 
 
@@ -157,8 +161,7 @@ def test_strong_decays(cottn, dtype):
     got = cottn.cottn_bwd_causal_delta(**d, dO=m["dO"], state_in=m["state_in"])
     check("O", O, want_O, dtype)
     check("state", state, want_S, None)
-    for name, t in zip(("dQ", "dK", "dV", "ds", "dlog_decay", "dbeta"), got):
-        check(name, t, want[name], dtype if name in ("dQ", "dK", "dV") else None)
+    check_gradients(got, want, dtype, ds_terms(want_O, more["dO"], x["s"]))
 
 
 @pytest.mark.parametrize("beta", [0.0, 1.0, 2.0])
@@ -216,7 +219,7 @@ def test_pieces_are_the_whole(cottn, dtype):
         grads.insert(0, cottn.cottn_bwd_causal_delta(**pieces[i], dO=part(m["dO"], cuts[i]), state_in=before[i], dstate=D, dstate_in=D,
                                                      fwd_workspace=spaces[i] if i != 1 else None))
     check("dstate_in", D, want["dstate_in"], None)
-    check("ds", sum(g[3] for g in grads), want["ds"], None)
+    check("ds", sum(g[3] for g in grads), want["ds"], None, terms=ds_terms(want_O, more["dO"], x["s"]))
     for i, name in ((0, "dQ"), (1, "dK"), (2, "dV"), (4, "dlog_decay"), (5, "dbeta")):
         check(name, torch.cat([g[i] for g in grads], 2), want[name], dtype if i < 3 else None)
 
