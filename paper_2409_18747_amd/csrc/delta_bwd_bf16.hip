@@ -518,7 +518,7 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
 // of H and D once; accumulators hold them transposed, four consecutive columns of a token in a lane.
 template <typename T, int DK, int DV>
 struct DeltaGradCfg {
-  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, PAD = sizeof(T) == 4 ? 8 : 16;
+  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, PAD = 8;
   using KTile = PartTile<CHUNK, DK, IN, PAD>;
   using GTile = PartTile<CHUNK, DV, IN, PAD>;
   using ETile = PartTile<CHUNK, DV, LEVEL, PAD>;
@@ -594,6 +594,16 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     return;
   }
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
+  // wave w: key tiles kt0 .. kt0 + NK - 1, token tiles tt0 .. tt0 + NTOK - 1
+  const int kt0 = Cfg::KT >= 4 ? w * NK : w % 2, tt0 = Cfg::KT >= 4 ? 0 : w / 2 * 2;
+  f32x4 hd[NK][4];   // eight values of a key's row of H, and of D, 32 columns ahead
+  const auto fetch_states = [&](int x, int vs) {
+    const size_t at = size_t(blockIdx.x) * DK * DV + size_t(16 * (kt0 + x) + r) * DV + 32 * vs + 8 * q4;
+    hd[x][0] = reinterpret_cast<const f32x4*>(states + at)[0];
+    hd[x][1] = reinterpret_cast<const f32x4*>(states + at)[1];
+    hd[x][2] = reinterpret_cast<const f32x4*>(dstates + at)[0];
+    hd[x][3] = reinterpret_cast<const f32x4*>(dstates + at)[1];
+  };
   RowTile<T, DK, Cfg::PAD> kt, qt;
   {
     using RT = RowTile<T, DV, Cfg::PAD>;
@@ -638,10 +648,10 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     }
     qt.store_factors(rq, inv_eps);
   }
+#pragma unroll
+  for (int x = 0; x < NK; ++x) fetch_states(x, 0);
   __syncthreads();
 
-  // wave w: key tiles kt0 .. kt0 + NK - 1, token tiles tt0 .. tt0 + NTOK - 1
-  const int kt0 = Cfg::KT >= 4 ? w * NK : w % 2, tt0 = Cfg::KT >= 4 ? 0 : w / 2 * 2;
   f32x4 aq[NK][NTOK], ak[NK][NTOK];
   float through = 0.f;   // <D, H>, of the wave's rows
   {
@@ -654,10 +664,8 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     for (int vs = 0; vs < VS; ++vs) {
 #pragma unroll
       for (int x = 0; x < NK; ++x) {
-        const size_t at = size_t(blockIdx.x) * DK * DV + size_t(16 * (kt0 + x) + r) * DV + 32 * vs + 8 * q4;
-        const f32x4* hp = reinterpret_cast<const f32x4*>(states + at);
-        const f32x4* dp = reinterpret_cast<const f32x4*>(dstates + at);
-        const f32x4 h0 = hp[0], h1 = hp[1], d0 = dp[0], d1 = dp[1];
+        const f32x4 h0 = hd[x][0], h1 = hd[x][1], d0 = hd[x][2], d1 = hd[x][3];
+        if (vs + 1 < VS) fetch_states(x, vs + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) through = __builtin_fmaf(h0[i], d0[i], __builtin_fmaf(h1[i], d1[i], through));
         bf16x8 hf[LEVEL], df[LEVEL];
