@@ -370,27 +370,53 @@ size_t decay_workspace_bytes(int op, int B, int H, int dk, int dv, const DecayPl
   return op != COTTN_OP_BWD_DECAY ? states : 2 * states + round_up_256(size_t(units) * p.G * sizeof(float));
 }
 
-// ---- the gated delta rule: what a workspace holds (launch.h: DeltaArgs), one array after the other
+// ---- the gated delta rule: the split of a sequence, and what a workspace holds (launch.h: DeltaArgs), one array after the other
 struct DeltaSpace {
-  size_t records, w_rows, alone, w_cols, errors, states, forward;      // a forward's; `alone`, `forward`: bytes of the two kinds
-  size_t zs, dstates, ds_parts, saved;                                // a backward's that is handed one; `saved`: its bytes
+  int G, seg;
+  size_t records, w_rows, starts, transitions, alone, w_cols, errors, states, forward;   // a forward's; `alone`, `forward`: bytes of the two kinds
+  size_t zs, dstates, ds_parts, ends, saved;                                             // a backward's that is handed one; `saved`: its bytes
 };
+// Time of a forward in G segments, in steps of a workgroup, of which a compute unit has one.  More than one segment walk the
+// rows twice, once for the totals of all but the last, with the columns of M beside those of the values, and the states at their
+// starts are found one after the other; two launches more.
+double delta_steps(long units, long chunks, long G, int dk, int dv) {
+  const long per = dv == 32 ? 32 : 64, parts = dv / per, seg = (chunks + G - 1) / G;
+  const auto rounds = [](long workgroups) { return double((workgroups + kComputeUnits - 1) / kComputeUnits); };
+  const double whole = rounds(units * parts * G) * double(seg);
+  if (G == 1) return whole;
+  return whole + 0.8 * rounds(units * (parts * (G - 1) + (dk + per - 1) / per * (G - 1))) * double(seg) + (dk == 128 ? 1.5 : 0.6) * double(G) + 4.0;
+}
 bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, DeltaSpace* p) {
   if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
   if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != 64)) return false;
   const long units = long(B) * H, chunks = (long(N) + 63) / 64;
   if (!threads_fit(units * std::max<long>(chunks, dv / 16), 256)) return false;
+  long G = g_tuned_segments;
+  if (G <= 0) {
+    G = 1;
+    for (long g = 2; g <= 64 && g <= chunks && units * g <= 4 * kComputeUnits; ++g)
+      if (delta_steps(units, chunks, g, dk, dv) < 0.9 * delta_steps(units, chunks, G, dk, dv)) G = g;
+  }
+  if (G > chunks) G = chunks;
+  if (G < 1 || (dtype == COTTN_F32 && dk == 128)) G = 1;   // (kernels for whole sequences alone)
+  p->seg = chunks > 0 ? int((chunks + G - 1) / G) : 1;
+  p->G = chunks > 0 ? int((chunks + p->seg - 1) / p->seg) : 1;
+  if (!threads_fit(units * p->G, 512)) return false;
   const size_t all = size_t(units) * chunks, state = round_up_256(all * dk * dv * 4), rows = round_up_256(all * 64 * dv * 4);
+  const size_t segments = p->G > 1 ? size_t(units) * p->G : 0;
   p->records = 0;
   p->w_rows = round_up_256(all * DELTA_RECORD_BYTES);
-  p->w_cols = p->alone = p->w_rows + all * DELTA_W_BYTES;
+  p->starts = p->w_rows + all * DELTA_W_BYTES;
+  p->transitions = p->starts + round_up_256(segments * dk * dv * 4);
+  p->w_cols = p->alone = p->transitions + round_up_256(segments * dk * dk * 4);
   p->errors = p->w_cols + all * DELTA_W_BYTES;
   p->states = p->errors + rows;
   p->forward = p->states + state;
   p->zs = 0;
   p->dstates = rows;
   p->ds_parts = p->dstates + state;
-  p->saved = p->ds_parts + round_up_256(all * 4);
+  p->ends = p->ds_parts + round_up_256(all * 4);
+  p->saved = p->ends + round_up_256(segments * dk * dv * 4);
   return true;
 }
 size_t delta_workspace_bytes(int op, const DeltaSpace& p) {
@@ -401,6 +427,10 @@ bool is_delta(int op) { return op >= COTTN_OP_FWD_DELTA && op <= COTTN_OP_BWD_DE
 // the arrays of a forward's workspace at `base`
 void place_delta(DeltaArgs* a, const void* base, const DeltaSpace& p, bool with_states) {
   char* at = static_cast<char*>(const_cast<void*>(base));
+  a->G = p.G;
+  a->seg = p.seg;
+  a->starts = reinterpret_cast<float*>(at + p.starts);
+  a->transitions = reinterpret_cast<float*>(at + p.transitions);
   a->records = at + p.records;
   a->w_rows = reinterpret_cast<unsigned short*>(at + p.w_rows);
   a->w_cols = with_states ? reinterpret_cast<unsigned short*>(at + p.w_cols) : nullptr;
@@ -521,9 +551,9 @@ int cottn_segments_dkdv(int op, int B, int H, int N, int dk, int dv, int chunk, 
     DecayPlan plan;
     return make_decay_plan(op == COTTN_OP_FWD_DECAY_ALONE, B, H, N, dk, dv, chunk, dtype, &plan) ? plan.G : 0;
   }
-  if (is_delta(op)) {   // a sequence is walked from one end to the other
+  if (is_delta(op)) {
     DeltaSpace space;
-    return delta_space(B, H, N, dk, dv, chunk, dtype, &space) ? 1 : 0;
+    return delta_space(B, H, N, dk, dv, chunk, dtype, &space) ? space.G : 0;
   }
   if (op < COTTN_OP_FWD_CAUSAL || op > COTTN_OP_BWD_BIDIR) return 0;
   SeqPlan plan;
@@ -1139,6 +1169,7 @@ int cottn_bwd_causal_delta(const void* Q, const void* K, const void* V, const fl
   a.zs = reinterpret_cast<float*>(own + space.zs);
   a.dstates = reinterpret_cast<float*>(own + space.dstates);
   a.ds_parts = reinterpret_cast<float*>(own + space.ds_parts);
+  a.ends = reinterpret_cast<float*>(own + space.ends);
   place_delta(&a, saved ? fwd_workspace : own + space.saved, space, true);
   a.B = B; a.H = H; a.N = N; a.dk = dk; a.dv = dv; a.eps = eps; a.stream = stream;
   return map_hip(dtype == COTTN_BF16 ? delta_bwd_bf16(a) : dtype == COTTN_F16 ? delta_bwd_f16(a) : delta_bwd_f32(a));

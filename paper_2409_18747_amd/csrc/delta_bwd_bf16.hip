@@ -31,12 +31,14 @@ __device__ __forceinline__ void weighted_rows(const bf16x8 (&g)[IN], const float
   split8<LEVEL>(lo * (four(rq + t0) * (scale * four(since + t0))), hi * (four(rq + t0 + 16) * (scale * four(since + t0 + 16))), out);
 }
 
-template <typename T, int DK, int NW>
+// Segments as in the forward scan: TOTALS leaves what a segment makes of zeros (the last one: of dstate) in the place of the
+// gradient with respect to the state in front of it.
+template <typename T, int DK, int NW, bool TOTALS>
 __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
-    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, Divisor H, Divisor parts, int N,
-    int units, int DV, float inv_eps) {
+    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, float* ends, Divisor H,
+    Divisor G, Divisor parts, int seg, int N, int units, int DV, float inv_eps) {
   using Cfg = DeltaRevCfg<T, DK, NW>;
   using KTile = typename Cfg::KTile;
   using GTile = typename Cfg::GTile;
@@ -50,29 +52,40 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
   __shared__ f32x4 Rs[Cfg::HANDS_R ? NW * 2 * KS * 64 : 1];    // (G Qh)^T dO'
   __shared__ ChunkRecord rec;
   __shared__ __attribute__((aligned(16))) float rq[CHUNK];
-  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, H, parts, N, units, DV, inv_eps);
-  int unit, part;
-  unit_and_segment(blockIdx.x, units, parts, unit, part);
+  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, ends, H, G, parts, seg, N, units, DV,
+                     inv_eps);
+  int unit, part, g = 0;
+  if (G.n == 1) {
+    unit_and_segment(blockIdx.x, units, parts, unit, part);
+  } else {   // (blockIdx.y: the part)
+    unit_and_segment(blockIdx.x, units, G, unit, g);
+    part = blockIdx.y;
+  }
   const int tid = threadIdx.x % NT, role = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / NT);
   const int w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
-  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), steps = delta_chunks(there), col0 = part * VC;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), all = delta_chunks(there), first = g * seg, steps = min(all, first + seg);
+  const int col0 = part * VC;
+  if ((first >= all && g > 0) || (TOTALS && g == 0)) return;
+  const bool ends_here = steps == all;   // the last rows
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
 
   if (role == 0) {
     // ---- the gradients with respect to the states
     // this lane's value column in the first key row, and in the first token row, that it holds
     const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
+    const float* from = ends_here ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
+                                  : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
     f32x4 D[2 * KS];
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
-        D[t][v] = dstate != nullptr ? (dstate + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
-    for (int c = steps - 1; c >= 0; --c) {
+        D[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+    for (int c = steps - 1; c >= first; --c) {
       bf16x8 df[KS][LEVEL];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) split8<LEVEL>(D[2 * ks], D[2 * ks + 1], df[ks]);
-      {
+      if constexpr (!TOTALS) {
         float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
@@ -118,9 +131,11 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
               z = mm<LEVEL>(wf, ff[k], z);
             }
           z = f[t] - z;
-          float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
+          if constexpr (!TOTALS) {
+            float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
 #pragma unroll
-          for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+            for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+          }
           x[h] = -(b[t] * z) * four(rec.rk_since + 16 * t + 4 * q4);
         }
         split8<LEVEL>(x[0], x[1], xf[p]);
@@ -156,8 +171,8 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
         for (int t = 0; t < 2 * KS; ++t) D[t] += Rs[(w * 2 * KS + t) * 64 + l];
       }
     }
-    if (dstate_in != nullptr) {
-      float* to = dstate_in + size_t(unit) * DK * DV;
+    float* to = TOTALS ? ends + (size_t(unit) * G.n + g - 1) * DK * DV : dstate_in != nullptr && g == 0 ? dstate_in + size_t(unit) * DK * DV : nullptr;
+    if (to != nullptr) {
 #pragma unroll
       for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
@@ -188,8 +203,8 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
       if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
         w_next[i] = reinterpret_cast<const u32x4*>(w_cols + at * W_ELEMS)[i * NT + tid];
   };
-  if (steps > 0) fetch(steps - 1);
-  for (int c = steps - 1; c >= 0; --c) {
+  if (steps > first) fetch(steps - 1);
+  for (int c = steps - 1; c >= first; --c) {
     kt.commit(Ks);
     qt.commit(Qs);
     qt.store_factors(rq, inv_eps);
@@ -201,7 +216,7 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
     for (int i = 0; i < W_PIECES; ++i)
       if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
     lds_barrier();   // the chunk is there
-    if (c > 0) fetch(c - 1);
+    if (c > first) fetch(c - 1);
 
     // s P, a tile of columns to a wave (two where there are two waves), queries down: an operand as it stands
 #pragma unroll
@@ -896,14 +911,26 @@ __global__ __launch_bounds__(256) void delta_sum_ds(const float* __restrict__ pa
 template <typename T, int DK, int NW>
 hipError_t run_rev(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
-  const auto run = [&](auto kernel, int threads) {
-    return launch_kernel("delta_rev_scan", kernel, dim3(unsigned(units * parts)), dim3(threads), 0, a.stream,
+  const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
+  if constexpr (DeltaRevCfg<T, DK, NW>::FITS) {
+    const auto run = [&](auto kernel) {
+      return launch_kernel("delta_rev_scan", kernel, a.G == 1 ? dim3(unsigned(units * parts)) : dim3(unsigned(units * a.G), unsigned(parts)),
+                           dim3(128 * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
+                           static_cast<const T*>(a.dO), a.s, a.seq_len, a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates,
+                           a.ends, Divisor(a.H), Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
+    };
+    if (a.G > 1) {
+      hipError_t err = run(delta_rev_scan<T, DK, NW, true>);
+      if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, true);
+      if (err != hipSuccess) return err;
+    }
+    return run(delta_rev_scan<T, DK, NW, false>);
+  } else {
+    return launch_kernel("delta_rev_scan", delta_wide_rev_scan<T, DK, NW>, dim3(unsigned(units * parts)), dim3(64 * NW), 0, a.stream,
                          static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.seq_len,
-                         a.dstate, a.dstate_in, static_cast<const ChunkRecord*>(a.records), a.w_cols, a.zs, a.dstates, Divisor(a.H),
-                         Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
-  };
-  if constexpr (DeltaRevCfg<T, DK, NW>::FITS) return run(delta_rev_scan<T, DK, NW>, 128 * NW);
-  else return run(delta_wide_rev_scan<T, DK, NW>, 64 * NW);
+                         a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates, Divisor(a.H), Divisor(parts), a.N, units, a.dv,
+                         1.0f / a.eps);
+  }
 }
 
 template <typename T, int DK, int DV>

@@ -28,17 +28,23 @@ struct DeltaFwdCfg {
   static constexpr bool FITS = BYTES <= 160 * 1024;
 };
 
-template <typename T, int DK, int NW, int LEVEL>
+// A sequence in G segments of `seg` chunks: the workgroups of TOTALS leave what a segment makes of a state, B from zeros (the first
+// segment: from state_in) in the place of the state behind it, and the matrix M that the state at its start enters with, as if
+// unit columns without values were its state; delta_carry makes of those the states at the starts, from which the segments are
+// walked again.
+template <typename T, int DK, int NW, int LEVEL, bool TOTALS>
 __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
-    float* __restrict__ states, Divisor H, Divisor parts, int N, int units, int DV, float inv_eps) {
+    float* __restrict__ states, float* starts, float* __restrict__ transitions, Divisor H, Divisor G, Divisor parts, int seg, int N,
+    int units, int DV, float inv_eps) {
   using Cfg = DeltaFwdCfg<T, DK, NW, LEVEL>;
   using KTile = typename Cfg::KTile;
   using VTile = typename Cfg::VTile;
   constexpr int IN = Cfg::IN, OUT = Cfg::OUT, KS = Cfg::KS, NT = 64 * NW, VC = Cfg::VC;
   typedef __attribute__((ext_vector_type(4))) T vec4;
+  static_assert(!TOTALS || LEVEL == 3, "states");
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[Cfg::V_IN_LDS ? VTile::SIZE : 8];
@@ -48,32 +54,47 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
   __shared__ __attribute__((aligned(16))) uint16_t Us[Cfg::U_SIZE];
   __shared__ ChunkRecord rec;
   __shared__ __attribute__((aligned(16))) float rq[CHUNK];
-  fetch_argument_now(Q, K, V, s, lengths, state_in, O, state_out, records, w_rows, errors, states, H, parts, N, units, DV, inv_eps);
-  int unit, part;
-  unit_and_segment(blockIdx.x, units, parts, unit, part);
+  fetch_argument_now(Q, K, V, s, lengths, state_in, O, state_out, records, w_rows, errors, states, starts, transitions, H, G, parts, seg,
+                     N, units, DV, inv_eps);
+  int unit, part, g = 0;
+  if (G.n == 1) {
+    unit_and_segment(blockIdx.x, units, parts, unit, part);
+  } else {   // (blockIdx.y: the part)
+    unit_and_segment(blockIdx.x, units, G, unit, g);
+    part = blockIdx.y;
+  }
   const int tid = threadIdx.x % NT, role = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / NT);
   const int w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
-  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), steps = delta_chunks(there), col0 = part * VC;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), all = delta_chunks(there), first = g * seg, steps = min(all, first + seg);
+  const bool ends_here = steps == all && (first < all || g == 0);   // the state after the last row
+  // TOTALS: columns of M, behind those of the values
+  const bool unit_columns = TOTALS && part * VC >= DV;
+  const int col0 = unit_columns ? part * VC - DV : part * VC, width = unit_columns ? DK : DV;
+  if (TOTALS && (first >= all || (unit_columns ? g == 0 : ends_here))) return;   // (nobody asks)
 
   if (role == 0) {
     // ---- the states
     const T* Vu = V + size_t(unit) * N * DV + col0;
     // this lane's value column in the first key row, and in the first token row, that it holds
-    const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
+    const unsigned at_key = unsigned(8 * q4 * width + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
     f32x4 S[2 * KS];
+    const float* from = g == 0 ? (state_in != nullptr ? state_in + size_t(unit) * DK * DV : nullptr)
+                               : TOTALS ? nullptr : starts + (size_t(unit) * G.n + g) * DK * DV;
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        S[t][v] = state_in != nullptr ? (state_in + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
-    for (int c = 0; c < steps; ++c) {
+      for (int v = 0; v < 4; ++v) {
+        S[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+        if (unit_columns) S[t][v] = key_of(t / 2, t % 2, q4, v) == col0 + 16 * w + r ? 1.f : 0.f;
+      }
+    for (int c = first; c < steps; ++c) {
       bf16x8 sf[KS][LEVEL];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         split8<LEVEL>(S[2 * ks], S[2 * ks + 1], sf[ks]);
-        store_frag<OUT>(Ss, w * KS + ks, l, sf[ks]);
+        if constexpr (!TOTALS) store_frag<OUT>(Ss, w * KS + ks, l, sf[ks]);
       }
-      if (states != nullptr) {
+      if (!TOTALS && states != nullptr) {
         float* to = states + (size_t(unit) * chunks + c) * DK * DV;
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
@@ -87,7 +108,7 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const int row = c * CHUNK + 16 * t + v;
-            y[t][v] = row + 4 * q4 < there ? float((Vu + size_t(row) * DV)[unsigned(4 * q4 * DV + 16 * w + r)]) : 0.f;
+            y[t][v] = !unit_columns && row + 4 * q4 < there ? float((Vu + size_t(row) * DV)[unsigned(4 * q4 * DV + 16 * w + r)]) : 0.f;
           }
       }
       lds_barrier();   // the chunk is there
@@ -105,7 +126,7 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
       bf16x8 yf[2][LEVEL];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        if constexpr (Cfg::V_IN_LDS) y[t] = VTile::col4(Vs, 16 * t + 4 * q4, 16 * w, r);
+        if constexpr (Cfg::V_IN_LDS) y[t] = unit_columns ? f32x4{0.f, 0.f, 0.f, 0.f} : VTile::col4(Vs, 16 * t + 4 * q4, 16 * w, r);
         const f32x4 since = four(rec.rk_since + 16 * t + 4 * q4);
 #pragma unroll
         for (int v = 0; v < 4; ++v) y[t][v] = __builtin_fmaf(-since[v], kh[t][v], y[t][v]);
@@ -129,19 +150,21 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
           e = y[it] - e;
           u[h] = e * four(rec.beta + 16 * it + 4 * q4);
           t[h] = u[h] * four(rec.rk_to_end + 16 * it + 4 * q4);
-          if (errors != nullptr) {
+          if (!TOTALS && errors != nullptr) {
             float* to = errors + (size_t(unit) * chunks + c) * CHUNK * DV;
 #pragma unroll
             for (int v = 0; v < 4; ++v) (to + (16 * it + v) * DV)[at_token] = e[v];
           }
         }
-        bf16x8 uf[OUT];
-        split8<OUT>(u[0], u[1], uf);
-        store_frag<OUT>(Us, w * 2 + p, l, uf);
+        if constexpr (!TOTALS) {
+          bf16x8 uf[OUT];
+          split8<OUT>(u[0], u[1], uf);
+          store_frag<OUT>(Us, w * 2 + p, l, uf);
+        }
         split8<LEVEL>(t[0], t[1], tf[p]);
       }
       const float times = rec.times, plus = rec.plus;
-      lds_barrier();   // U and P are there
+      if constexpr (!TOTALS) lds_barrier();   // U and P are there
 #pragma unroll
       for (int t = 0; t < 2 * KS; ++t) {
 #pragma unroll
@@ -157,12 +180,13 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
         }
       lds_barrier();   // everything of the chunk is read
     }
-    if (state_out != nullptr) {
-      float* to = state_out + size_t(unit) * DK * DV;
+    float* to = state_out != nullptr && ends_here ? state_out + size_t(unit) * DK * DV : nullptr;
+    if (TOTALS) to = unit_columns ? transitions + (size_t(unit) * G.n + g) * DK * DK : starts + (size_t(unit) * G.n + g + 1) * DK * DV;
+    if (to != nullptr && col0 + 16 * w < width) {
 #pragma unroll
       for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * width)[at_key] = S[t][v];
     }
     return;
   }
@@ -180,8 +204,8 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
   const auto fetch = [&](int c) {
     const int row0 = c * CHUNK;
     kt.fetch(Ku + size_t(row0) * DK, there - row0);
-    qt.fetch(Qu + size_t(row0) * DK, there - row0);
-    if constexpr (Cfg::V_IN_LDS) vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
+    if constexpr (!TOTALS) qt.fetch(Qu + size_t(row0) * DK, there - row0);
+    if (Cfg::V_IN_LDS && !unit_columns) vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
     const size_t at = size_t(unit) * chunks + c;
 #pragma unroll
     for (int i = 0; i < REC_PIECES; ++i)
@@ -193,13 +217,15 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
         w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
     }
   };
-  if (steps > 0) fetch(0);
-  for (int c = 0; c < steps; ++c) {
+  if (first < steps) fetch(first);
+  for (int c = first; c < steps; ++c) {
     const int row0 = c * CHUNK;
     kt.commit(Ks);
-    qt.commit(Qs);
-    qt.store_factors(rq, inv_eps);
-    if constexpr (Cfg::V_IN_LDS) vt.commit(Vs);
+    if constexpr (!TOTALS) {
+      qt.commit(Qs);
+      qt.store_factors(rq, inv_eps);
+    }
+    if (Cfg::V_IN_LDS && !unit_columns) vt.commit(Vs);
 #pragma unroll
     for (int i = 0; i < REC_PIECES; ++i)
       if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
@@ -208,6 +234,10 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
       if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
     lds_barrier();   // the chunk is there
     if (c + 1 < steps) fetch(c + 1);
+    if constexpr (TOTALS) {
+      lds_barrier();   // everything of the chunk is read
+      continue;
+    }
 
     // P, a tile of rows to a wave (two where there are two waves), keys down: an operand as it stands
 #pragma unroll
@@ -284,9 +314,10 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
     lds_barrier();   // everything of the chunk is read
   }
   // rows that do not exist
-  if (O == nullptr) return;
-  for (long i = tid; i < long(N - there) * (VC / 4); i += NT)
-    *reinterpret_cast<vec4*>(Ou + size_t(there + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
+  if (TOTALS || O == nullptr) return;
+  const int lo = max(there, first * CHUNK), hi = min(N, (first + seg) * CHUNK);
+  for (long i = tid; i < long(hi - lo) * (VC / 4); i += NT)
+    *reinterpret_cast<vec4*>(Ou + size_t(lo + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
 }
 
 // The same by waves that do all of it, for rows of 128 in fp32, whose three parts leave the LDS no room for what one half of the
@@ -559,14 +590,29 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
 template <typename T, int DK, int NW, int LEVEL>
 hipError_t run_scan(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
-  const auto run = [&](auto kernel, int threads) {
-    return launch_kernel("delta_fwd_scan", kernel, dim3(unsigned(units * parts)), dim3(threads), 0, a.stream,
-                         static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len,
-                         a.state_in, static_cast<T*>(a.O), a.state, static_cast<const ChunkRecord*>(a.records), a.w_rows, a.errors,
-                         a.states, Divisor(a.H), Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
-  };
-  if constexpr (DeltaFwdCfg<T, DK, NW, LEVEL>::FITS) return run(delta_fwd_scan<T, DK, NW, LEVEL>, 128 * NW);
-  else return run(delta_wide_fwd_scan<T, DK, NW, LEVEL>, 64 * NW);
+  const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
+  if constexpr (DeltaFwdCfg<T, DK, NW, LEVEL>::FITS) {
+    const auto run = [&](auto kernel, int n_parts) {
+      return launch_kernel("delta_fwd_scan", kernel, a.G == 1 ? dim3(unsigned(units * n_parts)) : dim3(unsigned(units * a.G), unsigned(n_parts)),
+                           dim3(128 * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
+                           static_cast<const T*>(a.V), a.s, a.seq_len, a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows,
+                           a.errors, a.states, a.starts, a.transitions, Divisor(a.H), Divisor(a.G), Divisor(n_parts), a.seg, a.N,
+                           units, a.dv, 1.0f / a.eps);
+    };
+    if (a.G > 1) {
+      // M is not asked for where the states at the starts of two segments are known without, and no backward follows
+      const int with_M = a.G > 2 || a.errors != nullptr ? (DK + 16 * NW - 1) / (16 * NW) : 0;
+      hipError_t err = run(delta_fwd_scan<T, DK, NW, 3, true>, parts + with_M);
+      if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, false);
+      if (err != hipSuccess) return err;
+    }
+    return run(delta_fwd_scan<T, DK, NW, LEVEL, false>, parts);
+  } else {
+    return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW, LEVEL>, dim3(unsigned(units * parts)), dim3(64 * NW), 0,
+                         a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s,
+                         a.seq_len, a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows, a.errors, a.states, Divisor(a.H),
+                         Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
+  }
 }
 
 template <typename T, int DK, int LEVEL>

@@ -315,6 +315,11 @@ struct DeltaArgs {
   const int* seq_len;               // null, or int[B] row counts: then s and ds are [B][H]
   const float* state_in;            // may be null
   void* O; float* state;            // forward: results (state may be null); backward: no O, and only errors and states are formed
+  // G segments of `seg` chunks, one after the other where G is 1: the states at the starts of the segments but the first, what a
+  // segment makes of the state at its start, [units][G][dk][dk], and the gradients with respect to the states at the ends of the
+  // segments but the last
+  int G, seg;
+  float* starts; float* transitions; float* ends;
   void* records; unsigned short* w_rows;
   unsigned short* w_cols; float* errors; float* states;     // forward: may be null
   // backward
@@ -380,6 +385,7 @@ hipError_t delta_fwd_f32(const DeltaArgs& a);
 hipError_t delta_bwd_bf16(const DeltaArgs& a);
 hipError_t delta_bwd_f16(const DeltaArgs& a);
 hipError_t delta_bwd_f32(const DeltaArgs& a);
+hipError_t launch_delta_carry(const DeltaArgs& a, bool reverse);   // delta_carry.hip
 hipError_t step_delta_any(const StepDeltaArgs& a, int dtype);
 hipError_t rotary_any(const RotaryArgs& a, int dtype);
 

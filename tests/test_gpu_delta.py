@@ -234,3 +234,38 @@ def test_no_rows(cottn):
     D = torch.empty_like(S)
     got = cottn.cottn_bwd_causal_delta(rows(32), rows(32), rows(64), s, gates, gates, rows(64), state_in=S, dstate=S, dstate_in=D)
     assert torch.equal(D, S) and not got[3].any() and got[5].shape == (2, 3, 0)
+
+
+@pytest.fixture
+def segments(cottn):
+    yield cottn.cottn_tune_segments
+    cottn.cottn_tune_segments(0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(32, 32), (32, 128), (64, 64), (128, 32), (128, 128)])
+@pytest.mark.parametrize("G", [2, 3, 5])
+def test_segments(cottn, segments, dtype, dk, dv, G):
+    """A sequence cut into segments that are walked side by side."""
+    segments(G)
+    code = {"f32": 0, "bf16": 1, "f16": 2}[dtype]
+    got = cottn.cottn_segments_dkdv(cottn.OP_FWD_DELTA, 1, 2, 300, dk, dv, 0, code)
+    assert got == (1 if dtype == "f32" and dk == 128 else G)
+    x, more = draw(1, 2, 300, dk, dv, dtype, G + dk)
+    run_both(cottn, x, more, dtype, states=G != 3)
+    want, _ = ref.forward(**double(x))
+    check("O", cottn.cottn_fwd_causal_delta(**cuda(x)), want, dtype, two_parts=dtype != "f32")
+
+
+@pytest.mark.parametrize("G", [2, 4, 5])
+def test_segments_of_a_padded_batch(cottn, segments, G):
+    segments(G)
+    lens = [0, 1, 64, 65, 200, 257, 300, 129]
+    x, more = draw(8, 2, 300, 64, 64, "bf16", G, per_unit=True)
+    for b, n in enumerate(lens):
+        for t in (x["Q"], x["K"], x["V"], more["dO"], x["log_decay"], x["beta"]):
+            t[b, :, n:] = float("nan")
+    d, m, O, state, got = run_both_padded(cottn, x, more, "bf16", lens)
+    for t in (O,) + tuple(got[:3]) + tuple(got[4:]):
+        for b, n in enumerate(lens):
+            assert not t[b, :, n:].any()
