@@ -377,14 +377,15 @@ struct DeltaSpace {
   size_t zs, dstates, ds_parts, ends, saved;                                             // a backward's that is handed one; `saved`: its bytes
 };
 // Time of a forward in G segments, in steps of a workgroup, of which a compute unit has one.  More than one segment walk the
-// rows twice, once for the totals of all but the last, with the columns of M beside those of the values, and the states at their
-// starts are found one after the other; two launches more.
+// rows twice, first for the totals of all but the last, with the columns of M beside those of the values, two workgroups to a
+// compute unit; then the states at their starts are found one after the other.  Two launches more.
 double delta_steps(long units, long chunks, long G, int dk, int dv) {
   const long per = dv == 32 ? 32 : 64, parts = dv / per, seg = (chunks + G - 1) / G;
-  const auto rounds = [](long workgroups) { return double((workgroups + kComputeUnits - 1) / kComputeUnits); };
-  const double whole = rounds(units * parts * G) * double(seg);
-  if (G == 1) return whole;
-  return whole + 0.8 * rounds(units * (parts * (G - 1) + (dk + per - 1) / per * (G - 1))) * double(seg) + (dk == 128 ? 1.5 : 0.6) * double(G) + 4.0;
+  const auto rounds = [](long workgroups, long at_once) { return double((workgroups + at_once - 1) / at_once); };
+  const double whole = rounds(units * parts * G, kComputeUnits) * double(seg);
+  if (G == 1) return whole + 1.0;
+  const long columns = G > 2 ? (dk + per - 1) / per * (G - 1) : 0;
+  return whole + 0.8 * rounds(units * (parts * (G - 1) + columns), 2 * kComputeUnits) * double(seg) + 3.0 + (G > 2 ? 0.35 * double(G) + 1.0 : 0.0);
 }
 bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, DeltaSpace* p) {
   if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
@@ -394,8 +395,8 @@ bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, Delt
   long G = g_tuned_segments;
   if (G <= 0) {
     G = 1;
-    for (long g = 2; g <= 64 && g <= chunks && units * g <= 4 * kComputeUnits; ++g)
-      if (delta_steps(units, chunks, g, dk, dv) < 0.9 * delta_steps(units, chunks, G, dk, dv)) G = g;
+    for (long g = 2; g <= 64 && g <= chunks && units * g <= 2 * kComputeUnits; ++g)
+      if (delta_steps(units, chunks, g, dk, dv) < 0.95 * delta_steps(units, chunks, G, dk, dv)) G = g;
   }
   if (G > chunks) G = chunks;
   if (G < 1 || (dtype == COTTN_F32 && dk == 128)) G = 1;   // (kernels for whole sequences alone)
