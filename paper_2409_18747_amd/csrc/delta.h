@@ -128,6 +128,12 @@ struct Raw8 {
     }
   }
   __device__ __forceinline__ float sum_sq() const {
+    if constexpr (PARTS == 1) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = dot2_self(w[0][i], s);
+      return s;
+    }
     f32x4 lo, hi;
     values(lo, hi);
     float s = 0.f;
@@ -167,6 +173,20 @@ struct PartTile {
       const s16x4 lo = lds_read_tr(p + r0 * PITCH), hi = lds_read_tr(p + r1 * PITCH);
       f[i] = __builtin_bit_cast(bf16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     }
+  }
+  // columns c .. c + 3 of a row as fp32
+  static __device__ __forceinline__ f32x4 row4(const uint16_t* tile, int row, int c) {
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = PARTS - 1; i >= 0; --i) {
+      const uint2 w = *reinterpret_cast<const uint2*>(tile + i * PLANE + row * PITCH + c);
+      float t[4];
+      unpack2(w.x, t[0], t[1]);
+      unpack2(w.y, t[2], t[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += t[e];
+    }
+    return x;
   }
   // rows row0 .. row0 + 3 of column col0 + r as fp32
   static __device__ __forceinline__ f32x4 col4(const uint16_t* tile, int row0, int col0, int r) {

@@ -547,14 +547,6 @@ struct DeltaGradCfg {
   static constexpr int KT = DK / 16, NK = KT >= 4 ? KT / 4 : 1, NTOK = KT >= 4 ? 4 : 2;
 };
 
-// four consecutive elements
-template <typename T>
-__device__ __forceinline__ f32x4 load_row4(const T* p) {
-  typedef __attribute__((ext_vector_type(4))) T vec4;
-  const vec4 x = *reinterpret_cast<const vec4*>(p);
-  return f32x4{float(x[0]), float(x[1]), float(x[2]), float(x[3])};
-}
-
 template <typename T, int DK, int DV>
 __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_gradients(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
@@ -628,15 +620,25 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     kt.fetch(K + (row_at + row0) * DK, there - row0);
     qt.fetch(Q + (row_at + row0) * DK, there - row0);
     if (tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[tid] = reinterpret_cast<const u32x4*>(records + blockIdx.x)[tid];
+    f32x4 ez[RT::PASSES][4];
+    float b_row[RT::PASSES];
+#pragma unroll
+    for (int p = 0; p < RT::PASSES; ++p) {
+      const size_t at = (size_t(blockIdx.x) * CHUNK + RT::row(p)) * DV + RT::col();
+      ez[p][0] = reinterpret_cast<const f32x4*>(errors + at)[0];
+      ez[p][1] = reinterpret_cast<const f32x4*>(errors + at)[1];
+      ez[p][2] = reinterpret_cast<const f32x4*>(zs + at)[0];
+      ez[p][3] = reinterpret_cast<const f32x4*>(zs + at)[1];
+      b_row[p] = row0 + RT::row(p) < there ? beta[row_at + row0 + RT::row(p)] : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < NK; ++x) fetch_states(x, 0);
     gt.commit(Os);
 #pragma unroll
     for (int p = 0; p < RT::PASSES; ++p) {
       const int row = RT::row(p), col = RT::col();
-      const size_t at = (size_t(blockIdx.x) * CHUNK + row) * DV + col;
-      const f32x4* ep = reinterpret_cast<const f32x4*>(errors + at);
-      const f32x4* zp = reinterpret_cast<const f32x4*>(zs + at);
-      const f32x4 e0 = ep[0], e1 = ep[1], z0 = zp[0], z1 = zp[1];
-      const float b = row0 + row < there ? beta[row_at + row0 + row] : 0.f;
+      const f32x4 e0 = ez[p][0], e1 = ez[p][1], z0 = ez[p][2], z1 = ez[p][3];
+      const float b = b_row[p];
       bf16x8 parts[LEVEL];
       split8<LEVEL>(e0, e1, parts);
       ETile::store8(Es, row, col, parts);
@@ -663,14 +665,11 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     }
     qt.store_factors(rq, inv_eps);
   }
-#pragma unroll
-  for (int x = 0; x < NK; ++x) fetch_states(x, 0);
   __syncthreads();
 
-  f32x4 aq[NK][NTOK], ak[NK][NTOK];
+  f32x4 aq[NK][NTOK], ak[NK][NTOK], az[NK][NTOK];
   float through = 0.f;   // <D, H>, of the wave's rows
   {
-    f32x4 az[NK][NTOK];
 #pragma unroll
     for (int x = 0; x < NK; ++x)
 #pragma unroll
@@ -699,30 +698,18 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
         }
       }
     }
-    // each token's factors; and what the updates of the chunk give to <D, H behind the chunk>
-    if (Cfg::KT < 4 && w >= 2) through = 0.f;
-    through *= rec.since[CHUNK - 1];
+    // each token's factors
 #pragma unroll
     for (int t = 0; t < NTOK; ++t) {
       const int i = 16 * (tt0 + t) + r;
       const float since = rec.since[i], to_end = rec.beta[i] * decay_between(rec.decay[CHUNK - 1], rec.decay[i]);
-      float dot = 0.f;
 #pragma unroll
       for (int x = 0; x < NK; ++x) {
-        f32x4 k = {0.f, 0.f, 0.f, 0.f};
-        if (row0 + i < there) k = load_row4(K + (row_at + row0 + i) * DK + 16 * (kt0 + x) + 4 * q4);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          aq[x][t][v] *= since;
-          ak[x][t][v] *= to_end;
-          dot = __builtin_fmaf(k[v], ak[x][t][v], dot);
-          ak[x][t][v] = __builtin_fmaf(-rec.beta[i] * since, az[x][t][v], ak[x][t][v]);
-        }
+        aq[x][t] *= since;
+        ak[x][t] *= to_end;
+        az[x][t] *= -rec.beta[i] * since;
       }
-      through = __builtin_fmaf(rec.rk[i], dot, through);
     }
-    through = group_sum<64>(through);
-    if (l == 0) tail[w] = through;
   }
 
   // the masked tiles: rows i of wave w's tile, columns j; lanes hold four columns of a row
@@ -769,6 +756,24 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     MTile::store4(Mt, own, 16 * jt + 4 * q4, pt[jt] * (scale * rq_own));
   }
   __syncthreads();
+  // <D, H behind the chunk>: what goes through it, and what its updates give
+  if (Cfg::KT < 4 && w >= 2) through = 0.f;
+  through *= rec.since[CHUNK - 1];
+#pragma unroll
+  for (int t = 0; t < NTOK; ++t) {
+    const int i = 16 * (tt0 + t) + r;
+    float dot = 0.f;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      const f32x4 k = KTile::row4(Ks, i, 16 * (kt0 + x) + 4 * q4);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) dot = __builtin_fmaf(k[v], ak[x][t][v], dot);
+      ak[x][t] += az[x][t];
+    }
+    through = __builtin_fmaf(rec.rk[i], dot, through);
+  }
+  through = group_sum<64>(through);
+  if (l == 0) tail[w] = through;
 #pragma unroll
   for (int round = 0; round < 2; ++round) {
 #pragma unroll
@@ -819,11 +824,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     float dq = 0.f, dk = 0.f;
 #pragma unroll
     for (int x = 0; x < NK; ++x) {
-      f32x4 q = {0.f, 0.f, 0.f, 0.f}, k = q;
-      if (row0 + i < there) {
-        q = load_row4(Q + (row_at + row0 + i) * DK + 16 * (kt0 + x) + 4 * q4);
-        k = load_row4(K + (row_at + row0 + i) * DK + 16 * (kt0 + x) + 4 * q4);
-      }
+      const f32x4 q = KTile::row4(Qs, i, 16 * (kt0 + x) + 4 * q4), k = KTile::row4(Ks, i, 16 * (kt0 + x) + 4 * q4);
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
         dq = __builtin_fmaf(q[v], aq[x][t][v], dq);
@@ -856,7 +857,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
 #pragma unroll
       for (int x = 0; x < NK; ++x) {
         const size_t at_ = size_t(row0 + i) * DK + 16 * (kt0 + x) + 4 * q4;
-        const f32x4 q = load_row4(Q + row_at * DK + at_), k = load_row4(K + row_at * DK + at_);
+        const f32x4 q = KTile::row4(Qs, i, 16 * (kt0 + x) + 4 * q4), k = KTile::row4(Ks, i, 16 * (kt0 + x) + 4 * q4);
         typedef __attribute__((ext_vector_type(4))) T vec4;
         vec4 gq, gk;
 #pragma unroll
