@@ -94,6 +94,34 @@ __device__ __forceinline__ f32x4 mm(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB]
   return acc;
 }
 
+// The same for N tiles with an operand in common, product by product: neighbouring matrix instructions do not wait for each other.
+template <int LEVEL, int N, int NA, int NB>
+__device__ __forceinline__ void mm_each(const bf16x8 (&a)[N][NA], const bf16x8 (&b)[NB], f32x4* acc) {
+#pragma unroll
+  for (int sum = LEVEL - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      const int j = sum - i;
+      if (j >= 0 && j < NB) {
+#pragma unroll
+        for (int t = 0; t < N; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t][i], b[j], acc[t], 0, 0, 0);
+      }
+    }
+}
+template <int LEVEL, int N, int NA, int NB>
+__device__ __forceinline__ void mm_each(const bf16x8 (&a)[NA], const bf16x8 (&b)[N][NB], f32x4* acc) {
+#pragma unroll
+  for (int sum = LEVEL - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      const int j = sum - i;
+      if (j >= 0 && j < NB) {
+#pragma unroll
+        for (int t = 0; t < N; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[t][j], acc[t], 0, 0, 0);
+      }
+    }
+}
+
 // Eight consecutive elements of a row as they lie in memory, as fp32 and as parts.
 template <typename T>
 struct Raw8 {
@@ -323,6 +351,12 @@ template <int N, int M>
 __device__ __forceinline__ void store_frag(uint16_t* to, int at, int l, const bf16x8 (&f)[M]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) reinterpret_cast<u32x4*>(to)[(at * N + i) * 64 + l] = __builtin_bit_cast(u32x4, f[i]);
+}
+// A row length as a number that the compiler takes for another one in every step of a loop: the addresses of the step's rows are
+// then scalars and one lane offset, not a pair of vector registers to each row all through the loop.
+__device__ __forceinline__ int in_this_step(int n) {
+  asm volatile("" : "+s"(n));
+  return n;
 }
 __device__ __forceinline__ f32x4 four(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 

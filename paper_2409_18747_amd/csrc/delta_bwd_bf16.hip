@@ -71,6 +71,7 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
 
   if (role == 0) {
     // ---- the gradients with respect to the states
+    __builtin_amdgcn_s_setprio(3);   // the chain that all wait for
     // this lane's value column in the first key row, and in the first token row, that it holds
     const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
     const float* from = ends_here ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
@@ -87,10 +88,11 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
       for (int ks = 0; ks < KS; ++ks) split8<LEVEL>(D[2 * ks], D[2 * ks + 1], df[ks]);
       if constexpr (!TOTALS) {
         float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
+        const int ld = in_this_step(DV);
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * ld)[at_key] = D[t][v];
       }
       lds_barrier();   // the chunk is there
       f32x4 f[4];
@@ -133,8 +135,9 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
           z = f[t] - z;
           if constexpr (!TOTALS) {
             float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
+            const int ld = in_this_step(DV);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+            for (int v = 0; v < 4; ++v) (to + (16 * t + v) * ld)[at_token] = z[v];
           }
           x[h] = -(b[t] * z) * four(rec.rk_since + 16 * t + 4 * q4);
         }

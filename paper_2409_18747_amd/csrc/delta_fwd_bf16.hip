@@ -4,9 +4,9 @@
 // rows of K and Q and the matrices W and P are the same for all.  A step is three products that wait for one another, Kh H, W b Y
 // and Kh^T U.  Each is formed for the wave's columns with the tokens (or keys) down, and so is the next one's operand in the
 // lanes that it is needed in: the state, Y and U never leave the wave's registers.
-//   What nothing waits for is done beside that by as many waves more: they fetch the rows of the next chunk, form P, and of the
-// parts of the state and of U that the others leave in LDS the results, Q H + P U, transposed, so that four consecutive columns
-// of a token are in a lane.
+//   What nothing waits for is done beside that by twice as many waves more.  One half fetches the rows of the next chunk; the other
+// forms P, and of the parts of the state and of U that the first waves leave in LDS the results, Q H + P U, transposed, so that
+// four consecutive columns of a token are in a lane.
 //   With rows of tokens to a wave instead, and states and errors handed round through LDS, prompts of 32 x 16 heads of 2048 rows
 // at 128 x 128 took 811 us, the LDS busy in 64 % of the cycles.
 #include "device_common.h"
@@ -33,7 +33,7 @@ struct DeltaFwdCfg {
 // unit columns without values were its state; delta_carry makes of those the states at the starts, from which the segments are
 // walked again.
 template <typename T, int DK, int NW, int LEVEL, bool TOTALS>
-__global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
+__global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2 : 3) void delta_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
@@ -96,10 +96,11 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
       }
       if (!TOTALS && states != nullptr) {
         float* to = states + (size_t(unit) * chunks + c) * DK * DV;
+        const int ld = in_this_step(DV);
 #pragma unroll
         for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
+          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * ld)[at_key] = S[t][v];
       }
       f32x4 y[4];
       if constexpr (!Cfg::V_IN_LDS) {
@@ -120,8 +121,7 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
         bf16x8 kf[4][IN];
 #pragma unroll
         for (int t = 0; t < 4; ++t) KTile::row_frag(Ks, 16 * t + r, 32 * ks + 8 * q4, kf[t]);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) kh[t] = mm<LEVEL>(kf[t], sf[ks], kh[t]);
+        mm_each<LEVEL>(kf, sf[ks], kh);
       }
       bf16x8 yf[2][LEVEL];
 #pragma unroll
@@ -133,6 +133,19 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
       }
       split8<LEVEL>(y[0], y[1], yf[0]);
       split8<LEVEL>(y[2], y[3], yf[1]);
+      f32x4 e[4];
+      {
+        bf16x8 wf[4][LEVEL], wl[2][LEVEL];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          e[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          load_frag(Ws, w_row_frag(t, 0), l, wf[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) load_frag(Ws, w_row_frag(2 + t, 1), l, wl[t]);
+        mm_each<LEVEL>(wf, yf[0], e);
+        mm_each<LEVEL>(wl, yf[1], e + 2);
+      }
       bf16x8 tf[2][LEVEL];
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -140,21 +153,9 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int it = 2 * p + h;
-          f32x4 e = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k <= p; ++k) {
-            bf16x8 wf[LEVEL];
-            load_frag(Ws, w_row_frag(it, k), l, wf);
-            e = mm<LEVEL>(wf, yf[k], e);
-          }
-          e = y[it] - e;
-          u[h] = e * four(rec.beta + 16 * it + 4 * q4);
+          e[it] = y[it] - e[it];
+          u[h] = e[it] * four(rec.beta + 16 * it + 4 * q4);
           t[h] = u[h] * four(rec.rk_to_end + 16 * it + 4 * q4);
-          if (!TOTALS && errors != nullptr) {
-            float* to = errors + (size_t(unit) * chunks + c) * CHUNK * DV;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) (to + (16 * it + v) * DV)[at_token] = e[v];
-          }
         }
         if constexpr (!TOTALS) {
           bf16x8 uf[OUT];
@@ -164,21 +165,32 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
         split8<LEVEL>(t[0], t[1], tf[p]);
       }
       const float times = rec.times, plus = rec.plus;
-      if constexpr (!TOTALS) lds_barrier();   // U and P are there
+      lds_barrier();   // U and P are there, of the chunk K is needed yet
+      if (!TOTALS && errors != nullptr) {
+        float* to = errors + (size_t(unit) * chunks + c) * CHUNK * DV;
+        const int ld = in_this_step(DV);
 #pragma unroll
-      for (int t = 0; t < 2 * KS; ++t) {
+        for (int it = 0; it < 4; ++it)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) S[t][v] = __builtin_fmaf(S[t][v], plus, S[t][v] * times);
+          for (int v = 0; v < 4; ++v) (to + (16 * it + v) * ld)[at_token] = e[it][v];
       }
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+      for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
-        for (int t = 0; t < 2 * KS; ++t) {
-          bf16x8 kf[IN];
-          KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of(t / 2, t % 2, 0, 0), r, kf);
-          S[t] = mm<LEVEL>(kf, tf[p], S[t]);
+        for (int v = 0; v < 4; ++v) S[t][v] = __builtin_fmaf(S[t][v], plus, S[t][v] * times);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        constexpr int AT_ONCE = 2 * KS < 4 ? 2 * KS : 4;
+#pragma unroll
+        for (int t0 = 0; t0 < 2 * KS; t0 += AT_ONCE) {
+          bf16x8 kf[AT_ONCE][IN];
+#pragma unroll
+          for (int t = 0; t < AT_ONCE; ++t)
+            KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of((t0 + t) / 2, (t0 + t) % 2, 0, 0), r, kf[t]);
+          mm_each<LEVEL>(kf, tf[p], S + t0);
         }
-      lds_barrier();   // everything of the chunk is read
+      }
+      lds_barrier();   // K and the updates are read
     }
     float* to = state_out != nullptr && ends_here ? state_out + size_t(unit) * DK * DV : nullptr;
     if (TOTALS) to = unit_columns ? transitions + (size_t(unit) * G.n + g) * DK * DK : starts + (size_t(unit) * G.n + g + 1) * DK * DV;
@@ -191,118 +203,130 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
     return;
   }
 
-  // ---- the chunks' rows and the results
-  constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
-  const T* Qu = Q + size_t(unit) * N * DK;
-  const T* Ku = K + size_t(unit) * N * DK;
-  const T* Vu = V + size_t(unit) * N * DV + col0;
+  if (role == 1) {
+    // ---- the chunks' rows
+    constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
+    const T* Qu = Q + size_t(unit) * N * DK;
+    const T* Ku = K + size_t(unit) * N * DK;
+    const T* Vu = V + size_t(unit) * N * DV + col0;
+    RowTile<T, DK, 16, NT> kt, qt;
+    RowTile<T, VC, 16, NT> vt;
+    u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
+    const auto fetch = [&](int c) {
+      const int row0 = c * CHUNK;
+      const size_t at = size_t(unit) * chunks + c;
+#pragma unroll
+      for (int i = 0; i < REC_PIECES; ++i)
+        if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
+      if constexpr (!TOTALS) qt.fetch(Qu + size_t(row0) * DK, there - row0);
+      if (Cfg::V_IN_LDS && !unit_columns) vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
+#pragma unroll
+      for (int i = 0; i < W_PIECES; ++i) {   // [fragment][part][lane]: the first LEVEL of three parts
+        const int piece = i * NT + tid;
+        if (W_FRAGS * LEVEL * 64 % NT == 0 || piece < W_FRAGS * LEVEL * 64)
+          w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
+      }
+      kt.fetch(Ku + size_t(row0) * DK, there - row0);
+    };
+    const auto commit = [&]() {   // all but K
+      if constexpr (!TOTALS) {
+        qt.commit(Qs);
+        qt.store_factors(rq, inv_eps);
+      }
+      if (Cfg::V_IN_LDS && !unit_columns) vt.commit(Vs);
+#pragma unroll
+      for (int i = 0; i < REC_PIECES; ++i)
+        if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
+#pragma unroll
+      for (int i = 0; i < W_PIECES; ++i)
+        if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
+    };
+    if (first < steps) {
+      fetch(first);
+      commit();
+    }
+    for (int c = first; c < steps; ++c) {
+      kt.commit(Ks);
+      lds_barrier();   // the chunk is there
+      if (c + 1 < steps) fetch(c + 1);
+      lds_barrier();   // of the chunk K is needed yet
+      if (c + 1 < steps) commit();
+      lds_barrier();   // K is read
+    }
+    return;
+  }
+
+  // ---- the results
+  if constexpr (TOTALS) return;
   T* Ou = O + size_t(unit) * N * DV + col0;
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
-  RowTile<T, DK, 16, NT> kt, qt;
-  RowTile<T, VC, 16, NT> vt;
-  u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
-  const auto fetch = [&](int c) {
-    const int row0 = c * CHUNK;
-    kt.fetch(Ku + size_t(row0) * DK, there - row0);
-    if constexpr (!TOTALS) qt.fetch(Qu + size_t(row0) * DK, there - row0);
-    if (Cfg::V_IN_LDS && !unit_columns) vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
-    const size_t at = size_t(unit) * chunks + c;
-#pragma unroll
-    for (int i = 0; i < REC_PIECES; ++i)
-      if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
-#pragma unroll
-    for (int i = 0; i < W_PIECES; ++i) {   // [fragment][part][lane]: the first LEVEL of three parts
-      const int piece = i * NT + tid;
-      if (W_FRAGS * LEVEL * 64 % NT == 0 || piece < W_FRAGS * LEVEL * 64)
-        w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
-    }
-  };
-  if (first < steps) fetch(first);
   for (int c = first; c < steps; ++c) {
     const int row0 = c * CHUNK;
-    kt.commit(Ks);
-    if constexpr (!TOTALS) {
-      qt.commit(Qs);
-      qt.store_factors(rq, inv_eps);
-    }
-    if (Cfg::V_IN_LDS && !unit_columns) vt.commit(Vs);
-#pragma unroll
-    for (int i = 0; i < REC_PIECES; ++i)
-      if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
-#pragma unroll
-    for (int i = 0; i < W_PIECES; ++i)
-      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
     lds_barrier();   // the chunk is there
-    if (c + 1 < steps) fetch(c + 1);
-    if constexpr (TOTALS) {
-      lds_barrier();   // everything of the chunk is read
-      continue;
-    }
-
-    // P, a tile of rows to a wave (two where there are two waves), keys down: an operand as it stands
+    // P, a tile of rows to a wave (two where there are two waves), keys down: an operand as it stands.  (The tiles above the
+    // diagonal, too: the workgroup waits for the wave that has none.)
 #pragma unroll
     for (int turn = 0; turn < 4 / NW; ++turn) {
       const int it = turn == 0 ? w : 3 - w, own = 16 * it + r;
-      const float rq_own = rq[own];
-      bf16x8 qf[KS][IN];
+      f32x4 t[4];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Qs, own, 32 * ks + 8 * q4, qf[ks]);
-      for (int p = 0; w_row_there(it, p) && p < 2; ++p) {
-        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      for (int jt = 0; jt < 4; ++jt) t[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int jt = 2 * p + h;
-          if (jt > it) continue;
-          f32x4 t = {0.f, 0.f, 0.f, 0.f};
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 qf[IN], kf[4][IN];
+        KTile::row_frag(Qs, own, 32 * ks + 8 * q4, qf);
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            bf16x8 kf[IN];
-            KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf);
-            t = mm<OUT>(kf, qf[ks], t);
-          }
-          if (jt < it) {
-            half[h] = t * four(rec.rk_to_tile + 16 * jt + 4 * q4) * (rq_own * rec.in_tile[own] * rec.between[it][jt]);
-          } else {
-            const double g_own = rec.decay[own];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const int j = 16 * jt + 4 * q4 + v;
-              half[h][v] = j <= own ? t[v] * rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
-            }
-          }
-        }
-        bf16x8 pf[OUT];
-        split8<OUT>(half[0], half[1], pf);
-        store_frag<OUT>(Ps, w_row_frag(it, p), l, pf);
+        for (int jt = 0; jt < 4; ++jt) KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf[jt]);
+        mm_each<OUT>(kf, qf, t);
       }
+      const float rq_own = rq[own], in_tile = rq_own * rec.in_tile[own];
+      f32x4 diagonal;
+      {
+        const double g_own = rec.decay[own];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int j = 16 * it + 4 * q4 + v;
+          diagonal[v] = j <= own ? rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) {
+        const f32x4 below = four(rec.rk_to_tile + 16 * jt + 4 * q4) * (in_tile * rec.between[it][jt]);   // 0 from the diagonal on
+#pragma unroll
+        for (int v = 0; v < 4; ++v) t[jt][v] *= jt == it ? diagonal[v] : below[v];
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        if (w_row_there(it, p)) {
+          bf16x8 pf[OUT];
+          split8<OUT>(t[2 * p], t[2 * p + 1], pf);
+          store_frag<OUT>(Ps, w_row_frag(it, p), l, pf);
+        }
     }
     f32x4 o[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      bf16x8 sf[OUT];
+      bf16x8 sf[OUT], qf[4][IN];
       load_frag(Ss, w * KS + ks, l, sf);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        bf16x8 qf[IN];
-        KTile::row_frag(Qs, 16 * t + r, 32 * ks + 8 * q4, qf);
-        o[t] = mm<OUT>(sf, qf, o[t]);
-      }
+      for (int t = 0; t < 4; ++t) KTile::row_frag(Qs, 16 * t + r, 32 * ks + 8 * q4, qf[t]);
+      mm_each<OUT>(sf, qf, o);
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) o[t] *= rq[16 * t + r] * rec.since[16 * t + r];
-    lds_barrier();   // U and P are there
+    lds_barrier();   // U and P are there, of the chunk K is needed yet
+    {
+      bf16x8 uf[2][OUT], pf[4][OUT], pl[2][OUT];
+      load_frag(Us, w * 2, l, uf[0]);
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      bf16x8 uf[OUT];
-      load_frag(Us, w * 2 + p, l, uf);
+      for (int it = 0; it < 4; ++it) load_frag(Ps, w_row_frag(it, 0), l, pf[it]);
+      load_frag(Us, w * 2 + 1, l, uf[1]);
 #pragma unroll
-      for (int it = 2 * p; it < 4; ++it) {
-        bf16x8 pf[OUT];
-        load_frag(Ps, w_row_frag(it, p), l, pf);
-        o[it] = mm<OUT>(uf, pf, o[it]);
-      }
+      for (int it = 0; it < 2; ++it) load_frag(Ps, w_row_frag(2 + it, 1), l, pl[it]);
+      mm_each<OUT>(uf[0], pf, o);
+      mm_each<OUT>(uf[1], pl, o + 2);
     }
     if (O != nullptr) {
 #pragma unroll
@@ -311,10 +335,10 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_fwd_scan(
           *reinterpret_cast<vec4*>(Ou + (size_t(row0) + 16 * it) * DV + unsigned(r * DV + 16 * w + 4 * q4)) =
               vec4{T(scale * o[it][0]), T(scale * o[it][1]), T(scale * o[it][2]), T(scale * o[it][3])};
     }
-    lds_barrier();   // everything of the chunk is read
+    lds_barrier();   // the updates and P are read
   }
   // rows that do not exist
-  if (TOTALS || O == nullptr) return;
+  if (O == nullptr) return;
   const int lo = max(there, first * CHUNK), hi = min(N, (first + seg) * CHUNK);
   for (long i = tid; i < long(hi - lo) * (VC / 4); i += NT)
     *reinterpret_cast<vec4*>(Ou + size_t(lo + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
@@ -592,9 +616,9 @@ hipError_t run_scan(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
   const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
   if constexpr (DeltaFwdCfg<T, DK, NW, LEVEL>::FITS) {
-    const auto run = [&](auto kernel, int n_parts) {
+    const auto run = [&](auto kernel, int n_parts, int threads) {
       return launch_kernel("delta_fwd_scan", kernel, a.G == 1 ? dim3(unsigned(units * n_parts)) : dim3(unsigned(units * a.G), unsigned(n_parts)),
-                           dim3(128 * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
+                           dim3(threads), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
                            static_cast<const T*>(a.V), a.s, a.seq_len, a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows,
                            a.errors, a.states, a.starts, a.transitions, Divisor(a.H), Divisor(a.G), Divisor(n_parts), a.seg, a.N,
                            units, a.dv, 1.0f / a.eps);
@@ -602,11 +626,11 @@ hipError_t run_scan(const DeltaArgs& a) {
     if (a.G > 1) {
       // M is not asked for where the states at the starts of two segments are known without, and no backward follows
       const int with_M = a.G > 2 || a.errors != nullptr ? (DK + 16 * NW - 1) / (16 * NW) : 0;
-      hipError_t err = run(delta_fwd_scan<T, DK, NW, 3, true>, parts + with_M);
+      hipError_t err = run(delta_fwd_scan<T, DK, NW, 3, true>, parts + with_M, 128 * NW);
       if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, false);
       if (err != hipSuccess) return err;
     }
-    return run(delta_fwd_scan<T, DK, NW, LEVEL, false>, parts);
+    return run(delta_fwd_scan<T, DK, NW, LEVEL, false>, parts, 192 * NW);
   } else {
     return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW, LEVEL>, dim3(unsigned(units * parts)), dim3(64 * NW), 0,
                          a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s,
