@@ -30,6 +30,7 @@ class _NoMarshal:
         return None
     bwd = step = scale_varlen = bind = fwd
     fwd_decay = bwd_decay = step_decay = tree = tree_accept = fwd
+    fwd_delta = bwd_delta = step_delta = rotary = fwd
 
 
 def _import_marshal():
@@ -37,9 +38,10 @@ def _import_marshal():
     try:
         from . import _marshal
         built_for = getattr(_marshal, "built_for", "something else")
-        if built_for == target:
+        missing = [name for name in vars(_NoMarshal) if not name.startswith("_") and not hasattr(_marshal, name)]
+        if built_for == target and not missing:
             return _marshal
-        why = "was built for %s, not for %s" % (built_for, target)
+        why = "was built for %s, not for %s" % (built_for, target) if built_for != target else "lacks %s" % ", ".join(missing)
     except ImportError as e:
         built = os.path.exists(os.path.join(_HERE, "_marshal.so"))
         why = "does not load (%s)" % e if built else "is not built"
@@ -970,6 +972,10 @@ def cottn_fwd_causal_delta(Q, K, V, s, log_decay, beta, seq_len=None, state_in=N
     the state before the first row, and `state` receives that after the last one, both float32 [B, H, d_key, d_value]; they may be
     one tensor.  workspace: for a backward that takes it over as fwd_workspace, of cottn_workspace_bytes_dkdv(OP_FWD_DELTA, ..)
     bytes; without one the call allocates what it needs by itself."""
+    if stream is None:
+        done = _marshal.fwd_delta(Q, K, V, s, log_decay, beta, seq_len, state_in, O, state, workspace, eps)
+        if done is not None:
+            return done
     B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
     if O is None:
         O = torch.empty_like(V)
@@ -998,6 +1004,11 @@ def cottn_bwd_causal_delta(Q, K, V, s, log_decay, beta, dO, seq_len=None, state_
     float32 [H], or [B, H] with seq_len, dlog_decay (None where log_decay is) and dbeta float32 [B, H, N].  state_in as in the
     forward call; dstate, if given, is the gradient wrt its `state`, and dstate_in receives that wrt its state_in (one tensor is
     allowed).  fwd_workspace: the workspace tensor of the matching forward call (untouched since), or None."""
+    if stream is None:
+        done = _marshal.bwd_delta(Q, K, V, s, log_decay, beta, seq_len, dO, state_in, dstate, dQ, dK, dV, ds, dlog_decay, dbeta,
+                                  dstate_in, fwd_workspace, workspace, eps)
+        if done is not None:
+            return done
     B, H, N, dk, dv, dt = _dims_dkdv(Q, V)
     dQ, dK, dV, ds = _grads_dkdv(Q, V, dQ, dK, dV, ds, H if seq_len is None else (B, H))
     if dbeta is None:
@@ -1032,6 +1043,10 @@ def cottn_step_delta(q, k, v, s, log_decay, beta, state, state_in=None, parent=N
     """One token of B sequences by the gated delta rule (cottn_fwd_causal_delta); returns o = s_h qhat state (like v).  q, k are
     [B, H, d_key] and v [B, H, d_value]; log_decay (or None: no decay) and beta float32 [B, H]; state, state_in and parent as in
     cottn_step_decay."""
+    if stream is None:
+        done = _marshal.step_delta(q, k, v, s, log_decay, beta, state, state_in, parent, o, eps)
+        if done is not None:
+            return done
     B, H, dk, dv, dt = _token_widths(q, v, 3, "[B, H, d]")
     if o is None:
         o = torch.empty_like(v)
@@ -1065,6 +1080,10 @@ def cottn_rotary(Q, K, positions, freq, axis=None, neighbours=False, inverse=Fal
     [pairs], radians to a position; axis: int32 [pairs], or None for the first.  A pair is features 2 p and 2 p + 1 with
     `neighbours`, else p and p + pairs; features behind 2 pairs are copied.  inverse: turned back, which is the gradient.  Qr may
     be Q and Kr may be K."""
+    if stream is None:
+        done = _marshal.rotary(Q, K, positions, freq, axis, neighbours, inverse, Qr, Kr)
+        if done is not None:
+            return done
     if Q.dim() != 4:
         raise ValueError("rows must be [B, H, N, d], got shape %s" % (tuple(Q.shape),))
     B, H, N, d = Q.shape

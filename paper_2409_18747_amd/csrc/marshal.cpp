@@ -47,6 +47,10 @@ struct Library {
   decltype(&cottn_step_decay) step_decay;
   decltype(&cottn_tree) tree;
   decltype(&cottn_tree_accept) tree_accept;
+  decltype(&cottn_fwd_causal_delta) fwd_causal_delta;
+  decltype(&cottn_bwd_causal_delta) bwd_causal_delta;
+  decltype(&cottn_step_delta) step_delta;
+  decltype(&cottn_rotary) rotary;
   decltype(&cottn_scale_from_m_varlen) scale_from_m_varlen;
   decltype(&cottn_scale_backward_varlen) scale_backward_varlen;
 } lib;
@@ -158,6 +162,30 @@ struct Call {
     ok = ok && ref != nullptr && t->dim() == ref->dim() && t->scalar_type() == ref->scalar_type() && t->device() == device &&
          t->sizes().slice(0, t->dim() - 1) == ref->sizes().slice(0, ref->dim() - 1) && t->size(t->dim() - 1) <= INT_MAX;
     return t;
+  }
+  // the states that a step goes on from: `own`, those of as many sequences, or, where a parent comes next, those of B_in
+  const float* states_from(const float* own, int64_t one, int& B_in) {
+    if (*next == Py_None) {
+      ++next;
+      ok = ok && *next == Py_None;   // (a parent without state_in)
+      return own;
+    }
+    const at::Tensor* t = tensor();
+    if (!ok) return nullptr;
+    if (*next != Py_None) {
+      if (t->dim() != 4 || t->size(0) > INT_MAX) {
+        ok = false;
+        return nullptr;
+      }
+      B_in = int(t->size(0));
+    }
+    ok = t->scalar_type() == at::kFloat && t->numel() == int64_t(B_in) * one && t->device() == device;
+    return ok ? static_cast<const float*>(t->data_ptr()) : nullptr;
+  }
+  bool truth() {
+    PyObject* o = *next++;
+    ok = ok && PyBool_Check(o);
+    return o == Py_True;
   }
   // a workspace and its size
   void* bytes(size_t& size) {
@@ -591,20 +619,7 @@ PyObject* step_decay(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const float* log_decay = static_cast<const float*>(c.floats(H, true));
   float* state = static_cast<float*>(c.floats(int64_t(B) * H * dk * dv));
   int B_in = B;
-  const float* from = state;
-  if (*c.next == Py_None) {
-    ++c.next;
-    if (*c.next != Py_None) Py_RETURN_NONE;   // (a parent without state_in)
-  } else {
-    const at::Tensor* t = c.tensor();
-    if (!c.ok) Py_RETURN_NONE;
-    if (*c.next != Py_None) {
-      if (t->dim() != 4 || t->size(0) > INT_MAX) Py_RETURN_NONE;
-      B_in = int(t->size(0));
-    }
-    if (t->scalar_type() != at::kFloat || t->numel() != int64_t(B_in) * H * dk * dv || t->device() != c.device) Py_RETURN_NONE;
-    from = static_cast<const float*>(t->data_ptr());
-  }
+  const float* from = c.states_from(state, int64_t(H) * dk * dv, B_in);
   const int* parent = c.indices({B}, true);
   PyObject* given = *c.next;
   const at::Tensor* o = c.rows_like(v, true);
@@ -686,6 +701,230 @@ PyObject* tree_accept(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// fwd_delta(Q, K, V, s, log_decay, beta, seq_len, state_in, O, state, workspace, eps)
+PyObject* fwd_delta(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 12 || modes_on() || lib.fwd_causal_delta == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *Q = c.first(4), *K = c.rows_like(Q), *V = c.rows_beside(Q);
+  if (!c.ok || !sizes_fit(*Q)) Py_RETURN_NONE;
+  const int B = int(Q->size(0)), H = int(Q->size(1)), N = int(Q->size(2)), dk = int(Q->size(3)), dv = int(V->size(3)),
+            dt = dtype_code(*Q);
+  const int64_t units = int64_t(B) * H, states = units * dk * dv;
+  const bool padded = args[6] != Py_None;
+  const float* s = static_cast<const float*>(c.floats(padded ? units : H));
+  const float* log_decay = static_cast<const float*>(c.floats(units * N, true));
+  const float* beta = static_cast<const float*>(c.floats(units * N));
+  const int* seq_len = padded ? c.lengths(B) : (++c.next, nullptr);
+  const float* state_in = static_cast<const float*>(c.floats(states, true));
+  PyObject* given = *c.next;
+  const at::Tensor* O = c.rows_like(V, true);
+  float* state = static_cast<float*>(c.floats(states, true));
+  const bool given_workspace = *c.next != Py_None;
+  size_t have = 0;
+  void* workspace = c.bytes(have);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  if (!given_workspace) {
+    have = lib.workspace_bytes_dkdv(COTTN_OP_FWD_DELTA_ALONE, B, H, N, dk, dv, 0, dt);
+    if (have == size_t(-1)) Py_RETURN_NONE;
+  }
+  at::Tensor made, scratch;
+  int st;
+  {
+    const Unlocked unlocked;
+    if (O == nullptr) {
+      made = at::empty(V->sizes(), V->options());
+      O = &made;
+    }
+    if (!given_workspace && have > 0) {
+      scratch = at::empty({int64_t(have)}, Q->options().dtype(at::kByte));
+      workspace = scratch.data_ptr();
+    }
+    st = lib.fwd_causal_delta(Q->data_ptr(), K->data_ptr(), V->data_ptr(), s, log_decay, beta, seq_len, state_in, O->data_ptr(),
+                              state, workspace, have, B, H, N, dk, dv, dt, eps, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_fwd_causal_delta");
+  return result(given, made);
+  END_HANDLE_TH_ERRORS
+}
+
+// bwd_delta(Q, K, V, s, log_decay, beta, seq_len, dO, state_in, dstate, dQ, dK, dV, ds, dlog_decay, dbeta, dstate_in,
+//           fwd_workspace, workspace, eps)
+PyObject* bwd_delta(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 20 || modes_on() || lib.bwd_causal_delta == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *Q = c.first(4), *K = c.rows_like(Q), *V = c.rows_beside(Q);
+  if (!c.ok || !sizes_fit(*Q)) Py_RETURN_NONE;
+  const int B = int(Q->size(0)), H = int(Q->size(1)), N = int(Q->size(2)), dk = int(Q->size(3)), dv = int(V->size(3)),
+            dt = dtype_code(*Q);
+  const int64_t units = int64_t(B) * H, states = units * dk * dv, gates = units * N;
+  const bool padded = args[6] != Py_None, decays = args[4] != Py_None;
+  const int64_t scales = padded ? units : H;
+  const float* s = static_cast<const float*>(c.floats(scales));
+  const float* log_decay = static_cast<const float*>(c.floats(gates, true));
+  const float* beta = static_cast<const float*>(c.floats(gates));
+  const int* seq_len = padded ? c.lengths(B) : (++c.next, nullptr);
+  const at::Tensor* dO = c.rows_like(V);
+  const float* state_in = static_cast<const float*>(c.floats(states, true));
+  const float* dstate = static_cast<const float*>(c.floats(states, true));
+  PyObject* const* given = c.next;   // dQ, dK, dV, ds, dlog_decay, dbeta
+  const at::Tensor* grads[3] = {c.rows_like(Q, true), nullptr, nullptr};
+  grads[1] = c.rows_like(Q, true);
+  grads[2] = c.rows_like(V, true);
+  float* gates_of[3] = {static_cast<float*>(c.floats(scales, true)), nullptr, nullptr};
+  gates_of[1] = static_cast<float*>(c.floats(gates, true));
+  gates_of[2] = static_cast<float*>(c.floats(gates, true));
+  float* dstate_in = static_cast<float*>(c.floats(states, true));
+  size_t fwd_have = 0, have = 0;
+  const void* fwd_workspace = c.bytes(fwd_have);
+  const bool given_workspace = *c.next != Py_None;
+  void* workspace = c.bytes(have);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  if (!given_workspace) {
+    have = lib.workspace_bytes_dkdv(fwd_workspace != nullptr ? COTTN_OP_BWD_DELTA_SAVED : COTTN_OP_BWD_DELTA, B, H, N, dk, dv, 0, dt);
+    if (have == size_t(-1)) Py_RETURN_NONE;
+  }
+  at::Tensor made[6], scratch;
+  int st;
+  {
+    const Unlocked unlocked;
+    for (int i = 0; i < 3; ++i)
+      if (grads[i] == nullptr) {
+        const at::Tensor* ref = i < 2 ? Q : V;
+        made[i] = at::empty(ref->sizes(), ref->options());
+        grads[i] = &made[i];
+      }
+    for (int i = 0; i < 3; ++i)
+      if (given[3 + i] == Py_None && (i != 1 || decays)) {
+        made[3 + i] = i > 0 ? at::empty({B, H, N}, Q->options().dtype(at::kFloat))
+                      : padded ? at::empty({B, H}, Q->options().dtype(at::kFloat)) : at::empty({H}, Q->options().dtype(at::kFloat));
+        gates_of[i] = static_cast<float*>(made[3 + i].data_ptr());
+      }
+    if (!given_workspace && have > 0) {
+      scratch = at::empty({int64_t(have)}, Q->options().dtype(at::kByte));
+      workspace = scratch.data_ptr();
+    }
+    st = lib.bwd_causal_delta(Q->data_ptr(), K->data_ptr(), V->data_ptr(), s, log_decay, beta, seq_len, dO->data_ptr(), state_in,
+                              dstate, grads[0]->data_ptr(), grads[1]->data_ptr(), grads[2]->data_ptr(), gates_of[0], gates_of[1],
+                              gates_of[2], dstate_in, fwd_workspace, fwd_have, workspace, have, B, H, N, dk, dv, dt, eps,
+                              current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_bwd_causal_delta");
+  PyObject* all = PyTuple_New(6);
+  if (all == nullptr) return nullptr;
+  for (int i = 0; i < 6; ++i) {
+    PyObject* o;
+    if (i == 4 && !decays && given[4] == Py_None) {
+      Py_INCREF(Py_None);
+      o = Py_None;
+    } else {
+      o = result(given[i], made[i]);
+    }
+    if (o == nullptr) {
+      Py_DECREF(all);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(all, i, o);
+  }
+  return all;
+  END_HANDLE_TH_ERRORS
+}
+
+// step_delta(q, k, v, s, log_decay, beta, state, state_in, parent, o, eps)
+PyObject* step_delta(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11 || modes_on() || lib.step_delta == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *q = c.first(3), *k = c.rows_like(q), *v = c.rows_beside(q);
+  if (!c.ok || !sizes_fit(*q)) Py_RETURN_NONE;
+  const int B = int(q->size(0)), H = int(q->size(1)), dk = int(q->size(2)), dv = int(v->size(2)), dt = dtype_code(*q);
+  const int64_t units = int64_t(B) * H;
+  const float* s = static_cast<const float*>(c.floats(H));
+  const float* log_decay = static_cast<const float*>(c.floats(units, true));
+  const float* beta = static_cast<const float*>(c.floats(units));
+  float* state = static_cast<float*>(c.floats(units * dk * dv));
+  int B_in = B;
+  const float* from = c.states_from(state, int64_t(H) * dk * dv, B_in);
+  const int* parent = c.indices({B}, true);
+  PyObject* given = *c.next;
+  const at::Tensor* o = c.rows_like(v, true);
+  const float eps = c.real();
+  if (!c.ok) Py_RETURN_NONE;
+  at::Tensor made;
+  int st;
+  {
+    const Unlocked unlocked;
+    if (o == nullptr) {
+      made = at::empty(v->sizes(), v->options());
+      o = &made;
+    }
+    st = lib.step_delta(q->data_ptr(), k->data_ptr(), v->data_ptr(), s, log_decay, beta, from, parent, B_in, state, o->data_ptr(),
+                        B, H, dk, dv, dt, eps, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_step_delta");
+  return result(given, made);
+  END_HANDLE_TH_ERRORS
+}
+
+// rotary(Q, K or None, positions, freq, axis, neighbours, inverse, Qr, Kr)
+PyObject* rotary(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 9 || modes_on() || lib.rotary == nullptr) Py_RETURN_NONE;
+  Call c{args};
+  const at::Tensor *Q = c.first(4), *K = c.rows_like(Q, true);
+  if (!c.ok || !sizes_fit(*Q)) Py_RETURN_NONE;
+  const int B = int(Q->size(0)), H = int(Q->size(1)), N = int(Q->size(2)), d = int(Q->size(3)), dt = dtype_code(*Q);
+  const at::Tensor* positions = c.tensor();
+  const at::Tensor* freq = c.tensor();
+  if (!c.ok || positions->scalar_type() != at::kInt || positions->device() != c.device || positions->dim() < 2 ||
+      positions->dim() > 3 || positions->size(0) != B || positions->size(1) != N || freq->dim() != 1 ||
+      freq->scalar_type() != at::kFloat || freq->device() != c.device || freq->size(0) > INT_MAX)
+    Py_RETURN_NONE;
+  if (positions->dim() == 3 && positions->size(2) > INT_MAX) Py_RETURN_NONE;
+  const int axes = positions->dim() == 3 ? int(positions->size(2)) : 1, pairs = int(freq->size(0));
+  const int* axis = c.indices({pairs}, true);
+  const bool neighbours = c.truth(), inverse = c.truth();
+  PyObject* const* given = c.next;   // Qr, Kr
+  const at::Tensor* out[2] = {c.rows_like(Q, true), nullptr};
+  out[1] = c.rows_like(Q, true);
+  if (!c.ok || (K == nullptr && out[1] != nullptr)) Py_RETURN_NONE;
+  at::Tensor made[2];
+  int st;
+  {
+    const Unlocked unlocked;
+    for (int i = 0; i < 2; ++i)
+      if (out[i] == nullptr && (i == 0 || K != nullptr)) {
+        made[i] = at::empty(Q->sizes(), Q->options());
+        out[i] = &made[i];
+      }
+    st = lib.rotary(Q->data_ptr(), K != nullptr ? K->data_ptr() : nullptr, static_cast<const int*>(positions->data_ptr()),
+                    static_cast<const float*>(freq->data_ptr()), axis, out[0]->data_ptr(),
+                    K != nullptr ? out[1]->data_ptr() : nullptr, B, H, N, d, pairs, axes, neighbours, inverse, dt, current_stream());
+  }
+  if (st != COTTN_OK) return raise_status(st, "cottn_rotary");
+  PyObject* all = PyTuple_New(2);
+  if (all == nullptr) return nullptr;
+  for (int i = 0; i < 2; ++i) {
+    PyObject* o;
+    if (i == 1 && K == nullptr) {
+      Py_INCREF(Py_None);
+      o = Py_None;
+    } else {
+      o = result(given[i], made[i]);
+    }
+    if (o == nullptr) {
+      Py_DECREF(all);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(all, i, o);
+  }
+  return all;
+  END_HANDLE_TH_ERRORS
+}
+
 // scale_varlen(m, seq_len, ds or None, result): s from m, or with ds the gradient of m
 PyObject* scale_varlen(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -762,6 +1001,10 @@ PyObject* bind(PyObject*, PyObject* args) {
   COTTN_FIND(step_decay);
   COTTN_FIND(tree);
   COTTN_FIND(tree_accept);
+  COTTN_FIND(fwd_causal_delta);
+  COTTN_FIND(bwd_causal_delta);
+  COTTN_FIND(step_delta);
+  COTTN_FIND(rotary);
 #undef COTTN_FIND
   if (!needed) {
     PyErr_Format(PyExc_ImportError, "%s lacks a function of cottn.h", path);
@@ -784,6 +1027,10 @@ PyMethodDef methods[] = {
     {"step_decay", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(step_decay)), METH_FASTCALL, nullptr},
     {"tree", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree)), METH_FASTCALL, nullptr},
     {"tree_accept", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_accept)), METH_FASTCALL, nullptr},
+    {"fwd_delta", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fwd_delta)), METH_FASTCALL, nullptr},
+    {"bwd_delta", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bwd_delta)), METH_FASTCALL, nullptr},
+    {"step_delta", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(step_delta)), METH_FASTCALL, nullptr},
+    {"rotary", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rotary)), METH_FASTCALL, nullptr},
     {"scale_varlen", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(scale_varlen)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
