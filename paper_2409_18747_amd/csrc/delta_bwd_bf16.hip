@@ -9,16 +9,16 @@ namespace {
 
 // ---------------------------------------------------------------------------------------
 // As in the forward scan a wave has 16 value columns, whose D, F and X never leave its registers: F = P^T dO' + (G_n/G) Kh D, Z =
-// F - W^T (b F), and D in front of the chunk, one after the other.  Beside those as many waves more fetch the rows, form P, and
-// hand over what does not depend on D: P^T dO' and, where the LDS has room for it, (G Qh)^T dO'.
+// F - W^T (b F), and D in front of the chunk, one after the other.  What does not depend on D, P^T dO' and R = (G Qh)^T dO', is
+// formed beside that, a chunk ahead, by as many waves more; and again as many fetch the rows.
 template <typename T, int DK, int NW>
-struct DeltaRevCfg {
-  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, KS = DK / 32, PAD = sizeof(T) == 4 ? 8 : 16;
-  using KTile = PartTile<CHUNK, DK, IN, PAD>;
-  using GTile = PartTile<CHUNK, VC, IN, PAD>;      // rows of dO
+struct DeltaAheadCfg {
+  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, KS = DK / 32;
+  using KTile = PartTile<CHUNK, DK, IN>;
+  using GTile = PartTile<CHUNK, VC, IN>;      // rows of dO
   static constexpr int W_SIZE = W_FRAGS * LEVEL * 512;
-  static constexpr int BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + 2 * W_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK + NW * 4 * 1024;
-  static constexpr bool HANDS_R = BYTES + NW * 2 * KS * 1024 <= 160 * 1024;
+  static constexpr int BYTES = 2 * (3 * KTile::SIZE + GTile::SIZE + 2 * W_SIZE) + 2 * int(sizeof(ChunkRecord)) + 4 * CHUNK +
+                               NW * (4 + 2 * KS) * 1024;
   static constexpr bool FITS = BYTES <= 160 * 1024;
 };
 
@@ -33,6 +33,316 @@ __device__ __forceinline__ void weighted_rows(const bf16x8 (&g)[IN], const float
 
 // Segments as in the forward scan: TOTALS leaves what a segment makes of zeros (the last one: of dstate) in the place of the
 // gradient with respect to the state in front of it.
+template <typename T, int DK, int NW, bool TOTALS>
+__global__ __launch_bounds__(192 * NW, NW <= 2 ? 1 : 3) void delta_ahead_rev_scan(
+    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
+    const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
+    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, float* ends, Divisor H,
+    Divisor G, Divisor parts, int seg, int N, int units, int DV, float inv_eps) {
+  using Cfg = DeltaAheadCfg<T, DK, NW>;
+  using KTile = typename Cfg::KTile;
+  using GTile = typename Cfg::GTile;
+  constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, KS = Cfg::KS, NT = 64 * NW, VC = Cfg::VC;
+  __shared__ __attribute__((aligned(16))) uint16_t K2[2][KTile::SIZE];   // of the chunks with even and with odd numbers
+  __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Os[GTile::SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ws[Cfg::W_SIZE];
+  __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::W_SIZE];
+  __shared__ f32x4 Fs[NW * 4 * 64];         // P^T dO', tiles in accumulator order
+  __shared__ f32x4 Rs[NW * 2 * KS * 64];    // R
+  __shared__ ChunkRecord recs[2];
+  __shared__ __attribute__((aligned(16))) float rq[CHUNK];
+  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, ends, H, G, parts, seg, N, units, DV,
+                     inv_eps);
+  int unit, part, g = 0;
+  if (G.n == 1) {
+    unit_and_segment(blockIdx.x, units, parts, unit, part);
+  } else {   // (blockIdx.y: the part)
+    unit_and_segment(blockIdx.x, units, G, unit, g);
+    part = blockIdx.y;
+  }
+  const int tid = threadIdx.x % NT, role = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / NT);
+  const int w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), all = delta_chunks(there), first = g * seg, steps = min(all, first + seg);
+  const int col0 = part * VC;
+  if ((first >= all && g > 0) || (TOTALS && g == 0)) return;
+  const bool ends_here = steps == all;   // the last rows
+  const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
+
+  // In step c the first waves take chunk c and the others form what they will need of chunk c - 1, from the one behind the last on.
+  if (role == 0) {
+    // ---- the gradients with respect to the states
+    // this lane's value column in the first key row, and in the first token row, that it holds
+    const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
+    const float* from = ends_here ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
+                                  : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
+    f32x4 D[2 * KS];
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        D[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+    lds_barrier();
+    lds_barrier();
+    lds_barrier();
+    for (int c = steps - 1; c >= first; --c) {
+      const uint16_t* Ks = K2[c & 1];
+      const ChunkRecord& rec = recs[c & 1];
+      bf16x8 df[KS][LEVEL];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) split8<LEVEL>(D[2 * ks], D[2 * ks + 1], df[ks]);
+      if constexpr (!TOTALS) {
+        float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
+        const int ld = in_this_step(DV);
+#pragma unroll
+        for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * ld)[at_key] = D[t][v];
+      }
+      lds_barrier();   // the chunk is there
+      f32x4 f[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) f[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf[4][IN];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) KTile::row_frag(Ks, 16 * t + r, 32 * ks + 8 * q4, kf[t]);
+        mm_each<LEVEL>(kf, df[ks], f);
+      }
+      f32x4 b[4], z[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f[t] = f[t] * four(rec.rk_to_end + 16 * t + 4 * q4) + Fs[(w * 4 + t) * 64 + l];
+        b[t] = four(rec.beta + 16 * t + 4 * q4);
+        z[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      bf16x8 ff[2][LEVEL], xf[2][LEVEL];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) split8<LEVEL>(b[2 * p] * f[2 * p], b[2 * p + 1] * f[2 * p + 1], ff[p]);
+      {
+        bf16x8 wf[2][LEVEL], wl[4][LEVEL];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) load_frag(Ws, w_col_frag(t, 0), l, wf[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) load_frag(Ws, w_col_frag(t, 1), l, wl[t]);
+        mm_each<LEVEL>(wl, ff[1], z);
+        mm_each<LEVEL>(wf, ff[0], z);
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        f32x4 x[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int t = 2 * p + h;
+          z[t] = f[t] - z[t];
+          x[h] = -(b[t] * z[t]) * four(rec.rk_since + 16 * t + 4 * q4);
+        }
+        split8<LEVEL>(x[0], x[1], xf[p]);
+      }
+      const float times = rec.times, plus = rec.plus;
+      lds_barrier();   // of the chunk K is needed yet
+      if constexpr (!TOTALS) {
+        float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
+        const int ld = in_this_step(DV);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) (to + (16 * t + v) * ld)[at_token] = z[t][v];
+      }
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) D[t][v] = __builtin_fmaf(D[t][v], plus, D[t][v] * times);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        constexpr int AT_ONCE = 2 * KS < 4 ? 2 * KS : 4;
+#pragma unroll
+        for (int t0 = 0; t0 < 2 * KS; t0 += AT_ONCE) {
+          bf16x8 kf[AT_ONCE][IN];
+#pragma unroll
+          for (int t = 0; t < AT_ONCE; ++t)
+            KTile::spread_col_frag(Ks, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of((t0 + t) / 2, (t0 + t) % 2, 0, 0), r, kf[t]);
+          mm_each<LEVEL>(kf, xf[p], D + t0);
+        }
+      }
+      lds_barrier();   // K is read, R is there
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t) D[t] += Rs[(w * 2 * KS + t) * 64 + l];
+    }
+    float* to = TOTALS ? ends + (size_t(unit) * G.n + g - 1) * DK * DV : dstate_in != nullptr && g == 0 ? dstate_in + size_t(unit) * DK * DV : nullptr;
+    if (to != nullptr) {
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+    }
+    return;
+  }
+
+  if (role == 1) {
+    // ---- the chunks' rows
+    constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
+    const T* Qu = Q + size_t(unit) * N * DK;
+    const T* Ku = K + size_t(unit) * N * DK;
+    const T* dOu = dO + size_t(unit) * N * DV + col0;
+    RowTile<T, DK, 16, NT> kt, qt;
+    RowTile<T, VC, 16, NT> gt;
+    u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
+    const auto fetch = [&](int c) {
+      const int row0 = c * CHUNK;
+#pragma unroll
+      for (int i = 0; i < REC_PIECES; ++i)
+        if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + size_t(unit) * chunks + c)[i * NT + tid];
+      kt.fetch(Ku + size_t(row0) * DK, there - row0);
+      qt.fetch(Qu + size_t(row0) * DK, there - row0);
+      gt.fetch(dOu + size_t(row0) * DV, there - row0, DV);
+    };
+    const auto commit = [&](int c) {
+      kt.commit(K2[c & 1]);
+      qt.commit(Qs);
+      qt.store_factors(rq, inv_eps);
+      gt.commit(Os);
+#pragma unroll
+      for (int i = 0; i < REC_PIECES; ++i)
+        if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&recs[c & 1])[i * NT + tid] = rec_next[i];
+    };
+    const auto fetch_W = [&](int c) {
+#pragma unroll
+      for (int i = 0; i < W_PIECES; ++i)
+        if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
+          w_next[i] = reinterpret_cast<const u32x4*>(w_cols + (size_t(unit) * chunks + c) * W_ELEMS)[i * NT + tid];
+    };
+    if (steps > first) {
+      fetch(steps - 1);
+      fetch_W(steps - 1);
+      commit(steps - 1);
+    }
+    for (int c = steps; c >= first; --c) {
+      lds_barrier();   // the chunk in front is there
+      if (c - 2 >= first) fetch(c - 2);
+      lds_barrier();   // of the chunk K is needed yet
+      if (c - 1 >= first) {
+#pragma unroll
+        for (int i = 0; i < W_PIECES; ++i)
+          if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
+      }
+      if (c - 2 >= first) fetch_W(c - 2);
+      lds_barrier();   // K is read, and the rows of the one in front
+      if (c - 2 >= first) commit(c - 2);
+    }
+    return;
+  }
+
+  // ---- what a chunk comes to by itself
+  f32x4 R[2 * KS];
+#pragma unroll
+  for (int t = 0; t < 2 * KS; ++t) R[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c = steps; c >= first; --c) {
+    const uint16_t* Ks = K2[(c - 1) & 1];
+    const ChunkRecord& rec = recs[(c - 1) & 1];
+    lds_barrier();   // the chunk in front is there
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t) Rs[(w * 2 * KS + t) * 64 + l] = R[t];
+    if (c == first) {
+      lds_barrier();
+      lds_barrier();
+      break;
+    }
+    // s P, a tile of columns to a wave (two where there are two waves), queries down: an operand as it stands.  (The tiles above
+    // the diagonal, too: the workgroup waits for the wave that has none.)
+#pragma unroll
+    for (int turn = 0; turn < 4 / NW; ++turn) {
+      const int jt = turn == 0 ? w : 3 - w, own = 16 * jt + r;
+      f32x4 t[4];
+#pragma unroll
+      for (int it = 0; it < 4; ++it) t[it] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        bf16x8 kf[IN], qf[4][IN];
+        KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) KTile::row_frag(Qs, 16 * it + r, 32 * ks + 8 * q4, qf[it]);
+        mm_each<LEVEL>(qf, kf, t);
+      }
+      f32x4 diagonal;
+      {
+        const double g_own = rec.decay[own];
+        const float rk_own = scale * rec.rk[own];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int i = 16 * jt + 4 * q4 + v;
+          diagonal[v] = i >= own ? rk_own * decay_between(rec.decay[i], g_own) : 0.f;
+        }
+      }
+      const float to_tile = scale * rec.rk_to_tile[own];
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const f32x4 below = four(rec.in_tile + 16 * it + 4 * q4) * (to_tile * rec.between[it][jt]);   // 0 up to the diagonal
+        t[it] *= four(rq + 16 * it + 4 * q4);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) t[it][v] *= it == jt ? diagonal[v] : below[v];
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        if (w_col_there(jt, p)) {
+          bf16x8 pf[LEVEL];
+          split8<LEVEL>(t[2 * p], t[2 * p + 1], pf);
+          store_frag<LEVEL>(Ps, w_col_frag(jt, p), l, pf);
+        }
+    }
+    bf16x8 gf[2][IN];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) GTile::col_frag(Os, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, 16 * w, r, gf[p]);
+    lds_barrier();   // P is there, and the sums of the chunk behind are taken
+    {
+      f32x4 f[4];
+      bf16x8 pf[2][LEVEL], pl[4][LEVEL];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        load_frag(Ps, w_col_frag(t, 1), l, pl[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) load_frag(Ps, w_col_frag(t, 0), l, pf[t]);
+      mm_each<LEVEL>(pl, gf[1], f);
+      mm_each<LEVEL>(pf, gf[0], f);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) Fs[(w * 4 + t) * 64 + l] = f[t];
+    }
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t) R[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      bf16x8 wg[LEVEL];
+      weighted_rows<LEVEL>(gf[p], rq, rec.since, scale, 32 * p + 4 * q4, wg);
+      constexpr int AT_ONCE = 2 * KS < 4 ? 2 * KS : 4;
+#pragma unroll
+      for (int t0 = 0; t0 < 2 * KS; t0 += AT_ONCE) {
+        bf16x8 qf[AT_ONCE][IN];
+#pragma unroll
+        for (int t = 0; t < AT_ONCE; ++t)
+          KTile::spread_col_frag(Qs, 32 * p + 4 * q4, 32 * p + 16 + 4 * q4, key_of((t0 + t) / 2, (t0 + t) % 2, 0, 0), r, qf[t]);
+        mm_each<LEVEL>(qf, wg, R + t0);
+      }
+    }
+    lds_barrier();   // the rows are read
+  }
+}
+
+// Where the LDS has no room for a second chunk's K: what does not depend on D formed for the same chunk, and by the waves that fetch
+// the rows; R, where there is no room to hand it over, by the first waves.
+template <typename T, int DK, int NW>
+struct DeltaRevCfg {
+  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, KS = DK / 32, PAD = sizeof(T) == 4 ? 8 : 16;
+  using KTile = PartTile<CHUNK, DK, IN, PAD>;
+  using GTile = PartTile<CHUNK, VC, IN, PAD>;      // rows of dO
+  static constexpr int W_SIZE = W_FRAGS * LEVEL * 512;
+  static constexpr int BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + 2 * W_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK + NW * 4 * 1024;
+  static constexpr bool HANDS_R = BYTES + NW * 2 * KS * 1024 <= 160 * 1024;
+  static constexpr bool FITS = BYTES <= 160 * 1024;
+};
+
 template <typename T, int DK, int NW, bool TOTALS>
 __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
@@ -917,18 +1227,22 @@ hipError_t run_rev(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
   const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
   if constexpr (DeltaRevCfg<T, DK, NW>::FITS) {
+    constexpr bool AHEAD = DeltaAheadCfg<T, DK, NW>::FITS;
     const auto run = [&](auto kernel) {
       return launch_kernel("delta_rev_scan", kernel, a.G == 1 ? dim3(unsigned(units * parts)) : dim3(unsigned(units * a.G), unsigned(parts)),
-                           dim3(128 * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
+                           dim3((AHEAD ? 192 : 128) * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
                            static_cast<const T*>(a.dO), a.s, a.seq_len, a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates,
                            a.ends, Divisor(a.H), Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
     };
     if (a.G > 1) {
-      hipError_t err = run(delta_rev_scan<T, DK, NW, true>);
+      hipError_t err;
+      if constexpr (AHEAD) err = run(delta_ahead_rev_scan<T, DK, NW, true>);
+      else err = run(delta_rev_scan<T, DK, NW, true>);
       if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, true);
       if (err != hipSuccess) return err;
     }
-    return run(delta_rev_scan<T, DK, NW, false>);
+    if constexpr (AHEAD) return run(delta_ahead_rev_scan<T, DK, NW, false>);
+    else return run(delta_rev_scan<T, DK, NW, false>);
   } else {
     return launch_kernel("delta_rev_scan", delta_wide_rev_scan<T, DK, NW>, dim3(unsigned(units * parts)), dim3(64 * NW), 0, a.stream,
                          static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.seq_len,

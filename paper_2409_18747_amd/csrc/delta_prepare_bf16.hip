@@ -33,7 +33,7 @@ __device__ __forceinline__ void store_block(float* a, f32x4 x, int r, int q4) {
 // W_j, so that no power of A, which may be large, is formed; W of two neighbouring diagonal blocks then gives the block below
 // them, W21 = (I - W22 b2) A21 (I - b1 W11), of 16 and then of 32.
 template <typename T, int DK>
-__global__ __launch_bounds__(256, 3) void delta_prepare(const T* __restrict__ K, const float* __restrict__ log_decay,
+__global__ __launch_bounds__(256, DK * Rows<T>::PARTS > 128 ? 2 : 3) void delta_prepare(const T* __restrict__ K, const float* __restrict__ log_decay,
                                                         const float* __restrict__ beta, const int* __restrict__ lengths,
                                                         ChunkRecord* __restrict__ records, uint16_t* __restrict__ w_rows,
                                                         uint16_t* __restrict__ w_cols, Divisor H, Divisor chunks, int N,
