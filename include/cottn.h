@@ -363,8 +363,9 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  *   e_t = v_t - kh_t g_t H_(t-1),   H_t = g_t H_(t-1) + beta_t kh_t^T e_t.
  * log_decay and beta: float[B][H][N] device pointers.  log_decay may be NULL (no decay); values are <= 0, one above 0 counts as
  * 0, one below -128 (-inf among them) keeps nothing.  beta is usually in 0 .. 1, and any finite number: between 0 and 2 no state
- * grows but by its values.  States are float[B][H][dk][dv], without s; dk and dv are each one of 32, 64, 128.  Chunks
- * are of 64 rows.  All dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them
+ * grows but by its values.  States are float[B][H][dk][dv], without s; dk and dv are each one of 32, 64, 128.  Rows
+ * are taken in chunks of 64, and a long sequence of few units in segments that are walked side by side, as the operations above:
+ * cottn_segments_dkdv with chunk 0 says into how many, cottn_tune_segments sets it (fp32 with dk 128: always one).  All dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them
  * in bfloat16 parts).  Workspaces: cottn_workspace_bytes_dkdv with the COTTN_OP_*_DELTA* operations, chunk 0; always needed.
  * A value that is not finite, in a row, a gate or a state, can make results of its sequence and head not finite, those of
  * earlier rows of its chunk among them.  B H (N + 63) / 64 and B H dv / 16 are below 16 777 216; more is refused
@@ -380,8 +381,8 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  *   dstate      the gradient with respect to the forward call's `state`: the dstate_in of the piece behind;
  *   dstate_in   that with respect to its state_in.  May be dstate, else must overlap neither dstate nor state_in (COTTN_E_ARG).
  * fwd_workspace: NULL, or the workspace, of COTTN_OP_FWD_DELTA's size or more, of the matching completed cottn_fwd_causal_delta
- * call, untouched since; a smaller one is refused (COTTN_E_WORKSPACE).  With it `workspace` is of COTTN_OP_BWD_DELTA_SAVED's
- * size, without it of COTTN_OP_BWD_DELTA's. */
+ * call, untouched since, and with cottn_tune_segments as it was; a smaller one is refused (COTTN_E_WORKSPACE).  With it
+ * `workspace` is of COTTN_OP_BWD_DELTA_SAVED's size and must not overlap it (COTTN_E_ARG), without it of COTTN_OP_BWD_DELTA's. */
 int cottn_fwd_causal_delta(const void* Q, const void* K, const void* V, const float* s, const float* log_decay, const float* beta,
                            const int* seq_len, const float* state_in, void* O, float* state, void* workspace,
                            size_t workspace_bytes, int B, int H, int N, int dk, int dv, int dtype, float eps, void* hip_stream);
@@ -408,7 +409,8 @@ int cottn_step_delta(const void* q, const void* k, const void* v, const float* s
  *   an input or the other output (COTTN_E_ARG).  For single tokens N is 1.
  *   positions: int[B][N][axes], any values; freq: float[pairs], radians to a position; axis: int[pairs], the axis (time, row,
  *   column, ...) that a pair is turned by, NULL for 0; a pair whose axis is none of 0 .. axes - 1 is not turned.
- *   pairs: 1 .. d / 2; d one of 32, 64, 128; axes >= 1.
+ *   pairs: 1 .. d / 2; d one of 32, 64, 128; axes >= 1.  With v = 16 bytes of elements where pairs is a multiple of that, else
+ *   1, B (N + t - 1) / t is below 16 777 216 for t = 512 v / d; more is refused (COTTN_E_SHAPE).
  *   inverse: turned by - phi, which is the gradient of the call without.
  * Angles are formed in 64 bits.  N = 0 does nothing. */
 int cottn_rotary(const void* Q, const void* K, const int* positions, const float* freq, const int* axis, void* Qr, void* Kr,

@@ -402,7 +402,7 @@ bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, Delt
   if (G < 1 || (dtype == COTTN_F32 && dk == 128)) G = 1;   // (kernels for whole sequences alone)
   p->seg = chunks > 0 ? int((chunks + G - 1) / G) : 1;
   p->G = chunks > 0 ? int((chunks + p->seg - 1) / p->seg) : 1;
-  if (!threads_fit(units * p->G, 512)) return false;
+  if (p->G > 1 && (!threads_fit(units * p->G, 768) || !threads_fit(units * (dv / 16), 512))) return false;
   const size_t all = size_t(units) * chunks, state = round_up_256(all * dk * dv * 4), rows = round_up_256(all * 64 * dv * 4);
   const size_t segments = p->G > 1 ? size_t(units) * p->G : 0;
   p->records = 0;
@@ -1154,6 +1154,9 @@ int cottn_bwd_causal_delta(const void* Q, const void* K, const void* V, const fl
   if (saved && (st = check_workspace(fwd_workspace, fwd_workspace_bytes, space.forward)) != COTTN_OK) return st;
   st = check_workspace(workspace, workspace_bytes, delta_workspace_bytes(saved ? COTTN_OP_BWD_DELTA_SAVED : COTTN_OP_BWD_DELTA, space));
   if (st != COTTN_OK) return st;
+  if (saved && overlap(static_cast<const float*>(fwd_workspace), 0.25 * double(space.forward), static_cast<const float*>(workspace),
+                       0.25 * double(space.saved)))
+    return COTTN_E_ARG;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (N == 0) {
     hipError_t e = zero_f32(ds, seq_len != nullptr ? long(B) * H : H, stream);
@@ -1206,7 +1209,7 @@ int cottn_rotary(const void* Q, const void* K, const int* positions, const float
   if (pairs < 1 || pairs > d / 2 || axes < 1) return COTTN_E_SHAPE;
   if (freq == nullptr || (positions == nullptr && N > 0)) return COTTN_E_NULL;
   if (!is_aligned(positions, 4) || !is_aligned(freq, 4) || !is_aligned(axis, 4)) return COTTN_E_ALIGN;
-  if (double(B) * N * d >= 4294967296.0) return COTTN_E_SHAPE;   // threads of a launch: one to a pair of a token at most
+  if (!threads_fit(long(B) * rotary_tiles(N, d, rotary_run(pairs, dtype)), 256)) return COTTN_E_SHAPE;
   if (N == 0) return COTTN_OK;
   const double floats = double(B) * H * N * d * (dtype == COTTN_F32 ? 1.0 : 0.5);
   const float* in[] = {static_cast<const float*>(Q), static_cast<const float*>(K)};

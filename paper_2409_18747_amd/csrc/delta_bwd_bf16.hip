@@ -32,7 +32,7 @@ __device__ __forceinline__ void weighted_rows(const bf16x8 (&g)[IN], const float
 }
 
 // Segments as in the forward scan: TOTALS leaves what a segment makes of zeros (the last one: of dstate) in the place of the
-// gradient with respect to the state in front of it.
+// gradient with respect to the state in front of it.  Where dstate_in is to replace dstate, that walk puts dstate by.
 template <typename T, int DK, int NW, bool TOTALS>
 __global__ __launch_bounds__(192 * NW, NW <= 2 ? 1 : 3) void delta_ahead_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
@@ -67,6 +67,7 @@ __global__ __launch_bounds__(192 * NW, NW <= 2 ? 1 : 3) void delta_ahead_rev_sca
   const int col0 = part * VC;
   if ((first >= all && g > 0) || (TOTALS && g == 0)) return;
   const bool ends_here = steps == all;   // the last rows
+  const bool put_by = ends_here && g > 0 && dstate != nullptr && dstate == dstate_in;
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
 
   // In step c the first waves take chunk c and the others form what they will need of chunk c - 1, from the one behind the last on.
@@ -74,14 +75,21 @@ __global__ __launch_bounds__(192 * NW, NW <= 2 ? 1 : 3) void delta_ahead_rev_sca
     // ---- the gradients with respect to the states
     // this lane's value column in the first key row, and in the first token row, that it holds
     const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
-    const float* from = ends_here ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
-                                  : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
+    const float* from = ends_here && (TOTALS || !put_by) ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
+                        : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
     f32x4 D[2 * KS];
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
         D[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+    if (TOTALS && put_by) {
+      float* to = ends + (size_t(unit) * G.n + g) * DK * DV;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+    }
     lds_barrier();
     lds_barrier();
     lds_barrier();
@@ -377,6 +385,7 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
   const int col0 = part * VC;
   if ((first >= all && g > 0) || (TOTALS && g == 0)) return;
   const bool ends_here = steps == all;   // the last rows
+  const bool put_by = ends_here && g > 0 && dstate != nullptr && dstate == dstate_in;
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
 
   if (role == 0) {
@@ -384,14 +393,21 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
     __builtin_amdgcn_s_setprio(3);   // the chain that all wait for
     // this lane's value column in the first key row, and in the first token row, that it holds
     const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
-    const float* from = ends_here ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
-                                  : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
+    const float* from = ends_here && (TOTALS || !put_by) ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
+                        : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
     f32x4 D[2 * KS];
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
       for (int v = 0; v < 4; ++v)
         D[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+    if (TOTALS && put_by) {
+      float* to = ends + (size_t(unit) * G.n + g) * DK * DV;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+    }
     for (int c = steps - 1; c >= first; --c) {
       bf16x8 df[KS][LEVEL];
 #pragma unroll

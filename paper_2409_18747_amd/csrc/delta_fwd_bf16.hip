@@ -31,7 +31,8 @@ struct DeltaFwdCfg {
 // A sequence in G segments of `seg` chunks: the workgroups of TOTALS leave what a segment makes of a state, B from zeros (the first
 // segment: from state_in) in the place of the state behind it, and the matrix M that the state at its start enters with, as if
 // unit columns without values were its state; delta_carry makes of those the states at the starts, from which the segments are
-// walked again.
+// walked again.  Where the state is to replace state_in, which the last segment may do before the first one is walked again,
+// the walk for the totals puts state_in by.
 template <typename T, int DK, int NW, int LEVEL, bool TOTALS>
 __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2 : 3) void delta_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
@@ -70,6 +71,7 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
   // TOTALS: columns of M, behind those of the values
   const bool unit_columns = TOTALS && part * VC >= DV;
   const int col0 = unit_columns ? part * VC - DV : part * VC, width = unit_columns ? DK : DV;
+  const bool put_by = g == 0 && G.n > 1 && !ends_here && state_in != nullptr && state_in == state_out;
   if (TOTALS && (first >= all || (unit_columns ? g == 0 : ends_here))) return;   // (nobody asks)
 
   if (role == 0) {
@@ -78,8 +80,8 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
     // this lane's value column in the first key row, and in the first token row, that it holds
     const unsigned at_key = unsigned(8 * q4 * width + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
     f32x4 S[2 * KS];
-    const float* from = g == 0 ? (state_in != nullptr ? state_in + size_t(unit) * DK * DV : nullptr)
-                               : TOTALS ? nullptr : starts + (size_t(unit) * G.n + g) * DK * DV;
+    const float* from = g == 0 && (TOTALS || !put_by) ? (state_in != nullptr ? state_in + size_t(unit) * DK * DV : nullptr)
+                        : TOTALS ? nullptr : starts + (size_t(unit) * G.n + g) * DK * DV;
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
@@ -87,6 +89,13 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
         S[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
         if (unit_columns) S[t][v] = key_of(t / 2, t % 2, q4, v) == col0 + 16 * w + r ? 1.f : 0.f;
       }
+    if (TOTALS && put_by) {
+      float* to = starts + size_t(unit) * G.n * DK * DV;
+#pragma unroll
+      for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = S[t][v];
+    }
     for (int c = first; c < steps; ++c) {
       bf16x8 sf[KS][LEVEL];
 #pragma unroll

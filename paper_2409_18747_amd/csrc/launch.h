@@ -340,6 +340,16 @@ struct RotaryArgs {
   bool neighbours, inverse;
   hipStream_t stream;
 };
+// pairs that a thread takes of a row: 16 bytes of it on either side, where the pairs are whole runs of those; and the workgroups
+// of 256 threads to a sequence
+inline int rotary_run(int pairs, int dtype) {
+  const int whole = dtype == 0 ? 4 : 8;
+  return pairs % whole == 0 ? whole : 1;
+}
+inline long rotary_tiles(int N, int d, int run) {
+  const int tokens = 512 * run / d;
+  return (long(N) + tokens - 1) / tokens;
+}
 
 // defined in the kernel files; every function only enqueues work on args.stream
 hipError_t fwd_causal_bf16(const CausalArgs& a);

@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* Q, const T* K, con
 
 template <typename T, int VEC, bool NEIGHBOURS>
 hipError_t run_rotary(const RotaryArgs& a) {
-  const int lanes = a.d / (2 * VEC), per = 256 / lanes, tiles = (a.N + per - 1) / per;
+  const int lanes = a.d / (2 * VEC), tiles = int(rotary_tiles(a.N, a.d, VEC));
   // all heads to a workgroup where tokens alone fill the chip, else fewer
   int heads = a.H;
   while (heads > 1 && long(a.B) * tiles * ((a.H + heads - 1) / heads) < 1024) heads = (heads + 1) / 2;
@@ -101,7 +101,7 @@ hipError_t run_rotary(const RotaryArgs& a) {
 template <typename T>
 hipError_t run_type(const RotaryArgs& a) {
   constexpr int VEC = 16 / sizeof(T);
-  if (a.pairs % VEC != 0) return a.neighbours ? run_rotary<T, 1, true>(a) : run_rotary<T, 1, false>(a);
+  if (rotary_run(a.pairs, sizeof(T) == 4 ? 0 : 1) != VEC) return a.neighbours ? run_rotary<T, 1, true>(a) : run_rotary<T, 1, false>(a);
   return a.neighbours ? run_rotary<T, VEC, true>(a) : run_rotary<T, VEC, false>(a);
 }
 
