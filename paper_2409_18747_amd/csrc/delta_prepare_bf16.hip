@@ -29,20 +29,38 @@ __device__ __forceinline__ void store_block(float* a, f32x4 x, int r, int q4) {
   for (int v = 0; v < 4; ++v) a[(4 * q4 + v) * WP + r] = x[v];
 }
 
+// The sum of the lanes r, 16 + r, 32 + r and 48 + r, in all of them.  (Two registers to a swap: of one the compiler takes the two
+// results for the same.)
+__device__ __forceinline__ float over_quarters(float x) {
+  unsigned a = __builtin_bit_cast(unsigned, x), b = a;
+  asm("" : "+v"(b));
+  const auto pairs = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = b = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, unsigned(pairs[0])) + __builtin_bit_cast(float, unsigned(pairs[1])));
+  asm("" : "+v"(b));
+  const auto halves = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return __builtin_bit_cast(float, unsigned(halves[0])) + __builtin_bit_cast(float, unsigned(halves[1]));
+}
+
 // W takes A's place block by block.  Within a diagonal block of 16 it is found row by row, W_i = A_i - sum over j < i of A_ij b_j
 // W_j, so that no power of A, which may be large, is formed; W of two neighbouring diagonal blocks then gives the block below
 // them, W21 = (I - W22 b2) A21 (I - b1 W11), of 16 and then of 32.
 template <typename T, int DK>
-__global__ __launch_bounds__(256, DK * Rows<T>::PARTS > 128 ? 2 : 3) void delta_prepare(const T* __restrict__ K, const float* __restrict__ log_decay,
+struct DeltaPrepareCfg {
+  using Tile = PartTile<CHUNK, DK, Rows<T>::PARTS>;
+  static constexpr int ROOM = 2 * Tile::SIZE > 4 * 32 * WP ? 2 * Tile::SIZE : 4 * 32 * WP;
+  static constexpr int LDS_BYTES = ROOM + 4 * CHUNK * WP + int(sizeof(ChunkRecord));
+  static constexpr int AT_ONCE = 160 * 1024 / LDS_BYTES < 4 ? 160 * 1024 / LDS_BYTES : 4;   // workgroups to a compute unit
+};
+
+template <typename T, int DK>
+__global__ __launch_bounds__(256, (DeltaPrepareCfg<T, DK>::AT_ONCE)) void delta_prepare(const T* __restrict__ K, const float* __restrict__ log_decay,
                                                         const float* __restrict__ beta, const int* __restrict__ lengths,
                                                         ChunkRecord* __restrict__ records, uint16_t* __restrict__ w_rows,
                                                         uint16_t* __restrict__ w_cols, Divisor H, Divisor chunks, int N,
                                                         float inv_eps) {
   using Tile = PartTile<CHUNK, DK, Rows<T>::PARTS>;
-  constexpr int DP = 20;   // pitch of a diagonal block times b
-  constexpr int ROOM = 2 * Tile::SIZE > 4 * 32 * WP ? 2 * Tile::SIZE : 4 * 32 * WP;
-  __shared__ __attribute__((aligned(16))) char room[ROOM];   // the rows, then a step of the blocks below the diagonal
-  __shared__ __attribute__((aligned(16))) float As[CHUNK * WP], diagonal[4 * 16 * DP];
+  __shared__ __attribute__((aligned(16))) char room[DeltaPrepareCfg<T, DK>::ROOM];   // the rows, then a step of the blocks below the diagonal
+  __shared__ __attribute__((aligned(16))) float As[CHUNK * WP];   // (the diagonal blocks times b in the upper right quarter, which is no one's)
   __shared__ ChunkRecord rec;
   uint16_t* const Ks = reinterpret_cast<uint16_t*>(room);
   float* const Xs = reinterpret_cast<float*>(room);
@@ -52,6 +70,7 @@ __global__ __launch_bounds__(256, DK * Rows<T>::PARTS > 128 ? 2 : 3) void delta_
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
   RowTile<T, DK> kt;
   kt.fetch(K + (size_t(unit) * N + row0) * DK, there - row0);
+  float* const diagonal = As + 16 * (w / 2) * WP + 32 + 16 * (w % 2);
   double g = 0.0;
   if (w == 0) {
     const bool here = row0 + l < there;
@@ -102,33 +121,28 @@ __global__ __launch_bounds__(256, DK * Rows<T>::PARTS > 128 ? 2 : 3) void delta_
         for (int v = 0; v < 4; ++v) {
           const int i = 16 * w + 4 * q4 + v;
           t[v] = j < i ? t[v] * rec.rk[i] * rj * decay_between(rec.decay[i], gj) : 0.f;
-          if (jt == w) diagonal[(16 * w + 4 * q4 + v) * DP + r] = t[v] * rec.beta[j];
+          if (jt == w) diagonal[(4 * q4 + v) * WP + r] = t[v] * rec.beta[j];
         }
       }
       if (jt <= (w | 1)) store_block(As + 16 * w * WP + 16 * jt, t, r, q4);   // (what the fragments hold of the tiles above: zeros)
     }
   }
   wave_lds_sync();
-  {   // the diagonal blocks, one to a wave: a lane finds a column
+  {   // the diagonal blocks, one to a wave: a lane has every fourth row of a column, and a row is found from the sums of four lanes
     float* a = As + 16 * w * WP + 16 * w;
-    const float* d = diagonal + 16 * w * DP;
-    float x[16], start[16];
+    float x[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) start[i] = a[i * WP + r];
+    for (int t = 0; t < 4; ++t) x[t] = a[(4 * t + q4) * WP + r];   // (0 from the diagonal on; so is `diagonal`, where x is not found yet)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float even = start[i], odd = 0.f;
+    for (int i = 2; i < 16; ++i) {
+      float sum = 0.f;
 #pragma unroll
-      for (int j = 1; j < i; ++j) {
-        const float f = -d[i * DP + j];
-        if (j % 2) odd = __builtin_fmaf(f, x[j], odd);
-        else even = __builtin_fmaf(f, x[j], even);
-      }
-      x[i] = even + odd;   // (0 from the diagonal on, as A is)
+      for (int t = 0; 4 * t < i; ++t) sum = __builtin_fmaf(-diagonal[i * WP + 4 * t + q4], x[t], sum);
+      sum = over_quarters(sum);
+      x[i / 4] += q4 == i % 4 ? sum : 0.f;
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i % 4 == q4) a[i * WP + r] = x[i];
+    for (int t = 0; t < 4; ++t) a[(4 * t + q4) * WP + r] = x[t];
   }
   __syncthreads();   // (and the rows are read)
   if (w < 2) {   // blocks (1, 0) and (3, 2)
