@@ -47,8 +47,8 @@ __device__ __forceinline__ float over_quarters(float x) {
 template <typename T, int DK>
 struct DeltaPrepareCfg {
   using Tile = PartTile<CHUNK, DK, Rows<T>::PARTS>;
-  static constexpr int ROOM = 2 * Tile::SIZE > 4 * 32 * WP ? 2 * Tile::SIZE : 4 * 32 * WP;
-  static constexpr int LDS_BYTES = ROOM + 4 * CHUNK * WP + int(sizeof(ChunkRecord));
+  static constexpr int ROOM = 2 * Tile::SIZE > 4 * 96 * WP ? 2 * Tile::SIZE : 4 * 96 * WP;
+  static constexpr int LDS_BYTES = ROOM + int(sizeof(ChunkRecord));
   static constexpr int AT_ONCE = 160 * 1024 / LDS_BYTES < 4 ? 160 * 1024 / LDS_BYTES : 4;   // workgroups to a compute unit
 };
 
@@ -59,11 +59,11 @@ __global__ __launch_bounds__(256, (DeltaPrepareCfg<T, DK>::AT_ONCE)) void delta_
                                                         uint16_t* __restrict__ w_cols, Divisor H, Divisor chunks, int N,
                                                         float inv_eps) {
   using Tile = PartTile<CHUNK, DK, Rows<T>::PARTS>;
-  __shared__ __attribute__((aligned(16))) char room[DeltaPrepareCfg<T, DK>::ROOM];   // the rows, then a step of the blocks below the diagonal
-  __shared__ __attribute__((aligned(16))) float As[CHUNK * WP];   // (the diagonal blocks times b in the upper right quarter, which is no one's)
+  __shared__ __attribute__((aligned(16))) char room[DeltaPrepareCfg<T, DK>::ROOM];   // the rows, then As and Xs
   __shared__ ChunkRecord rec;
   uint16_t* const Ks = reinterpret_cast<uint16_t*>(room);
-  float* const Xs = reinterpret_cast<float*>(room);
+  float* const As = reinterpret_cast<float*>(room);   // (the diagonal blocks times b in the upper right quarter, which is no one's)
+  float* const Xs = As + CHUNK * WP;                  // a step of the blocks below the diagonal
   const int unit = quotient(blockIdx.x, chunks), c = blockIdx.x - unit * chunks.n, row0 = c * CHUNK;
   const int there = valid_rows(lengths, unit, H, N);
   if (row0 >= there) return;
@@ -104,6 +104,7 @@ __global__ __launch_bounds__(256, (DeltaPrepareCfg<T, DK>::AT_ONCE)) void delta_
     bf16x8 own[DK / 32][Rows<T>::PARTS];
 #pragma unroll
     for (int ks = 0; ks < DK / 32; ++ks) Tile::row_frag(Ks, 16 * w + r, 32 * ks + 8 * q4, own[ks]);
+    f32x4 tiles[4];
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       f32x4 t = {0.f, 0.f, 0.f, 0.f};
@@ -121,10 +122,15 @@ __global__ __launch_bounds__(256, (DeltaPrepareCfg<T, DK>::AT_ONCE)) void delta_
         for (int v = 0; v < 4; ++v) {
           const int i = 16 * w + 4 * q4 + v;
           t[v] = j < i ? t[v] * rec.rk[i] * rj * decay_between(rec.decay[i], gj) : 0.f;
-          if (jt == w) diagonal[(4 * q4 + v) * WP + r] = t[v] * rec.beta[j];
         }
       }
-      if (jt <= (w | 1)) store_block(As + 16 * w * WP + 16 * jt, t, r, q4);   // (what the fragments hold of the tiles above: zeros)
+      tiles[jt] = t;
+    }
+    __syncthreads();   // the rows are read
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      if (jt == w) store_block(diagonal, tiles[jt] * rec.beta[16 * jt + r], r, q4);
+      if (jt <= (w | 1)) store_block(As + 16 * w * WP + 16 * jt, tiles[jt], r, q4);   // (what the fragments hold of the tiles above: zeros)
     }
   }
   wave_lds_sync();
@@ -144,7 +150,7 @@ __global__ __launch_bounds__(256, (DeltaPrepareCfg<T, DK>::AT_ONCE)) void delta_
 #pragma unroll
     for (int t = 0; t < 4; ++t) a[(4 * t + q4) * WP + r] = x[t];
   }
-  __syncthreads();   // (and the rows are read)
+  __syncthreads();
   if (w < 2) {   // blocks (1, 0) and (3, 2)
     const int i0 = 32 * w + 16, j0 = 32 * w;
     float* a = As + i0 * WP + j0;
