@@ -47,9 +47,9 @@ __device__ __forceinline__ float over_quarters(float x) {
 template <typename T, int DK>
 struct DeltaPrepareCfg {
   using Tile = PartTile<CHUNK, DK, Rows<T>::PARTS>;
-  static constexpr int ROOM = 2 * Tile::SIZE > 4 * 96 * WP ? 2 * Tile::SIZE : 4 * 96 * WP;
+  static constexpr int ROOM = 2 * Tile::SIZE > 4 * CHUNK * WP ? 2 * Tile::SIZE : 4 * CHUNK * WP;
   static constexpr int LDS_BYTES = ROOM + int(sizeof(ChunkRecord));
-  static constexpr int AT_ONCE = 160 * 1024 / LDS_BYTES < 4 ? 160 * 1024 / LDS_BYTES : 4;   // workgroups to a compute unit
+  static constexpr int AT_ONCE = 160 * 1024 / LDS_BYTES < 8 ? 160 * 1024 / LDS_BYTES : 8;   // workgroups to a compute unit
 };
 
 template <typename T, int DK>
@@ -59,18 +59,18 @@ __global__ __launch_bounds__(256, (DeltaPrepareCfg<T, DK>::AT_ONCE)) void delta_
                                                         uint16_t* __restrict__ w_cols, Divisor H, Divisor chunks, int N,
                                                         float inv_eps) {
   using Tile = PartTile<CHUNK, DK, Rows<T>::PARTS>;
-  __shared__ __attribute__((aligned(16))) char room[DeltaPrepareCfg<T, DK>::ROOM];   // the rows, then As and Xs
+  __shared__ __attribute__((aligned(16))) char room[DeltaPrepareCfg<T, DK>::ROOM];   // the rows, then As
   __shared__ ChunkRecord rec;
   uint16_t* const Ks = reinterpret_cast<uint16_t*>(room);
-  float* const As = reinterpret_cast<float*>(room);   // (the diagonal blocks times b in the upper right quarter, which is no one's)
-  float* const Xs = As + CHUNK * WP;                  // a step of the blocks below the diagonal
+  float* const As = reinterpret_cast<float*>(room);
+  float* const Xs = As + 32;   // the upper right quarter, which is no one's: the diagonal blocks times b, then a step of the blocks below
   const int unit = quotient(blockIdx.x, chunks), c = blockIdx.x - unit * chunks.n, row0 = c * CHUNK;
   const int there = valid_rows(lengths, unit, H, N);
   if (row0 >= there) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
   RowTile<T, DK> kt;
   kt.fetch(K + (size_t(unit) * N + row0) * DK, there - row0);
-  float* const diagonal = As + 16 * (w / 2) * WP + 32 + 16 * (w % 2);
+  float* const diagonal = Xs + 16 * (w / 2) * WP + 16 * (w % 2);
   double g = 0.0;
   if (w == 0) {
     const bool here = row0 + l < there;
