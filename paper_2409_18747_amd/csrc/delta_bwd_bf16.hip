@@ -390,7 +390,6 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
 
   if (role == 0) {
     // ---- the gradients with respect to the states
-    __builtin_amdgcn_s_setprio(3);   // the chain that all wait for
     // this lane's value column in the first key row, and in the first token row, that it holds
     const unsigned at_key = unsigned(8 * q4 * DV + col0 + 16 * w + r), at_token = unsigned(4 * q4 * DV + col0 + 16 * w + r);
     const float* from = ends_here && (TOTALS || !put_by) ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
@@ -870,14 +869,15 @@ struct DeltaGradCfg {
   // first the rows of dO, E and Z, then two masked tiles and the rows of K and Q
   static constexpr int FIRST = GTile::SIZE + 2 * ETile::SIZE, SECOND = 2 * MTile::SIZE + 2 * KTile::SIZE;
   static constexpr int SIZE = FIRST > SECOND ? FIRST : SECOND;
-  static constexpr int LDS_BYTES = 2 * SIZE + CHUNK * 8 + 16 + int(sizeof(ChunkRecord));
+  static constexpr int LDS_BYTES = 2 * SIZE + CHUNK * 8 + 32 + int(sizeof(ChunkRecord));
   static constexpr int GROUPS = (160 * 1024) / LDS_BYTES >= 2 ? 2 : 1;
-  // key tiles of a wave and token tiles that it forms of them
-  static constexpr int KT = DK / 16, NK = KT >= 4 ? KT / 4 : 1, NTOK = KT >= 4 ? 4 : 2;
+  // key tiles, one to a wave, and token tiles that it forms of them
+  static constexpr int WAVES = GROUPS == 2 ? 4 : 8, THREADS = 64 * WAVES, KT = DK / 16, NTOK = 4 * KT / WAVES;
+  static_assert(WAVES % KT == 0, "a key tile to a wave");
 };
 
 template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_gradients(
+__global__ __launch_bounds__((DeltaGradCfg<T, DK, DV>::THREADS), (DeltaGradCfg<T, DK, DV>::WAVES / 4 * DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_gradients(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ dO,
     const float* __restrict__ s, const float* __restrict__ log_decay, const float* __restrict__ beta,
     const int* __restrict__ lengths, const ChunkRecord* __restrict__ records, const float* __restrict__ errors,
@@ -889,12 +889,12 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
   using GTile = typename Cfg::GTile;
   using ETile = typename Cfg::ETile;
   using MTile = typename Cfg::MTile;
-  constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, NK = Cfg::NK, NTOK = Cfg::NTOK, VS = DV / 32;
+  constexpr int IN = Cfg::IN, LEVEL = Cfg::LEVEL, NTOK = Cfg::NTOK, VS = DV / 32, THREADS = Cfg::THREADS, KT = Cfg::KT;
   __shared__ __attribute__((aligned(16))) uint16_t room[Cfg::SIZE];
   __shared__ ChunkRecord rec;
   __shared__ __attribute__((aligned(16))) float rq[CHUNK], xv[CHUNK];
-  __shared__ float tail[4];
-  typedef float Dots[4][CHUNK];
+  __shared__ float tail[Cfg::WAVES];
+  typedef float Dots[KT][CHUNK];
   Dots& qdot = *reinterpret_cast<Dots*>(room);   // when nothing else is there any more
   Dots& kdot = *(&qdot + 1);
   uint16_t* const Os = room;
@@ -915,11 +915,11 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     typedef __attribute__((ext_vector_type(4))) T vec4;
     const vec4 none = {T(0.f), T(0.f), T(0.f), T(0.f)};
     const int lo = max(row0, there), hi = min(N, row0 + CHUNK);
-    for (int i = tid; i < (hi - lo) * (DK / 4); i += 256) {
+    for (int i = tid; i < (hi - lo) * (DK / 4); i += THREADS) {
       *reinterpret_cast<vec4*>(dQu + size_t(lo) * DK + i * 4) = none;
       *reinterpret_cast<vec4*>(dKu + size_t(lo) * DK + i * 4) = none;
     }
-    for (int i = tid; i < (hi - lo) * (DV / 4); i += 256) *reinterpret_cast<vec4*>(dVu + size_t(lo) * DV + i * 4) = none;
+    for (int i = tid; i < (hi - lo) * (DV / 4); i += THREADS) *reinterpret_cast<vec4*>(dVu + size_t(lo) * DV + i * 4) = none;
     if (tid < hi - lo) {
       dbeta[row_at + lo + tid] = 0.f;
       if (dlog_decay != nullptr) dlog_decay[row_at + lo + tid] = 0.f;
@@ -930,19 +930,19 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     return;
   }
   const float scale = s[lengths != nullptr ? unit : unit - quotient(unit, H) * H.n];
-  // wave w: key tiles kt0 .. kt0 + NK - 1, token tiles tt0 .. tt0 + NTOK - 1
-  const int kt0 = Cfg::KT >= 4 ? w * NK : w % 2, tt0 = Cfg::KT >= 4 ? 0 : w / 2 * 2;
-  f32x4 hd[NK][4];   // eight values of a key's row of H, and of D, 32 columns ahead
-  const auto fetch_states = [&](int x, int vs) {
-    const size_t at = size_t(blockIdx.x) * DK * DV + size_t(16 * (kt0 + x) + r) * DV + 32 * vs + 8 * q4;
-    hd[x][0] = reinterpret_cast<const f32x4*>(states + at)[0];
-    hd[x][1] = reinterpret_cast<const f32x4*>(states + at)[1];
-    hd[x][2] = reinterpret_cast<const f32x4*>(dstates + at)[0];
-    hd[x][3] = reinterpret_cast<const f32x4*>(dstates + at)[1];
+  // wave w: key tile kt0, token tiles tt0 .. tt0 + NTOK - 1
+  const int kt0 = w % KT, tt0 = w / KT * NTOK;
+  f32x4 hd[4];   // eight values of a key's row of H, and of D, 32 columns ahead
+  const auto fetch_states = [&](int vs) {
+    const size_t at = size_t(blockIdx.x) * DK * DV + size_t(16 * kt0 + r) * DV + 32 * vs + 8 * q4;
+    hd[0] = reinterpret_cast<const f32x4*>(states + at)[0];
+    hd[1] = reinterpret_cast<const f32x4*>(states + at)[1];
+    hd[2] = reinterpret_cast<const f32x4*>(dstates + at)[0];
+    hd[3] = reinterpret_cast<const f32x4*>(dstates + at)[1];
   };
-  RowTile<T, DK, Cfg::PAD> kt, qt;
+  RowTile<T, DK, Cfg::PAD, THREADS> kt, qt;
   {
-    using RT = RowTile<T, DV, Cfg::PAD>;
+    using RT = RowTile<T, DV, Cfg::PAD, THREADS>;
     RT gt, vt;
     gt.fetch(dO + (row_at + row0) * DV, there - row0);
     vt.fetch(V + (row_at + row0) * DV, there - row0);
@@ -953,6 +953,7 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     float b_row[RT::PASSES];
 #pragma unroll
     for (int p = 0; p < RT::PASSES; ++p) {
+      if (!RT::in(p)) continue;   // (whole waves)
       const size_t at = (size_t(blockIdx.x) * CHUNK + RT::row(p)) * DV + RT::col();
       ez[p][0] = reinterpret_cast<const f32x4*>(errors + at)[0];
       ez[p][1] = reinterpret_cast<const f32x4*>(errors + at)[1];
@@ -960,11 +961,11 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
       ez[p][3] = reinterpret_cast<const f32x4*>(zs + at)[1];
       b_row[p] = row0 + RT::row(p) < there ? beta[row_at + row0 + RT::row(p)] : 0.f;
     }
-#pragma unroll
-    for (int x = 0; x < NK; ++x) fetch_states(x, 0);
+    fetch_states(0);
     gt.commit(Os);
 #pragma unroll
     for (int p = 0; p < RT::PASSES; ++p) {
+      if (!RT::in(p)) continue;
       const int row = RT::row(p), col = RT::col();
       const f32x4 e0 = ez[p][0], e1 = ez[p][1], z0 = ez[p][2], z1 = ez[p][3];
       const float b = b_row[p];
@@ -996,35 +997,30 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
   }
   __syncthreads();
 
-  f32x4 aq[NK][NTOK], ak[NK][NTOK], az[NK][NTOK];
+  f32x4 aq[NTOK], ak[NTOK], az[NTOK];
   float through = 0.f;   // <D, H>, of the wave's rows
   {
 #pragma unroll
-    for (int x = 0; x < NK; ++x)
-#pragma unroll
-      for (int t = 0; t < NTOK; ++t) aq[x][t] = ak[x][t] = az[x][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NTOK; ++t) aq[t] = ak[t] = az[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int vs = 0; vs < VS; ++vs) {
+      const f32x4 h0 = hd[0], h1 = hd[1], d0 = hd[2], d1 = hd[3];
+      if (vs + 1 < VS) fetch_states(vs + 1);
 #pragma unroll
-      for (int x = 0; x < NK; ++x) {
-        const f32x4 h0 = hd[x][0], h1 = hd[x][1], d0 = hd[x][2], d1 = hd[x][3];
-        if (vs + 1 < VS) fetch_states(x, vs + 1);
+      for (int i = 0; i < 4; ++i) through = __builtin_fmaf(h0[i], d0[i], __builtin_fmaf(h1[i], d1[i], through));
+      bf16x8 hf[LEVEL], df[LEVEL];
+      split8<LEVEL>(h0, h1, hf);
+      split8<LEVEL>(d0, d1, df);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) through = __builtin_fmaf(h0[i], d0[i], __builtin_fmaf(h1[i], d1[i], through));
-        bf16x8 hf[LEVEL], df[LEVEL];
-        split8<LEVEL>(h0, h1, hf);
-        split8<LEVEL>(d0, d1, df);
-#pragma unroll
-        for (int t = 0; t < NTOK; ++t) {
-          const int row = 16 * (tt0 + t) + r, col = 32 * vs + 8 * q4;
-          bf16x8 gf[IN], ef[LEVEL], zf[LEVEL];
-          GTile::row_frag(Os, row, col, gf);
-          ETile::row_frag(Es, row, col, ef);
-          ETile::row_frag(Zs, row, col, zf);
-          aq[x][t] = mm<LEVEL>(hf, gf, aq[x][t]);
-          ak[x][t] = mm<LEVEL>(df, ef, ak[x][t]);
-          az[x][t] = mm<LEVEL>(hf, zf, az[x][t]);
-        }
+      for (int t = 0; t < NTOK; ++t) {
+        const int row = 16 * (tt0 + t) + r, col = 32 * vs + 8 * q4;
+        bf16x8 gf[IN], ef[LEVEL], zf[LEVEL];
+        GTile::row_frag(Os, row, col, gf);
+        ETile::row_frag(Es, row, col, ef);
+        ETile::row_frag(Zs, row, col, zf);
+        aq[t] = mm<LEVEL>(hf, gf, aq[t]);
+        ak[t] = mm<LEVEL>(df, ef, ak[t]);
+        az[t] = mm<LEVEL>(hf, zf, az[t]);
       }
     }
     // each token's factors
@@ -1032,73 +1028,75 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
     for (int t = 0; t < NTOK; ++t) {
       const int i = 16 * (tt0 + t) + r;
       const float since = rec.since[i], to_end = rec.beta[i] * decay_between(rec.decay[CHUNK - 1], rec.decay[i]);
-#pragma unroll
-      for (int x = 0; x < NK; ++x) {
-        aq[x][t] *= since;
-        ak[x][t] *= to_end;
-        az[x][t] *= -rec.beta[i] * since;
-      }
+      aq[t] *= since;
+      ak[t] *= to_end;
+      az[t] *= -rec.beta[i] * since;
     }
   }
 
-  // the masked tiles: rows i of wave w's tile, columns j; lanes hold four columns of a row
-  f32x4 pt[4], at[4];
-  const int own = 16 * w + r;
+  // the masked tiles: rows i of tile w % 4, columns j of all tiles or of every other one; lanes hold four columns of a row
+  constexpr int APART = Cfg::WAVES / 4, TILES = 4 / APART;
+  f32x4 pt[TILES], at[TILES];
+  const int it = w % 4, jt0 = w / 4, own = 16 * it + r;
   const double g_own = rec.decay[own];
   const float b_own = rec.beta[own];
-  {
-    bf16x8 gf[VS][IN], zf[VS][LEVEL];
 #pragma unroll
-    for (int vs = 0; vs < VS; ++vs) {
-      GTile::row_frag(Os, own, 32 * vs + 8 * q4, gf[vs]);
-      ETile::row_frag(Zs, own, 32 * vs + 8 * q4, zf[vs]);
-    }
+  for (int u = 0; u < TILES; ++u) pt[u] = at[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int jt = 0; jt < 4; ++jt) {
-      pt[jt] = at[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (jt <= w) {
+  for (int vs = 0; vs < VS; ++vs) {
+    bf16x8 gf[IN], zf[LEVEL];
+    GTile::row_frag(Os, own, 32 * vs + 8 * q4, gf);
+    ETile::row_frag(Zs, own, 32 * vs + 8 * q4, zf);
 #pragma unroll
-        for (int vs = 0; vs < VS; ++vs) {
-          bf16x8 ef[LEVEL];
-          ETile::row_frag(Es, 16 * jt + r, 32 * vs + 8 * q4, ef);
-          pt[jt] = mm<LEVEL>(ef, gf[vs], pt[jt]);
-          at[jt] = mm<LEVEL>(ef, zf[vs], at[jt]);
-        }
+    for (int u = 0; u < TILES; ++u)
+      if (jt0 + APART * u <= it) {
+        bf16x8 ef[LEVEL];
+        ETile::row_frag(Es, 16 * (jt0 + APART * u) + r, 32 * vs + 8 * q4, ef);
+        pt[u] = mm<LEVEL>(ef, gf, pt[u]);
+        at[u] = mm<LEVEL>(ef, zf, at[u]);
+      }
+  }
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int j = 16 * jt + 4 * q4 + v;
-          const float f = rec.beta[j] * decay_between(g_own, rec.decay[j]);
-          pt[jt][v] = j <= own ? pt[jt][v] * f : 0.f;
-          at[jt][v] = j < own ? -b_own * at[jt][v] * f : 0.f;
-        }
+  for (int u = 0; u < TILES; ++u)
+    if (jt0 + APART * u <= it) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int j = 16 * (jt0 + APART * u) + 4 * q4 + v;
+        const float f = rec.beta[j] * decay_between(g_own, rec.decay[j]);
+        pt[u][v] = j <= own ? pt[u][v] * f : 0.f;
+        at[u][v] = j < own ? -b_own * at[u][v] * f : 0.f;
       }
     }
-  }
   const float rq_own = rq[own], rk_own = rec.rk[own];
+  const auto store_masked = [&](const f32x4 (&m)[TILES], float by_row, bool zeros) {
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) {
+      const int jt = jt0 + APART * u, j = 16 * jt + 4 * q4;
+      if (jt <= it) {
+        MTile::store4(Ms, own, j, m[u] * four(rec.rk + j));
+        MTile::store4(Mt, own, j, m[u] * by_row);
+      } else if (zeros && jt == (it | 1)) {   // (of the tiles above the diagonal the products read those beside it)
+        MTile::store4(Ms, own, j, f32x4{0.f, 0.f, 0.f, 0.f});
+        MTile::store4(Mt, own, j, f32x4{0.f, 0.f, 0.f, 0.f});
+      }
+    }
+  };
   __syncthreads();   // the rows of dO, E and Z are read
   kt.commit(Ks);
   qt.commit(Qs);
-#pragma unroll
-  for (int jt = 0; jt < 4; ++jt) {
-    const f32x4 k4 = *reinterpret_cast<const f32x4*>(rec.rk + 16 * jt + 4 * q4);
-    MTile::store4(Ms, own, 16 * jt + 4 * q4, pt[jt] * k4);
-    MTile::store4(Mt, own, 16 * jt + 4 * q4, pt[jt] * (scale * rq_own));
-  }
+  store_masked(pt, scale * rq_own, true);
   __syncthreads();
   // <D, H behind the chunk>: what goes through it, and what its updates give
-  if (Cfg::KT < 4 && w >= 2) through = 0.f;
+  if (w >= KT) through = 0.f;   // (another wave has the same rows)
   through *= rec.since[CHUNK - 1];
 #pragma unroll
   for (int t = 0; t < NTOK; ++t) {
     const int i = 16 * (tt0 + t) + r;
     float dot = 0.f;
+    const f32x4 k = KTile::row4(Ks, i, 16 * kt0 + 4 * q4);
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-      const f32x4 k = KTile::row4(Ks, i, 16 * (kt0 + x) + 4 * q4);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) dot = __builtin_fmaf(k[v], ak[x][t][v], dot);
-      ak[x][t] += az[x][t];
-    }
+    for (int v = 0; v < 4; ++v) dot = __builtin_fmaf(k[v], ak[t][v], dot);
+    ak[t] += az[t];
     through = __builtin_fmaf(rec.rk[i], dot, through);
   }
   through = group_sum<64>(through);
@@ -1106,41 +1104,31 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
 #pragma unroll
   for (int round = 0; round < 2; ++round) {
 #pragma unroll
-    for (int t = 0; t < NTOK; ++t) {
-      const int tt = tt0 + t;
+    for (int ks = 0; ks < 2; ++ks) {
+      const int t0 = 32 * ks + 8 * q4;
+      bf16x8 kf[IN], qf[IN];
+      KTile::col_frag(Ks, t0, t0 + 4, 16 * kt0, r, kf);
+      if (round == 0) KTile::col_frag(Qs, t0, t0 + 4, 16 * kt0, r, qf);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const int t0 = 32 * ks + 8 * q4;
+      for (int t = 0; t < NTOK; ++t) {
+        const int tt = tt0 + t;
         const bool before = 2 * ks <= tt, after = 2 * ks + 1 >= tt;   // columns up to row tt's tile; rows from column tt's tile on
-        bf16x8 mf[LEVEL], mt[LEVEL];
-        if (before) MTile::row_frag(Ms, 16 * tt + r, t0, mf);
-        if (after) MTile::col_frag(Mt, t0, t0 + 4, 16 * tt, r, mt);
-#pragma unroll
-        for (int x = 0; x < NK; ++x) {
-          bf16x8 kf[IN];
-          KTile::col_frag(Ks, t0, t0 + 4, 16 * (kt0 + x), r, kf);
-          if (round == 0) {
-            bf16x8 qf[IN];
-            if (before) aq[x][t] = mm<LEVEL>(kf, mf, aq[x][t]);
-            if (after) {
-              KTile::col_frag(Qs, t0, t0 + 4, 16 * (kt0 + x), r, qf);
-              ak[x][t] = mm<LEVEL>(qf, mt, ak[x][t]);
-            }
-          } else {
-            if (before) ak[x][t] = mm<LEVEL>(kf, mf, ak[x][t]);
-            if (after) ak[x][t] = mm<LEVEL>(kf, mt, ak[x][t]);
-          }
+        bf16x8 m[LEVEL];
+        if (before) {
+          MTile::row_frag(Ms, 16 * tt + r, t0, m);
+          if (round == 0) aq[t] = mm<LEVEL>(kf, m, aq[t]);
+          else ak[t] = mm<LEVEL>(kf, m, ak[t]);
+        }
+        if (after) {
+          MTile::col_frag(Mt, t0, t0 + 4, 16 * tt, r, m);
+          if (round == 0) ak[t] = mm<LEVEL>(qf, m, ak[t]);
+          else ak[t] = mm<LEVEL>(kf, m, ak[t]);
         }
       }
     }
     if (round == 0) {
       __syncthreads();
-#pragma unroll
-      for (int jt = 0; jt < 4; ++jt) {
-        const f32x4 k4 = *reinterpret_cast<const f32x4*>(rec.rk + 16 * jt + 4 * q4);
-        MTile::store4(Ms, own, 16 * jt + 4 * q4, at[jt] * k4);
-        MTile::store4(Mt, own, 16 * jt + 4 * q4, at[jt] * rk_own);
-      }
+      store_masked(at, rk_own, false);
       __syncthreads();
     }
   }
@@ -1151,58 +1139,51 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
   for (int t = 0; t < NTOK; ++t) {
     const int i = 16 * (tt0 + t) + r;
     float dq = 0.f, dk = 0.f;
+    const f32x4 q = KTile::row4(Qs, i, 16 * kt0 + 4 * q4), k = KTile::row4(Ks, i, 16 * kt0 + 4 * q4);
 #pragma unroll
-    for (int x = 0; x < NK; ++x) {
-      const f32x4 q = KTile::row4(Qs, i, 16 * (kt0 + x) + 4 * q4), k = KTile::row4(Ks, i, 16 * (kt0 + x) + 4 * q4);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        dq = __builtin_fmaf(q[v], aq[x][t][v], dq);
-        dk = __builtin_fmaf(k[v], ak[x][t][v], dk);
-      }
+    for (int v = 0; v < 4; ++v) {
+      dq = __builtin_fmaf(q[v], aq[t][v], dq);
+      dk = __builtin_fmaf(k[v], ak[t][v], dk);
     }
     dq += __shfl_xor(dq, 16, 64);
     dk += __shfl_xor(dk, 16, 64);
     dq += __shfl_xor(dq, 32, 64);
     dk += __shfl_xor(dk, 32, 64);
     if (q4 == 0) {
-      qdot[Cfg::KT >= 4 ? w : w % 2][i] = dq;
-      kdot[Cfg::KT >= 4 ? w : w % 2][i] = dk;
+      qdot[kt0][i] = dq;
+      kdot[kt0][i] = dk;
     }
   }
   __syncthreads();
-  constexpr int SHARES = Cfg::KT >= 4 ? 4 : 2;
 #pragma unroll
   for (int t = 0; t < NTOK; ++t) {
     const int i = 16 * (tt0 + t) + r;
     float dq = 0.f, dk = 0.f;
 #pragma unroll
-    for (int n = 0; n < SHARES; ++n) {
+    for (int n = 0; n < KT; ++n) {
       dq += qdot[n][i];
       dk += kdot[n][i];
     }
     const float fq = rq[i], fk = rec.rk[i];
     const float cq = fq == inv_eps ? 0.f : fq * (fq * dq), ck = fk == inv_eps ? 0.f : fk * (fk * dk);
     if (row0 + i < there) {
+      const size_t at_ = size_t(row0 + i) * DK + 16 * kt0 + 4 * q4;
+      const f32x4 q = KTile::row4(Qs, i, 16 * kt0 + 4 * q4), k = KTile::row4(Ks, i, 16 * kt0 + 4 * q4);
+      typedef __attribute__((ext_vector_type(4))) T vec4;
+      vec4 gq, gk;
 #pragma unroll
-      for (int x = 0; x < NK; ++x) {
-        const size_t at_ = size_t(row0 + i) * DK + 16 * (kt0 + x) + 4 * q4;
-        const f32x4 q = KTile::row4(Qs, i, 16 * (kt0 + x) + 4 * q4), k = KTile::row4(Ks, i, 16 * (kt0 + x) + 4 * q4);
-        typedef __attribute__((ext_vector_type(4))) T vec4;
-        vec4 gq, gk;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          gq[v] = T(scale * (fq * __builtin_fmaf(-cq, q[v], aq[x][t][v])));
-          gk[v] = T(fk * __builtin_fmaf(-ck, k[v], ak[x][t][v]));
-        }
-        *reinterpret_cast<vec4*>(dQu + at_) = gq;
-        *reinterpret_cast<vec4*>(dKu + at_) = gk;
+      for (int v = 0; v < 4; ++v) {
+        gq[v] = T(scale * (fq * __builtin_fmaf(-cq, q[v], aq[t][v])));
+        gk[v] = T(fk * __builtin_fmaf(-ck, k[v], ak[t][v]));
       }
+      *reinterpret_cast<vec4*>(dQu + at_) = gq;
+      *reinterpret_cast<vec4*>(dKu + at_) = gk;
     }
   }
   if (w == 0) {   // lane l: token l
     float dot = 0.f;
 #pragma unroll
-    for (int n = 0; n < SHARES; ++n) dot += qdot[n][l];
+    for (int n = 0; n < KT; ++n) dot += qdot[n][l];
     dot *= rq[l];   // qh . dqh / s
     const float sum = group_sum<64>(dot);
     if (l == 0) ds_parts[blockIdx.x] = sum;
@@ -1213,7 +1194,8 @@ __global__ __launch_bounds__(256, (DeltaGradCfg<T, DK, DV>::GROUPS)) void delta_
         const double behind = __shfl_down(flow, d, 64);
         if (l + d < 64) flow += behind;
       }
-      flow += double(tail[0]) + double(tail[1]) + double(tail[2]) + double(tail[3]);
+#pragma unroll
+      for (int n = 0; n < Cfg::WAVES; ++n) flow += double(tail[n]);
       if (row0 + l < there) {
         const float ld = log_decay[row_at + row0 + l];
         // 0 where the decay does not depend on it, or there is nothing yet to decay
@@ -1270,8 +1252,9 @@ hipError_t run_rev(const DeltaArgs& a) {
 template <typename T, int DK, int DV>
 hipError_t run_gradients(const DeltaArgs& a) {
   const int chunks = delta_chunks(a.N);
-  return launch_kernel("delta_gradients", delta_gradients<T, DK, DV>, dim3(unsigned(a.B * a.H * chunks)), dim3(256), 0, a.stream,
-                       static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V),
+  return launch_kernel("delta_gradients", delta_gradients<T, DK, DV>, dim3(unsigned(a.B * a.H * chunks)),
+                       dim3(DeltaGradCfg<T, DK, DV>::THREADS), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
+                       static_cast<const T*>(a.V),
                        static_cast<const T*>(a.dO), a.s, a.log_decay, a.beta, a.seq_len,
                        static_cast<const ChunkRecord*>(a.records), a.errors, a.states, a.zs,
                        a.dstates, static_cast<T*>(a.dQ), static_cast<T*>(a.dK), static_cast<T*>(a.dV), a.dlog_decay, a.dbeta,
