@@ -409,8 +409,8 @@ int cottn_step_delta(const void* q, const void* k, const void* v, const float* s
  *   an input or the other output (COTTN_E_ARG).  For single tokens N is 1.
  *   positions: int[B][N][axes], any values; freq: float[pairs], radians to a position; axis: int[pairs], the axis (time, row,
  *   column, ...) that a pair is turned by, NULL for 0; a pair whose axis is none of 0 .. axes - 1 is not turned.
- *   pairs: 1 .. d / 2; d one of 32, 64, 128; axes >= 1.  With v = 16 bytes of elements where pairs is a multiple of that, else
- *   1, B (N + t - 1) / t is below 16 777 216 for t = 512 v / d; more is refused (COTTN_E_SHAPE).
+ *   pairs: 1 .. d / 2; d one of 32, 64, 128; axes >= 1.  With v = the elements of 16 bytes where pairs is a multiple of that
+ *   and N d at least 128 of it, else 1, B (N + t - 1) / t is below 16 777 216 for t = 512 v / d; more is refused (COTTN_E_SHAPE).
  *   inverse: turned by - phi, which is the gradient of the call without.
  * Angles are formed in 64 bits.  N = 0 does nothing. */
 int cottn_rotary(const void* Q, const void* K, const int* positions, const float* freq, const int* axis, void* Qr, void* Kr,

@@ -378,7 +378,9 @@ struct DeltaSpace {
 };
 // Time of a forward in G segments, in steps of a workgroup, of which a compute unit has one.  More than one segment walk the
 // rows twice, first for the totals of all but the last, with the columns of M beside those of the values, two workgroups to a
-// compute unit; then the states at their starts are found one after the other.  Two launches more.
+// compute unit; then the states at their starts are found one after the other.  Two launches more.  (16 heads of 32768 rows at
+// 64 x 64, forward and backward: 3240 us in one segment, 890 in the 16 that it takes.  Over 16 shapes its split was the fastest of those
+// tried or within 15 % of it.)
 double delta_steps(long units, long chunks, long G, int dk, int dv) {
   const long per = dv == 32 ? 32 : 64, parts = dv / per, seg = (chunks + G - 1) / G;
   const auto rounds = [](long workgroups, long at_once) { return double((workgroups + at_once - 1) / at_once); };
@@ -1209,7 +1211,7 @@ int cottn_rotary(const void* Q, const void* K, const int* positions, const float
   if (pairs < 1 || pairs > d / 2 || axes < 1) return COTTN_E_SHAPE;
   if (freq == nullptr || (positions == nullptr && N > 0)) return COTTN_E_NULL;
   if (!is_aligned(positions, 4) || !is_aligned(freq, 4) || !is_aligned(axis, 4)) return COTTN_E_ALIGN;
-  if (!threads_fit(long(B) * rotary_tiles(N, d, rotary_run(pairs, dtype)), 256)) return COTTN_E_SHAPE;
+  if (!threads_fit(long(B) * rotary_tiles(N, d, rotary_run(N, d, pairs, dtype)), 256)) return COTTN_E_SHAPE;
   if (N == 0) return COTTN_OK;
   const double floats = double(B) * H * N * d * (dtype == COTTN_F32 ? 1.0 : 0.5);
   const float* in[] = {static_cast<const float*>(Q), static_cast<const float*>(K)};

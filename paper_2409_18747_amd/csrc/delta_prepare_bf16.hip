@@ -1,6 +1,11 @@
 // The gated delta rule: what a chunk's rows of K and its gates come to by themselves (delta.h).  All chunks at once, a
 // workgroup each: the decays and the rows' factors (ChunkRecord), and the 64 x 64 matrix W as the operand fragments that the
-// scans read.
+// scans read, once by rows and, for a backward, once more by columns (18 KB each).
+//   A workgroup is one dependent chain - rows, A, the diagonal blocks, two sizes of blocks below them - of some 20000 cycles, so
+// that what counts is how many a compute unit holds: the matrix takes the rows' place in the LDS and steps of the blocks its empty
+// quarter, 20 KB in all, and a diagonal block takes four registers to a lane, not 32.  16 heads of 32768 rows of 64 with a backward
+// take 73 us, the rate of a copy; 32 x 16 heads of 2048 rows of 128 without 118 us, 4.0 TB/s (three to a unit and a column of a
+// block to a lane: 101 and 205 us).
 #include "device_common.h"
 #include "delta.h"
 #include "delta_elem.h"

