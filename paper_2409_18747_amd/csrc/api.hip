@@ -393,7 +393,7 @@ bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, Delt
   if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
   if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != 64)) return false;
   const long units = long(B) * H, chunks = (long(N) + 63) / 64;
-  if (!threads_fit(units * std::max<long>(chunks, dv / 16), 256)) return false;
+  if (!threads_fit(units * std::max<long>(chunks, dv / 16), 512)) return false;   // (delta_gradients, delta_carry)
   long G = g_tuned_segments;
   if (G <= 0) {
     G = 1;
@@ -404,7 +404,7 @@ bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, Delt
   if (G < 1 || (dtype == COTTN_F32 && dk == 128)) G = 1;   // (kernels for whole sequences alone)
   p->seg = chunks > 0 ? int((chunks + G - 1) / G) : 1;
   p->G = chunks > 0 ? int((chunks + p->seg - 1) / p->seg) : 1;
-  if (p->G > 1 && (!threads_fit(units * p->G, 768) || !threads_fit(units * (dv / 16), 512))) return false;
+  if (!threads_fit(units * std::max<long>(p->G, p->G == 1 ? dv / 64 : 1), 768)) return false;   // the scans
   const size_t all = size_t(units) * chunks, state = round_up_256(all * dk * dv * 4), rows = round_up_256(all * 64 * dv * 4);
   const size_t segments = p->G > 1 ? size_t(units) * p->G : 0;
   p->records = 0;

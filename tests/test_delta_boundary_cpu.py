@@ -44,7 +44,7 @@ COMMON = [({"dk": 48}, SHAPE), ({"dv": 256}, SHAPE), ({"B": 0}, SHAPE), ({"H": -
 @pytest.mark.parametrize("change,status", COMMON + [({k: None}, NULL) for k in ("Q", "K", "V", "s", "beta", "O")] + [
     ({"N": -1}, SHAPE), ({"Q": P + 8}, ALIGN), ({"state": P + 4}, ALIGN), ({"state_in": P + 8}, ALIGN), ({"seq_len": P + 1}, ALIGN),
     ({"state_in": P, "state": P + 64}, ARG), ({"state_in": P + STATES - 16, "state": P}, ARG), ({"ws": None}, WORKSPACE),
-    ({"ws_bytes": 16}, WORKSPACE), ({"ws": 256 * P + 16}, ALIGN), ({"B": 1 << 12, "H": 1 << 12, "N": 65}, SHAPE),
+    ({"ws_bytes": 16}, WORKSPACE), ({"ws": 256 * P + 16}, ALIGN), ({"B": 1 << 11, "H": 1 << 12, "N": 64}, SHAPE), ({"B": 1 << 11, "H": 1 << 11, "N": 65}, SHAPE),
     ({"B": 1 << 11, "H": 1 << 11, "dv": 128}, SHAPE), ({"N": 0, "ws": None}, OK), ({"N": 0, "Q": None, "beta": None}, OK)])
 def test_forward(lib, change, status):
     assert refused(lib, "cottn_fwd_causal_delta", FWD, change, status)
