@@ -365,8 +365,9 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  * 0, one below -128 (-inf among them) keeps nothing.  beta is usually in 0 .. 1, and any finite number: between 0 and 2 no state
  * grows but by its values.  States are float[B][H][dk][dv], without s; dk and dv are each one of 32, 64, 128.  Rows
  * are taken in chunks of 64, and a long sequence of few units in segments that are walked side by side, as the operations above:
- * cottn_segments_dkdv with chunk 0 says into how many, cottn_tune_segments sets it (fp32 with dk 128: always one).  All dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them
- * in bfloat16 parts).  Workspaces: cottn_workspace_bytes_dkdv with the COTTN_OP_*_DELTA* operations, chunk 0; always needed.
+ * cottn_segments_dkdv with chunk 0 says into how many, cottn_tune_segments sets it (fp32 with dk 128: always one).  All
+ * dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them in bfloat16 parts).
+ * Workspaces: cottn_workspace_bytes_dkdv with the COTTN_OP_*_DELTA* operations, chunk 0; always needed.
  * A value that is not finite, in a row, a gate or a state, can make results of its sequence and head not finite, those of
  * earlier rows of its chunk among them.  B H (N + 63) / 64 and B H dv / 16 are below 8 388 608; more is refused
  * (COTTN_E_SHAPE).
@@ -377,7 +378,8 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  * without one, and then a 16-bit call without state is the faster one.
  * Backward, of the same call: gradients with respect to the raw Q, K, V, to s (float[H], with seq_len float[B][H]), to
  * log_decay and to beta (float[B][H][N], zeros at or beyond a sequence's end; dlog_decay may be NULL, and must be where log_decay
- * is; it is 0 where log_decay is above 0 or below -128).  For a sequence in pieces, last piece first (both optional):
+ * is; it is 0 where log_decay is above 0 or below -128, else a sum of the rows' <o, dO> and <v, dV> from t on, to fp32
+ * roundings of those, which may cancel).  For a sequence in pieces, last piece first (both optional):
  *   dstate      the gradient with respect to the forward call's `state`: the dstate_in of the piece behind;
  *   dstate_in   that with respect to its state_in.  May be dstate, else must overlap neither dstate nor state_in (COTTN_E_ARG).
  * fwd_workspace: NULL, or the workspace, of COTTN_OP_FWD_DELTA's size or more, of the matching completed cottn_fwd_causal_delta
