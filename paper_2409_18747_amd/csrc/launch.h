@@ -317,7 +317,7 @@ struct DeltaArgs {
   void* O; float* state;            // forward: results (state may be null); backward: no O, and only errors and states are formed
   // G segments of `seg` chunks, one after the other where G is 1: the states at the starts of the segments but the first, what a
   // segment makes of the state at its start, [units][G][dk][dk], and the gradients with respect to the states at the ends of the
-  // segments but the last
+  // segments but the last.  (In the slots that are left: state_in, and dstate, where the result is to take its place.)
   int G, seg;
   float* starts; float* transitions; float* ends;
   void* records; unsigned short* w_rows;
