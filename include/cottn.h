@@ -365,7 +365,7 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  * 0, one below -128 (-inf among them) keeps nothing.  beta is usually in 0 .. 1, and any finite number: between 0 and 2 no state
  * grows but by its values.  States are float[B][H][dk][dv], without s; dk and dv are each one of 32, 64, 128.  Rows
  * are taken in chunks of 64, and a long sequence of few units in segments that are walked side by side, as the operations above:
- * cottn_segments_dkdv with chunk 0 says into how many, cottn_tune_segments sets it (fp32 with dk 128: always one).  All
+ * cottn_segments_dkdv with chunk 0 says into how many, cottn_tune_segments sets it.  All
  * dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them in bfloat16 parts).
  * Workspaces: cottn_workspace_bytes_dkdv with the COTTN_OP_*_DELTA* operations, chunk 0; always needed.
  * A value that is not finite, in a row, a gate or a state, can make results of its sequence and head not finite, those of

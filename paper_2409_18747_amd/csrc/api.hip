@@ -401,7 +401,7 @@ bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, Delt
       if (delta_steps(units, chunks, g, dk, dv) < 0.95 * delta_steps(units, chunks, G, dk, dv)) G = g;
   }
   if (G > chunks) G = chunks;
-  if (G < 1 || (dtype == COTTN_F32 && dk == 128)) G = 1;   // (kernels for whole sequences alone)
+  if (G < 1) G = 1;
   p->seg = chunks > 0 ? int((chunks + G - 1) / G) : 1;
   p->G = chunks > 0 ? int((chunks + p->seg - 1) / p->seg) : 1;
   if (!threads_fit(units * std::max<long>(p->G, p->G == 1 ? dv / 64 : 1), 768)) return false;   // the scans

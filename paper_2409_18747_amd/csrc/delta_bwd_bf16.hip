@@ -636,12 +636,12 @@ struct DeltaWideRevCfg {
   static constexpr int WAVES = (AT_ONCE < MOST ? AT_ONCE : MOST) * (NW <= 4 ? 1 : 2);   // to a SIMD
 };
 
-template <typename T, int DK, int NW>
+template <typename T, int DK, int NW, bool TOTALS>
 __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void delta_wide_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
-    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, Divisor H, Divisor parts, int N,
-    int units, int DV, float inv_eps) {
+    const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, float* ends, Divisor H, Divisor G,
+    Divisor parts, int seg, int N, int units, int DV, float inv_eps) {
   using Cfg = DeltaWideRevCfg<T, DK, NW>;
   using KTile = typename Cfg::KTile;
   using GTile = typename Cfg::GTile;
@@ -654,11 +654,22 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
   __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::W_SIZE];
   __shared__ ChunkRecord rec;
   __shared__ __attribute__((aligned(16))) float rq[CHUNK];
-  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, H, parts, N, units, DV, inv_eps);
-  int unit, part;
-  unit_and_segment(blockIdx.x, units, parts, unit, part);
+  fetch_argument_now(Q, K, dO, s, lengths, dstate, dstate_in, records, w_cols, zs, dstates, ends, H, G, parts, seg, N, units, DV,
+                     inv_eps);
+  int unit, part, g = 0;
+  if (G.n == 1) {
+    unit_and_segment(blockIdx.x, units, parts, unit, part);
+  } else {   // (blockIdx.y: the part)
+    unit_and_segment(blockIdx.x, units, G, unit, g);
+    part = blockIdx.y;
+  }
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
-  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), steps = delta_chunks(there), col0 = part * VC;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), all = delta_chunks(there), first = g * seg, steps = min(all, first + seg), col0 = part * VC;
+  if ((first >= all && g > 0) || (TOTALS && g == 0)) return;
+  const bool ends_here = steps == all;   // the last rows
+  const bool put_by = ends_here && g > 0 && dstate != nullptr && dstate == dstate_in;
+  const float* from = ends_here && (TOTALS || !put_by) ? (dstate != nullptr ? dstate + size_t(unit) * DK * DV : nullptr)
+                      : TOTALS ? nullptr : ends + (size_t(unit) * G.n + g) * DK * DV;
   const T* Qu = Q + size_t(unit) * N * DK;
   const T* Ku = K + size_t(unit) * N * DK;
   const T* dOu = dO + size_t(unit) * N * DV + col0;
@@ -671,7 +682,14 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
   for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
     for (int v = 0; v < 4; ++v)
-      D[t][v] = dstate != nullptr ? (dstate + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+      D[t][v] = from != nullptr ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+  if (TOTALS && put_by) {
+    float* to = ends + (size_t(unit) * G.n + g) * DK * DV;
+#pragma unroll
+    for (int t = 0; t < 2 * KS; ++t)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) (to + key_of(t / 2, t % 2, 0, v) * DV)[at_key] = D[t][v];
+  }
 
   RowTile<T, DK, Cfg::PAD, NT> kt, qt;
   RowTile<T, VC, Cfg::PAD, NT> gt;
@@ -690,8 +708,8 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
       if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
         w_next[i] = reinterpret_cast<const u32x4*>(w_cols + at * W_ELEMS)[i * NT + tid];
   };
-  if (steps > 0) fetch(steps - 1);
-  for (int c = steps - 1; c >= 0; --c) {
+  if (steps > first) fetch(steps - 1);
+  for (int c = steps - 1; c >= first; --c) {
     kt.commit(Ks);
     qt.commit(Qs);
     qt.store_factors(rq, inv_eps);
@@ -703,8 +721,8 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
     for (int i = 0; i < W_PIECES; ++i)
       if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
     __syncthreads();
-    if (c > 0) fetch(c - 1);
-    {
+    if (c > first) fetch(c - 1);
+    if constexpr (!TOTALS) {
       float* to = dstates + (size_t(unit) * chunks + c) * DK * DV;
 #pragma unroll
       for (int t = 0; t < 2 * KS; ++t)
@@ -814,9 +832,11 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
             z = mm<LEVEL>(wf, ff[k], z);
           }
         z = f[t] - z;
-        float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
+        if constexpr (!TOTALS) {
+          float* to = zs + (size_t(unit) * chunks + c) * CHUNK * DV;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+          for (int v = 0; v < 4; ++v) (to + (16 * t + v) * DV)[at_token] = z[v];
+        }
         x[h] = -(b[t] * z) * *reinterpret_cast<const f32x4*>(rec.rk_since + 16 * t + 4 * q4);
       }
       split8<LEVEL>(x[0], x[1], xf[p]);
@@ -849,8 +869,8 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
     }
     __syncthreads();   // everything of the chunk is read
   }
-  if (dstate_in != nullptr) {
-    float* to = dstate_in + size_t(unit) * DK * DV;
+  float* to = TOTALS ? ends + (size_t(unit) * G.n + g - 1) * DK * DV : dstate_in != nullptr && g == 0 ? dstate_in + size_t(unit) * DK * DV : nullptr;
+  if (to != nullptr) {
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
@@ -1230,29 +1250,24 @@ template <typename T, int DK, int NW>
 hipError_t run_rev(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
   const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
-  if constexpr (DeltaRevCfg<T, DK, NW>::FITS) {
-    constexpr bool AHEAD = DeltaAheadCfg<T, DK, NW>::FITS;
-    const auto run = [&](auto kernel) {
-      return launch_kernel("delta_rev_scan", kernel, a.G == 1 ? dim3(unsigned(units * parts)) : dim3(unsigned(units * a.G), unsigned(parts)),
-                           dim3((AHEAD ? 192 : 128) * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
-                           static_cast<const T*>(a.dO), a.s, a.seq_len, a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates,
-                           a.ends, Divisor(a.H), Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
-    };
-    if (a.G > 1) {
-      hipError_t err;
-      if constexpr (AHEAD) err = run(delta_ahead_rev_scan<T, DK, NW, true>);
-      else err = run(delta_rev_scan<T, DK, NW, true>);
-      if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, true);
-      if (err != hipSuccess) return err;
-    }
-    if constexpr (AHEAD) return run(delta_ahead_rev_scan<T, DK, NW, false>);
-    else return run(delta_rev_scan<T, DK, NW, false>);
-  } else {
-    return launch_kernel("delta_rev_scan", delta_wide_rev_scan<T, DK, NW>, dim3(unsigned(units * parts)), dim3(64 * NW), 0, a.stream,
-                         static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.dO), a.s, a.seq_len,
-                         a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates, Divisor(a.H), Divisor(parts), a.N, units, a.dv,
-                         1.0f / a.eps);
+  constexpr bool AHEAD = DeltaAheadCfg<T, DK, NW>::FITS, BESIDE = DeltaRevCfg<T, DK, NW>::FITS;
+  const auto run = [&](auto kernel) {
+    return launch_kernel("delta_rev_scan", kernel, a.G == 1 ? dim3(unsigned(units * parts)) : dim3(unsigned(units * a.G), unsigned(parts)),
+                         dim3((AHEAD ? 192 : BESIDE ? 128 : 64) * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
+                         static_cast<const T*>(a.dO), a.s, a.seq_len, a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates,
+                         a.ends, Divisor(a.H), Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
+  };
+  if (a.G > 1) {
+    hipError_t err;
+    if constexpr (AHEAD) err = run(delta_ahead_rev_scan<T, DK, NW, true>);
+    else if constexpr (BESIDE) err = run(delta_rev_scan<T, DK, NW, true>);
+    else err = run(delta_wide_rev_scan<T, DK, NW, true>);
+    if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, true);
+    if (err != hipSuccess) return err;
   }
+  if constexpr (AHEAD) return run(delta_ahead_rev_scan<T, DK, NW, false>);
+  else if constexpr (BESIDE) return run(delta_rev_scan<T, DK, NW, false>);
+  else return run(delta_wide_rev_scan<T, DK, NW, false>);
 }
 
 template <typename T, int DK, int DV>

@@ -376,7 +376,8 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
-    float* __restrict__ states, Divisor H, Divisor parts, int N, int units, int DV, float inv_eps) {
+    float* __restrict__ states, const float* __restrict__ starts, Divisor H, Divisor G, Divisor parts, int seg, int N, int units,
+    int DV, float inv_eps) {
   using Cfg = DeltaWideFwdCfg<T, DK, NW, LEVEL>;
   using KTile = typename Cfg::KTile;
   using VTile = typename Cfg::VTile;
@@ -390,11 +391,20 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
   __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::P_SIZE];
   __shared__ ChunkRecord rec;
   __shared__ __attribute__((aligned(16))) float rq[CHUNK];
-  fetch_argument_now(Q, K, V, s, lengths, state_in, O, state_out, records, w_rows, errors, states, H, parts, N, units, DV, inv_eps);
-  int unit, part;
-  unit_and_segment(blockIdx.x, units, parts, unit, part);
+  fetch_argument_now(Q, K, V, s, lengths, state_in, O, state_out, records, w_rows, errors, states, starts, H, G, parts, seg, N, units, DV,
+                     inv_eps);
+  int unit, part, g = 0;
+  if (G.n == 1) {
+    unit_and_segment(blockIdx.x, units, parts, unit, part);
+  } else {   // (blockIdx.y: the part)
+    unit_and_segment(blockIdx.x, units, G, unit, g);
+    part = blockIdx.y;
+  }
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid / 64), l = tid % 64, r = l % 16, q4 = l / 16;
-  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), steps = delta_chunks(there), col0 = part * VC;
+  const int there = valid_rows(lengths, unit, H, N), chunks = delta_chunks(N), all = delta_chunks(there), first = g * seg, steps = min(all, first + seg), col0 = part * VC;
+  const bool ends_here = steps == all && (first < all || g == 0);   // the state after the last row
+  const bool put_by = g == 0 && G.n > 1 && !ends_here && state_in != nullptr && state_in == state_out;
+  const float* from = g == 0 && !put_by ? (state_in != nullptr ? state_in + size_t(unit) * DK * DV : nullptr) : starts + (size_t(unit) * G.n + g) * DK * DV;
   const T* Qu = Q + size_t(unit) * N * DK;
   const T* Ku = K + size_t(unit) * N * DK;
   const T* Vu = V + size_t(unit) * N * DV + col0;
@@ -408,7 +418,7 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
   for (int t = 0; t < 2 * KS; ++t)
 #pragma unroll
     for (int v = 0; v < 4; ++v)
-      S[t][v] = state_in != nullptr ? (state_in + size_t(unit) * DK * DV + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
+      S[t][v] = from != nullptr && (g == 0 || first < all) ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
 
   RowTile<T, DK, 16, NT> kt, qt;
   RowTile<T, VC, 16, NT> vt;
@@ -441,8 +451,8 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
         w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
     }
   };
-  if (steps > 0) fetch(0);
-  for (int c = 0; c < steps; ++c) {
+  if (steps > first) fetch(first);
+  for (int c = first; c < steps; ++c) {
     const int row0 = c * CHUNK;
     kt.commit(Ks);
     qt.commit(Qs);
@@ -611,7 +621,7 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
     }
     __syncthreads();   // everything of the chunk is read
   }
-  if (state_out != nullptr) {
+  if (state_out != nullptr && ends_here) {
     float* to = state_out + size_t(unit) * DK * DV;
 #pragma unroll
     for (int t = 0; t < 2 * KS; ++t)
@@ -620,35 +630,36 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
   }
   // rows that do not exist
   if (O == nullptr) return;
-  for (long i = tid; i < long(N - there) * (VC / 4); i += NT)
-    *reinterpret_cast<vec4*>(Ou + size_t(there + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
+  const int lo = max(there, first * CHUNK), hi = min(N, (first + seg) * CHUNK);
+  for (long i = tid; i < long(hi - lo) * (VC / 4); i += NT)
+    *reinterpret_cast<vec4*>(Ou + size_t(lo + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
 }
 
 template <typename T, int DK, int NW, int LEVEL>
 hipError_t run_scan(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
   const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
+  const auto grid = [&](int n_parts) { return a.G == 1 ? dim3(unsigned(units * n_parts)) : dim3(unsigned(units * a.G), unsigned(n_parts)); };
+  const auto run = [&](auto kernel, int n_parts, int threads) {
+    return launch_kernel("delta_fwd_scan", kernel, grid(n_parts), dim3(threads), 0, a.stream, static_cast<const T*>(a.Q),
+                         static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len, a.state_in, static_cast<T*>(a.O), a.state,
+                         records, a.w_rows, a.errors, a.states, a.starts, a.transitions, Divisor(a.H), Divisor(a.G), Divisor(n_parts),
+                         a.seg, a.N, units, a.dv, 1.0f / a.eps);
+  };
+  if (a.G > 1) {
+    // M is not asked for where the states at the starts of two segments are known without, and no backward follows
+    const int with_M = a.G > 2 || a.errors != nullptr ? (DK + 16 * NW - 1) / (16 * NW) : 0;
+    hipError_t err = run(delta_fwd_scan<T, DK, NW, 3, true>, parts + with_M, 128 * NW);
+    if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, false);
+    if (err != hipSuccess) return err;
+  }
   if constexpr (DeltaFwdCfg<T, DK, NW, LEVEL>::FITS) {
-    const auto run = [&](auto kernel, int n_parts, int threads) {
-      return launch_kernel("delta_fwd_scan", kernel, a.G == 1 ? dim3(unsigned(units * n_parts)) : dim3(unsigned(units * a.G), unsigned(n_parts)),
-                           dim3(threads), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
-                           static_cast<const T*>(a.V), a.s, a.seq_len, a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows,
-                           a.errors, a.states, a.starts, a.transitions, Divisor(a.H), Divisor(a.G), Divisor(n_parts), a.seg, a.N,
-                           units, a.dv, 1.0f / a.eps);
-    };
-    if (a.G > 1) {
-      // M is not asked for where the states at the starts of two segments are known without, and no backward follows
-      const int with_M = a.G > 2 || a.errors != nullptr ? (DK + 16 * NW - 1) / (16 * NW) : 0;
-      hipError_t err = run(delta_fwd_scan<T, DK, NW, 3, true>, parts + with_M, 128 * NW);
-      if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, false);
-      if (err != hipSuccess) return err;
-    }
     return run(delta_fwd_scan<T, DK, NW, LEVEL, false>, parts, 192 * NW);
   } else {
-    return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW, LEVEL>, dim3(unsigned(units * parts)), dim3(64 * NW), 0,
-                         a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s,
-                         a.seq_len, a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows, a.errors, a.states, Divisor(a.H),
-                         Divisor(parts), a.N, units, a.dv, 1.0f / a.eps);
+    return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW, LEVEL>, grid(parts), dim3(64 * NW), 0, a.stream,
+                         static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len,
+                         a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows, a.errors, a.states, a.starts, Divisor(a.H),
+                         Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
   }
 }
 

@@ -250,7 +250,7 @@ def test_segments(cottn, segments, dtype, dk, dv, G):
     segments(G)
     code = {"f32": 0, "bf16": 1, "f16": 2}[dtype]
     got = cottn.cottn_segments_dkdv(cottn.OP_FWD_DELTA, 1, 2, 300, dk, dv, 0, code)
-    assert got == (1 if dtype == "f32" and dk == 128 else G)
+    assert got == G
     x, more = draw(1, 2, 300, dk, dv, dtype, G + dk)
     run_both(cottn, x, more, dtype, states=G != 3)
     want, _ = ref.forward(**double(x))

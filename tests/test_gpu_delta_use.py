@@ -20,13 +20,13 @@ def cottn():
 
 
 @pytest.mark.parametrize("G", [1, 2, 4])
-@pytest.mark.parametrize("dk,dv", [(32, 32), (64, 128), (128, 64)])
-def test_states_in_place(cottn, G, dk, dv):
+@pytest.mark.parametrize("dk,dv,dtype", [(32, 32, "bf16"), (64, 128, "bf16"), (128, 64, "bf16"), (128, 64, "f32")])
+def test_states_in_place(cottn, G, dk, dv, dtype):
     """state for state_in and dstate_in for dstate: the same results as apart, also where the segments' workgroups are more than
     the chip has room for, so that the last one of a sequence can be done before the first begins."""
     cottn.cottn_tune_segments(G)
     B, H, N = 24, 16, 200
-    x, more = draw(B, H, N, dk, dv, "bf16", G, per_unit=True)
+    x, more = draw(B, H, N, dk, dv, dtype, G, per_unit=True)
     d, m = cuda(x), cuda(more)
     lens = torch.randint(0, N + 1, (B,), generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()
     ws = train_workspace(cottn, d)
@@ -158,12 +158,12 @@ def test_drawn_sizes(cottn, seed):
         run_both(cottn, x, more, dtype, states=states)
 
 
-@pytest.mark.parametrize("dtype,G", [("bf16", 0), ("bf16", 1), ("f32", 0)])
-def test_a_long_sequence(cottn, dtype, G):
+@pytest.mark.parametrize("dtype,dk,G", [("bf16", 64, 0), ("bf16", 64, 1), ("f32", 64, 0), ("f32", 128, 0)])
+def test_a_long_sequence(cottn, dtype, dk, G):
     """64 chunks, forward and back again: 768 roundings a chunk and walk, whose signs are as good as random, sqrt(2 x 64 x 768) =
     313 of 2^-24 on top of what the shorter ones are given."""
     cottn.cottn_tune_segments(G)
-    x, more = draw(1, 2, 4096, 64, 32, dtype, 9)
+    x, more = draw(1, 2, 4096, dk, 32, dtype, 9)
     run_both(cottn, x, more, dtype, off=313 * 2.0 ** -24)
 
 
