@@ -381,24 +381,28 @@ struct DeltaSpace {
 // compute unit; then the states at their starts are found one after the other.  Two launches more.  (16 heads of 32768 rows at
 // 64 x 64, forward and backward: 3240 us in one segment, 890 in the 16 that it takes.  Over 16 shapes its split was the fastest of those
 // tried or within 15 % of it.)
-double delta_steps(long units, long chunks, long G, int dk, int dv) {
-  const long per = dv == 32 ? 32 : 64, parts = dv / per, seg = (chunks + G - 1) / G;
+// Rows of 128 in fp32 (`wide`): 32 columns to a workgroup in the backward, and steps of 11 us, not 3, to which launches and the
+// chain of segments count less (8 heads of 4096 rows: 1508 us in one segment, 489 in 13, 434 in the 8 that it takes).
+double delta_steps(long units, long chunks, long G, int dk, int dv, bool wide) {
+  const long per = dv == 32 || wide ? 32 : 64, parts = dv / per, seg = (chunks + G - 1) / G;
   const auto rounds = [](long workgroups, long at_once) { return double((workgroups + at_once - 1) / at_once); };
   const double whole = rounds(units * parts * G, kComputeUnits) * double(seg);
   if (G == 1) return whole + 1.0;
   const long columns = G > 2 ? (dk + per - 1) / per * (G - 1) : 0;
-  return whole + 0.8 * rounds(units * (parts * (G - 1) + columns), 2 * kComputeUnits) * double(seg) + 3.0 + (G > 2 ? 0.35 * double(G) + 1.0 : 0.0);
+  const double totals = (wide ? 0.7 : 0.8) * rounds(units * (parts * (G - 1) + columns), 2 * kComputeUnits) * double(seg);
+  return whole + totals + (wide ? 0.3 : 1.0) * (3.0 + (G > 2 ? (dk == 128 ? 0.6 : 0.35) * double(G) + 1.0 : 0.0));
 }
 bool delta_space(int B, int H, int N, int dk, int dv, int chunk, int dtype, DeltaSpace* p) {
   if (dtype != COTTN_F32 && dtype != COTTN_BF16 && dtype != COTTN_F16) return false;
   if (!dims_ok(B, H, N, dk, dv) || (chunk != 0 && chunk != 64)) return false;
   const long units = long(B) * H, chunks = (long(N) + 63) / 64;
   if (!threads_fit(units * std::max<long>(chunks, dv / 16), 512)) return false;   // (delta_gradients, delta_carry)
+  const bool wide = dtype == COTTN_F32 && dk == 128;
   long G = g_tuned_segments;
   if (G <= 0) {
     G = 1;
     for (long g = 2; g <= 64 && g <= chunks && units * g <= 2 * kComputeUnits; ++g)
-      if (delta_steps(units, chunks, g, dk, dv) < 0.95 * delta_steps(units, chunks, G, dk, dv)) G = g;
+      if (delta_steps(units, chunks, g, dk, dv, wide) < 0.95 * delta_steps(units, chunks, G, dk, dv, wide)) G = g;
   }
   if (G > chunks) G = chunks;
   if (G < 1) G = 1;
