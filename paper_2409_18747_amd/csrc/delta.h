@@ -244,6 +244,12 @@ struct PartTile {
   }
 };
 
+// Factors of rows are 2^75 at most: no sum of squares but 0 gives more (2^74.5), and 0 is what a row of zeros times any is; a value
+// times 1 / eps may leave fp32, and infinity times a zero row is not 0.  The product of two rows takes their factors one after the
+// other, for the same reason.  Gradients with respect to rows below eps are over eps itself.
+constexpr float LARGEST_FACTOR = 0x1p75f;
+inline float largest_factor(float eps) { return fminf(1.0f / eps, LARGEST_FACTOR); }
+inline float over_eps(float eps) { return fminf(1.0f / eps, 0x1.fffffep127f); }
 // 1 / max(norm, eps) of a row from its sum of squares, to a unit of fp32.
 __device__ __forceinline__ float row_factor(float sum_sq, float inv_eps) { return fminf(__builtin_amdgcn_rsqf(sum_sq), inv_eps); }
 

@@ -909,7 +909,7 @@ __global__ __launch_bounds__((DeltaGradCfg<T, DK, DV>::THREADS), (DeltaGradCfg<T
     const int* __restrict__ lengths, const ChunkRecord* __restrict__ records, const float* __restrict__ errors,
     const float* __restrict__ states, const float* __restrict__ zs, const float* __restrict__ dstates, T* __restrict__ dQ,
     T* __restrict__ dK, T* __restrict__ dV, float* __restrict__ dlog_decay, float* __restrict__ dbeta,
-    float* __restrict__ ds_parts, Divisor H, Divisor chunks, int N, float inv_eps, int from_state) {
+    float* __restrict__ ds_parts, Divisor H, Divisor chunks, int N, float inv_eps, float below_eps, int from_state) {
   using Cfg = DeltaGradCfg<T, DK, DV>;
   using KTile = typename Cfg::KTile;
   using GTile = typename Cfg::GTile;
@@ -1190,8 +1190,10 @@ __global__ __launch_bounds__((DeltaGradCfg<T, DK, DV>::THREADS), (DeltaGradCfg<T
       dq += qdot[n][i];
       dk += kdot[n][i];
     }
-    const float fq = rq[i], fk = rec.rk[i];
+    float fq = rq[i], fk = rec.rk[i];
     const float cq = fq == inv_eps ? 0.f : fq * (fq * dq), ck = fk == inv_eps ? 0.f : fk * (fk * dk);
+    fq = fq == inv_eps ? below_eps : fq;
+    fk = fk == inv_eps ? below_eps : fk;
     if (row0 + i < there) {
       const size_t at_ = size_t(row0 + i) * DK + 16 * kt0 + 4 * q4;
       const f32x4 q = KTile::row4(Qs, i, 16 * kt0 + 4 * q4), k = KTile::row4(Ks, i, 16 * kt0 + 4 * q4);
@@ -1255,7 +1257,7 @@ hipError_t run_rev(const DeltaArgs& a) {
     return launch_kernel("delta_rev_scan", kernel, a.G == 1 ? dim3(unsigned(units * parts)) : dim3(unsigned(units * a.G), unsigned(parts)),
                          dim3((AHEAD ? 192 : BESIDE ? 128 : 64) * NW), 0, a.stream, static_cast<const T*>(a.Q), static_cast<const T*>(a.K),
                          static_cast<const T*>(a.dO), a.s, a.seq_len, a.dstate, a.dstate_in, records, a.w_cols, a.zs, a.dstates,
-                         a.ends, Divisor(a.H), Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
+                         a.ends, Divisor(a.H), Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, largest_factor(a.eps));
   };
   if (a.G > 1) {
     hipError_t err;
@@ -1279,7 +1281,7 @@ hipError_t run_gradients(const DeltaArgs& a) {
                        static_cast<const T*>(a.dO), a.s, a.log_decay, a.beta, a.seq_len,
                        static_cast<const ChunkRecord*>(a.records), a.errors, a.states, a.zs,
                        a.dstates, static_cast<T*>(a.dQ), static_cast<T*>(a.dK), static_cast<T*>(a.dV), a.dlog_decay, a.dbeta,
-                       a.ds_parts, Divisor(a.H), Divisor(chunks), a.N, 1.0f / a.eps, int(a.state_in != nullptr));
+                       a.ds_parts, Divisor(a.H), Divisor(chunks), a.N, largest_factor(a.eps), over_eps(a.eps), int(a.state_in != nullptr));
 }
 
 template <typename T, int DK>

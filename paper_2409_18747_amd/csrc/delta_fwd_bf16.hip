@@ -292,19 +292,20 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
         for (int jt = 0; jt < 4; ++jt) KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf[jt]);
         mm_each<OUT>(kf, qf, t);
       }
-      const float rq_own = rq[own], in_tile = rq_own * rec.in_tile[own];
+      const float rq_own = rq[own], in_tile = rec.in_tile[own];
       f32x4 diagonal;
       {
         const double g_own = rec.decay[own];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           const int j = 16 * it + 4 * q4 + v;
-          diagonal[v] = j <= own ? rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
+          diagonal[v] = j <= own ? rec.rk[j] * decay_between(g_own, rec.decay[j]) : 0.f;
         }
       }
 #pragma unroll
       for (int jt = 0; jt < 4; ++jt) {
         const f32x4 below = four(rec.rk_to_tile + 16 * jt + 4 * q4) * (in_tile * rec.between[it][jt]);   // 0 from the diagonal on
+        t[jt] *= rq_own;
 #pragma unroll
         for (int v = 0; v < 4; ++v) t[jt][v] *= jt == it ? diagonal[v] : below[v];
       }
@@ -644,7 +645,7 @@ hipError_t run_scan(const DeltaArgs& a) {
     return launch_kernel("delta_fwd_scan", kernel, grid(n_parts), dim3(threads), 0, a.stream, static_cast<const T*>(a.Q),
                          static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len, a.state_in, static_cast<T*>(a.O), a.state,
                          records, a.w_rows, a.errors, a.states, a.starts, a.transitions, Divisor(a.H), Divisor(a.G), Divisor(n_parts),
-                         a.seg, a.N, units, a.dv, 1.0f / a.eps);
+                         a.seg, a.N, units, a.dv, largest_factor(a.eps));
   };
   if (a.G > 1) {
     // M is not asked for where the states at the starts of two segments are known without, and no backward follows
@@ -659,7 +660,7 @@ hipError_t run_scan(const DeltaArgs& a) {
     return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW, LEVEL>, grid(parts), dim3(64 * NW), 0, a.stream,
                          static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len,
                          a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows, a.errors, a.states, a.starts, Divisor(a.H),
-                         Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, 1.0f / a.eps);
+                         Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, largest_factor(a.eps));
   }
 }
 

@@ -217,7 +217,7 @@ hipError_t DELTA_SYM(delta_prepare)(const DeltaArgs& a) {
   const auto run = [&](auto kernel) {
     return launch_kernel("delta_prepare", kernel, dim3(unsigned(a.B * a.H * chunks)), dim3(256), 0, a.stream,
                          static_cast<const T*>(a.K), a.log_decay, a.beta, a.seq_len, static_cast<ChunkRecord*>(a.records), a.w_rows,
-                         a.w_cols, Divisor(a.H), Divisor(chunks), a.N, 1.0f / a.eps);
+                         a.w_cols, Divisor(a.H), Divisor(chunks), a.N, largest_factor(a.eps));
   };
   return a.dk == 32 ? run(delta_prepare<T, 32>) : a.dk == 64 ? run(delta_prepare<T, 64>) : run(delta_prepare<T, 128>);
 }

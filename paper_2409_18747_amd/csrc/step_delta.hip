@@ -58,8 +58,9 @@ __global__ __launch_bounds__(256) void step_delta_kernel(
   const float scale = s[head], b1 = beta[unit];
   float times, plus;
   state_factor(log_decay != nullptr ? log2_decay(log_decay[unit]) : 0.0, times, plus);
-  const float rq = inv_norm(group_sum<64>(__builtin_fmaf(q0, q0, q1 * q1)), eps);
-  const float rk = inv_norm(group_sum<64>(__builtin_fmaf(k0, k0, k1 * k1)), eps);
+  // (bounded for zero rows, whose 1 / eps may be infinite: delta.h)
+  const float rq = fminf(inv_norm(group_sum<64>(__builtin_fmaf(q0, q0, q1 * q1)), eps), LARGEST_FACTOR);
+  const float rk = fminf(inv_norm(group_sum<64>(__builtin_fmaf(k0, k0, k1 * k1)), eps), LARGEST_FACTOR);
   q0 *= rq; q1 *= rq; k0 *= rk; k1 *= rk;
   const float qk = group_sum<64>(__builtin_fmaf(q0, k0, q1 * k1));
   if (w == 0) {
