@@ -375,7 +375,7 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  * Forward.  seq_len, s, N = 0 and the state as in cottn_fwd_causal_decay; rows and gates at or beyond a sequence's end are not
  * read.  state may be state_in (in place), else the two must not overlap (COTTN_E_ARG).  With a workspace of
  * COTTN_OP_FWD_DELTA's size or more the call leaves there what a backward takes over; COTTN_OP_FWD_DELTA_ALONE's is enough
- * without one, and then a 16-bit call without state is the faster one.
+ * without one.  The results are the same, with and without `state`.
  * Backward, of the same call: gradients with respect to the raw Q, K, V, to s (float[H], with seq_len float[B][H]), to
  * log_decay and to beta (float[B][H][N], zeros at or beyond a sequence's end; dlog_decay may be NULL, and must be where log_decay
  * is; it is 0 where log_decay is above 0 or below -128, else a sum of the rows' <o, dO> and <v, dV> from t on, to fp32

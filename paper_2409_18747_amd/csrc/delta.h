@@ -14,10 +14,11 @@
 // contractions, at most 1 in magnitude for 0 <= b <= 2.  Every decay that is formed has an exponent that is not positive.
 //
 // Precision.  Products take bfloat16 parts of their operands, each part the rest that rounding the ones before left over:
-// bfloat16 rows are one part, fp16 rows two and fp32 rows three, exactly; what is computed takes as many parts as its results
-// need.  Of the products of parts those i + j < LEVEL are formed: LEVEL 3 leaves out less than 2^-24 of a product, LEVEL 2 less
-// than 2^-15.  States, the error rows and gradients of gates are fp32 results and take 3; results in 16 bits alone take 2, so
-// that an element has met one rounding that counts, its own.
+// bfloat16 rows are one part, fp16 rows two and fp32 rows three, exactly; what is computed takes three, and of the products of
+// parts those i + j < LEVEL are formed: LEVEL 3 leaves out less than 2^-24 of a product, LEVEL 2 less than 2^-15.  All takes 3 but
+// for the last products of a forward in 16 bits, of rows with the state and of P with U, whose operands are in two parts (H, P and
+// U): nothing goes on from there, and an element has met one rounding that counts, its own (bf16 2^-8, fp16 2^-11).  Three parts
+// would be 26 KB of LDS more at dk = 128, which fp16 rows leave no room for.
 //
 // Included behind device_common.h.
 #pragma once
@@ -34,7 +35,7 @@ template <typename T> struct Rows;
 template <> struct Rows<__bf16> { static constexpr int PARTS = 1; };
 template <> struct Rows<_Float16> { static constexpr int PARTS = 2; };
 template <> struct Rows<float> { static constexpr int PARTS = 3; };
-// parts of operands that only enter results of the rows' type
+// parts of operands that only enter a forward's results in the rows' type
 template <typename T> constexpr int RESULT_LEVEL = sizeof(T) == 4 ? 3 : 2;
 
 // Four values as N parts, two to a word.

@@ -19,9 +19,9 @@
 namespace cottn {
 namespace {
 
-template <typename T, int DK, int NW, int LEVEL>
+template <typename T, int DK, int NW>
 struct DeltaFwdCfg {
-  static constexpr int IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW, KS = DK / 32;
+  static constexpr int LEVEL = 3, IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW, KS = DK / 32;
   using KTile = PartTile<CHUNK, DK, IN>;
   using VTile = PartTile<CHUNK, VC, IN>;
   static constexpr int W_SIZE = W_FRAGS * LEVEL * 512, P_SIZE = W_FRAGS * OUT * 512, S_SIZE = NW * KS * OUT * 512, U_SIZE = NW * 2 * OUT * 512;
@@ -37,19 +37,18 @@ struct DeltaFwdCfg {
 // unit columns without values were its state; delta_carry makes of those the states at the starts, from which the segments are
 // walked again.  Where the state is to replace state_in, which the last segment may do before the first one is walked again,
 // the walk for the totals puts state_in by.
-template <typename T, int DK, int NW, int LEVEL, bool TOTALS>
+template <typename T, int DK, int NW, bool TOTALS>
 __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2 : 3) void delta_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
     float* __restrict__ states, float* starts, float* __restrict__ transitions, Divisor H, Divisor G, Divisor parts, int seg, int N,
     int units, int DV, float inv_eps) {
-  using Cfg = DeltaFwdCfg<T, DK, NW, LEVEL>;
+  using Cfg = DeltaFwdCfg<T, DK, NW>;
   using KTile = typename Cfg::KTile;
   using VTile = typename Cfg::VTile;
-  constexpr int IN = Cfg::IN, OUT = Cfg::OUT, KS = Cfg::KS, NT = 64 * NW, VC = Cfg::VC;
+  constexpr int LEVEL = Cfg::LEVEL, IN = Cfg::IN, OUT = Cfg::OUT, KS = Cfg::KS, NT = 64 * NW, VC = Cfg::VC;
   typedef __attribute__((ext_vector_type(4))) T vec4;
-  static_assert(!TOTALS || LEVEL == 3, "states");
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Vs[Cfg::V_IN_LDS ? VTile::SIZE : 8];
@@ -234,11 +233,9 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
       if constexpr (!TOTALS) qt.fetch(Qu + size_t(row0) * DK, there - row0);
       if (Cfg::V_IN_LDS && !unit_columns) vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
 #pragma unroll
-      for (int i = 0; i < W_PIECES; ++i) {   // [fragment][part][lane]: the first LEVEL of three parts
-        const int piece = i * NT + tid;
-        if (W_FRAGS * LEVEL * 64 % NT == 0 || piece < W_FRAGS * LEVEL * 64)
-          w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
-      }
+      for (int i = 0; i < W_PIECES; ++i)
+        if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
+          w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[i * NT + tid];
       kt.fetch(Ku + size_t(row0) * DK, there - row0);
     };
     const auto commit = [&]() {   // all but K
@@ -360,9 +357,9 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
 
 // The same by waves that do all of it, for rows of 128 in fp32, whose three parts leave the LDS no room for what one half of the
 // waves hands the other.
-template <typename T, int DK, int NW, int LEVEL>
+template <typename T, int DK, int NW>
 struct DeltaWideFwdCfg {
-  static constexpr int IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW;
+  static constexpr int LEVEL = 3, IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW;
   static constexpr bool V_IN_LDS = sizeof(T) == 2;
   using KTile = PartTile<CHUNK, DK, IN>;
   using VTile = PartTile<CHUNK, VC, IN>;
@@ -372,17 +369,17 @@ struct DeltaWideFwdCfg {
   static constexpr int WAVES = (AT_ONCE < MOST ? AT_ONCE : MOST) * (NW <= 4 ? 1 : 2);   // to a SIMD
 };
 
-template <typename T, int DK, int NW, int LEVEL>
-__global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)) void delta_wide_fwd_scan(
+template <typename T, int DK, int NW>
+__global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void delta_wide_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
     float* __restrict__ states, const float* __restrict__ starts, Divisor H, Divisor G, Divisor parts, int seg, int N, int units,
     int DV, float inv_eps) {
-  using Cfg = DeltaWideFwdCfg<T, DK, NW, LEVEL>;
+  using Cfg = DeltaWideFwdCfg<T, DK, NW>;
   using KTile = typename Cfg::KTile;
   using VTile = typename Cfg::VTile;
-  constexpr int IN = Cfg::IN, OUT = Cfg::OUT, KS = DK / 32, NT = 64 * NW, VC = Cfg::VC;
+  constexpr int LEVEL = Cfg::LEVEL, IN = Cfg::IN, OUT = Cfg::OUT, KS = DK / 32, NT = 64 * NW, VC = Cfg::VC;
   constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
   typedef __attribute__((ext_vector_type(4))) T vec4;
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
@@ -446,11 +443,9 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
     for (int i = 0; i < REC_PIECES; ++i)
       if (i * NT + tid < RECORD_PIECES) rec_next[i] = reinterpret_cast<const u32x4*>(records + at)[i * NT + tid];
 #pragma unroll
-    for (int i = 0; i < W_PIECES; ++i) {   // [fragment][part][lane]: the first LEVEL of three parts
-      const int piece = i * NT + tid;
-      if (W_FRAGS * LEVEL * 64 % NT == 0 || piece < W_FRAGS * LEVEL * 64)
-        w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[piece / (LEVEL * 64) * 192 + piece % (LEVEL * 64)];
-    }
+    for (int i = 0; i < W_PIECES; ++i)
+      if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64)
+        w_next[i] = reinterpret_cast<const u32x4*>(w_rows + at * W_ELEMS)[i * NT + tid];
   };
   if (steps > first) fetch(first);
   for (int c = first; c < steps; ++c) {
@@ -636,7 +631,7 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW, LEVEL>::WAVES)
     *reinterpret_cast<vec4*>(Ou + size_t(lo + i / (VC / 4)) * DV + i % (VC / 4) * 4) = vec4{T(0.f), T(0.f), T(0.f), T(0.f)};
 }
 
-template <typename T, int DK, int NW, int LEVEL>
+template <typename T, int DK, int NW>
 hipError_t run_scan(const DeltaArgs& a) {
   const int units = a.B * a.H, parts = a.dv / (16 * NW);
   const ChunkRecord* records = static_cast<const ChunkRecord*>(a.records);
@@ -650,29 +645,23 @@ hipError_t run_scan(const DeltaArgs& a) {
   if (a.G > 1) {
     // M is not asked for where the states at the starts of two segments are known without, and no backward follows
     const int with_M = a.G > 2 || a.errors != nullptr ? (DK + 16 * NW - 1) / (16 * NW) : 0;
-    hipError_t err = run(delta_fwd_scan<T, DK, NW, 3, true>, parts + with_M, 128 * NW);
+    hipError_t err = run(delta_fwd_scan<T, DK, NW, true>, parts + with_M, 128 * NW);
     if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, false);
     if (err != hipSuccess) return err;
   }
-  if constexpr (DeltaFwdCfg<T, DK, NW, LEVEL>::FITS) {
-    return run(delta_fwd_scan<T, DK, NW, LEVEL, false>, parts, 192 * NW);
+  if constexpr (DeltaFwdCfg<T, DK, NW>::FITS) {
+    return run(delta_fwd_scan<T, DK, NW, false>, parts, 192 * NW);
   } else {
-    return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW, LEVEL>, grid(parts), dim3(64 * NW), 0, a.stream,
+    return launch_kernel("delta_fwd_scan", delta_wide_fwd_scan<T, DK, NW>, grid(parts), dim3(64 * NW), 0, a.stream,
                          static_cast<const T*>(a.Q), static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.s, a.seq_len,
                          a.state_in, static_cast<T*>(a.O), a.state, records, a.w_rows, a.errors, a.states, a.starts, Divisor(a.H),
                          Divisor(a.G), Divisor(parts), a.seg, a.N, units, a.dv, largest_factor(a.eps));
   }
 }
 
-template <typename T, int DK, int LEVEL>
-hipError_t run_level(const DeltaArgs& a) {
-  return a.dv == 32 ? run_scan<T, DK, 2, LEVEL>(a) : run_scan<T, DK, 4, LEVEL>(a);
-}
 template <typename T, int DK>
 hipError_t run_shape(const DeltaArgs& a) {
-  // without fp32 results two parts do (32 x 16 heads of 512 rows at 128 x 128 142 -> 118 us)
-  if (sizeof(T) == 2 && a.state == nullptr && a.errors == nullptr) return run_level<T, DK, RESULT_LEVEL<T>>(a);
-  return run_level<T, DK, 3>(a);
+  return a.dv == 32 ? run_scan<T, DK, 2>(a) : run_scan<T, DK, 4>(a);
 }
 
 }  // namespace
