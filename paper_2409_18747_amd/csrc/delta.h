@@ -251,8 +251,13 @@ struct PartTile {
 constexpr float LARGEST_FACTOR = 0x1p75f;
 inline float largest_factor(float eps) { return fminf(1.0f / eps, LARGEST_FACTOR); }
 inline float over_eps(float eps) { return fminf(1.0f / eps, 0x1.fffffep127f); }
-// 1 / max(norm, eps) of a row from its sum of squares, to a unit of fp32.
-__device__ __forceinline__ float row_factor(float sum_sq, float inv_eps) { return fminf(__builtin_amdgcn_rsqf(sum_sq), inv_eps); }
+// 1 / max(norm, eps) of a row from its sum of squares, to a unit of fp32: the reciprocal square root instruction, which takes what is
+// below the normal numbers for 0.
+__device__ __forceinline__ float row_factor(float sum_sq, float inv_eps) {
+  const bool tiny = sum_sq < 0x1p-126f;
+  const float y = __builtin_amdgcn_rsqf(tiny ? 0x1p64f * sum_sq : sum_sq);
+  return fminf(tiny ? 0x1p32f * y : y, inv_eps);
+}
 
 // 64 rows of D elements on their way from memory to LDS: D / 8 neighbouring lanes share a row.
 template <typename T, int D, int PAD = 16, int THREADS = 256>
