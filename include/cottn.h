@@ -410,7 +410,7 @@ int cottn_step_delta(const void* q, const void* k, const void* v, const float* s
  *   Q, K, Qr, Kr [B][H][N][d], K and Kr both NULL for Q alone; Qr may be Q and Kr may be K (in place), else no output overlaps
  *   an input or the other output (COTTN_E_ARG).  For single tokens N is 1.
  *   positions: int[B][N][axes], any values; freq: float[pairs], radians to a position; axis: int[pairs], the axis (time, row,
- *   column, ...) that a pair is turned by, NULL for 0; a pair whose axis is none of 0 .. axes - 1 is not turned.
+ *   column, ...) that a pair is turned by, NULL for 0; a pair whose axis is none of 0 .. axes - 1 is copied.
  *   pairs: 1 .. d / 2; d one of 32, 64, 128; axes >= 1.  With v = the elements of 16 bytes where pairs is a multiple of that
  *   and N d at least 128 of it, else 1, B (N + t - 1) / t is below 16 777 216 for t = 512 v / d; more is refused (COTTN_E_SHAPE).
  *   inverse: turned by - phi, which is the gradient of the call without.

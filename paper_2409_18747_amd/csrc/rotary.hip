@@ -29,10 +29,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* Q, const T* K, con
   const bool turns = lane < turning;
   const int first = NEIGHBOURS || !turns ? 2 * VEC * lane : VEC * lane, second = NEIGHBOURS || !turns ? first + VEC : first + pairs;
   float c[VEC], s[VEC];
+  bool turned[VEC];   // (a pair of an axis that there is not stays as it is, whatever its features are: no 0 times infinity)
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
     c[i] = 1.f;
     s[i] = 0.f;
+    turned[i] = false;
     if (turns) {
       const int p = VEC * lane + i;
       const int ax = axis != nullptr ? axis[p] : 0;
@@ -42,6 +44,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* Q, const T* K, con
         sincospif(2.f * float(turn - rint(turn)), &si, &co);
         c[i] = co;
         s[i] = sign * si;
+        turned[i] = true;
       }
     }
   }
@@ -62,8 +65,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* Q, const T* K, con
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             const float u = float(z[2 * i]), v = float(z[2 * i + 1]);
-            z[2 * i] = T(__builtin_fmaf(u, c[i], -(v * s[i])));
-            z[2 * i + 1] = T(__builtin_fmaf(v, c[i], u * s[i]));
+            z[2 * i] = turned[i] ? T(__builtin_fmaf(u, c[i], -(v * s[i]))) : z[2 * i];
+            z[2 * i + 1] = turned[i] ? T(__builtin_fmaf(v, c[i], u * s[i])) : z[2 * i + 1];
           }
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
@@ -74,8 +77,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* Q, const T* K, con
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             const float u = float(x.x[i]), v = float(y.x[i]);
-            x.x[i] = T(__builtin_fmaf(u, c[i], -(v * s[i])));
-            y.x[i] = T(__builtin_fmaf(v, c[i], u * s[i]));
+            x.x[i] = turned[i] ? T(__builtin_fmaf(u, c[i], -(v * s[i]))) : x.x[i];
+            y.x[i] = turned[i] ? T(__builtin_fmaf(v, c[i], u * s[i])) : y.x[i];
           }
         }
       }
