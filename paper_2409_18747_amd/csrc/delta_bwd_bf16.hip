@@ -627,17 +627,15 @@ __global__ __launch_bounds__(128 * NW, NW <= 2 ? 1 : 2) void delta_rev_scan(
 // The same by waves that do all of it, where the LDS has no room for what one half of the waves hands the other: fp32 at dk = 128.
 template <typename T, int DK, int NW>
 struct DeltaWideRevCfg {
-  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, PAD = sizeof(T) == 4 && DK == 128 ? 8 : 16;
+  static_assert(sizeof(T) == 4 && DK == 128 && NW == 2, "the rows that the other scans have no room for");
+  static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, PAD = 8;
   using KTile = PartTile<CHUNK, DK, IN, PAD>;
   using GTile = PartTile<CHUNK, VC, IN, PAD>;      // rows of dO
   static constexpr int W_SIZE = W_FRAGS * LEVEL * 512;
-  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + GTile::SIZE + 2 * W_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK;
-  static constexpr int AT_ONCE = (160 * 1024) / LDS_BYTES, MOST = NW <= 4 ? 2 : 1;
-  static constexpr int WAVES = (AT_ONCE < MOST ? AT_ONCE : MOST) * (NW <= 4 ? 1 : 2);   // to a SIMD
 };
 
 template <typename T, int DK, int NW, bool TOTALS>
-__global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void delta_wide_rev_scan(
+__global__ __launch_bounds__(64 * NW, 1) void delta_wide_rev_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ dO, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* dstate, float* dstate_in, const ChunkRecord* __restrict__ records,
     const uint16_t* __restrict__ w_cols, float* __restrict__ zs, float* __restrict__ dstates, float* ends, Divisor H, Divisor G,
@@ -731,48 +729,46 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideRevCfg<T, DK, NW>::WAVES)) void 
     }
 
     // s P, a tile of columns to a wave (two where there are two waves), queries down: an operand as it stands
-    if (NW <= 4 || w < 4) {
 #pragma unroll
-      for (int turn = 0; turn < (NW >= 4 ? 1 : 4 / NW); ++turn) {
-        const int jt = turn == 0 ? w : 3 - w, own = 16 * jt + r;
-        bf16x8 kf[KS][IN];
+    for (int turn = 0; turn < 4 / NW; ++turn) {
+      const int jt = turn == 0 ? w : 3 - w, own = 16 * jt + r;
+      bf16x8 kf[KS][IN];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf[ks]);
+      for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Ks, own, 32 * ks + 8 * q4, kf[ks]);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          if (!w_col_there(jt, p)) continue;
-          f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      for (int p = 0; p < 2; ++p) {
+        if (!w_col_there(jt, p)) continue;
+        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int it = 2 * p + h;
-            if (it < jt) continue;
-            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+          const int it = 2 * p + h;
+          if (it < jt) continue;
+          f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-              bf16x8 qf[IN];
-              KTile::row_frag(Qs, 16 * it + r, 32 * ks + 8 * q4, qf);
-              t = mm<LEVEL>(qf, kf[ks], t);
-            }
-            t *= *reinterpret_cast<const f32x4*>(rq + 16 * it + 4 * q4);
-            if (it > jt) {
-              half[h] = t * (*reinterpret_cast<const f32x4*>(rec.in_tile + 16 * it + 4 * q4) *
-                             (scale * rec.rk_to_tile[own] * rec.between[it][jt]));
-            } else {
-              const double g_own = rec.decay[own];
-              const float rk_own = scale * rec.rk[own];
+          for (int ks = 0; ks < KS; ++ks) {
+            bf16x8 qf[IN];
+            KTile::row_frag(Qs, 16 * it + r, 32 * ks + 8 * q4, qf);
+            t = mm<LEVEL>(qf, kf[ks], t);
+          }
+          t *= *reinterpret_cast<const f32x4*>(rq + 16 * it + 4 * q4);
+          if (it > jt) {
+            half[h] = t * (*reinterpret_cast<const f32x4*>(rec.in_tile + 16 * it + 4 * q4) *
+                           (scale * rec.rk_to_tile[own] * rec.between[it][jt]));
+          } else {
+            const double g_own = rec.decay[own];
+            const float rk_own = scale * rec.rk[own];
 #pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const int i = 16 * it + 4 * q4 + v;
-                half[h][v] = i >= own ? t[v] * (rk_own * decay_between(rec.decay[i], g_own)) : 0.f;
-              }
+            for (int v = 0; v < 4; ++v) {
+              const int i = 16 * it + 4 * q4 + v;
+              half[h][v] = i >= own ? t[v] * (rk_own * decay_between(rec.decay[i], g_own)) : 0.f;
             }
           }
-          bf16x8 pf[LEVEL];
-          split8<LEVEL>(half[0], half[1], pf);
-#pragma unroll
-          for (int i = 0; i < LEVEL; ++i)
-            reinterpret_cast<u32x4*>(Ps)[(w_col_frag(jt, p) * LEVEL + i) * 64 + l] = __builtin_bit_cast(u32x4, pf[i]);
         }
+        bf16x8 pf[LEVEL];
+        split8<LEVEL>(half[0], half[1], pf);
+#pragma unroll
+        for (int i = 0; i < LEVEL; ++i)
+          reinterpret_cast<u32x4*>(Ps)[(w_col_frag(jt, p) * LEVEL + i) * 64 + l] = __builtin_bit_cast(u32x4, pf[i]);
       }
     }
 

@@ -356,21 +356,17 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
 }
 
 // The same by waves that do all of it, for rows of 128 in fp32, whose three parts leave the LDS no room for what one half of the
-// waves hands the other.
+// waves hands the other, nor for rows of V.
 template <typename T, int DK, int NW>
 struct DeltaWideFwdCfg {
+  static_assert(sizeof(T) == 4 && DK == 128 && (NW == 2 || NW == 4), "the rows that the other scan has no room for");
   static constexpr int LEVEL = 3, IN = Rows<T>::PARTS, OUT = RESULT_LEVEL<T>, VC = 16 * NW;
-  static constexpr bool V_IN_LDS = sizeof(T) == 2;
   using KTile = PartTile<CHUNK, DK, IN>;
-  using VTile = PartTile<CHUNK, VC, IN>;
   static constexpr int W_SIZE = W_FRAGS * LEVEL * 512, P_SIZE = W_FRAGS * OUT * 512;
-  static constexpr int LDS_BYTES = 2 * (2 * KTile::SIZE + (V_IN_LDS ? VTile::SIZE : 0) + W_SIZE + P_SIZE) + int(sizeof(ChunkRecord)) + 4 * CHUNK;
-  static constexpr int AT_ONCE = (160 * 1024) / LDS_BYTES, MOST = NW <= 4 ? 2 : 1;
-  static constexpr int WAVES = (AT_ONCE < MOST ? AT_ONCE : MOST) * (NW <= 4 ? 1 : 2);   // to a SIMD
 };
 
 template <typename T, int DK, int NW>
-__global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void delta_wide_fwd_scan(
+__global__ __launch_bounds__(64 * NW, 1) void delta_wide_fwd_scan(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const float* __restrict__ s,
     const int* __restrict__ lengths, const float* state_in, T* __restrict__ O, float* state_out,
     const ChunkRecord* __restrict__ records, const uint16_t* __restrict__ w_rows, float* __restrict__ errors,
@@ -378,13 +374,11 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void 
     int DV, float inv_eps) {
   using Cfg = DeltaWideFwdCfg<T, DK, NW>;
   using KTile = typename Cfg::KTile;
-  using VTile = typename Cfg::VTile;
   constexpr int LEVEL = Cfg::LEVEL, IN = Cfg::IN, OUT = Cfg::OUT, KS = DK / 32, NT = 64 * NW, VC = Cfg::VC;
   constexpr int W_PIECES = (W_FRAGS * LEVEL * 64 + NT - 1) / NT, REC_PIECES = (RECORD_PIECES + NT - 1) / NT;
   typedef __attribute__((ext_vector_type(4))) T vec4;
   __shared__ __attribute__((aligned(16))) uint16_t Ks[KTile::SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Qs[KTile::SIZE];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[Cfg::V_IN_LDS ? VTile::SIZE : 8];
   __shared__ __attribute__((aligned(16))) uint16_t Ws[Cfg::W_SIZE];
   __shared__ __attribute__((aligned(16))) uint16_t Ps[Cfg::P_SIZE];
   __shared__ ChunkRecord rec;
@@ -419,25 +413,20 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void 
       S[t][v] = from != nullptr && (g == 0 || first < all) ? (from + key_of(t / 2, t % 2, 0, v) * DV)[at_key] : 0.f;
 
   RowTile<T, DK, 16, NT> kt, qt;
-  RowTile<T, VC, 16, NT> vt;
-  T vraw[4][4];
+  f32x4 vraw[4];
   u32x4 rec_next[REC_PIECES], w_next[W_PIECES];
   const auto fetch = [&](int c) {
     const int row0 = c * CHUNK;
     kt.fetch(Ku + size_t(row0) * DK, there - row0);
     qt.fetch(Qu + size_t(row0) * DK, there - row0);
-    if constexpr (Cfg::V_IN_LDS) {
-      vt.fetch(Vu + size_t(row0) * DV, there - row0, DV);
-    } else {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int row = 16 * t + 4 * q4 + v;
-          vraw[t][v] = T(0.f);
-          if (row0 + row < there) vraw[t][v] = (Vu + (size_t(row0) + 16 * t + v) * DV)[unsigned(4 * q4 * DV + 16 * w + r)];
-        }
-    }
+      for (int v = 0; v < 4; ++v) {
+        const int row = 16 * t + 4 * q4 + v;
+        vraw[t][v] = 0.f;
+        if (row0 + row < there) vraw[t][v] = (Vu + (size_t(row0) + 16 * t + v) * DV)[unsigned(4 * q4 * DV + 16 * w + r)];
+      }
     const size_t at = size_t(unit) * chunks + c;
 #pragma unroll
     for (int i = 0; i < REC_PIECES; ++i)
@@ -453,7 +442,6 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void 
     kt.commit(Ks);
     qt.commit(Qs);
     qt.store_factors(rq, inv_eps);
-    if constexpr (Cfg::V_IN_LDS) vt.commit(Vs);
 #pragma unroll
     for (int i = 0; i < REC_PIECES; ++i)
       if (i * NT + tid < RECORD_PIECES) reinterpret_cast<u32x4*>(&rec)[i * NT + tid] = rec_next[i];
@@ -461,10 +449,8 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void 
     for (int i = 0; i < W_PIECES; ++i)
       if (W_FRAGS * LEVEL * 64 % NT == 0 || i * NT + tid < W_FRAGS * LEVEL * 64) reinterpret_cast<u32x4*>(Ws)[i * NT + tid] = w_next[i];
     f32x4 y[4];
-    if constexpr (!Cfg::V_IN_LDS) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) y[t] = f32x4{float(vraw[t][0]), float(vraw[t][1]), float(vraw[t][2]), float(vraw[t][3])};
-    }
+    for (int t = 0; t < 4; ++t) y[t] = vraw[t];
     __syncthreads();
     if (c + 1 < steps) fetch(c + 1);
     if (states != nullptr) {
@@ -497,7 +483,6 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void 
     bf16x8 yf[2][LEVEL];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      if constexpr (Cfg::V_IN_LDS) y[t] = VTile::col4(Vs, 16 * t + 4 * q4, 16 * w, r);
       const f32x4 since = *reinterpret_cast<const f32x4*>(rec.rk_since + 16 * t + 4 * q4);
 #pragma unroll
       for (int v = 0; v < 4; ++v) y[t][v] = __builtin_fmaf(-since[v], kh[t][v], y[t][v]);
@@ -507,47 +492,45 @@ __global__ __launch_bounds__(64 * NW, (DeltaWideFwdCfg<T, DK, NW>::WAVES)) void 
 
     __builtin_amdgcn_sched_barrier(0);
     // P, a tile of rows to a wave (two where there are two waves), keys down: an operand as it stands
-    if (NW <= 4 || w < 4) {
 #pragma unroll
-      for (int turn = 0; turn < (NW >= 4 ? 1 : 4 / NW); ++turn) {
-        const int it = turn == 0 ? w : 3 - w, own = 16 * it + r;
-        const float rq_own = rq[own];
-        bf16x8 qf[KS][IN];
+    for (int turn = 0; turn < 4 / NW; ++turn) {
+      const int it = turn == 0 ? w : 3 - w, own = 16 * it + r;
+      const float rq_own = rq[own];
+      bf16x8 qf[KS][IN];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Qs, own, 32 * ks + 8 * q4, qf[ks]);
+      for (int ks = 0; ks < KS; ++ks) KTile::row_frag(Qs, own, 32 * ks + 8 * q4, qf[ks]);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          if (!w_row_there(it, p)) break;
-          f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      for (int p = 0; p < 2; ++p) {
+        if (!w_row_there(it, p)) break;
+        f32x4 half[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int jt = 2 * p + h;
-            if (jt > it) break;
-            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+          const int jt = 2 * p + h;
+          if (jt > it) break;
+          f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-              bf16x8 kf[IN];
-              KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf);
-              t = mm<OUT>(kf, qf[ks], t);
-            }
-            if (jt < it) {
-              half[h] = t * *reinterpret_cast<const f32x4*>(rec.rk_to_tile + 16 * jt + 4 * q4) *
-                        (rq_own * rec.in_tile[own] * rec.between[it][jt]);
-            } else {
-              const double g_own = rec.decay[own];
+          for (int ks = 0; ks < KS; ++ks) {
+            bf16x8 kf[IN];
+            KTile::row_frag(Ks, 16 * jt + r, 32 * ks + 8 * q4, kf);
+            t = mm<OUT>(kf, qf[ks], t);
+          }
+          if (jt < it) {
+            half[h] = t * *reinterpret_cast<const f32x4*>(rec.rk_to_tile + 16 * jt + 4 * q4) *
+                      (rq_own * rec.in_tile[own] * rec.between[it][jt]);
+          } else {
+            const double g_own = rec.decay[own];
 #pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const int j = 16 * jt + 4 * q4 + v;
-                half[h][v] = j <= own ? t[v] * rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
-              }
+            for (int v = 0; v < 4; ++v) {
+              const int j = 16 * jt + 4 * q4 + v;
+              half[h][v] = j <= own ? t[v] * rec.rk[j] * (rq_own * decay_between(g_own, rec.decay[j])) : 0.f;
             }
           }
-          bf16x8 pf[OUT];
-          split8<OUT>(half[0], half[1], pf);
-#pragma unroll
-          for (int i = 0; i < OUT; ++i)
-            reinterpret_cast<u32x4*>(Ps)[(w_row_frag(it, p) * OUT + i) * 64 + l] = __builtin_bit_cast(u32x4, pf[i]);
         }
+        bf16x8 pf[OUT];
+        split8<OUT>(half[0], half[1], pf);
+#pragma unroll
+        for (int i = 0; i < OUT; ++i)
+          reinterpret_cast<u32x4*>(Ps)[(w_row_frag(it, p) * OUT + i) * 64 + l] = __builtin_bit_cast(u32x4, pf[i]);
       }
     }
 
