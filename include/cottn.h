@@ -369,7 +369,8 @@ int cottn_tree_accept(const void* k, const void* v, const float* log_decay, cons
  * dtypes; states, ds, dlog_decay and dbeta are accurate to fp32 whatever the dtype (operands enter them in bfloat16 parts).
  * Workspaces: cottn_workspace_bytes_dkdv with the COTTN_OP_*_DELTA* operations, chunk 0; always needed.
  * A value that is not finite, in a row, a gate or a state, can make results of its sequence and head not finite, those of
- * earlier rows of its chunk among them.  B H (N + 63) / 64 and B H dv / 16 are below 8 388 608; more is refused
+ * earlier rows of its chunk among them, as can an fp32 element or state beyond bfloat16's largest number (3.39e38) or a row of Q or
+ * K longer than 1.8e19.  B H (N + 63) / 64 and B H dv / 16 are below 8 388 608; more is refused
  * (COTTN_E_SHAPE).
  *
  * Forward.  seq_len, s, N = 0 and the state as in cottn_fwd_causal_decay; rows and gates at or beyond a sequence's end are not

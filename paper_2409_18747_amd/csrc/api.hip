@@ -382,7 +382,9 @@ struct DeltaSpace {
 // 64 x 64, forward and backward: 3240 us in one segment, 890 in the 16 that it takes.  Over 16 shapes its split was the fastest of those
 // tried or within 15 % of it.)
 // Rows of 128 in fp32 (`wide`): 32 columns to a workgroup in the backward, and steps of 11 us, not 3, to which launches and the
-// chain of segments count less (8 heads of 4096 rows: 1508 us in one segment, 489 in 13, 434 in the 8 that it takes).
+// chain of segments count less (8 heads of 4096 rows: 1508 us in one segment, 489 in 13, 444 in the 8 that it takes).
+// A backward goes by the same split, since it takes over the forward's states, though its walk for the totals has one workgroup to a
+// compute unit.
 double delta_steps(long units, long chunks, long G, int dk, int dv, bool wide) {
   const long per = dv == 32 || wide ? 32 : 64, parts = dv / per, seg = (chunks + G - 1) / G;
   const auto rounds = [](long workgroups, long at_once) { return double((workgroups + at_once - 1) / at_once); };

@@ -12,7 +12,8 @@ namespace {
 // F - W^T (b F), and D in front of the chunk, one after the other.  What does not depend on D, P^T dO' and R = (G Qh)^T dO', is
 // formed beside that, a chunk ahead, by as many waves more; and again as many fetch the rows.  8 x 12 heads of 1024 rows at 64 x 64
 // take 55 us, formed for the same chunk and by the waves that fetch 66.  What bounds it is, as there, the chain: steps of 7500
-// cycles in which vector instructions issue in 49 % of them, matrix instructions in 27.
+// cycles in which vector instructions issue in 49 % of them, matrix instructions in 27.  (Twelve waves have 168 registers each; one to
+// three of a lane are spilled.)
 template <typename T, int DK, int NW>
 struct DeltaAheadCfg {
   static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, VC = 16 * NW, KS = DK / 32;
@@ -880,7 +881,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_wide_rev_scan(
 // a token in a lane.  16 heads of 32768 rows at 64 x 64 take 306 us: HBM moves 621 MB (2.0 TB/s), the LDS 43 % of the time (39 % of
 // that lanes that want the same bank), vector instructions issue in 39 %: phases with barriers between them, two workgroups to a
 // compute unit.  Where the LDS holds but one, eight waves share it: 8 x 12 heads of 1024 rows at 128 x 128 177 -> 165 us, 32 heads
-// in fp32 72 -> 64; two workgroups of eight waves have 128 registers, too few (64 x 64: 60 -> 68).
+// in fp32 72 -> 64; two workgroups of eight waves have 128 registers, too few (64 x 64: 60 -> 68).  (bf16 at 128 x 64 spills eight
+// of 256.)
 template <typename T, int DK, int DV>
 struct DeltaGradCfg {
   static constexpr int IN = Rows<T>::PARTS, LEVEL = 3, PAD = 8;

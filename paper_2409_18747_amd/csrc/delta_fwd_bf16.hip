@@ -356,7 +356,7 @@ __global__ __launch_bounds__((TOTALS ? 128 : 192) * NW, NW <= 2 ? 1 : TOTALS ? 2
 }
 
 // The same by waves that do all of it, for rows of 128 in fp32, whose three parts leave the LDS no room for what one half of the
-// waves hands the other, nor for rows of V.
+// waves hands the other, nor for rows of V.  (Two waves, dv = 32, take 512 registers and spill 33 of a lane.)
 template <typename T, int DK, int NW>
 struct DeltaWideFwdCfg {
   static_assert(sizeof(T) == 4 && DK == 128 && (NW == 2 || NW == 4), "the rows that the other scan has no room for");
@@ -626,7 +626,8 @@ hipError_t run_scan(const DeltaArgs& a) {
                          a.seg, a.N, units, a.dv, largest_factor(a.eps));
   };
   if (a.G > 1) {
-    // M is not asked for where the states at the starts of two segments are known without, and no backward follows
+    // M is for delta_carry, which runs where there are more than two segments.  (With two a call that a backward follows forms it as
+    // well, and with more the last segment does: nothing reads those.)
     const int with_M = a.G > 2 || a.errors != nullptr ? (DK + 16 * NW - 1) / (16 * NW) : 0;
     hipError_t err = run(delta_fwd_scan<T, DK, NW, true>, parts + with_M, 128 * NW);
     if (err == hipSuccess && a.G > 2) err = launch_delta_carry(a, false);
